@@ -301,6 +301,90 @@ ilargi_status_t ilargi_plan_trace_name(const ilargi_plan_t* plan, int i, char* b
 ilargi_status_t ilargi_stream_probe(int kind, float* dst, const float* src, int64_t n_floats, int blocks,
                                     void* stream);
 
+/* --- Models with learned features --------------------------------------------------------------------------------
+ * Operators beside the plan: rows of a learned table picked by the keys of a join, a dense layer over joined rows, their
+ * gradients, and the orthogonalised update of a layer's matrix.  They take no plan.  Matrices are row-major with a leading
+ * dimension `ld` in elements (ld >= columns; the columns between are neither read nor written) and any address that an
+ * element of their type may have; 16-byte aligned rows are the fast ones.  The rules of this header hold: device pointers,
+ * work enqueued on `stream`, no device memory allocated, the same bits for the same inputs, a status for every call.
+ * `workspace` is device memory of the caller, 256-byte aligned, used while the call's work runs: calls that overlap in
+ * time need a workspace each.  Outputs may not overlap inputs or each other, except where said. */
+typedef enum { ILARGI_TYPE_F32 = 0, ILARGI_TYPE_BF16 = 1 } ilargi_type_t; /* bf16: rounded to nearest even when stored */
+
+/* Rows of a learned table (the local result I_k D_k of Sec. 2.2 for a table that changes and keys that are not planned):
+ *   out[i, :] = scale * table[ids[i], :]   (+ out[i, :] when accumulate is not 0),    i < n.
+ * An id outside [0, rows) takes nothing: its row is zero (unchanged when accumulating).  Computed in float32 and rounded once.
+ * table rows x cols of table_type, ids device int32[n], out n x cols of out_type.  n may be 0.
+ * Errors: NULL, SHAPE (n, rows < 0, cols < 1, a leading dimension below cols, more than 2^31 - 1 rows or ids),
+ * UNSUPPORTED (a type that is none), DEVICE. */
+ilargi_status_t ilargi_embed(const void* table, ilargi_type_t table_type, int64_t rows, int64_t cols, int64_t ld_table,
+                             const int32_t* ids, int64_t n, float scale, int accumulate, void* out,
+                             ilargi_type_t out_type, int64_t ld_out, void* stream);
+
+/* Its gradient (I_k^T Y of Sec. 2.2, keys sorted in the call):
+ *   d_table[v, :] = scale * sum over ids[i] == v of d_out[i, :]   (+ d_table[v, :] when accumulate is not 0).
+ * Every row of d_table is written (when accumulating, those that some id names).  Ids outside [0, rows) add nothing.  Sums
+ * run in float32 over the ids sorted stably, in an order that depends on n, cols, the types and the ids only.
+ * Errors: as ilargi_embed, and WORKSPACE. */
+ilargi_status_t ilargi_embed_grad_workspace_bytes(int64_t n, int64_t rows, int64_t cols, size_t* bytes);
+ilargi_status_t ilargi_embed_grad(const void* d_out, ilargi_type_t out_type, int64_t ld_out, const int32_t* ids, int64_t n,
+                                  float scale, int accumulate, void* d_table, ilargi_type_t table_type, int64_t rows,
+                                  int64_t cols, int64_t ld_table, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum {
+  ILARGI_ACT_NONE = 0,
+  ILARGI_ACT_RELU = 1,    /* max(z, 0); slope 0 at 0 */
+  ILARGI_ACT_SIGMOID = 2, /* 1 / (1 + exp(-z)) */
+  ILARGI_ACT_SILU = 3,    /* z / (1 + exp(-z)) */
+  ILARGI_ACT_GELU = 4     /* z (1 + erf(z / sqrt 2)) / 2 */
+} ilargi_activation_t;
+
+/* A dense layer: its sizes, the element type of all its matrices and vectors, and its activation. */
+typedef struct {
+  int64_t n, k, m;        /* rows, input columns, output columns; n may be 0 */
+  ilargi_type_t type;     /* products accumulate in float32 for both types */
+  ilargi_activation_t act;
+} ilargi_layer_t;
+
+/* Bytes of workspace of ilargi_linear and ilargi_linear_grad for this layer (either pointer may be NULL).
+ * Errors: NULL (layer), SHAPE (n < 0, k or m < 1, any above 2^31 - 1), UNSUPPORTED (type, act). */
+ilargi_status_t ilargi_linear_workspace_bytes(const ilargi_layer_t* layer, size_t* forward, size_t* gradient);
+
+/* z = X W + bias;  out = act(z) + residual.
+ * X n x k, W k x m, bias[m] (optional), residual n x m (optional; may be `out` itself), out n x m, pre n x m (optional)
+ * receives z, which ilargi_linear_grad needs unless act is NONE.  z, act(z) and the sums are float32; each output is
+ * rounded once.  Errors: NULL, SHAPE, UNSUPPORTED, WORKSPACE, DEVICE. */
+ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_t ld_x, const void* W, int64_t ld_w,
+                              const void* bias, const void* residual, int64_t ld_res, void* out, int64_t ld_out,
+                              void* pre, int64_t ld_pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of ilargi_linear (the residual's is d_out itself):
+ *   g = d_out o act'(pre);  d_X = g W^T;  d_W = X^T g;  d_bias = column sums of g.
+ * pre is read unless act is NONE (then it may be NULL).  d_X, d_W and d_bias are each optional.  With accumulate not 0 the
+ * results are added to d_W and d_bias (d_X is always set).  g is formed in float32 and rounded to the layer's type before
+ * the two products, and not rounded for d_bias.  X is not read without d_W, nor W without d_X.
+ * Errors: NULL, SHAPE, UNSUPPORTED, WORKSPACE, DEVICE. */
+ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_out, int64_t ld_out, const void* pre,
+                                   int64_t ld_pre, const void* X, int64_t ld_x, const void* W, int64_t ld_w, void* d_X,
+                                   int64_t ld_dx, void* d_W, int64_t ld_dw, void* d_bias, int accumulate,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Orthogonalised update by Newton-Schulz products, for `batch` matrices G of rows x cols:
+ *   X = G / (||G||_F + eps);  `steps` times  A = X X^T (X^T X if cols < rows),  X <- a X + (b A + c A^2) X
+ *   out = alpha X + beta base.
+ * coef: host float[3] a, b, c (NULL: 3.4445, -4.7750, 2.0315, which bring singular values near 1 in five steps).
+ * G of g_type with leading dimension ld_g and `stride_g` elements between matrices; base (read if beta is not 0) and
+ * out of out_type with ld_out and stride_out; base may be `out` itself, so alpha = -lr, beta = 1 - lr decay updates weights
+ * in place.  The norm is summed in float64; products accumulate in float32.
+ * Errors: NULL, SHAPE (batch < 0, rows or cols < 1 or above 16384, steps outside [1, 100], leading dimensions or strides
+ * that overlap), UNSUPPORTED (types), WORKSPACE, DEVICE. */
+ilargi_status_t ilargi_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, ilargi_type_t g_type,
+                                                     size_t* bytes);
+ilargi_status_t ilargi_orthogonalize(const void* G, ilargi_type_t g_type, int64_t batch, int64_t rows, int64_t cols,
+                                     int64_t ld_g, int64_t stride_g, int steps, const float* coef, float eps, float alpha,
+                                     float beta, const void* base, void* out, ilargi_type_t out_type, int64_t ld_out,
+                                     int64_t stride_out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Message for the most recent failure on this thread ("" if none).  Static storage. */
 const char* ilargi_last_error(void);
 

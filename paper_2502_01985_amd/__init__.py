@@ -43,6 +43,8 @@ EXPORTED = [
     "ilargi_col_sum", "ilargi_choose", "ilargi_segment_sum",
     "ilargi_plan_inverse_index", "ilargi_plan_trace_begin", "ilargi_plan_trace_label", "ilargi_plan_trace_end",
     "ilargi_plan_trace_name", "ilargi_stream_probe",
+    "ilargi_embed", "ilargi_embed_grad", "ilargi_embed_grad_workspace_bytes", "ilargi_linear", "ilargi_linear_grad",
+    "ilargi_linear_workspace_bytes", "ilargi_orthogonalize", "ilargi_orthogonalize_workspace_bytes",
     "ilargi_static_scratch_bytes",
     "ilargi_last_error",
     "ilargi_version",
@@ -54,6 +56,11 @@ class SourceStruct(ctypes.Structure):
                 ("row_idx", ctypes.c_void_p), ("col_map", ctypes.c_void_p),
                 ("csr_rowptr", ctypes.c_void_p), ("csr_col", ctypes.c_void_p), ("csr_val", ctypes.c_void_p),
                 ("nnz", ctypes.c_int64)]
+
+
+class LayerStruct(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("k", ctypes.c_int64), ("m", ctypes.c_int64), ("type", ctypes.c_int),
+                ("act", ctypes.c_int)]
 
 
 _vp, _i64, _int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
@@ -84,6 +91,18 @@ lib.ilargi_plan_trace_end.argtypes = [_vp, ctypes.POINTER(ctypes.c_float), _int,
 lib.ilargi_plan_trace_label.argtypes = [_vp, ctypes.c_char_p]
 lib.ilargi_plan_trace_name.argtypes = [_vp, _int, ctypes.c_char_p, _int]
 lib.ilargi_stream_probe.argtypes = [_int, _vp, _vp, _i64, _int, _vp]
+_f32, _size = ctypes.c_float, ctypes.c_size_t
+lib.ilargi_embed.argtypes = [_vp, _int, _i64, _i64, _i64, _vp, _i64, _f32, _int, _vp, _int, _i64, _vp]
+lib.ilargi_embed_grad_workspace_bytes.argtypes = [_i64, _i64, _i64, ctypes.POINTER(_size)]
+lib.ilargi_embed_grad.argtypes = [_vp, _int, _i64, _vp, _i64, _f32, _int, _vp, _int, _i64, _i64, _i64, _vp, _size, _vp]
+lib.ilargi_linear_workspace_bytes.argtypes = [ctypes.POINTER(LayerStruct), ctypes.POINTER(_size), ctypes.POINTER(_size)]
+lib.ilargi_linear.argtypes = [ctypes.POINTER(LayerStruct), _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
+                              _size, _vp]
+lib.ilargi_linear_grad.argtypes = [ctypes.POINTER(LayerStruct), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
+                                   _i64, _vp, _int, _vp, _size, _vp]
+lib.ilargi_orthogonalize_workspace_bytes.argtypes = [_i64, _i64, _i64, _int, ctypes.POINTER(_size)]
+lib.ilargi_orthogonalize.argtypes = [_vp, _int, _i64, _i64, _i64, _i64, _i64, _int, _vp, _f32, _f32, _f32, _vp, _vp, _int,
+                                     _i64, _i64, _vp, _size, _vp]
 for _name in EXPORTED[:-3]:
     getattr(lib, _name).restype = _int
 lib.ilargi_static_scratch_bytes.restype = ctypes.c_size_t
@@ -572,6 +591,243 @@ def ilargi_plan_trace_end(plan: Plan, capacity: int, names: bool = False):
 def ilargi_stream_probe(kind: int, dst, src, n_floats: int, blocks: int = 4096, stream=None) -> None:
     _check(lib.ilargi_stream_probe(kind, dst.data_ptr(), src.data_ptr() if src is not None else None, n_floats,
                                    blocks, _stream_ptr(stream)), "ilargi_stream_probe")
+
+
+# ------------------------------------------------------------------------------------ models with learned features
+TYPES = {torch.float32: 0, torch.bfloat16: 1}
+ACTS = {"none": 0, "relu": 1, "sigmoid": 2, "silu": 3, "gelu": 4}
+
+
+def _typed(t, name: str) -> int:
+    code = TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if code is None:
+        raise TypeError(f"{name} must be a float32 or bfloat16 CUDA tensor")
+    return code
+
+
+def _rows_of(t, name: str, rows: int, cols: int, dtype=None) -> int:
+    """Checks a matrix ``rows x cols`` of unit column stride and returns its leading dimension."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and (t.dtype == dtype if dtype is not None else t.dtype in TYPES)):
+        raise TypeError(f"{name} must be a {'float32 or bfloat16' if dtype is None else dtype} CUDA tensor")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be {rows} x {cols}")
+    ld, unit = t.stride()
+    if rows <= 1:
+        ld = max(ld, cols)
+    if (unit != 1 and cols > 1) or (ld < cols and rows > 0):
+        raise TypeError(f"{name} must have unit column stride and rows that do not overlap")
+    return max(ld, cols)
+
+
+def _vector(t, name: str, length: int, dtype) -> int:
+    if t is None:
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    if t.numel() != length:
+        raise ValueError(f"{name} must hold {length} values")
+    return t.data_ptr()
+
+
+def _act_code(act) -> int:
+    if isinstance(act, str):
+        if act not in ACTS:
+            raise ValueError(f"act must be one of {sorted(ACTS)}")
+        return ACTS[act]
+    return int(act)
+
+
+def _new(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(workspace, nbytes: int, device, stream):
+    """The caller's workspace, or a new one of ``nbytes`` bytes: (tensor, pointer, bytes)."""
+    if workspace is None:
+        workspace = _new(nbytes, torch.uint8, device, stream)
+    elif not (workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous uint8 CUDA tensor")
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def ilargi_embed(table, ids, scale: float = 1.0, out=None, accumulate: bool = False, out_dtype=None, stream=None):
+    """``out[i] = scale * table[ids[i]]`` (added to ``out`` with ``accumulate``); an id outside the table takes nothing.
+    ``table``: float32 or bfloat16, ``ids``: int32[n].  ``out`` (n x cols) is new unless given, of ``out_dtype`` (the
+    table's by default)."""
+    ttype = _typed(table, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be 2-D")
+    rows, cols = table.shape
+    _dev_i32(ids, "ids")
+    n = ids.numel()
+    ld = _rows_of(table, "table", rows, cols)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = _new((n, cols), out_dtype or table.dtype, table.device, stream)
+    ldo = _rows_of(out, "out", n, cols)
+    _check(lib.ilargi_embed(table.data_ptr(), ttype, rows, cols, ld, ids.data_ptr(), n, scale, int(accumulate),
+                            out.data_ptr(), TYPES[out.dtype], ldo, _stream_ptr(stream)), "ilargi_embed")
+    return out
+
+
+def ilargi_embed_grad_workspace_bytes(n: int, rows: int, cols: int) -> int:
+    nbytes = _size(0)
+    _check(lib.ilargi_embed_grad_workspace_bytes(n, rows, cols, ctypes.byref(nbytes)), "ilargi_embed_grad_workspace_bytes")
+    return nbytes.value
+
+
+def ilargi_embed_grad(d_out, ids, rows: int, scale: float = 1.0, d_table=None, accumulate: bool = False, dtype=None,
+                      workspace=None, stream=None):
+    """``d_table[v] = scale * sum of d_out[i] over ids[i] == v`` (added to ``d_table`` with ``accumulate``) for a table of
+    ``rows`` rows.  ``d_table`` is new unless given, of ``dtype`` (that of ``d_out`` by default)."""
+    otype = _typed(d_out, "d_out")
+    _dev_i32(ids, "ids")
+    n = ids.numel()
+    if d_out.dim() != 2:
+        raise ValueError("d_out must be 2-D")
+    cols = d_out.shape[1]
+    ldo = _rows_of(d_out, "d_out", n, cols)
+    if d_table is None:
+        if accumulate:
+            raise ValueError("accumulate needs d_table")
+        d_table = _new((rows, cols), dtype or d_out.dtype, d_out.device, stream)
+    ldt = _rows_of(d_table, "d_table", rows, cols)
+    need = ilargi_embed_grad_workspace_bytes(n, rows, cols) if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, d_out.device, stream)
+    _check(lib.ilargi_embed_grad(d_out.data_ptr(), otype, ldo, ids.data_ptr(), n, scale, int(accumulate), d_table.data_ptr(),
+                                 TYPES[d_table.dtype], rows, cols, ldt, ws, ws_bytes, _stream_ptr(stream)),
+           "ilargi_embed_grad")
+    return d_table
+
+
+def ilargi_linear_workspace_bytes(n: int, k: int, m: int, dtype) -> Tuple[int, int]:
+    """Bytes of workspace of ``ilargi_linear`` and of ``ilargi_linear_grad``."""
+    fwd, grad = _size(0), _size(0)
+    _check(lib.ilargi_linear_workspace_bytes(ctypes.byref(LayerStruct(n, k, m, TYPES[dtype], 0)), ctypes.byref(fwd),
+                                             ctypes.byref(grad)), "ilargi_linear_workspace_bytes")
+    return fwd.value, grad.value
+
+
+def ilargi_linear(X, W, bias=None, residual=None, act="none", out=None, pre=None, workspace=None, stream=None):
+    """``act(X W + bias) + residual`` for ``X`` n x k and ``W`` k x m of one type (float32 or bfloat16).  ``pre`` (n x m,
+    optional) receives ``X W + bias``, which ``ilargi_linear_grad`` reads; ``residual`` may be ``out``."""
+    dtype = X.dtype
+    code = _typed(X, "X")
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X and W must be 2-D")
+    n, k = X.shape
+    m = W.shape[1]
+    ldx, ldw = _rows_of(X, "X", n, k, dtype), _rows_of(W, "W", k, m, dtype)
+    if out is None:
+        out = _new((n, m), dtype, X.device, stream)
+    ldo = _rows_of(out, "out", n, m, dtype)
+    ldr = _rows_of(residual, "residual", n, m, dtype) if residual is not None else 0
+    ldp = _rows_of(pre, "pre", n, m, dtype) if pre is not None else 0
+    y = LayerStruct(n, k, m, code, _act_code(act))
+    need = ilargi_linear_workspace_bytes(n, k, m, dtype)[0] if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, X.device, stream)
+    _check(lib.ilargi_linear(ctypes.byref(y), X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(bias, "bias", m, dtype) or None,
+                             residual.data_ptr() if residual is not None else None, ldr, out.data_ptr(), ldo,
+                             pre.data_ptr() if pre is not None else None, ldp, ws, ws_bytes, _stream_ptr(stream)),
+           "ilargi_linear")
+    return out
+
+
+def ilargi_linear_grad(d_out, X, W, pre=None, act="none", d_X="new", d_W="new", d_bias="new", accumulate: bool = False,
+                       workspace=None, stream=None):
+    """``(d_X, d_W, d_bias)`` of ``ilargi_linear`` (the residual's gradient is ``d_out``).  Each result is a tensor to fill,
+    ``"new"``, or ``None`` where it is not wanted; ``accumulate`` adds to the given ``d_W`` and ``d_bias``."""
+    dtype = d_out.dtype
+    code = _typed(d_out, "d_out")
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X and W must be 2-D")
+    n, k = X.shape
+    m = W.shape[1]
+    ldo = _rows_of(d_out, "d_out", n, m, dtype)
+    ldx, ldw = _rows_of(X, "X", n, k, dtype), _rows_of(W, "W", k, m, dtype)
+    a = _act_code(act)
+    if a and pre is None:
+        raise ValueError("pre is needed unless act is none")
+    ldp = _rows_of(pre, "pre", n, m, dtype) if pre is not None else 0
+    if accumulate and (isinstance(d_W, str) or isinstance(d_bias, str)):
+        raise ValueError("accumulate needs d_W and d_bias (or None)")
+    if isinstance(d_X, str):
+        d_X = _new((n, k), dtype, X.device, stream)
+    if isinstance(d_W, str):
+        d_W = _new((k, m), dtype, X.device, stream)
+    if isinstance(d_bias, str):
+        d_bias = _new((m,), dtype, X.device, stream)
+    lddx = _rows_of(d_X, "d_X", n, k, dtype) if d_X is not None else 0
+    lddw = _rows_of(d_W, "d_W", k, m, dtype) if d_W is not None else 0
+    y = LayerStruct(n, k, m, code, a)
+    need = ilargi_linear_workspace_bytes(n, k, m, dtype)[1] if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, X.device, stream)
+    _check(lib.ilargi_linear_grad(ctypes.byref(y), d_out.data_ptr(), ldo, pre.data_ptr() if pre is not None else None, ldp,
+                                  X.data_ptr(), ldx, W.data_ptr(), ldw, d_X.data_ptr() if d_X is not None else None, lddx,
+                                  d_W.data_ptr() if d_W is not None else None, lddw, _vector(d_bias, "d_bias", m, dtype) or None,
+                                  int(accumulate), ws, ws_bytes, _stream_ptr(stream)), "ilargi_linear_grad")
+    return d_X, d_W, d_bias
+
+
+def ilargi_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, dtype) -> int:
+    nbytes = _size(0)
+    _check(lib.ilargi_orthogonalize_workspace_bytes(batch, rows, cols, TYPES[dtype], ctypes.byref(nbytes)),
+           "ilargi_orthogonalize_workspace_bytes")
+    return nbytes.value
+
+
+def _batch_of(t, name: str, shape):
+    """Leading dimension and distance of the matrices of a batch x rows x cols tensor."""
+    _typed(t, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {' x '.join(str(v) for v in shape)}")
+    batch, rows, cols = shape
+    far, ld, unit = t.stride()
+    if rows <= 1:
+        ld = max(ld, cols)
+    if batch <= 1:
+        far = max(far, (rows - 1) * ld + cols)
+    if (unit != 1 and cols > 1) or ld < cols or far < (rows - 1) * ld + cols:
+        raise TypeError(f"{name} must have unit column stride and matrices that do not overlap")
+    return ld, far
+
+
+def ilargi_orthogonalize(G, out=None, alpha: float = 1.0, beta: float = 0.0, base=None, steps: int = 5, coef=None,
+                         eps: float = 1e-7, out_dtype=None, workspace=None, stream=None):
+    """``alpha * NS(G) + beta * base``: ``G`` (rows x cols, or batch x rows x cols) near its orthogonal factor by ``steps``
+    Newton-Schulz products with the coefficients ``coef`` (three numbers).  ``base`` has the type and layout of ``out`` and
+    may be ``out``, so ``ilargi_orthogonalize(update, out=W, base=W, alpha=-lr, beta=1 - lr * decay)`` updates weights."""
+    shape = G.shape
+    if G.dim() == 2:
+        G3 = G.unsqueeze(0)
+    elif G.dim() == 3:
+        G3 = G
+    else:
+        raise ValueError("G must be rows x cols or batch x rows x cols")
+    gtype = _typed(G, "G")
+    ldg, farg = _batch_of(G3, "G", G3.shape)
+    if out is None:
+        out = _new(shape, out_dtype or G.dtype, G.device, stream)
+    if out.shape != shape:
+        raise ValueError("out must have the shape of G")
+    o3 = out if out.dim() == 3 else out.unsqueeze(0)
+    ldo, faro = _batch_of(o3, "out", G3.shape)
+    if beta != 0.0:
+        if base is None or base.dtype != out.dtype or base.shape != shape or base.stride() != out.stride() or not base.is_cuda:
+            raise ValueError("base must have the type, shape and strides of out")
+    batch, rows, cols = G3.shape
+    need = ilargi_orthogonalize_workspace_bytes(batch, rows, cols, G.dtype) if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, G.device, stream)
+    abc = (ctypes.c_float * 3)(*coef) if coef is not None else None
+    _check(lib.ilargi_orthogonalize(G.data_ptr(), gtype, batch, rows, cols, ldg, farg, steps, abc, eps, alpha, beta,
+                                    base.data_ptr() if beta != 0.0 else None, out.data_ptr(), TYPES[out.dtype], ldo, faro, ws,
+                                    ws_bytes, _stream_ptr(stream)), "ilargi_orthogonalize")
+    return out
 
 
 def schema_to_device(schema, device="cuda:0", sparse=False):

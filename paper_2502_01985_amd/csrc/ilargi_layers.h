@@ -1,0 +1,178 @@
+// Internal declarations of the operators of models with learned features: embedding rows, dense layers, orthogonalised
+// updates (not installed).
+#ifndef ILARGI_LAYERS_H_
+#define ILARGI_LAYERS_H_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ilargi.h"
+#include "ilargi_internal.h"
+
+namespace ilargi {
+
+using bf16_t = __bf16;
+
+template <class T> struct ElemOf;
+template <> struct ElemOf<float> { static constexpr int kVec = 4; };     // elements of a 16-byte piece
+template <> struct ElemOf<bf16_t> { static constexpr int kVec = 8; };
+
+// Sixteen bytes at any address an element may have: the memory system takes dword and halfword addresses.
+template <class T, int N> struct __attribute__((packed)) Piece { T v[N]; };
+
+// N consecutive elements as floats, the ones from `valid` on as zeros.
+template <class T, int N>
+__device__ __forceinline__ void load_piece(const T* __restrict__ p, int valid, float (&f)[N]) {
+  if (valid >= N) {
+    const Piece<T, N> t = *reinterpret_cast<const Piece<T, N>*>(p);
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = (float)t.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = j < valid ? (float)p[j] : 0.0f;
+  }
+}
+
+template <class T, int N>
+__device__ __forceinline__ void store_piece(T* __restrict__ p, int valid, const float (&f)[N]) {
+  if (valid >= N) {
+    Piece<T, N> t;
+#pragma unroll
+    for (int j = 0; j < N; ++j) t.v[j] = (T)f[j];
+    *reinterpret_cast<Piece<T, N>*>(p) = t;
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < valid) p[j] = (T)f[j];
+  }
+}
+
+// f(z) of a layer in 32 bits.  exp and erf are the device library's.
+__device__ __forceinline__ float act_value(float z, int act) {
+  switch (act) {
+    case ILARGI_ACT_RELU: return z > 0.0f ? z : (z != z ? z : 0.0f);
+    case ILARGI_ACT_SIGMOID: return 1.0f / (1.0f + expf(-z));
+    // exp(-z) overflows to infinity below z = -88, where z / (1 + exp(-z)) is -0; -infinity itself has the limit 0
+    case ILARGI_ACT_SILU: return z == -INFINITY ? 0.0f : z / (1.0f + expf(-z));
+    case ILARGI_ACT_GELU: return z == -INFINITY ? 0.0f : 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    default: return z;
+  }
+}
+// f'(z)
+__device__ __forceinline__ float act_slope(float z, int act) {
+  switch (act) {
+    case ILARGI_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case ILARGI_ACT_SIGMOID: {
+      const float e = expf(-fabsf(z)), q = 1.0f / (1.0f + e);
+      return e * q * q;
+    }
+    case ILARGI_ACT_SILU: {
+      const float e = expf(-fabsf(z)), q = 1.0f / (1.0f + e);        // sigmoid(|z|)
+      const float p = z >= 0.0f ? q : e * q, r = z >= 0.0f ? e * q : q;   // sigmoid(z), sigmoid(-z)
+      return p + (r == 0.0f || p == 0.0f ? 0.0f : z * p * r);
+    }
+    case ILARGI_ACT_GELU: {
+      const float g = 0.39894228040143268f * expf(-0.5f * z * z);
+      return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + (g == 0.0f ? 0.0f : z * g);
+    }
+    default: return 1.0f;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- embedding rows
+struct EmbedArgs {
+  const void* table;
+  int64_t rows, cols, ld_table;
+  const int32_t* ids;
+  int64_t n;
+  float scale;
+  int accumulate;
+  void* out;
+  int64_t ld_out;
+  int table_bf16, out_bf16;
+};
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
+
+struct EmbedGradArgs {
+  const void* d_out;
+  int64_t ld_out;
+  const int32_t* ids;
+  int64_t n, rows, cols;
+  float scale;
+  int accumulate;
+  void* d_table;
+  int64_t ld_table;
+  int out_bf16, table_bf16;
+};
+size_t embed_grad_bytes(int64_t n, int64_t rows, int64_t cols);
+hipError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, hipStream_t st);
+
+// ------------------------------------------------------------------------------------------------- matrix products
+// C(i, j) = sum_k P(i, k) Q(k, j).  An operand is a matrix of rows of `ld` elements; `k_rows` says that its rows run over
+// k (then its columns are the i or j of the result), else that its columns do.
+struct Operand {
+  const void* p;
+  int64_t ld;
+  int k_rows;
+  int bf16;
+  int64_t batch;        // elements from one matrix of a batch to the next
+};
+enum { kEpiLinear = 0, kEpiScale = 1 };
+struct Epilogue {
+  int mode;
+  // kEpiLinear: z = acc + bias[j] kept in `pre`, out = f(z) + src
+  // kEpiScale: out = s0 acc + s1 src + s2 base; `flip` writes out(j, i), with `base` laid out as `out`
+  float s0, s1, s2;
+  const void* base;
+  const void* bias;
+  const void* src;
+  int64_t ld_src, batch_src;
+  int src_bf16;
+  void* pre;
+  int64_t ld_pre;
+  int act;
+  void* out;
+  int64_t ld_out, batch_out;
+  int out_bf16;
+  int flip;
+};
+struct Product {
+  Operand P, Q;
+  int64_t M, N, K, batches;
+  Epilogue epi;
+};
+hipError_t launch_mm_f32(const Product& a, hipStream_t st);
+
+struct LayerGradArgs {
+  int64_t n, m;
+  const void* d_out;
+  int64_t ld_out;
+  const void* pre;
+  int64_t ld_pre;
+  int act, bf16;
+  void* dz;             // n x m, ld_dz (NULL: not written)
+  int64_t ld_dz;
+  void* d_bias;         // may be NULL
+  int accumulate;
+};
+size_t layer_grad_partial_bytes(int64_t n, int64_t m);
+hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t st);
+
+// ------------------------------------------------------------------------------------------------- orthogonal updates
+struct OrthoArgs {
+  const void* G;
+  int64_t batch, rows, cols, ld_g, batch_g;
+  int g_bf16;
+  int steps;
+  float coef[3];
+  float eps, alpha, beta;
+  const void* base;     // may be NULL; laid out as out
+  void* out;
+  int64_t ld_out, batch_out;
+  int out_bf16;
+};
+size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols);
+hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st);
+
+}  // namespace ilargi
+#endif

@@ -1,0 +1,198 @@
+// Matrix products in float32 on the matrix cores, for operands of either type, order, stride and alignment, and the
+// elementwise pass of a layer's gradient.
+#include "mm_epilogue.h"
+
+namespace ilargi {
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kTile = 128, kStep = 16, kPad = kTile + 4;
+
+// Eight elements of a 128 x 16 piece of an operand for every thread, as floats; zeros outside the matrix.
+template <class T, bool KROWS>
+__device__ __forceinline__ void fetch(const T* __restrict__ p, int64_t ld, int64_t r0, int64_t R, int64_t k0, int64_t K, float (&f)[8]) {
+  const int t = threadIdx.x;
+  const int64_t outer = KROWS ? k0 + (t >> 4) : r0 + (t >> 1), inner = KROWS ? r0 + (t & 15) * 8 : k0 + (t & 1) * 8;
+  const int64_t n_outer = KROWS ? K : R, n_inner = KROWS ? R : K;
+  const int64_t left = outer < n_outer ? n_inner - inner : 0;
+  load_piece<T, 8>(p + (left > 0 ? outer * ld + inner : 0), (int)(left < 0 ? 0 : left > 8 ? 8 : left), f);
+}
+
+template <bool KROWS>
+__device__ __forceinline__ void put(float (*lds)[kPad], const float (&f)[8]) {
+  const int t = threadIdx.x;
+  if constexpr (KROWS) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<float4*>(&lds[t >> 4][(t & 15) * 8 + 4 * h]) = make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lds[(t & 1) * 8 + j][t >> 1] = f[j];
+  }
+}
+
+// A workgroup forms 128 x 128 sums, a wavefront 64 x 64 of them, 16 steps of k at a time from LDS while the next are fetched.
+// The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
+template <class TP, class TQ, bool PK, bool QK>
+__global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n) {
+  __shared__ __attribute__((aligned(16))) float lp[2][kStep][kPad], lq[2][kStep][kPad];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t i0 = (int64_t)(blockIdx.x / tiles_n) * kTile, j0 = (int64_t)(blockIdx.x % tiles_n) * kTile, b = blockIdx.y;
+  const TP* P = (const TP*)a.P.p + b * a.P.batch;
+  const TQ* Q = (const TQ*)a.Q.p + b * a.Q.batch;
+  const int wi = (wave / 2) * 64, wj = (wave % 2) * 64, r = lane % 32, h = lane / 32;
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int q = 0; q < 16; ++q) acc[x / 2][x % 2][q] = 0.0f;
+  float fp[8], fq[8];
+  if (a.K > 0) {
+    fetch<TP, PK>(P, a.P.ld, i0, a.M, 0, a.K, fp);
+    fetch<TQ, QK>(Q, a.Q.ld, j0, a.N, 0, a.K, fq);
+    put<PK>(lp[0], fp);
+    put<QK>(lq[0], fq);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int64_t k0 = 0; k0 < a.K; k0 += kStep, cur ^= 1) {
+    const bool more = k0 + kStep < a.K;
+    if (more) {
+      fetch<TP, PK>(P, a.P.ld, i0, a.M, k0 + kStep, a.K, fp);
+      fetch<TQ, QK>(Q, a.Q.ld, j0, a.N, k0 + kStep, a.K, fq);
+    }
+#pragma unroll
+    for (int k = 0; k < kStep; k += 2) {
+      const float p0 = lp[cur][k + h][wi + r], p1 = lp[cur][k + h][wi + 32 + r];
+      const float q0 = lq[cur][k + h][wj + r], q1 = lq[cur][k + h][wj + 32 + r];
+      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q0, p0, acc[0][0], 0, 0, 0);
+      acc[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(q1, p0, acc[0][1], 0, 0, 0);
+      acc[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q0, p1, acc[1][0], 0, 0, 0);
+      acc[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(q1, p1, acc[1][1], 0, 0, 0);
+    }
+    if (more) {
+      put<PK>(lp[cur ^ 1], fp);
+      put<QK>(lq[cur ^ 1], fq);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int64_t i = i0 + wi + 32 * x + r;
+    if (i >= a.M) continue;
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int64_t j = j0 + wj + 32 * y + 8 * g + 4 * h;
+        if (j >= a.N) continue;
+        float v[4] = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
+        epilogue4(a.epi, b, i, j, (int)(a.N - j < 4 ? a.N - j : 4), v);
+      }
+  }
+}
+
+template <class TP, class TQ>
+hipError_t mm_f32_typed(const Product& a, hipStream_t st) {
+  const int64_t tm = (a.M + kTile - 1) / kTile, tn = (a.N + kTile - 1) / kTile;
+  const dim3 grid((unsigned)(tm * tn), (unsigned)a.batches);
+  const int n = (int)tn;
+  if (a.P.k_rows) {
+    if (a.Q.k_rows) mm_f32_kernel<TP, TQ, true, true><<<grid, 256, 0, st>>>(a, n);
+    else mm_f32_kernel<TP, TQ, true, false><<<grid, 256, 0, st>>>(a, n);
+  } else {
+    if (a.Q.k_rows) mm_f32_kernel<TP, TQ, false, true><<<grid, 256, 0, st>>>(a, n);
+    else mm_f32_kernel<TP, TQ, false, false><<<grid, 256, 0, st>>>(a, n);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mm_f32(const Product& a, hipStream_t st) {
+  if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
+  if (a.P.bf16 != a.Q.bf16) return hipErrorInvalidValue;
+  return a.P.bf16 ? mm_f32_typed<bf16_t, bf16_t>(a, st) : mm_f32_typed<float, float>(a, st);
+}
+
+// --------------------------------------------------------------------------------------- elementwise pass of a gradient
+namespace {
+
+constexpr int kBiasChunks = 256;
+
+// g = d_out f'(pre), written in the layer's type; column sums of the unrounded g over this workgroup's rows.
+// 32 lanes of four columns, eight rows at a time.
+template <class T>
+__global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_t rows_per, float* __restrict__ partial) {
+  __shared__ float4 part[8][32];
+  const int cl = threadIdx.x % 32, rl = threadIdx.x / 32;
+  const int64_t j = ((int64_t)blockIdx.x * 32 + cl) * 4;
+  const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < a.n ? r0 + rows_per : a.n;
+  const int valid = (int)(a.m - j < 4 ? a.m - j : 4);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (valid > 0) {
+    for (int64_t i = r0 + rl; i < r1; i += 8) {
+      float g[4];
+      load_piece<T, 4>((const T*)a.d_out + i * a.ld_out + j, valid, g);
+      if (a.act != ILARGI_ACT_NONE) {
+        float z[4];
+        load_piece<T, 4>((const T*)a.pre + i * a.ld_pre + j, valid, z);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) g[q] *= act_slope(z[q], a.act);
+      }
+      if (a.dz != nullptr) store_piece<T, 4>((T*)a.dz + i * a.ld_dz + j, valid, g);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s[q] += g[q];
+    }
+  }
+  if (partial == nullptr) return;
+  part[rl][cl] = make_float4(s[0], s[1], s[2], s[3]);
+  __syncthreads();
+  if (rl == 0 && valid > 0) {
+    float4 t = part[0][cl];
+    for (int q = 1; q < 8; ++q) { t.x += part[q][cl].x; t.y += part[q][cl].y; t.z += part[q][cl].z; t.w += part[q][cl].w; }
+    const float f[4] = {t.x, t.y, t.z, t.w};
+    store_piece<float, 4>(partial + blockIdx.y * a.m + j, valid, f);
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, int chunks, int64_t m, int accumulate, T* __restrict__ out) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= m) return;
+  float s = 0.0f;
+  for (int c = 0; c < chunks; ++c) s += partial[c * m + j];
+  out[j] = (T)(accumulate ? (float)out[j] + s : s);
+}
+
+int64_t bias_rows(int64_t n) {
+  int64_t rows = (n + kBiasChunks - 1) / kBiasChunks;
+  return rows < 32 ? 32 : (rows + 7) / 8 * 8;
+}
+
+}  // namespace
+
+size_t layer_grad_partial_bytes(int64_t n, int64_t m) {
+  const int64_t per = bias_rows(n), chunks = (n + per - 1) / per;
+  return (size_t)chunks * (size_t)m * 4;
+}
+
+hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t st) {
+  const int64_t per = bias_rows(a.n), chunks = (a.n + per - 1) / per;
+  if (a.d_bias == nullptr) partial = nullptr;
+  if (chunks > 0 && (a.dz != nullptr || partial != nullptr)) {
+    const dim3 grid((unsigned)((a.m + 127) / 128), (unsigned)chunks);
+    if (a.bf16) layer_grad_kernel<bf16_t><<<grid, 256, 0, st>>>(a, per, partial);
+    else layer_grad_kernel<float><<<grid, 256, 0, st>>>(a, per, partial);
+  }
+  if (a.d_bias != nullptr) {
+    const unsigned grid = (unsigned)((a.m + 255) / 256);
+    if (a.bf16) bias_sum_kernel<bf16_t><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (bf16_t*)a.d_bias);
+    else bias_sum_kernel<float><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (float*)a.d_bias);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ilargi

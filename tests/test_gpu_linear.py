@@ -1,0 +1,263 @@
+"""A dense layer and its gradients against 64 bits.
+
+Bounds, with u32 = 2^-24, u16 = 2^-8 and u the roundoff of the layer's type.  z: a sum of k products and a bias in float32 in some
+order, |err z| <= (k + 3) u32 (sum|x||w| + |bias|).  f: its slope is at most 1.13 for all activations, its evaluation is good to
+16 u32 (1 + |z|).  A stored value adds u of itself.  Gradients: g = d f'(z) with f' good to 32 u32 absolutely, rounded to the
+type (u); a sum of r products of it: sum|g||w| (u [bf16] + (r + 3) u32) + 32 u32 sum|d||w|.  The float32 bias sums: (n + 3) u32.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F32, BF16 = torch.float32, torch.bfloat16
+U = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+E32 = 2.0 ** -24
+ACTS = ["none", "relu", "sigmoid", "silu", "gelu"]
+
+
+@pytest.fixture(scope="module")
+def il():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_01985_amd as mod
+    return mod
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _matrix(rows, cols, dtype, gen, pad=0, shift=0, scale=1.0):
+    store = torch.full((rows * (cols + pad) + shift + 8,), float("nan"), dtype=dtype, device="cuda")
+    m = store[shift: shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    m.copy_(torch.randn(rows, cols, generator=gen, device="cuda") * scale)
+    return m
+
+
+def _f(z, act):
+    if act == "relu":
+        return z.clamp(min=0)
+    if act == "sigmoid":
+        return torch.sigmoid(z)
+    if act == "silu":
+        return z * torch.sigmoid(z)
+    if act == "gelu":
+        return 0.5 * z * torch.erfc(-z * math.sqrt(0.5))
+    return z
+
+
+def _slope(z, act):
+    if act == "relu":
+        return (z > 0).double()
+    if act == "sigmoid":
+        return torch.sigmoid(z) * torch.sigmoid(-z)
+    if act == "silu":
+        return torch.sigmoid(z) * (1 + z * torch.sigmoid(-z))
+    if act == "gelu":
+        return 0.5 * torch.erfc(-z * math.sqrt(0.5)) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    return torch.ones_like(z)
+
+
+# rows, inputs, outputs: single rows, single columns, odd, ragged against every tile, aligned
+SHAPES = [(0, 5, 3), (1, 1, 1), (1, 64, 96), (1, 1000, 333), (2, 72, 40), (3, 2048, 64), (5, 40, 8), (7, 16, 1030), (16, 136, 520), (17, 129, 131),
+          (33, 250, 24), (64, 512, 256), (65, 63, 129), (127, 8, 200), (128, 128, 128), (130, 264, 136), (200, 1, 7), (257, 96, 264), (300, 777, 1),
+          (512, 320, 512), (1003, 333, 517), (1024, 64, 4096)]
+
+
+@pytest.mark.parametrize("n,k,m", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 8), (3, 1)])
+def test_forward(il, n, k, m, dtype, pad, shift):
+    gen = _gen(n + 3 * k + 5 * m)
+    X, W = _matrix(n, k, dtype, gen, pad, shift), _matrix(k, m, dtype, gen, pad, shift, 1 / math.sqrt(k))
+    bias = torch.randn(m, generator=gen, device="cuda").to(dtype)
+    R, out, pre = (_matrix(n, m, dtype, gen, pad, shift) for _ in range(3))
+    for q, act in enumerate(ACTS):
+        b, r, keep = (bias if q != 1 else None), (R if q % 2 == 0 else None), q != 3
+        z = X.double() @ W.double() + (b.double() if b is not None else 0.0)
+        ez = (k + 3) * E32 * (X.double().abs() @ W.double().abs() + (b.double().abs() if b is not None else 0.0))
+        want = _f(z, act) + (r.double() if r is not None else 0.0)
+        got = il.ilargi_linear(X, W, bias=b, residual=r, act=act, out=out, pre=pre if keep else None)
+        assert got is out
+        err = 1.13 * ez + (0.0 if act == "none" else 16 * E32 * (1 + z.abs())) + E32 * (want.abs() + _f(z, act).abs())
+        assert bool(((out.double() - want).abs() <= err + U[dtype] * (want.abs() + err)).all())
+        if keep:
+            assert bool(((pre.double() - z).abs() <= ez + U[dtype] * (z.abs() + ez)).all())
+    # the residual may be the output itself, and a second run has the same bits
+    first = il.ilargi_linear(X, W, bias=bias, residual=R, act="silu")
+    out.copy_(R)
+    il.ilargi_linear(X, W, bias=bias, residual=out, act="silu", out=out)
+    assert torch.equal(first, out)
+
+
+@pytest.mark.parametrize("n,k,m", SHAPES + [(2000, 24, 40), (5000, 64, 96), (3001, 17, 9)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 8), (3, 1)])
+def test_gradient(il, n, k, m, dtype, pad, shift):
+    gen = _gen(n + 3 * k + 5 * m)
+    X, W = _matrix(n, k, dtype, gen, pad, shift), _matrix(k, m, dtype, gen, pad, shift, 1 / math.sqrt(k))
+    D, Z = _matrix(n, m, dtype, gen, pad, shift), _matrix(n, m, dtype, gen, pad, shift, 2.0)
+    dX, dW = _matrix(n, k, dtype, gen, pad, shift), _matrix(k, m, dtype, gen, pad, shift)
+    db = torch.empty(m, dtype=dtype, device="cuda")
+    x, w, d = X.double(), W.double(), D.double()
+    ug = U[dtype] if dtype == BF16 else 0.0
+    for act in ACTS:
+        g = d * _slope(Z.double(), act)
+        slack = 0.0 if act == "none" else 32 * E32
+        il.ilargi_linear_grad(D, X, W, pre=Z if act != "none" else None, act=act, d_X=dX, d_W=dW, d_bias=db)
+        for got, want, size, raw, r, rounded in (
+                (dX, g @ w.t(), g.abs() @ w.t().abs(), d.abs() @ w.t().abs(), m, ug),
+                (dW, x.t() @ g, x.t().abs() @ g.abs(), x.t().abs() @ d.abs(), n, ug),
+                (db, g.sum(0), g.abs().sum(0), d.abs().sum(0), n, 0.0)):
+            err = size * ((rounded if act != "none" else 0.0) + (r + 4) * E32) * 1.01 + 1.01 * slack * raw
+            assert bool(((got.double() - want).abs() <= err + U[dtype] * (want.abs() + err)).all()), act
+    # added to what is there; parts that are not asked for
+    old_W, old_b = dW.double().clone(), db.double().clone()
+    add_W, add_b = dW.clone(), db.clone()
+    one = il.ilargi_linear_grad(D, X, W, pre=Z, act="gelu", d_X=None, d_W=add_W, d_bias=add_b, accumulate=True)
+    assert one[0] is None
+    near = lambda a, b, u: bool(((a.double() - b).abs() <= 2.02 * u * (b.abs() + old_W.abs().max() + old_b.abs().max())).all())
+    assert near(add_W, 2 * old_W, U[dtype]) and near(add_b, 2 * old_b, U[dtype])
+    only = il.ilargi_linear_grad(D, X, W, pre=Z, act="gelu", d_W=None, d_bias=None)
+    assert only[1] is None and only[2] is None and torch.equal(only[0], dX)
+    bias_only = il.ilargi_linear_grad(D, X, W, pre=Z, act="gelu", d_X=None, d_W=None)
+    assert torch.equal(bias_only[2], db)
+    again = il.ilargi_linear_grad(D, X, W, pre=Z, act="gelu")
+    assert torch.equal(again[0], dX) and torch.equal(again[1], dW) and torch.equal(again[2], db)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradient_against_differences(il, act):
+    """L = sum(Y o layer(X, W, b)): central differences of L in 64 bits along random directions against the kernels' gradients.
+    The differences are off by h^2 / 6 of the third derivative, below 1e-7 of L here; the gradients by float32's rounding.
+    (relu: a kink costs nothing where no z changes sign, and h is small against all |z|.)"""
+    gen = _gen(11)
+    n, k, m, h = 150, 36, 44, 1e-5
+    X, W, b = (torch.randn(s, generator=gen, device="cuda") for s in ((n, k), (k, m), (m,)))
+    W /= 6
+    Y = torch.randn(n, m, generator=gen, device="cuda")
+    pre = torch.empty(n, m, device="cuda")
+    il.ilargi_linear(X, W, bias=b, act=act, pre=pre)
+    dX, dW, db = il.ilargi_linear_grad(Y, X, W, pre=pre, act=act)
+    L = lambda x, w, c: (Y.double() * _f(x @ w + c, act)).sum()
+    x, w, c = X.double(), W.double(), b.double()
+    for grad, step in ((dX, "x"), (dW, "w"), (db, "c")):
+        v = torch.randn(grad.shape, generator=gen, device="cuda").double()
+        p, q = dict(x=x, w=w, c=c), dict(x=x, w=w, c=c)
+        p[step], q[step] = p[step] + h * v, q[step] - h * v
+        numeric = float(L(**p) - L(**q)) / (2 * h)
+        exact = float((grad.double() * v).sum())
+        # the kinks crossed by relu within h change L by at most |Y| h |dz|: a few entries in 6600
+        tol = 1e-5 * float((grad.double() * v).abs().sum()) + (20 * h * float(Y.abs().max()) * float(v.abs().max()) * 40 if act == "relu" else 0.0)
+        assert abs(numeric - exact) <= tol
+
+
+def test_large_arguments_and_values_that_are_not_finite(il):
+    z = torch.tensor([-float("inf"), -1e30, -200.0, -89.0, -30.0, -0.0, 0.0, 30.0, 89.0, 200.0, 1e30, float("inf"), float("nan")], device="cuda")
+    one = torch.ones(1, 1, device="cuda")
+    X, ones = z[:, None].contiguous(), torch.ones(z.numel(), 1, device="cuda")
+    for act in ACTS[1:]:
+        got = il.ilargi_linear(X, one, act=act)[:, 0]
+        want = _f(z.double(), act)
+        want[0] = 0.0                                                # the limit at -infinity
+        if act == "relu":
+            want[-1] = float("nan")
+        fin = torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and bool(((got.double() - want).abs()[fin] <= 1e-6 * (1 + want.abs())[fin]).all())
+        assert float(got[11]) == (1.0 if act == "sigmoid" else float("inf"))
+        dz = il.ilargi_linear_grad(ones, X, one, pre=X, act=act)[0][:, 0]
+        assert bool(torch.isfinite(dz[1:-2]).all())
+        want = _slope(z.double(), act)[1:-2]
+        assert bool(((dz[1:-2].double() - want).abs() <= 1e-6).all())
+    # one row that holds NaN or infinity spoils itself only
+    gen = _gen(4)
+    for dtype in (F32, BF16):
+        for n, k, m in ((1, 64, 32), (6, 256, 64), (300, 96, 144)):
+            X, W = _matrix(n, k, dtype, gen), _matrix(k, m, dtype, gen)
+            X[n // 2, k // 3] = float("nan")
+            out = il.ilargi_linear(X, W)
+            bad = torch.isnan(out).any(1)
+            assert bool(bad[n // 2]) and int(bad.sum()) == 1 and bool(torch.isnan(out[n // 2]).all())
+            X[n // 2, k // 3] = float("inf")
+            out = il.ilargi_linear(X, W)
+            assert torch.equal(out[n // 2], torch.sign(W[k // 3]) * float("inf")) and int((~torch.isfinite(out)).any(1).sum()) == 1
+
+
+def test_parts_of_very_different_size(il):
+    """Columns of X in very different units against weights that undo them: every product counts."""
+    gen = _gen(9)
+    n, k, m = 140, 64, 72
+    unit = torch.logspace(-18, 18, k, device="cuda")
+    X, W = torch.randn(n, k, generator=gen, device="cuda") * unit, torch.randn(k, m, generator=gen, device="cuda") / unit[:, None]
+    out = il.ilargi_linear(X, W)
+    want, size = X.double() @ W.double(), X.double().abs() @ W.double().abs()
+    assert bool(((out.double() - want).abs() <= (k + 3) * E32 * size).all())
+
+
+def test_on_another_stream_and_in_a_graph(il):
+    gen = _gen(12)
+    n, k, m = 96, 200, 136
+    for dtype in (F32, BF16):
+        X, W, D = _matrix(n, k, dtype, gen), _matrix(k, m, dtype, gen, scale=0.1), _matrix(n, m, dtype, gen)
+        b = torch.randn(m, generator=gen, device="cuda").to(dtype)
+        out, pre = torch.empty(n, m, dtype=dtype, device="cuda"), torch.empty(n, m, dtype=dtype, device="cuda")
+        dX, dW, db = torch.empty_like(X), torch.empty_like(W), torch.empty_like(b)
+        fwd, bwd = il.ilargi_linear_workspace_bytes(n, k, m, dtype)
+        ws = torch.empty(max(fwd, bwd, 1), dtype=torch.uint8, device="cuda")
+
+        def step(stream=None):
+            il.ilargi_linear(X, W, bias=b, act="gelu", out=out, pre=pre, workspace=ws, stream=stream)
+            il.ilargi_linear_grad(D, X, W, pre=pre, act="gelu", d_X=dX, d_W=dW, d_bias=db, workspace=ws, stream=stream)
+
+        step()
+        want = [t.clone() for t in (out, pre, dX, dW, db)]
+        side = torch.cuda.Stream()
+        for t in (out, pre, dX, dW, db):
+            t.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        step(side)
+        side.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(want, (out, pre, dX, dW, db)))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        for _ in range(3):
+            X.copy_(torch.randn(n, k, generator=gen, device="cuda"))
+            step()
+            want = [t.clone() for t in (out, pre, dX, dW, db)]
+            for t in (out, pre, dX, dW, db):
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, c) for a, c in zip(want, (out, pre, dX, dW, db)))
+
+
+def test_refusals(il):
+    X, W = torch.zeros(4, 8, device="cuda"), torch.zeros(8, 6, device="cuda")
+    with pytest.raises(TypeError):
+        il.ilargi_linear(X.half(), W.half())
+    with pytest.raises(TypeError):
+        il.ilargi_linear(X, W.bfloat16())
+    with pytest.raises(ValueError):
+        il.ilargi_linear(X, torch.zeros(7, 6, device="cuda"))
+    with pytest.raises(ValueError):
+        il.ilargi_linear(X, W, bias=torch.zeros(5, device="cuda"))
+    with pytest.raises(ValueError):
+        il.ilargi_linear(X, W, act="tanh")
+    with pytest.raises(TypeError):
+        il.ilargi_linear(X, torch.zeros(6, 8, device="cuda").t())
+    with pytest.raises(ValueError):
+        il.ilargi_linear_grad(torch.zeros(4, 6, device="cuda"), X, W, act="relu")
+    with pytest.raises(ValueError):
+        il.ilargi_linear_grad(torch.zeros(4, 6, device="cuda"), X, W, accumulate=True)
+    with pytest.raises(il.IlargiError) as e:
+        il.ilargi_linear(X, W, act=9)
+    assert e.value.status == il.ERR_UNSUPPORTED
+    with pytest.raises(il.IlargiError) as e:
+        il.ilargi_linear_grad(torch.zeros(4, 6, device="cuda"), X, W, pre=torch.zeros(4, 6, device="cuda"), act="relu",
+                              workspace=torch.empty(256, dtype=torch.uint8, device="cuda")[:0])
+    assert e.value.status in (il.ERR_WORKSPACE, il.ERR_NULL)
