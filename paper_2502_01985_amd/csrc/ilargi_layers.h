@@ -143,6 +143,23 @@ struct Product {
 };
 hipError_t launch_mm_f32(const Product& a, hipStream_t st);
 
+// The same for 16-bit operands on the 16-bit matrix cores, with sums in float32.  An operand may be the sum of two planes,
+// hi + 2^-11 lo (`plane` elements apart, float16): then lo hi + hi lo + hi hi is formed, three products in place of one.
+struct Operand16 {
+  const void* p;
+  int64_t ld;
+  int k_rows;
+  int64_t batch, plane;
+};
+struct Product16 {
+  Operand16 P, Q;
+  int64_t M, N, K, batches;
+  int planes;           // 1: bfloat16 operands; 2: pairs of float16
+  Epilogue epi;
+};
+bool mm16_takes(const Operand16& x, int64_t across, int64_t K);
+hipError_t launch_mm16(const Product16& a, hipStream_t st);
+
 struct LayerGradArgs {
   int64_t n, m;
   const void* d_out;

@@ -64,6 +64,15 @@ LayerLayout layer_layout(const ilargi_layer_t& y) {
   return l;
 }
 
+// A product of the layer's matrices: bfloat16 operands that lie in whole 16-byte pieces on the 16-bit matrix cores, others in float32.
+hipError_t product(const Product& p, hipStream_t st) {
+  if (p.P.bf16) {
+    const Operand16 P = {p.P.p, p.P.ld, p.P.k_rows, p.P.batch, 0}, Q = {p.Q.p, p.Q.ld, p.Q.k_rows, p.Q.batch, 0};
+    if (mm16_takes(P, p.M, p.K) && mm16_takes(Q, p.N, p.K)) return launch_mm16({P, Q, p.M, p.N, p.K, p.batches, 1, p.epi}, st);
+  }
+  return launch_mm_f32(p, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -122,7 +131,7 @@ ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_
   p.epi.bias = bias; p.epi.src = residual; p.epi.ld_src = ld_res; p.epi.src_bf16 = h;
   p.epi.pre = pre; p.epi.ld_pre = ld_pre; p.epi.act = y.act;
   p.epi.out = out; p.epi.ld_out = ld_out; p.epi.out_bf16 = h;
-  return done("linear", launch_mm_f32(p, (hipStream_t)stream));
+  return done("linear", product(p, (hipStream_t)stream));
 }
 
 ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_out, int64_t ld_out, const void* pre, int64_t ld_pre,
@@ -154,7 +163,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     p.P = z;
     p.Q = {W, ld_w, 0, h, 0};
     p.epi.out = d_X; p.epi.ld_out = ld_dx;
-    if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return done("linear_grad", e);
+    if (hipError_t e = product(p, st); e != hipSuccess) return done("linear_grad", e);
   }
   if (d_W != nullptr) {
     p.M = y.k; p.N = y.m; p.K = y.n;
@@ -163,7 +172,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     p.Q.k_rows = 1;
     p.epi.out = d_W; p.epi.ld_out = ld_dw;
     if (accumulate) { p.epi.base = d_W; p.epi.s2 = 1.0f; }
-    if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return done("linear_grad", e);
+    if (hipError_t e = product(p, st); e != hipSuccess) return done("linear_grad", e);
   }
   return ILARGI_OK;
 }
