@@ -128,12 +128,14 @@ struct Epilogue {
   const void* src;
   int64_t ld_src, batch_src;
   int src_bf16;
+  int64_t src_plane;      // not 0: src is a pair of float16 planes so far apart
   void* pre;
   int64_t ld_pre;
   int act;
   void* out;
   int64_t ld_out, batch_out;
   int out_bf16;
+  int64_t out_plane;      // not 0: out is such a pair
   int flip;
 };
 struct Product {
@@ -145,20 +147,29 @@ hipError_t launch_mm_f32(const Product& a, hipStream_t st);
 
 // The same for 16-bit operands on the 16-bit matrix cores, with sums in float32.  An operand may be the sum of two planes,
 // hi + 2^-11 lo (`plane` elements apart, float16): then lo hi + hi lo + hi hi is formed, three products in place of one.
+// Rows and columns lie at 16-byte addresses and whole pieces of 8 elements may be read: `across` rows or columns (of i or j), and
+// along k up to the next multiple of 8, zeros behind K.
 struct Operand16 {
   const void* p;
   int64_t ld;
   int k_rows;
-  int64_t batch, plane;
+  int64_t batch, plane, across;
+};
+enum { kMm16Bf16 = 0, kMm16Pairs = 1 };     // bfloat16; pairs of float16 planes
+struct Mm16Plan {
+  int tile, splits;         // workgroups form tile x tile sums of a share of k
+  size_t partial_bytes;     // sums of the shares, where there are several
 };
 struct Product16 {
   Operand16 P, Q;
   int64_t M, N, K, batches;
-  int planes;           // 1: bfloat16 operands; 2: pairs of float16
+  int kind;
+  int symmetric;            // C = C^T: blocks above the diagonal are formed, and written twice
   Epilogue epi;
 };
-bool mm16_takes(const Operand16& x, int64_t across, int64_t K);
-hipError_t launch_mm16(const Product16& a, hipStream_t st);
+Mm16Plan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric);
+bool mm16_takes(const Operand& x, int64_t across, int64_t K);
+hipError_t launch_mm16(const Product16& a, const Mm16Plan& plan, float* partial, hipStream_t st);
 
 struct LayerGradArgs {
   int64_t n, m;

@@ -52,23 +52,34 @@ ilargi_status_t check_layer(const char* what, const ilargi_layer_t* y) {
 }
 
 struct LayerLayout {
-  size_t forward = 0;                          // bytes of the forward call
-  size_t dz = 0, partial = 0, gradient = 0;    // offsets and bytes of the gradient call
+  size_t forward = 0;                                         // bytes of the forward call
+  size_t dz = 0, partial = 0, shares = 0, gradient = 0;       // offsets and bytes of the gradient call
 };
 LayerLayout layer_layout(const ilargi_layer_t& y) {
   LayerLayout l;
-  const size_t b = y.type == ILARGI_TYPE_BF16 ? 2 : 4;
+  const bool h = y.type == ILARGI_TYPE_BF16;
+  if (h) l.forward = up256(mm16_plan(y.n, y.m, y.k, 1, kMm16Bf16, 0).partial_bytes);
   l.dz = 0;
-  l.partial = up256((size_t)y.n * (size_t)y.m * b);
-  l.gradient = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
+  l.partial = up256((size_t)y.n * (size_t)((y.m + 7) / 8 * 8) * (h ? 2 : 4));
+  l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
+  l.gradient = l.shares;
+  if (h) {
+    const size_t x = mm16_plan(y.n, y.k, y.m, 1, kMm16Bf16, 0).partial_bytes, w = mm16_plan(y.k, y.m, y.n, 1, kMm16Bf16, 0).partial_bytes;
+    l.gradient += up256(x > w ? x : w);
+  }
   return l;
 }
 
 // A product of the layer's matrices: bfloat16 operands that lie in whole 16-byte pieces on the 16-bit matrix cores, others in float32.
-hipError_t product(const Product& p, hipStream_t st) {
-  if (p.P.bf16) {
-    const Operand16 P = {p.P.p, p.P.ld, p.P.k_rows, p.P.batch, 0}, Q = {p.Q.p, p.Q.ld, p.Q.k_rows, p.Q.batch, 0};
-    if (mm16_takes(P, p.M, p.K) && mm16_takes(Q, p.N, p.K)) return launch_mm16({P, Q, p.M, p.N, p.K, p.batches, 1, p.epi}, st);
+hipError_t product(const Product& p, float* partial, hipStream_t st) {
+  if (p.P.bf16 && mm16_takes(p.P, p.M, p.K) && mm16_takes(p.Q, p.N, p.K)) {
+    Product16 a{};
+    a.P = {p.P.p, p.P.ld, p.P.k_rows, 0, 0, p.M};
+    a.Q = {p.Q.p, p.Q.ld, p.Q.k_rows, 0, 0, p.N};
+    a.M = p.M; a.N = p.N; a.K = p.K; a.batches = 1;
+    a.kind = kMm16Bf16;
+    a.epi = p.epi;
+    return launch_mm16(a, mm16_plan(p.M, p.N, p.K, 1, kMm16Bf16, 0), partial, st);
   }
   return launch_mm_f32(p, st);
 }
@@ -131,7 +142,7 @@ ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_
   p.epi.bias = bias; p.epi.src = residual; p.epi.ld_src = ld_res; p.epi.src_bf16 = h;
   p.epi.pre = pre; p.epi.ld_pre = ld_pre; p.epi.act = y.act;
   p.epi.out = out; p.epi.ld_out = ld_out; p.epi.out_bf16 = h;
-  return done("linear", product(p, (hipStream_t)stream));
+  return done("linear", product(p, (float*)workspace, (hipStream_t)stream));
 }
 
 ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_out, int64_t ld_out, const void* pre, int64_t ld_pre,
@@ -163,7 +174,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     p.P = z;
     p.Q = {W, ld_w, 0, h, 0};
     p.epi.out = d_X; p.epi.ld_out = ld_dx;
-    if (hipError_t e = product(p, st); e != hipSuccess) return done("linear_grad", e);
+    if (hipError_t e = product(p, (float*)(ws + l.shares), st); e != hipSuccess) return done("linear_grad", e);
   }
   if (d_W != nullptr) {
     p.M = y.k; p.N = y.m; p.K = y.n;
@@ -172,7 +183,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     p.Q.k_rows = 1;
     p.epi.out = d_W; p.epi.ld_out = ld_dw;
     if (accumulate) { p.epi.base = d_W; p.epi.s2 = 1.0f; }
-    if (hipError_t e = product(p, st); e != hipSuccess) return done("linear_grad", e);
+    if (hipError_t e = product(p, (float*)(ws + l.shares), st); e != hipSuccess) return done("linear_grad", e);
   }
   return ILARGI_OK;
 }

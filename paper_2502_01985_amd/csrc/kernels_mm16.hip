@@ -9,6 +9,8 @@
 //     transposing LDS read gives each lane its four k of one column.
 // LDS is filled in lane order, so the places are permuted by the addresses that the lanes fetch from.
 // The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
+#include <utility>
+
 #include "mm_epilogue.h"
 
 namespace ilargi {
@@ -25,9 +27,9 @@ constexpr int kBK = 64, kOutPad = 68;
 
 __device__ __attribute__((aligned(16))) const unsigned int kZeros[4] = {0, 0, 0, 0};   // what lies behind the end of k
 
-template <int PLANES>
+template <int KIND>
 __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
-  if constexpr (PLANES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  if constexpr (KIND != kMm16Bf16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
@@ -69,10 +71,11 @@ struct Tile {
     }
   }
   // `base`: the step's first element of the tile
-  __device__ __forceinline__ void fetch(const char* base, uint32_t to) const {
+  template <int FIRST, int COUNT>
+  __device__ __forceinline__ void fetch_some(const char* base, uint32_t to) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) fetch16(base, off[q], to + (uint32_t)(q * NT + wave * 64) * 16);
+    for (int q = FIRST; q < FIRST + COUNT && q < kLoads; ++q) fetch16(base, off[q], to + (uint32_t)(q * NT + wave * 64) * 16);
   }
   // the last step, of `left` k
   __device__ __forceinline__ void fetch_last(const char* base, uint32_t to, int left) const {
@@ -99,27 +102,29 @@ struct Fragments {
       at[0] = (uint32_t)((first + i) * 128);
     }
   }
-  __device__ __forceinline__ void read(uint32_t lds, int half, s16x8 (&v)[F]) const {
+  __device__ __forceinline__ s16x8 read(uint32_t lds, int half, int f) const {
     if constexpr (KROWS) {
-#pragma unroll
-      for (int f = 0; f < F; ++f) {
-        typedef __attribute__((address_space(3))) s16x4 l4;
-        const uint32_t p = lds + at[f] + half * 32 * R * 2;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(uintptr_t)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(uintptr_t)(p + 4 * R * 2));
-        v[f] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
+      typedef __attribute__((address_space(3))) s16x4 l4;
+      const uint32_t p = lds + at[f] + half * 32 * R * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(uintptr_t)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(uintptr_t)(p + 4 * R * 2));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       const int lane = threadIdx.x % 64;
       typedef __attribute__((address_space(3))) s16x8 l8;
       const uint32_t p = lds + at[0] + (uint32_t)(((half * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
-#pragma unroll
-      for (int f = 0; f < F; ++f) v[f] = *(const l8*)(uintptr_t)(p + f * 16 * 128);
+      return *(const l8*)(uintptr_t)(p + f * 16 * 128);
     }
   }
 };
 
-__device__ __forceinline__ void arrived_and_together() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the last LEFT fetches of every wavefront are in LDS, and all LDS reads done (0xc07f waits for those alone, in a form that
+// the compiler counts with: it would else wait for them again behind the next reads).
+template <int LEFT>
+__device__ __forceinline__ void arrived_and_together() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 
 // Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring blocks, walked eight rows of blocks at a time,
 // so that its L2 keeps the operand tiles they share.
@@ -132,50 +137,110 @@ __device__ __forceinline__ void block_of(int id, int tm, int tn, int* ti, int* t
   *tj = in / rows;
 }
 
-template <int PLANES, bool PK, bool QK, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void mm16_kernel(Product16 a, int tm, int tn) {
+// The n-th block on or above the diagonal of tn x tn blocks, row by row.
+__device__ __forceinline__ void upper_block(int id, int tn, int* ti, int* tj) {
+  int r = 0;
+  while (id >= tn - r) id -= tn - r++;
+  *ti = r;
+  *tj = r + id;
+}
+
+// What is done with four neighbouring sums of row i; `mirrored`: of a symmetric result, at their places below the diagonal.
+template <int KIND>
+__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, bool mirrored, f32x4 t) {
+  if (i >= M || j >= N) return;
+  const int valid = (int)(N - j < 4 ? N - j : 4);
+  float v[4] = {t[0], t[1], t[2], t[3]};
+  if constexpr (KIND != kMm16Bf16) {
+    if (e.out_plane != 0) {
+      if (mirrored) epilogue4_pairs_mirrored(e, b, i, j, valid, v);
+      else epilogue4_pairs(e, b, i, j, valid, v);
+      return;
+    }
+  }
+  epilogue4(e, b, i, j, valid, v);
+}
+
+// The products of the second half of a step, between them the fetches of a later step into the buffer that has become free
+// and the reads of the next step's first half.
+template <class TileP, class TileQ, int KIND, int FM, int FN, class FragP, class FragQ>
+__device__ __forceinline__ void second_half(bool fetching, const TileP& tp, const TileQ& tq, const char* from_p, const char* from_q, uint32_t to, const FragP& fp,
+                                            const FragQ& fq, uint32_t next, s16x8 (&p0)[FM], s16x8 (&q0)[FN], const s16x8 (&p1)[FM],
+                                            const s16x8 (&q1)[FN], f32x4 (&acc)[FM][FN]) {
+  constexpr int kP = (TileP::kLoads + FM - 1) / FM, kQ = (TileQ::kLoads + FM - 1) / FM;
+  q0[0] = fq.read(next + TileP::kBytes, 0, 0);
+  [&]<int... X>(std::integer_sequence<int, X...>) {
+    (
+        [&] {
+          p0[X] = fp.read(next, 0, X);
+          if constexpr (X + 1 < FN) q0[X + 1] = fq.read(next + TileP::kBytes, 0, X + 1);
+          if (fetching) {
+            tp.template fetch_some<X * kP, kP>(from_p, to);
+            tq.template fetch_some<X * kQ, kQ>(from_q, to + TileP::kBytes);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int y = 0; y < FN; ++y) acc[X][y] = mfma16<KIND>(q1[y], p1[X], acc[X][y]);
+          __builtin_amdgcn_sched_barrier(0);
+        }(),
+        ...);
+  }(std::make_integer_sequence<int, FM>());
+}
+
+// blockIdx: block, matrix of the batch, share of k.  With several shares the sums go to `partial`, one M x (N to a multiple of 4)
+// matrix after the other.
+template <int KIND, bool PK, bool QK, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64)) void mm16_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
   constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
   using TileP = Tile<PK, BM, NT>;
   using TileQ = Tile<QK, BN, NT>;
   static_assert(TN == 64 && TM % 64 == 0, "wavefronts of 64 columns and whole 64 rows");
-  constexpr int kTiles = 2 * (TileP::kBytes + TileQ::kBytes), kOut = NT * kOutPad * 4;
+  constexpr int kTiles = STAGES * (TileP::kBytes + TileQ::kBytes), kOut = NT * kOutPad * 4;
   __shared__ __attribute__((aligned(1024))) char lds_all[kTiles > kOut ? kTiles : kOut];
   char(*lds)[TileP::kBytes + TileQ::kBytes] = reinterpret_cast<char(*)[TileP::kBytes + TileQ::kBytes]>(lds_all);
   int ti, tj;
-  block_of(blockIdx.x, tm, tn, &ti, &tj);
+  if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
+  else block_of(blockIdx.x, tm, tn, &ti, &tj);
   const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN, b = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wi = (wave / WN) * TM, wj = (wave % WN) * TN;
-  const char* P = (const char*)a.P.p + 2 * (b * a.P.batch + (PK ? i0 : i0 * a.P.ld));
-  const char* Q = (const char*)a.Q.p + 2 * (b * a.Q.batch + (QK ? j0 : j0 * a.Q.ld));
   const int64_t step_p = PK ? kBK * a.P.ld * 2 : kBK * 2, step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
+  const int first = (int)blockIdx.z * share, ks_all = (int)((a.K + kBK - 1) / kBK), ks = ks_all - first < share ? ks_all - first : share;
+  const char* P = (const char*)a.P.p + 2 * (b * a.P.batch + (PK ? i0 : i0 * a.P.ld)) + first * step_p;
+  const char* Q = (const char*)a.Q.p + 2 * (b * a.Q.batch + (QK ? j0 : j0 * a.Q.ld)) + first * step_q;
   TileP tp;
   TileQ tq;
-  tp.plan(a.P.ld, a.M - i0);
-  tq.plan(a.Q.ld, a.N - j0);
+  tp.plan(a.P.ld, a.P.across - i0);
+  tq.plan(a.Q.ld, a.Q.across - j0);
   Fragments<PK, BM, FM> fp;
   Fragments<QK, BN, FN> fq;
   fp.plan(wi);
   fq.plan(wj);
-  const int ks = (int)((a.K + kBK - 1) / kBK), steps = PLANES == 2 ? 3 * ks : ks;
-  const bool whole = a.K % kBK == 0;
-  auto fetch = [&](int t) {
+  const int steps = KIND == kMm16Pairs ? 3 * ks : ks;
+  const bool whole = a.K % kBK == 0 || first + ks < ks_all;
+  // Where step t's pieces come from, and the k that its last step has.
+  auto source = [&](int t, const char** p, const char** q) {
     int k = t;
-    const char *p = P, *q = Q;
-    if constexpr (PLANES == 2) {
+    *p = P; *q = Q;
+    if constexpr (KIND == kMm16Pairs) {
       const int part = t / ks;                       // lo hi, hi lo, hi hi
       k = t - part * ks;
-      if (part == 0) p += 2 * a.P.plane;
-      if (part == 1) q += 2 * a.Q.plane;
+      if (part == 0) *p += 2 * a.P.plane;
+      if (part == 1) *q += 2 * a.Q.plane;
     }
-    const uint32_t to = lds_address(lds[t & 1]);
-    p += k * step_p;
-    q += k * step_q;
-    if (k + 1 < ks || whole) {
-      tp.fetch(p, to);
-      tq.fetch(q, to + TileP::kBytes);
+    *p += k * step_p;
+    *q += k * step_q;
+    return k + 1 < ks || whole ? kBK : (int)(a.K - (int64_t)(first + k) * kBK);
+  };
+  auto fetch = [&](int t) {
+    const char *p, *q;
+    const int left = source(t, &p, &q);
+    const uint32_t to = lds_address(lds[t % STAGES]);
+    if (left == kBK) {
+      tp.template fetch_some<0, TileP::kLoads>(p, to);
+      tq.template fetch_some<0, TileQ::kLoads>(q, to + TileP::kBytes);
     } else {
-      tp.fetch_last(p, to, (int)(a.K - (int64_t)k * kBK));
-      tq.fetch_last(q, to + TileP::kBytes, (int)(a.K - (int64_t)k * kBK));
+      tp.fetch_last(p, to, left);
+      tq.fetch_last(q, to + TileP::kBytes, left);
     }
   };
   f32x4 acc[FM][FN];
@@ -184,16 +249,17 @@ __global__ __launch_bounds__(WM* WN * 64) void mm16_kernel(Product16 a, int tm, 
 #pragma unroll
     for (int y = 0; y < FN; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
   s16x8 p0[FM], q0[FN], p1[FM], q1[FN];
-  if (steps > 0) fetch(0);
-  arrived_and_together();
-  if (steps > 1) fetch(1);
-  if (steps > 0) {
-    fp.read(lds_address(lds[0]), 0, p0);
-    fq.read(lds_address(lds[0]) + TileP::kBytes, 0, q0);
-  }
+  constexpr int kEach = TileP::kLoads + TileQ::kLoads;
+  for (int t = 0; t < STAGES && t < steps; ++t) fetch(t);
+  if (steps >= STAGES) arrived_and_together<kEach*(STAGES - 1)>();
+  else arrived_and_together<0>();
+#pragma unroll
+  for (int y = 0; y < FN; ++y) q0[y] = fq.read(lds_address(lds[0]) + TileP::kBytes, 0, y);
+#pragma unroll
+  for (int x = 0; x < FM; ++x) p0[x] = fp.read(lds_address(lds[0]), 0, x);
   for (int t = 0; t < steps; ++t) {
-    const uint32_t here = lds_address(lds[t & 1]), next = lds_address(lds[(t & 1) ^ 1]);
-    if constexpr (PLANES == 2) {
+    const uint32_t here = lds_address(lds[t % STAGES]), next = lds_address(lds[(t + 1) % STAGES]);
+    if constexpr (KIND == kMm16Pairs) {
       if (t == 2 * ks) {
 #pragma unroll
         for (int x = 0; x < FM; ++x)
@@ -201,22 +267,26 @@ __global__ __launch_bounds__(WM* WN * 64) void mm16_kernel(Product16 a, int tm, 
           for (int y = 0; y < FN; ++y) acc[x][y] *= 0x1p-11f;
       }
     }
-    fp.read(here, 1, p1);
-    fq.read(here + TileP::kBytes, 1, q1);
+    // A wavefront issues in order: the reads of the second half stand between the products of the first, else the matrix cores
+    // would wait for their issue.
+    q1[0] = fq.read(here + TileP::kBytes, 1, 0);
 #pragma unroll
-    for (int x = 0; x < FM; ++x)
+    for (int x = 0; x < FM; ++x) {
+      p1[x] = fp.read(here, 1, x);
+      if (x + 1 < FN) q1[x + 1] = fq.read(here + TileP::kBytes, 1, x + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int y = 0; y < FN; ++y) acc[x][y] = mfma16<PLANES>(q0[y], p0[x], acc[x][y]);
-    arrived_and_together();                          // step t is in registers, step t + 1 in LDS
-    if (t + 2 < steps) fetch(t + 2);
-    if (t + 1 < steps) {
-      fp.read(next, 0, p0);
-      fq.read(next + TileP::kBytes, 0, q0);
+      for (int y = 0; y < FN; ++y) acc[x][y] = mfma16<KIND>(q0[y], p0[x], acc[x][y]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int x = 0; x < FM; ++x)
-#pragma unroll
-      for (int y = 0; y < FN; ++y) acc[x][y] = mfma16<PLANES>(q1[y], p1[x], acc[x][y]);
+    // step t is in registers, step t + 1 in LDS
+    if (t + STAGES <= steps) arrived_and_together<kEach*(STAGES - 2)>();
+    else arrived_and_together<0>();
+    const char *from_p = P, *from_q = Q;
+    const int left = t + STAGES < steps ? source(t + STAGES, &from_p, &from_q) : 0;
+    // the next step's first half between the products of the second (behind the last step: of an old one, for nothing)
+    if (left > 0 && left < kBK) fetch(t + STAGES);
+    second_half<TileP, TileQ, KIND, FM, FN>(left == kBK, tp, tq, from_p, from_q, here, fp, fq, next, p0, q0, p1, q1, acc);
   }
   // The sums go through LDS, 64 rows of a wavefront at a time, so that stores run along the result's rows.
   const int lane = threadIdx.x % 64;
@@ -231,15 +301,27 @@ __global__ __launch_bounds__(WM* WN * 64) void mm16_kernel(Product16 a, int tm, 
         *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[4 * h + x][y];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    // a row of 64 columns takes 16 lanes; a flipped result is written along its own rows, which run over i
+    const int64_t ri = i0 + wi + 64 * h, cj = j0 + wj;
+    if (partial != nullptr) {
+      const int64_t ldp = (a.N + 3) / 4 * 4;
+      float* part = partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp;
 #pragma unroll 1
-    for (int q = 0; q < 16; ++q) {
-      const int r = a.epi.flip ? lane : 4 * q + (lane >> 4), c = a.epi.flip ? 4 * q : (lane & 15) * 4;
-      const f32x4 t = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
-      const int64_t i = i0 + wi + 64 * h + r, j = j0 + wj + c;
-      if (i < a.M && j < a.N) {
-        float v[4] = {t[0], t[1], t[2], t[3]};
-        epilogue4(a.epi, b, i, j, (int)(a.N - j < 4 ? a.N - j : 4), v);
+      for (int q = 0; q < 16; ++q) {
+        const int r = 4 * q + (lane >> 4), c = (lane & 15) * 4;
+        if (ri + r < a.M && cj + c < a.N) *reinterpret_cast<f32x4*>(part + (ri + r) * ldp + cj + c) = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
+      }
+    } else {
+      // a row of 64 columns takes 16 lanes; a flipped result is written along its own rows, which run over i
+      if (!a.epi.flip) {
+#pragma unroll 1
+        for (int q = 0; q < 16; ++q) {
+          const int r = 4 * q + (lane >> 4), c = (lane & 15) * 4;
+          emit4<KIND>(a.epi, b, ri + r, cj + c, a.M, a.N, false, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
+        }
+      }
+      if (a.epi.flip || (a.symmetric && ti != tj)) {
+#pragma unroll 1
+        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, cj + 4 * q, a.M, a.N, true, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -247,34 +329,103 @@ __global__ __launch_bounds__(WM* WN * 64) void mm16_kernel(Product16 a, int tm, 
   }
 }
 
-template <int PLANES, bool PK, bool QK>
-hipError_t mm16_order(const Product16& a, hipStream_t st) {
-  const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
-  if (tm * tn * a.batches >= 160) {
-    mm16_kernel<PLANES, PK, QK, 256, 256, 2, 4><<<dim3((unsigned)(tm * tn), (unsigned)a.batches), 512, 0, st>>>(a, (int)tm, (int)tn);
-  } else {
-    const int64_t sm = (a.M + 127) / 128, sn = (a.N + 127) / 128;
-    mm16_kernel<PLANES, PK, QK, 128, 128, 2, 2><<<dim3((unsigned)(sm * sn), (unsigned)a.batches), 256, 0, st>>>(a, (int)sm, (int)sn);
+// Adds the shares of k in their order and finishes: 64 x 64 sums a workgroup, those on and above the diagonal of a symmetric
+// result.
+template <int KIND>
+__global__ __launch_bounds__(256) void mm16_join_kernel(Product16 a, int tn, int splits, const float* __restrict__ partial) {
+  __shared__ __attribute__((aligned(16))) float tile[64][kOutPad];
+  int ti, tj;
+  if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
+  else { ti = blockIdx.x / tn; tj = blockIdx.x % tn; }
+  const int64_t b = blockIdx.y, i0 = (int64_t)ti * 64, j0 = (int64_t)tj * 64, ldp = (a.N + 3) / 4 * 4, far = a.batches * a.M * ldp;
+  const int row = threadIdx.x / 16, c = (threadIdx.x % 16) * 4;
+  const bool turned = a.epi.flip || (a.symmetric && ti != tj);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = 16 * q + row;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (i0 + r < a.M && j0 + c < a.N) {
+      const float* p = partial + b * a.M * ldp + (i0 + r) * ldp + j0 + c;
+      for (int z = 0; z < splits; ++z) s += *reinterpret_cast<const f32x4*>(p + z * far);
+    }
+    if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, s);
+    if (turned) *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
+  }
+  if (!turned) return;
+  __syncthreads();
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int cc = 16 * wave + 4 * q;
+    emit4<KIND>(a.epi, b, i0 + lane, j0 + cc, a.M, a.N, true, *reinterpret_cast<const f32x4*>(&tile[lane][cc]));
+  }
+}
+
+int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {
+  const int64_t tm = (M + tile - 1) / tile, tn = (N + tile - 1) / tile;
+  return symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+template <int KIND, bool PK, bool QK>
+hipError_t mm16_order(const Product16& a, const Mm16Plan& plan, float* partial, hipStream_t st) {
+  const int tm = (int)((a.M + plan.tile - 1) / plan.tile), tn = (int)((a.N + plan.tile - 1) / plan.tile);
+  const int ks = (int)((a.K + kBK - 1) / kBK), share = (ks + plan.splits - 1) / plan.splits;
+  const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, a.symmetric), (unsigned)a.batches, (unsigned)plan.splits);
+  float* part = plan.splits > 1 ? partial : nullptr;
+  if (plan.tile == 256) mm16_kernel<KIND, PK, QK, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a, tm, tn, share, part);
+  else mm16_kernel<KIND, PK, QK, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a, tm, tn, share, part);
+  if (part != nullptr) {
+    const dim3 join((unsigned)blocks_of(a.M, a.N, 64, a.symmetric), (unsigned)a.batches);
+    mm16_join_kernel<KIND><<<join, 256, 0, st>>>(a, (int)((a.N + 63) / 64), plan.splits, part);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Blocks of 256 or 128 and the shares of k, by what they cost in microseconds: a step of a 256-block takes 1.7 (one workgroup fits a
+// compute unit), of a 128-block 0.75 alone on its unit and 1.08 beside another; shares are written and added at 8 TB/s, in a launch
+// of 3.  Measured: 2048 x 2048 x 2048 in pairs, 128-blocks: 84 us in one share, 62 in two, 72 in four; 1024 x 1024 x 4096, bfloat16:
+// 50, 27 (four), 32 (eight); 4096 x 4096 x 4096, bfloat16: 117 in 256-blocks.
+Mm16Plan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric) {
+  Mm16Plan best{256, 1, 0};
+  double least = 1e300;
+  const int64_t ks = (K + kBK - 1) / kBK, parts = kind == kMm16Pairs ? 3 : 1;
+  for (int tile = 256; tile >= 128; tile /= 2) {
+    const int64_t blocks = blocks_of(M, N, tile, symmetric) * batches;
+    for (int64_t splits = 1; splits <= 32 && splits <= (ks > 0 ? ks : 1); ++splits) {
+      const int64_t share = (ks + splits - 1) / splits;
+      if (splits > 1 && ((ks + share - 1) / share != splits || share * parts < 4 || blocks * splits > 1024)) continue;   // no empty shares, no tiny ones
+      const int64_t groups = blocks * splits;
+      double step;
+      if (tile == 256) step = 1.7 * (double)((groups + 255) / 256);
+      else step = 1.08 * (double)(groups / 512) + (groups % 512 == 0 ? 0.0 : groups % 512 <= 256 ? 0.75 : 1.08);
+      double cost = (double)(share * parts) * step;
+      const double bytes = (double)splits * (double)batches * (double)M * (double)((N + 3) / 4 * 4) * 4.0;
+      if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;
+      if (cost < least) {
+        least = cost;
+        best = {tile, (int)splits, splits > 1 ? (size_t)bytes : 0};
+      }
+    }
+  }
+  return best;
+}
+
 // Whether the kernel reads this operand as it lies: 16-byte pieces that begin at 16-byte addresses and end with the matrix,
 // offsets within a tile of 32 bits.
-bool mm16_takes(const Operand16& x, int64_t across, int64_t K) {
+bool mm16_takes(const Operand& x, int64_t across, int64_t K) {
   return reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld % 8 == 0 && x.ld < (1 << 22) && (x.k_rows ? across : K) % 8 == 0;
 }
 
-hipError_t launch_mm16(const Product16& a, hipStream_t st) {
+hipError_t launch_mm16(const Product16& a, const Mm16Plan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
-  if (a.planes == 1) {
-    if (a.P.k_rows) return a.Q.k_rows ? mm16_order<1, true, true>(a, st) : hipErrorInvalidValue;
-    return a.Q.k_rows ? mm16_order<1, false, true>(a, st) : mm16_order<1, false, false>(a, st);
+  if (a.kind == kMm16Bf16) {
+    if (a.P.k_rows) return a.Q.k_rows ? mm16_order<kMm16Bf16, true, true>(a, plan, partial, st) : hipErrorInvalidValue;
+    return a.Q.k_rows ? mm16_order<kMm16Bf16, false, true>(a, plan, partial, st) : mm16_order<kMm16Bf16, false, false>(a, plan, partial, st);
   }
   if (a.P.k_rows) return hipErrorInvalidValue;
-  return a.Q.k_rows ? mm16_order<2, false, true>(a, st) : mm16_order<2, false, false>(a, st);
+  return a.Q.k_rows ? mm16_order<kMm16Pairs, false, true>(a, plan, partial, st) : mm16_order<kMm16Pairs, false, false>(a, plan, partial, st);
 }
 
 }  // namespace ilargi

@@ -7,6 +7,9 @@ namespace {
 
 constexpr int kNormParts = 64;
 
+// The pairs hold kUnit X, kUnit A and kUnit B: float16 keeps all eleven bits of its plane from 2.4e-7 to 255 then.
+constexpr float kUnit = 256.0f;
+
 // Sums of squares of a share of one matrix's rows, in 64 bits: the norm neither overflows nor loses small entries.
 template <class T>
 __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a, double* __restrict__ parts) {
@@ -25,9 +28,11 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a, double* __
   if (threadIdx.x == 0) parts[blockIdx.y * kNormParts + blockIdx.x] = (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]);
 }
 
-// X (short side x long side) = G or its transpose over the norm, 32 x 32 tiles through LDS.
-template <class T>
-__global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const double* __restrict__ parts, float* __restrict__ X, int tiles_c) {
+// X (short side x long side) = G or its transpose over the norm, 32 x 32 tiles through LDS; zeros up to `rows_x` x `ld_x`.
+// In pairs of float16 planes, X is held times kUnit.
+template <class T, bool PAIRS>
+__global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const double* __restrict__ parts, void* __restrict__ out, int64_t rows_x, int64_t ld_x,
+                                                         int tiles_c) {
   __shared__ float tile[32][33];
   __shared__ float scale;
   const int64_t b = blockIdx.y;
@@ -37,52 +42,128 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
     if (threadIdx.x == 0) scale = (float)(1.0 / (sqrt(s) + (double)a.eps));
   }
   const T* G = (const T*)a.G + b * a.batch_g;
-  const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * 32, c0 = (int64_t)(blockIdx.x % tiles_c) * 32;
+  const bool flip = a.rows > a.cols;
+  const int64_t y0 = (int64_t)(blockIdx.x / tiles_c) * 32, x0 = (int64_t)(blockIdx.x % tiles_c) * 32;     // of X
+  const int64_t r0 = flip ? x0 : y0, c0 = flip ? y0 : x0;                                                 // of G
   const int x = threadIdx.x % 32, y = threadIdx.x / 32;
 #pragma unroll
-  for (int q = 0; q < 32; q += 8)
-    if (r0 + y + q < a.rows && c0 + x < a.cols) tile[y + q][x] = (float)G[(r0 + y + q) * a.ld_g + c0 + x];
+  for (int q = 0; q < 32; q += 8) {
+    const int64_t r = r0 + y + q, c = c0 + x;
+    tile[y + q][x] = r < a.rows && c < a.cols ? (float)G[r * a.ld_g + c] : 0.0f;
+  }
   __syncthreads();
-  X += b * a.rows * a.cols;
-  const bool flip = a.rows > a.cols;
 #pragma unroll
   for (int q = 0; q < 32; q += 8) {
-    if (flip) {
-      if (c0 + y + q < a.cols && r0 + x < a.rows) X[(c0 + y + q) * a.rows + r0 + x] = tile[x][y + q] * scale;
-    } else {
-      if (r0 + y + q < a.rows && c0 + x < a.cols) X[(r0 + y + q) * a.cols + c0 + x] = tile[y + q][x] * scale;
-    }
+    if (y0 + y + q >= rows_x || x0 + x >= ld_x) continue;
+    const int64_t at = (b * rows_x + y0 + y + q) * ld_x + x0 + x;
+    const float v = (flip ? tile[x][y + q] : tile[y + q][x]) * scale;
+    if constexpr (PAIRS) pair_store((_Float16*)out, at, a.batch * rows_x * ld_x, v * kUnit);
+    else ((float*)out)[at] = v;
   }
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-}  // namespace
-
-size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols) {
-  const size_t s = (size_t)(rows < cols ? rows : cols), l = (size_t)(rows < cols ? cols : rows), n = (size_t)batch;
-  return up256(n * kNormParts * 8) + 2 * up256(4 * n * s * l) + 2 * up256(4 * n * s * s);
+// Whether the iteration stays where pairs of float16 hold it: some interval [0, R] that holds the first singular values (at
+// most 1) is mapped into [-R, R] by s (a + b s^2 + c s^4), and the entries of B, at most |b| R^2 + |c| R^4, are below 200.
+bool stays_bounded(const float* coef) {
+  const double a = coef[0], b = coef[1], c = coef[2];
+  for (int q = 0; q <= 40; ++q) {
+    const double R = 1.0 + 0.025 * q;
+    double top = 0.0;
+    bool number = true;
+    for (int k = 0; k <= 1000; ++k) {
+      const double s = R * k / 1000.0, v = s * (a + b * s * s + c * s * s * s * s);
+      if (!(v == v)) number = false;
+      if (v > top) top = v;
+      if (-v > top) top = -v;
+    }
+    if (number && top <= R && (b < 0 ? -b : b) * R * R + (c < 0 ? -c : c) * R * R * R * R < 200.0) return true;
+  }
+  return false;
 }
 
-hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st) {
-  if (a.batch == 0) return hipSuccess;
-  const int64_t s = a.rows < a.cols ? a.rows : a.cols, l = a.rows < a.cols ? a.cols : a.rows;
-  double* parts = (double*)ws;
-  ws += up256((size_t)a.batch * kNormParts * 8);
-  float* X[2] = {(float*)ws, (float*)(ws + up256(4 * (size_t)(a.batch * s * l)))};
-  ws += 2 * up256(4 * (size_t)(a.batch * s * l));
-  float *A = (float*)ws, *B = (float*)(ws + up256(4 * (size_t)(a.batch * s * s)));
-  const int tc = (int)((a.cols + 31) / 32);
-  const dim3 tiles((unsigned)((a.rows + 31) / 32 * tc), (unsigned)a.batch), norms(kNormParts, (unsigned)a.batch);
-  if (a.g_bf16) {
-    ortho_norm_kernel<bf16_t><<<norms, 256, 0, st>>>(a, parts);
-    ortho_load_kernel<bf16_t><<<tiles, 256, 0, st>>>(a, parts, X[0], tc);
-  } else {
-    ortho_norm_kernel<float><<<norms, 256, 0, st>>>(a, parts);
-    ortho_load_kernel<float><<<tiles, 256, 0, st>>>(a, parts, X[0], tc);
-  }
+struct OrthoLayout {
+  int64_t s, l, sp, lp;                 // short and long side, and the same up to a multiple of 8
+  Mm16Plan gram, square, apply;
+  size_t x[2], A, B, partial, total;
+};
+OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
+  OrthoLayout o{};
+  o.s = rows < cols ? rows : cols;
+  o.l = rows < cols ? cols : rows;
+  o.sp = (o.s + 7) / 8 * 8;
+  o.lp = (o.l + 7) / 8 * 8;
+  o.gram = mm16_plan(o.sp, o.sp, o.lp, batch, kMm16Pairs, 1);
+  o.square = mm16_plan(o.sp, o.sp, o.sp, batch, kMm16Pairs, 1);
+  o.apply = mm16_plan(o.sp, o.lp, o.sp, batch, kMm16Pairs, 0);
+  size_t at = up256((size_t)batch * kNormParts * 8);
+  auto take = [&at](size_t bytes) { const size_t p = at; at += up256(bytes); return p; };
+  o.x[0] = take(4 * (size_t)(batch * o.sp * o.lp));
+  o.x[1] = take(4 * (size_t)(batch * o.sp * o.lp));
+  o.A = take(4 * (size_t)(batch * o.sp * o.sp));
+  o.B = take(4 * (size_t)(batch * o.sp * o.sp));
+  size_t most = o.gram.partial_bytes;
+  if (o.square.partial_bytes > most) most = o.square.partial_bytes;
+  if (o.apply.partial_bytes > most) most = o.apply.partial_bytes;
+  o.partial = take(most);
+  o.total = at;
+  return o;
+}
+
+// The last product of the last step writes the result.
+void finish(const OrthoArgs& a, float unit, Epilogue* e) {
+  e->s0 *= a.alpha / unit;
+  e->s1 *= a.alpha / unit;
+  e->s2 = a.beta;
+  e->base = a.beta != 0.0f ? a.base : nullptr;
+  e->out = a.out; e->ld_out = a.ld_out; e->batch_out = a.batch_out; e->out_bf16 = a.out_bf16; e->out_plane = 0;
+  e->flip = a.rows > a.cols;
+}
+
+hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipStream_t st) {
+  float* partial = (float*)(ws + o.partial);
+  const int64_t px = a.batch * o.sp * o.lp, pa = a.batch * o.sp * o.sp;
+  void *A = ws + o.A, *B = ws + o.B;
   for (int t = 0; t < a.steps; ++t) {
-    const float* x = X[t & 1];
+    void *x = ws + o.x[t & 1], *next = ws + o.x[(t & 1) ^ 1];
+    Product16 p{};
+    p.kind = kMm16Pairs;
+    p.batches = a.batch;
+    p.M = o.sp; p.N = o.sp; p.K = o.lp; p.symmetric = 1;
+    p.P = {x, o.lp, 0, o.sp * o.lp, px, o.sp};
+    p.Q = p.P;
+    p.epi.mode = kEpiScale;
+    p.epi.s0 = 1.0f / kUnit;
+    p.epi.out = A; p.epi.ld_out = o.sp; p.epi.batch_out = o.sp * o.sp; p.epi.out_plane = pa;
+    if (hipError_t e = launch_mm16(p, o.gram, partial, st); e != hipSuccess) return e;
+    p.K = o.sp;
+    p.P = {A, o.sp, 0, o.sp * o.sp, pa, o.sp};
+    p.Q = p.P;
+    p.epi.s0 = a.coef[2] / kUnit; p.epi.s1 = a.coef[1];
+    p.epi.src = A; p.epi.ld_src = o.sp; p.epi.batch_src = o.sp * o.sp; p.epi.src_plane = pa;
+    p.epi.out = B;
+    if (hipError_t e = launch_mm16(p, o.square, partial, st); e != hipSuccess) return e;
+    p.N = o.lp; p.symmetric = 0;
+    p.P.p = B;
+    p.Q = {x, o.lp, 1, o.sp * o.lp, px, o.lp};
+    p.epi.s0 = 1.0f / kUnit; p.epi.s1 = a.coef[0];
+    p.epi.src = x; p.epi.ld_src = o.lp; p.epi.batch_src = o.sp * o.lp; p.epi.src_plane = px;
+    p.epi.out = next; p.epi.ld_out = o.lp; p.epi.batch_out = o.sp * o.lp; p.epi.out_plane = px;
+    if (t + 1 == a.steps) {
+      finish(a, kUnit, &p.epi);
+      p.M = o.s; p.N = o.l;
+    }
+    if (hipError_t e = launch_mm16(p, o.apply, partial, st); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipStream_t st) {
+  float *A = (float*)(ws + o.A), *B = (float*)(ws + o.B);
+  const int64_t s = o.s, l = o.l;
+  for (int t = 0; t < a.steps; ++t) {
+    float *x = (float*)(ws + o.x[t & 1]), *next = (float*)(ws + o.x[(t & 1) ^ 1]);
     Product p{};
     p.M = s; p.N = s; p.K = l; p.batches = a.batch;
     p.P = {x, l, 0, 0, s * l};
@@ -102,15 +183,35 @@ hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st) {
     p.Q = {x, l, 1, 0, s * l};
     p.epi.s0 = 1.0f; p.epi.s1 = a.coef[0];
     p.epi.src = x; p.epi.ld_src = l; p.epi.batch_src = s * l;
-    p.epi.out = X[(t & 1) ^ 1]; p.epi.ld_out = l; p.epi.batch_out = s * l;
-    if (t + 1 == a.steps) {
-      p.epi.s0 = a.alpha; p.epi.s1 = a.alpha * a.coef[0]; p.epi.s2 = a.beta; p.epi.base = a.beta != 0.0f ? a.base : nullptr;
-      p.epi.out = a.out; p.epi.ld_out = a.ld_out; p.epi.batch_out = a.batch_out; p.epi.out_bf16 = a.out_bf16;
-      p.epi.flip = a.rows > a.cols;
-    }
+    p.epi.out = next; p.epi.ld_out = l; p.epi.batch_out = s * l;
+    if (t + 1 == a.steps) finish(a, 1.0f, &p.epi);
     if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
+}
+
+template <class T>
+hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
+  const OrthoLayout o = ortho_layout(a.batch, a.rows, a.cols);
+  double* parts = (double*)ws;
+  const bool pairs = stays_bounded(a.coef);
+  const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;
+  const int tc = (int)((ld_x + 31) / 32);
+  const dim3 tiles((unsigned)((rows_x + 31) / 32 * tc), (unsigned)a.batch), norms(kNormParts, (unsigned)a.batch);
+  ortho_norm_kernel<T><<<norms, 256, 0, st>>>(a, parts);
+  if (pairs) ortho_load_kernel<T, true><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
+  else ortho_load_kernel<T, false><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  return pairs ? iterate_pairs(a, o, ws, st) : iterate_f32(a, o, ws, st);
+}
+
+}  // namespace
+
+size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols) { return ortho_layout(batch, rows, cols).total; }
+
+hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st) {
+  if (a.batch == 0) return hipSuccess;
+  return a.g_bf16 ? ortho_typed<bf16_t>(a, ws, st) : ortho_typed<float>(a, ws, st);
 }
 
 }  // namespace ilargi

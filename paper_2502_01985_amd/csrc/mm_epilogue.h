@@ -15,6 +15,42 @@ __device__ __forceinline__ void store4_any(void* p, int64_t at, int bf16, int va
   else store_piece<float, 4>((float*)p + at, valid, f);
 }
 
+// A pair of float16 planes: x = hi + 2^-11 lo, 22 bits.
+__device__ __forceinline__ float pair_value(const _Float16* p, int64_t at, int64_t plane) { return fmaf((float)p[at + plane], 0x1p-11f, (float)p[at]); }
+__device__ __forceinline__ void pair_store(_Float16* p, int64_t at, int64_t plane, float x) {
+  const _Float16 hi = (_Float16)x;
+  p[at] = hi;
+  p[at + plane] = (_Float16)((x - (float)hi) * 0x1p11f);
+}
+
+// out(i, j) = s0 v + s1 src(i, j) in pairs, columns j .. j + valid.
+__device__ __forceinline__ void epilogue4_pairs(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, float (&v)[4]) {
+  const _Float16* src = (const _Float16*)e.src + b * e.batch_src + i * e.ld_src + j;
+  _Float16* out = (_Float16*)e.out + b * e.batch_out + i * e.ld_out + j;
+  float t[4] = {0.f, 0.f, 0.f, 0.f}, hi[4], lo[4];
+  if (e.src != nullptr) {
+    load_piece<_Float16, 4>(src, valid, hi);
+    load_piece<_Float16, 4>(src + e.src_plane, valid, lo);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = fmaf(lo[q], 0x1p-11f, hi[q]);
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float x = fmaf(e.s0, v[q], e.s1 * t[q]);
+    hi[q] = (float)(_Float16)x;
+    lo[q] = (x - hi[q]) * 0x1p11f;
+  }
+  store_piece<_Float16, 4>(out, valid, hi);
+  store_piece<_Float16, 4>(out + e.out_plane, valid, lo);
+}
+// The same values at (j .. j + valid, i), for a symmetric src: lanes next to each other hold neighbouring i.
+__device__ __forceinline__ void epilogue4_pairs_mirrored(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&v)[4]) {
+  for (int q = 0; q < valid && q < 4; ++q) {
+    const float t = e.src != nullptr ? pair_value((const _Float16*)e.src, b * e.batch_src + (j + q) * e.ld_src + i, e.src_plane) : 0.0f;
+    pair_store((_Float16*)e.out, b * e.batch_out + (j + q) * e.ld_out + i, e.out_plane, fmaf(e.s0, v[q], e.s1 * t));
+  }
+}
+
 // Columns j .. j + valid of row i of matrix b of the batch.
 __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, float (&v)[4]) {
   if (e.mode == kEpiLinear) {
@@ -42,7 +78,13 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
   for (int q = 0; q < 4; ++q) v[q] *= e.s0;
   if (e.src != nullptr) {
     float t[4];
-    load4_any(e.src, b * e.batch_src + i * e.ld_src + j, e.src_bf16, valid, t);
+    const int64_t from = b * e.batch_src + i * e.ld_src + j;
+    if (e.src_plane != 0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) t[q] = q < valid ? pair_value((const _Float16*)e.src, from + q, e.src_plane) : 0.0f;
+    } else {
+      load4_any(e.src, from, e.src_bf16, valid, t);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = fmaf(e.s1, t[q], v[q]);
   }

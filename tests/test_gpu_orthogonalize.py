@@ -104,6 +104,13 @@ def test_coefficients_and_scale(il):
         assert _far(il.ilargi_orthogonalize(x, eps=0.0), _exact(x, 5, eps=0.0)) <= _tol(48, 80, 5, F32)
 
 
+def test_coefficients_that_leave_the_unit_interval(il):
+    """a = 4, b = c = 0 multiplies by 4 a step (A^2 stays below 2e19); 3 s - 30 s^3 leaves every interval."""
+    G = torch.randn(70, 40, generator=_gen(7), device="cuda")
+    for steps, coef in ((8, (4.0, 0.0, 0.0)), (3, (3.0, -30.0, 1.0))):
+        assert _far(il.ilargi_orthogonalize(G, steps=steps, coef=coef), _exact(G, steps, coef)) <= 1e-4
+
+
 def test_zero_and_values_that_are_not_finite(il):
     G = torch.zeros(3, 20, 33, device="cuda")
     G[1] = torch.randn(20, 33, generator=_gen(4), device="cuda")
