@@ -55,18 +55,19 @@ struct LayerLayout {
   size_t forward = 0;                                         // bytes of the forward call
   size_t dz = 0, partial = 0, shares = 0, gradient = 0;       // offsets and bytes of the gradient call
 };
+size_t shares_bytes(bool h, int64_t M, int64_t N, int64_t K) {
+  const size_t f = mm_f32_plan(M, N, K, 1).partial_bytes, m = h ? mm16_plan(M, N, K, 1, kMm16Bf16, 0).partial_bytes : 0;
+  return up256(f > m ? f : m);
+}
 LayerLayout layer_layout(const ilargi_layer_t& y) {
   LayerLayout l;
   const bool h = y.type == ILARGI_TYPE_BF16;
-  if (h) l.forward = up256(mm16_plan(y.n, y.m, y.k, 1, kMm16Bf16, 0).partial_bytes);
+  l.forward = shares_bytes(h, y.n, y.m, y.k);
   l.dz = 0;
   l.partial = up256((size_t)y.n * (size_t)((y.m + 7) / 8 * 8) * (h ? 2 : 4));
   l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
-  l.gradient = l.shares;
-  if (h) {
-    const size_t x = mm16_plan(y.n, y.k, y.m, 1, kMm16Bf16, 0).partial_bytes, w = mm16_plan(y.k, y.m, y.n, 1, kMm16Bf16, 0).partial_bytes;
-    l.gradient += up256(x > w ? x : w);
-  }
+  const size_t x = shares_bytes(h, y.n, y.k, y.m), w = shares_bytes(h, y.k, y.m, y.n);
+  l.gradient = l.shares + (x > w ? x : w);
   return l;
 }
 
@@ -81,7 +82,7 @@ hipError_t product(const Product& p, float* partial, hipStream_t st) {
     a.epi = p.epi;
     return launch_mm16(a, mm16_plan(p.M, p.N, p.K, 1, kMm16Bf16, 0), partial, st);
   }
-  return launch_mm_f32(p, st);
+  return launch_mm_f32(p, mm_f32_plan(p.M, p.N, p.K, 1), partial, st);
 }
 
 }  // namespace

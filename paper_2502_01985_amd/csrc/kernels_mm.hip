@@ -8,113 +8,154 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kTile = 128, kStep = 16, kPad = kTile + 4;
-
-// Eight elements of a 128 x 16 piece of an operand for every thread, as floats; zeros outside the matrix.
-template <class T, bool KROWS>
+// Eight elements of a TILE x STEP piece of an operand for every thread, as floats; zeros outside the matrix.
+template <class T, bool KROWS, int TILE, int STEP>
 __device__ __forceinline__ void fetch(const T* __restrict__ p, int64_t ld, int64_t r0, int64_t R, int64_t k0, int64_t K, float (&f)[8]) {
+  static_assert(TILE * STEP == 8 * 256, "eight elements a thread");
   const int t = threadIdx.x;
-  const int64_t outer = KROWS ? k0 + (t >> 4) : r0 + (t >> 1), inner = KROWS ? r0 + (t & 15) * 8 : k0 + (t & 1) * 8;
+  const int64_t outer = KROWS ? k0 + t / (TILE / 8) : r0 + t / (STEP / 8), inner = KROWS ? r0 + t % (TILE / 8) * 8 : k0 + t % (STEP / 8) * 8;
   const int64_t n_outer = KROWS ? K : R, n_inner = KROWS ? R : K;
   const int64_t left = outer < n_outer ? n_inner - inner : 0;
   load_piece<T, 8>(p + (left > 0 ? outer * ld + inner : 0), (int)(left < 0 ? 0 : left > 8 ? 8 : left), f);
 }
 
-template <bool KROWS>
-__device__ __forceinline__ void put(float (*lds)[kPad], const float (&f)[8]) {
+template <bool KROWS, int TILE, int STEP>
+__device__ __forceinline__ void put(float (*lds)[TILE + 4], const float (&f)[8]) {
   const int t = threadIdx.x;
   if constexpr (KROWS) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      *reinterpret_cast<float4*>(&lds[t >> 4][(t & 15) * 8 + 4 * h]) = make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
+      *reinterpret_cast<float4*>(&lds[t / (TILE / 8)][t % (TILE / 8) * 8 + 4 * h]) = make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) lds[(t & 1) * 8 + j][t >> 1] = f[j];
+    for (int j = 0; j < 8; ++j) lds[t % (STEP / 8) * 8 + j][t / (STEP / 8)] = f[j];
   }
 }
 
-// A workgroup forms 128 x 128 sums, a wavefront 64 x 64 of them, 16 steps of k at a time from LDS while the next are fetched.
-// The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
-template <class TP, class TQ, bool PK, bool QK>
-__global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n) {
-  __shared__ __attribute__((aligned(16))) float lp[2][kStep][kPad], lq[2][kStep][kPad];
+// A workgroup forms TILE x TILE sums over a share of k, a wavefront a quarter of them, STEP k at a time from LDS while the next are
+// fetched.  The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
+// blockIdx: block, matrix of the batch, share.  With several shares the sums go to `partial`, as in kernels_mm16.hip.
+template <class TP, class TQ, bool PK, bool QK, int TILE, int STEP>
+__global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n, int64_t share, float* __restrict__ partial) {
+  constexpr int F = TILE / 64;        // 32 x 32 pieces of a wavefront, each way
+  __shared__ __attribute__((aligned(16))) float lp[2][STEP][TILE + 4], lq[2][STEP][TILE + 4];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t i0 = (int64_t)(blockIdx.x / tiles_n) * kTile, j0 = (int64_t)(blockIdx.x % tiles_n) * kTile, b = blockIdx.y;
+  const int64_t i0 = (int64_t)(blockIdx.x / tiles_n) * TILE, j0 = (int64_t)(blockIdx.x % tiles_n) * TILE, b = blockIdx.y;
+  const int64_t first = blockIdx.z * share, K = a.K < first + share ? a.K : first + share;
   const TP* P = (const TP*)a.P.p + b * a.P.batch;
   const TQ* Q = (const TQ*)a.Q.p + b * a.Q.batch;
-  const int wi = (wave / 2) * 64, wj = (wave % 2) * 64, r = lane % 32, h = lane / 32;
-  f32x16 acc[2][2];
+  const int wi = (wave / 2) * (TILE / 2), wj = (wave % 2) * (TILE / 2), r = lane % 32, h = lane / 32;
+  f32x16 acc[F][F];
 #pragma unroll
-  for (int x = 0; x < 4; ++x)
+  for (int x = 0; x < F; ++x)
 #pragma unroll
-    for (int q = 0; q < 16; ++q) acc[x / 2][x % 2][q] = 0.0f;
+    for (int y = 0; y < F; ++y)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.0f;
   float fp[8], fq[8];
-  if (a.K > 0) {
-    fetch<TP, PK>(P, a.P.ld, i0, a.M, 0, a.K, fp);
-    fetch<TQ, QK>(Q, a.Q.ld, j0, a.N, 0, a.K, fq);
-    put<PK>(lp[0], fp);
-    put<QK>(lq[0], fq);
+  if (first < K) {
+    fetch<TP, PK, TILE, STEP>(P, a.P.ld, i0, a.M, first, K, fp);
+    fetch<TQ, QK, TILE, STEP>(Q, a.Q.ld, j0, a.N, first, K, fq);
+    put<PK, TILE, STEP>(lp[0], fp);
+    put<QK, TILE, STEP>(lq[0], fq);
   }
   __syncthreads();
   int cur = 0;
-  for (int64_t k0 = 0; k0 < a.K; k0 += kStep, cur ^= 1) {
-    const bool more = k0 + kStep < a.K;
+  for (int64_t k0 = first; k0 < K; k0 += STEP, cur ^= 1) {
+    const bool more = k0 + STEP < K;
     if (more) {
-      fetch<TP, PK>(P, a.P.ld, i0, a.M, k0 + kStep, a.K, fp);
-      fetch<TQ, QK>(Q, a.Q.ld, j0, a.N, k0 + kStep, a.K, fq);
+      fetch<TP, PK, TILE, STEP>(P, a.P.ld, i0, a.M, k0 + STEP, K, fp);
+      fetch<TQ, QK, TILE, STEP>(Q, a.Q.ld, j0, a.N, k0 + STEP, K, fq);
     }
 #pragma unroll
-    for (int k = 0; k < kStep; k += 2) {
-      const float p0 = lp[cur][k + h][wi + r], p1 = lp[cur][k + h][wi + 32 + r];
-      const float q0 = lq[cur][k + h][wj + r], q1 = lq[cur][k + h][wj + 32 + r];
-      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q0, p0, acc[0][0], 0, 0, 0);
-      acc[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(q1, p0, acc[0][1], 0, 0, 0);
-      acc[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q0, p1, acc[1][0], 0, 0, 0);
-      acc[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(q1, p1, acc[1][1], 0, 0, 0);
+    for (int k = 0; k < STEP; k += 2) {
+      float p[F], q[F];
+#pragma unroll
+      for (int x = 0; x < F; ++x) p[x] = lp[cur][k + h][wi + 32 * x + r];
+#pragma unroll
+      for (int y = 0; y < F; ++y) q[y] = lq[cur][k + h][wj + 32 * y + r];
+#pragma unroll
+      for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int y = 0; y < F; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[y], p[x], acc[x][y], 0, 0, 0);
     }
     if (more) {
-      put<PK>(lp[cur ^ 1], fp);
-      put<QK>(lq[cur ^ 1], fq);
+      put<PK, TILE, STEP>(lp[cur ^ 1], fp);
+      put<QK, TILE, STEP>(lq[cur ^ 1], fq);
     }
     __syncthreads();
   }
+  const int64_t ldp = (a.N + 3) / 4 * 4;
+  float* part = partial != nullptr ? partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp : nullptr;
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
+  for (int x = 0; x < F; ++x) {
     const int64_t i = i0 + wi + 32 * x + r;
     if (i >= a.M) continue;
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < F; ++y)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int64_t j = j0 + wj + 32 * y + 8 * g + 4 * h;
         if (j >= a.N) continue;
         float v[4] = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-        epilogue4(a.epi, b, i, j, (int)(a.N - j < 4 ? a.N - j : 4), v);
+        if (part != nullptr) {
+          *reinterpret_cast<float4*>(part + i * ldp + j) = make_float4(v[0], v[1], v[2], v[3]);
+          continue;
+        }
+        const int valid = (int)(a.N - j < 4 ? a.N - j : 4);
+        float bias[4];
+        epilogue_bias(a.epi, j, valid, bias);
+        epilogue4(a.epi, b, i, j, valid, bias, v);
       }
   }
 }
 
-template <class TP, class TQ>
-hipError_t mm_f32_typed(const Product& a, hipStream_t st) {
-  const int64_t tm = (a.M + kTile - 1) / kTile, tn = (a.N + kTile - 1) / kTile;
-  const dim3 grid((unsigned)(tm * tn), (unsigned)a.batches);
-  const int n = (int)tn;
-  if (a.P.k_rows) {
-    if (a.Q.k_rows) mm_f32_kernel<TP, TQ, true, true><<<grid, 256, 0, st>>>(a, n);
-    else mm_f32_kernel<TP, TQ, true, false><<<grid, 256, 0, st>>>(a, n);
-  } else {
-    if (a.Q.k_rows) mm_f32_kernel<TP, TQ, false, true><<<grid, 256, 0, st>>>(a, n);
-    else mm_f32_kernel<TP, TQ, false, false><<<grid, 256, 0, st>>>(a, n);
-  }
+template <class TP, class TQ, bool PK, bool QK>
+hipError_t mm_f32_order(const Product& a, const MmPlan& plan, float* partial, hipStream_t st) {
+  const int64_t tm = (a.M + plan.tile - 1) / plan.tile, tn = (a.N + plan.tile - 1) / plan.tile;
+  const dim3 grid((unsigned)(tm * tn), (unsigned)a.batches, (unsigned)plan.splits);
+  const int64_t step = plan.tile == 64 ? 32 : 16, steps = (a.K + step - 1) / step, share = (steps + plan.splits - 1) / plan.splits * step;
+  float* part = plan.splits > 1 ? partial : nullptr;
+  if (plan.tile == 64) mm_f32_kernel<TP, TQ, PK, QK, 64, 32><<<grid, 256, 0, st>>>(a, (int)tn, share, part);
+  else mm_f32_kernel<TP, TQ, PK, QK, 128, 16><<<grid, 256, 0, st>>>(a, (int)tn, share, part);
+  if (part != nullptr) return launch_mm_join(a.M, a.N, a.batches, 0, a.epi, plan.splits, part, st);
   return hipGetLastError();
+}
+
+template <class TP, class TQ>
+hipError_t mm_f32_typed(const Product& a, const MmPlan& plan, float* partial, hipStream_t st) {
+  if (a.P.k_rows) return a.Q.k_rows ? mm_f32_order<TP, TQ, true, true>(a, plan, partial, st) : hipErrorInvalidValue;
+  return a.Q.k_rows ? mm_f32_order<TP, TQ, false, true>(a, plan, partial, st) : mm_f32_order<TP, TQ, false, false>(a, plan, partial, st);
 }
 
 }  // namespace
 
-hipError_t launch_mm_f32(const Product& a, hipStream_t st) {
+MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
+  MmPlan best{128, 1, 0};
+  double least = 1e300;
+  for (int tile = 128; tile >= 64; tile /= 2) {
+    const int64_t blocks = ((M + tile - 1) / tile) * ((N + tile - 1) / tile) * batches;
+    const int64_t step = tile == 64 ? 32 : 16, steps = K > step ? (K + step - 1) / step : 1;
+    for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
+      const int64_t share = (steps + splits - 1) / splits, groups = blocks * splits;
+      if (splits > 1 && ((steps + share - 1) / share != splits || groups > 2048)) continue;
+      const double rounds = (double)((groups + 255) / 256), work = tile == 64 ? 0.47 : 0.95, alone = tile == 64 ? 0.8 : 1.1;
+      double cost = (double)share * (rounds * work > alone ? rounds * work : alone);
+      const double bytes = (double)groups / (double)blocks * (double)batches * (double)M * (double)((N + 3) / 4 * 4) * 4.0;
+      if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;
+      if (cost < least) {
+        least = cost;
+        best = {tile, (int)splits, splits > 1 ? (size_t)bytes : 0};
+      }
+    }
+  }
+  return best;
+}
+
+hipError_t launch_mm_f32(const Product& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.P.bf16 != a.Q.bf16) return hipErrorInvalidValue;
-  return a.P.bf16 ? mm_f32_typed<bf16_t, bf16_t>(a, st) : mm_f32_typed<float, float>(a, st);
+  return a.P.bf16 ? mm_f32_typed<bf16_t, bf16_t>(a, plan, partial, st) : mm_f32_typed<float, float>(a, plan, partial, st);
 }
 
 // --------------------------------------------------------------------------------------- elementwise pass of a gradient

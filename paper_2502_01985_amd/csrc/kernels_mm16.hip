@@ -147,7 +147,7 @@ __device__ __forceinline__ void upper_block(int id, int tn, int* ti, int* tj) {
 
 // What is done with four neighbouring sums of row i; `mirrored`: of a symmetric result, at their places below the diagonal.
 template <int KIND>
-__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, bool mirrored, f32x4 t) {
+__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, bool mirrored, const float (&bias)[4], f32x4 t) {
   if (i >= M || j >= N) return;
   const int valid = (int)(N - j < 4 ? N - j : 4);
   float v[4] = {t[0], t[1], t[2], t[3]};
@@ -158,7 +158,7 @@ __device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, i
       return;
     }
   }
-  epilogue4(e, b, i, j, valid, v);
+  epilogue4(e, b, i, j, valid, bias, v);
 }
 
 // The products of the second half of a step, between them the fetches of a later step into the buffer that has become free
@@ -302,6 +302,7 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int64_t ri = i0 + wi + 64 * h, cj = j0 + wj;
+    float none[4] = {0.f, 0.f, 0.f, 0.f};
     if (partial != nullptr) {
       const int64_t ldp = (a.N + 3) / 4 * 4;
       float* part = partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp;
@@ -313,15 +314,18 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
     } else {
       // a row of 64 columns takes 16 lanes; a flipped result is written along its own rows, which run over i
       if (!a.epi.flip) {
-#pragma unroll 1
+        const int c = (lane & 15) * 4;
+        float bias[4];
+        epilogue_bias(a.epi, cj + c, (int)(a.N - cj - c < 4 ? a.N - cj - c : 4), bias);
+#pragma unroll 2
         for (int q = 0; q < 16; ++q) {
-          const int r = 4 * q + (lane >> 4), c = (lane & 15) * 4;
-          emit4<KIND>(a.epi, b, ri + r, cj + c, a.M, a.N, false, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
+          const int r = 4 * q + (lane >> 4);
+          emit4<KIND>(a.epi, b, ri + r, cj + c, a.M, a.N, false, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
         }
       }
       if (a.epi.flip || (a.symmetric && ti != tj)) {
 #pragma unroll 1
-        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, cj + 4 * q, a.M, a.N, true, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
+        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, cj + 4 * q, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -331,14 +335,21 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
 
 // Adds the shares of k in their order and finishes: 64 x 64 sums a workgroup, those on and above the diagonal of a symmetric
 // result.
+struct Join {
+  int64_t M, N, batches;
+  int symmetric;
+  Epilogue epi;
+};
 template <int KIND>
-__global__ __launch_bounds__(256) void mm16_join_kernel(Product16 a, int tn, int splits, const float* __restrict__ partial) {
+__global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits, const float* __restrict__ partial) {
   __shared__ __attribute__((aligned(16))) float tile[64][kOutPad];
   int ti, tj;
   if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
   else { ti = blockIdx.x / tn; tj = blockIdx.x % tn; }
   const int64_t b = blockIdx.y, i0 = (int64_t)ti * 64, j0 = (int64_t)tj * 64, ldp = (a.N + 3) / 4 * 4, far = a.batches * a.M * ldp;
   const int row = threadIdx.x / 16, c = (threadIdx.x % 16) * 4;
+  float bias[4], none[4] = {0.f, 0.f, 0.f, 0.f};
+  epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
   const bool turned = a.epi.flip || (a.symmetric && ti != tj);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -348,7 +359,7 @@ __global__ __launch_bounds__(256) void mm16_join_kernel(Product16 a, int tn, int
       const float* p = partial + b * a.M * ldp + (i0 + r) * ldp + j0 + c;
       for (int z = 0; z < splits; ++z) s += *reinterpret_cast<const f32x4*>(p + z * far);
     }
-    if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, s);
+    if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, bias, s);
     if (turned) *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
   }
   if (!turned) return;
@@ -357,7 +368,7 @@ __global__ __launch_bounds__(256) void mm16_join_kernel(Product16 a, int tn, int
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int cc = 16 * wave + 4 * q;
-    emit4<KIND>(a.epi, b, i0 + lane, j0 + cc, a.M, a.N, true, *reinterpret_cast<const f32x4*>(&tile[lane][cc]));
+    emit4<KIND>(a.epi, b, i0 + lane, j0 + cc, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(&tile[lane][cc]));
   }
 }
 
@@ -367,28 +378,33 @@ int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {
 }
 
 template <int KIND, bool PK, bool QK>
-hipError_t mm16_order(const Product16& a, const Mm16Plan& plan, float* partial, hipStream_t st) {
+hipError_t mm16_order(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   const int tm = (int)((a.M + plan.tile - 1) / plan.tile), tn = (int)((a.N + plan.tile - 1) / plan.tile);
   const int ks = (int)((a.K + kBK - 1) / kBK), share = (ks + plan.splits - 1) / plan.splits;
   const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, a.symmetric), (unsigned)a.batches, (unsigned)plan.splits);
   float* part = plan.splits > 1 ? partial : nullptr;
   if (plan.tile == 256) mm16_kernel<KIND, PK, QK, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a, tm, tn, share, part);
   else mm16_kernel<KIND, PK, QK, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a, tm, tn, share, part);
-  if (part != nullptr) {
-    const dim3 join((unsigned)blocks_of(a.M, a.N, 64, a.symmetric), (unsigned)a.batches);
-    mm16_join_kernel<KIND><<<join, 256, 0, st>>>(a, (int)((a.N + 63) / 64), plan.splits, part);
-  }
+  if (part != nullptr) return launch_mm_join(a.M, a.N, a.batches, a.symmetric, a.epi, plan.splits, part, st);
   return hipGetLastError();
 }
 
 }  // namespace
 
+hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, const Epilogue& epi, int splits, const float* partial, hipStream_t st) {
+  const dim3 grid((unsigned)blocks_of(M, N, 64, symmetric), (unsigned)batches);
+  const Join a{M, N, batches, symmetric, epi};
+  if (epi.out_plane != 0) mm_join_kernel<kMm16Pairs><<<grid, 256, 0, st>>>(a, (int)((N + 63) / 64), splits, partial);
+  else mm_join_kernel<kMm16Bf16><<<grid, 256, 0, st>>>(a, (int)((N + 63) / 64), splits, partial);
+  return hipGetLastError();
+}
+
 // Blocks of 256 or 128 and the shares of k, by what they cost in microseconds: a step of a 256-block takes 1.7 (one workgroup fits a
 // compute unit), of a 128-block 0.75 alone on its unit and 1.08 beside another; shares are written and added at 8 TB/s, in a launch
 // of 3.  Measured: 2048 x 2048 x 2048 in pairs, 128-blocks: 84 us in one share, 62 in two, 72 in four; 1024 x 1024 x 4096, bfloat16:
 // 50, 27 (four), 32 (eight); 4096 x 4096 x 4096, bfloat16: 117 in 256-blocks.
-Mm16Plan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric) {
-  Mm16Plan best{256, 1, 0};
+MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric) {
+  MmPlan best{256, 1, 0};
   double least = 1e300;
   const int64_t ks = (K + kBK - 1) / kBK, parts = kind == kMm16Pairs ? 3 : 1;
   for (int tile = 256; tile >= 128; tile /= 2) {
@@ -418,7 +434,7 @@ bool mm16_takes(const Operand& x, int64_t across, int64_t K) {
   return reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld % 8 == 0 && x.ld < (1 << 22) && (x.k_rows ? across : K) % 8 == 0;
 }
 
-hipError_t launch_mm16(const Product16& a, const Mm16Plan& plan, float* partial, hipStream_t st) {
+hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.kind == kMm16Bf16) {
     if (a.P.k_rows) return a.Q.k_rows ? mm16_order<kMm16Bf16, true, true>(a, plan, partial, st) : hipErrorInvalidValue;

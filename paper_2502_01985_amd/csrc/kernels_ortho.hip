@@ -85,7 +85,7 @@ bool stays_bounded(const float* coef) {
 
 struct OrthoLayout {
   int64_t s, l, sp, lp;                 // short and long side, and the same up to a multiple of 8
-  Mm16Plan gram, square, apply;
+  MmPlan gram, square, apply;
   size_t x[2], A, B, partial, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
@@ -170,14 +170,14 @@ hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipSt
     p.Q = p.P;
     p.epi.mode = kEpiScale;
     p.epi.s0 = 1.0f; p.epi.out = A; p.epi.ld_out = s; p.epi.batch_out = s * s;
-    if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return e;
+    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
     p.K = s;
     p.P = {A, s, 0, 0, s * s};
     p.Q = p.P;
     p.epi.s0 = a.coef[2]; p.epi.s1 = a.coef[1];
     p.epi.src = A; p.epi.ld_src = s; p.epi.batch_src = s * s;
     p.epi.out = B;
-    if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return e;
+    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
     p.N = l;
     p.P.p = B;
     p.Q = {x, l, 1, 0, s * l};
@@ -185,7 +185,7 @@ hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipSt
     p.epi.src = x; p.epi.ld_src = l; p.epi.batch_src = s * l;
     p.epi.out = next; p.epi.ld_out = l; p.epi.batch_out = s * l;
     if (t + 1 == a.steps) finish(a, 1.0f, &p.epi);
-    if (hipError_t e = launch_mm_f32(p, st); e != hipSuccess) return e;
+    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
   }
   return hipSuccess;
 }

@@ -51,15 +51,18 @@ __device__ __forceinline__ void epilogue4_pairs_mirrored(const Epilogue& e, int6
   }
 }
 
-// Columns j .. j + valid of row i of matrix b of the batch.
-__device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, float (&v)[4]) {
-  if (e.mode == kEpiLinear) {
-    if (e.bias != nullptr) {
-      float t[4];
-      load4_any(e.bias, j, e.out_bf16, valid, t);
+// The bias of columns j .. j + valid, zeros where there is none.
+__device__ __forceinline__ void epilogue_bias(const Epilogue& e, int64_t j, int valid, float (&bias)[4]) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += t[q];
-    }
+  for (int q = 0; q < 4; ++q) bias[q] = 0.0f;
+  if (e.mode == kEpiLinear && e.bias != nullptr && valid > 0) load4_any(e.bias, j, e.out_bf16, valid, bias);
+}
+
+// Columns j .. j + valid of row i of matrix b of the batch.
+__device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&bias)[4], float (&v)[4]) {
+  if (e.mode == kEpiLinear) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] += bias[q];
     if (e.pre != nullptr) store4_any(e.pre, i * e.ld_pre + j, e.out_bf16, valid, v);
     if (e.act != ILARGI_ACT_NONE) {
 #pragma unroll
