@@ -199,12 +199,22 @@ __global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_
   }
 }
 
+// Sixteen threads share a column: each adds every sixteenth chunk, then they are added in order.
 template <class T>
 __global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, int chunks, int64_t m, int accumulate, T* __restrict__ out) {
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (j >= m) return;
+  __shared__ float part[16][17];
+  const int c = threadIdx.x % 16, q = threadIdx.x / 16;
+  const int64_t j = (int64_t)blockIdx.x * 16 + c;
   float s = 0.0f;
-  for (int c = 0; c < chunks; ++c) s += partial[c * m + j];
+  if (j < m) {
+#pragma unroll
+    for (int u = 0; u < kBiasChunks / 16; ++u)
+      if (16 * u + q < chunks) s += partial[(16 * u + q) * m + j];
+  }
+  part[q][c] = s;
+  __syncthreads();
+  if (q != 0 || j >= m) return;
+  for (int u = 1; u < 16; ++u) s += part[u][c];
   out[j] = (T)(accumulate ? (float)out[j] + s : s);
 }
 
@@ -229,7 +239,7 @@ hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t
     else layer_grad_kernel<float><<<grid, 256, 0, st>>>(a, per, partial);
   }
   if (a.d_bias != nullptr) {
-    const unsigned grid = (unsigned)((a.m + 255) / 256);
+    const unsigned grid = (unsigned)((a.m + 15) / 16);
     if (a.bf16) bias_sum_kernel<bf16_t><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (bf16_t*)a.d_bias);
     else bias_sum_kernel<float><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (float*)a.d_bias);
   }

@@ -333,43 +333,66 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
   }
 }
 
-// Adds the shares of k in their order and finishes: 64 x 64 sums a workgroup, those on and above the diagonal of a symmetric
-// result.
 struct Join {
   int64_t M, N, batches;
   int symmetric;
   Epilogue epi;
 };
+
+// Four sums of every share, added in order; eight shares are on their way at a time.
+__device__ __forceinline__ f32x4 add_shares(const float* __restrict__ p, int64_t far, int splits) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  int z = 0;
+  for (; z + 8 <= splits; z += 8) {
+    f32x4 t[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t[u] = *reinterpret_cast<const f32x4*>(p + (z + u) * far);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += t[u];
+  }
+  f32x4 t[7];
+#pragma unroll
+  for (int u = 0; u < 7; ++u)
+    if (z + u < splits) t[u] = *reinterpret_cast<const f32x4*>(p + (z + u) * far);
+#pragma unroll
+  for (int u = 0; u < 7; ++u)
+    if (z + u < splits) s += t[u];
+  return s;
+}
+
+// Adds the shares of k and finishes, a thread for four sums of a row.
+__global__ __launch_bounds__(256) void mm_join_rows_kernel(Join a, int splits, const float* __restrict__ partial) {
+  const int64_t quads = (a.N + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x, i = at / quads, j = (at - i * quads) * 4, b = blockIdx.y;
+  if (i >= a.M) return;
+  const int64_t ldp = quads * 4;
+  const f32x4 s = add_shares(partial + (b * a.M + i) * ldp + j, a.batches * a.M * ldp, splits);
+  const int valid = (int)(a.N - j < 4 ? a.N - j : 4);
+  float bias[4], v[4] = {s[0], s[1], s[2], s[3]};
+  epilogue_bias(a.epi, j, valid, bias);
+  if (a.epi.out_plane != 0) epilogue4_pairs(a.epi, b, i, j, valid, v);
+  else epilogue4(a.epi, b, i, j, valid, bias, v);
+}
+
+// The same for results that are written along j too, 32 x 32 sums a workgroup: those on and above the diagonal of a symmetric
+// result, or all of a flipped one.
 template <int KIND>
 __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits, const float* __restrict__ partial) {
-  __shared__ __attribute__((aligned(16))) float tile[64][kOutPad];
+  __shared__ __attribute__((aligned(16))) float tile[32][36];
   int ti, tj;
   if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
   else { ti = blockIdx.x / tn; tj = blockIdx.x % tn; }
-  const int64_t b = blockIdx.y, i0 = (int64_t)ti * 64, j0 = (int64_t)tj * 64, ldp = (a.N + 3) / 4 * 4, far = a.batches * a.M * ldp;
-  const int row = threadIdx.x / 16, c = (threadIdx.x % 16) * 4;
-  float bias[4], none[4] = {0.f, 0.f, 0.f, 0.f};
-  epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
+  const int64_t b = blockIdx.y, i0 = (int64_t)ti * 32, j0 = (int64_t)tj * 32, ldp = (a.N + 3) / 4 * 4;
+  const int r = threadIdx.x / 8, c = (threadIdx.x % 8) * 4;
+  const float none[4] = {0.f, 0.f, 0.f, 0.f};
   const bool turned = a.epi.flip || (a.symmetric && ti != tj);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int r = 16 * q + row;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (i0 + r < a.M && j0 + c < a.N) {
-      const float* p = partial + b * a.M * ldp + (i0 + r) * ldp + j0 + c;
-      for (int z = 0; z < splits; ++z) s += *reinterpret_cast<const f32x4*>(p + z * far);
-    }
-    if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, bias, s);
-    if (turned) *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
-  }
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (i0 + r < a.M && j0 + c < a.N) s = add_shares(partial + (b * a.M + i0 + r) * ldp + j0 + c, a.batches * a.M * ldp, splits);
+  if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, none, s);
   if (!turned) return;
+  *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
   __syncthreads();
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int cc = 16 * wave + 4 * q;
-    emit4<KIND>(a.epi, b, i0 + lane, j0 + cc, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(&tile[lane][cc]));
-  }
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
+  emit4<KIND>(a.epi, b, i0 + x, j0 + y, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(&tile[x][y]));
 }
 
 int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {
@@ -392,10 +415,15 @@ hipError_t mm16_order(const Product16& a, const MmPlan& plan, float* partial, hi
 }  // namespace
 
 hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, const Epilogue& epi, int splits, const float* partial, hipStream_t st) {
-  const dim3 grid((unsigned)blocks_of(M, N, 64, symmetric), (unsigned)batches);
   const Join a{M, N, batches, symmetric, epi};
-  if (epi.out_plane != 0) mm_join_kernel<kMm16Pairs><<<grid, 256, 0, st>>>(a, (int)((N + 63) / 64), splits, partial);
-  else mm_join_kernel<kMm16Bf16><<<grid, 256, 0, st>>>(a, (int)((N + 63) / 64), splits, partial);
+  if (!symmetric && !epi.flip) {
+    const dim3 grid((unsigned)((M * ((N + 3) / 4) + 255) / 256), (unsigned)batches);
+    mm_join_rows_kernel<<<grid, 256, 0, st>>>(a, splits, partial);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)blocks_of(M, N, 32, symmetric), (unsigned)batches);
+  if (epi.out_plane != 0) mm_join_kernel<kMm16Pairs><<<grid, 256, 0, st>>>(a, (int)((N + 31) / 32), splits, partial);
+  else mm_join_kernel<kMm16Bf16><<<grid, 256, 0, st>>>(a, (int)((N + 31) / 32), splits, partial);
   return hipGetLastError();
 }
 

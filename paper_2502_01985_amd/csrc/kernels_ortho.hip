@@ -5,7 +5,7 @@ namespace ilargi {
 
 namespace {
 
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 256;
 
 // The pairs hold kUnit X, kUnit A and kUnit B: float16 keeps all eleven bits of its plane from 2.4e-7 to 255 then.
 constexpr float kUnit = 256.0f;
@@ -13,14 +13,17 @@ constexpr float kUnit = 256.0f;
 // Sums of squares of a share of one matrix's rows, in 64 bits: the norm neither overflows nor loses small entries.
 template <class T>
 __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a, double* __restrict__ parts) {
+  constexpr int V = ElemOf<T>::kVec;
   __shared__ double wsum[4];
   const T* G = (const T*)a.G + blockIdx.y * a.batch_g;
-  const int64_t total = a.rows * a.cols;
+  const int64_t pieces = (a.cols + V - 1) / V, total = a.rows * pieces;
   double s = 0.0;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += kNormParts * 256) {
-    const int64_t r = at / a.cols;
-    const double g = (double)(float)G[r * a.ld_g + (at - r * a.cols)];
-    s += g * g;
+    const int64_t r = (uint32_t)at / (uint32_t)pieces, c = (at - r * pieces) * V;     // (at most 2^26 pieces)
+    float f[V];
+    load_piece<T, V>(G + r * a.ld_g + c, (int)(a.cols - c < V ? a.cols - c : V), f);
+#pragma unroll
+    for (int q = 0; q < V; ++q) s = fma((double)f[q], (double)f[q], s);
   }
   for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
   if (threadIdx.x % 64 == 0) wsum[threadIdx.x / 64] = s;
@@ -37,7 +40,8 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
   __shared__ float scale;
   const int64_t b = blockIdx.y;
   if (threadIdx.x < 64) {
-    double s = parts[b * kNormParts + threadIdx.x];
+    const double* p = parts + b * kNormParts + threadIdx.x;
+    double s = (p[0] + p[64]) + (p[128] + p[192]);
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if (threadIdx.x == 0) scale = (float)(1.0 / (sqrt(s) + (double)a.eps));
   }
