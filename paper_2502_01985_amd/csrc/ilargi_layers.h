@@ -135,7 +135,7 @@ struct EmbedGradArgs {
   int64_t ld_table;
   int out_bf16, table_bf16;
 };
-size_t embed_grad_bytes(int64_t n, int64_t rows, int64_t cols);
+size_t embed_grad_bytes(int64_t n, int64_t cols);
 hipError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, hipStream_t st);
 
 // ------------------------------------------------------------------------------------------------- matrix products

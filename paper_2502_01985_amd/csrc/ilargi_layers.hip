@@ -101,7 +101,7 @@ ilargi_status_t ilargi_embed(const void* table, ilargi_type_t table_type, int64_
 ilargi_status_t ilargi_embed_grad_workspace_bytes(int64_t n, int64_t rows, int64_t cols, size_t* bytes) {
   if (bytes == nullptr) return refuse(ILARGI_ERR_NULL, "embed_grad: bytes is NULL");
   if (ilargi_status_t e = check_rows("embed_grad", n, rows, cols, cols, cols, 0, 0); e != ILARGI_OK) return e;
-  *bytes = embed_grad_bytes(n, rows, cols);
+  *bytes = embed_grad_bytes(n, cols);
   return ILARGI_OK;
 }
 
@@ -111,7 +111,7 @@ ilargi_status_t ilargi_embed_grad(const void* d_out, ilargi_type_t out_type, int
   if (ilargi_status_t e = check_rows("embed_grad", n, rows, cols, ld_table, ld_out, table_type, out_type); e != ILARGI_OK) return e;
   if (rows == 0) return ILARGI_OK;
   if (d_table == nullptr || (n > 0 && (d_out == nullptr || ids == nullptr))) return refuse(ILARGI_ERR_NULL, "embed_grad: d_out, ids or d_table is NULL");
-  if (ilargi_status_t e = check_workspace("embed_grad", workspace, workspace_bytes, embed_grad_bytes(n, rows, cols)); e != ILARGI_OK) return e;
+  if (ilargi_status_t e = check_workspace("embed_grad", workspace, workspace_bytes, embed_grad_bytes(n, cols)); e != ILARGI_OK) return e;
   EmbedGradArgs a{d_out, ld_out, ids, n, rows, cols, scale, accumulate, d_table, ld_table, out_type == ILARGI_TYPE_BF16, table_type == ILARGI_TYPE_BF16};
   return done("embed_grad", launch_embed_grad(a, (char*)workspace, (hipStream_t)stream));
 }
