@@ -61,7 +61,7 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
 namespace {
 
 constexpr int kBits = 9, kBins = 1 << kBits;      // two passes for tables of up to 262,143 rows
-constexpr int kChunk = 4096;                      // ids a workgroup sorts by one digit
+constexpr int kChunk = 4096, kSort = 512;         // ids a workgroup sorts by one digit, and its threads
 constexpr int kOneSort = 16384;                   // ids that one workgroup sorts in LDS by itself
 
 __device__ __forceinline__ uint32_t id_key(int32_t id, uint32_t rows) { return id >= 0 && (uint32_t)id < rows ? (uint32_t)id : rows; }
@@ -79,19 +79,21 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool live) {
 }
 
 template <bool FIRST>
-__global__ __launch_bounds__(kBlock) void id_hist_kernel(const int32_t* __restrict__ keys, int64_t n, uint32_t rows, int shift, int chunks,
-                                                         int32_t* __restrict__ hist) {
+__global__ __launch_bounds__(kSort) void id_hist_kernel(const int32_t* __restrict__ keys, int64_t n, uint32_t rows, int shift, int chunks,
+                                                        int32_t* __restrict__ hist) {
   __shared__ int32_t h[kBins];
-  for (int i = threadIdx.x; i < kBins; i += kBlock) h[i] = 0;
-  __syncthreads();
+  static_assert(kBins == kSort, "a digit a thread");
+  h[threadIdx.x] = 0;
   const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
+  uint32_t k[kChunk / kSort];
 #pragma unroll
-  for (int u = 0; u < kChunk / kBlock; ++u) {
-    const int64_t i = at + u * kBlock;
-    if (i < n) atomicAdd(&h[((FIRST ? id_key(keys[i], rows) : (uint32_t)keys[i]) >> shift) & (kBins - 1)], 1);
-  }
+  for (int u = 0; u < kChunk / kSort; ++u) k[u] = at + u * kSort < n ? (FIRST ? id_key(keys[at + u * kSort], rows) : (uint32_t)keys[at + u * kSort]) : 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += kBlock) hist[(int64_t)i * chunks + blockIdx.x] = h[i];
+#pragma unroll
+  for (int u = 0; u < kChunk / kSort; ++u)
+    if (at + u * kSort < n) atomicAdd(&h[(k[u] >> shift) & (kBins - 1)], 1);
+  __syncthreads();
+  hist[(int64_t)threadIdx.x * chunks + blockIdx.x] = h[threadIdx.x];
 }
 
 // Exclusive sums over the chunks of one digit, and the digit's total.
@@ -122,22 +124,35 @@ __global__ __launch_bounds__(kBlock) void id_scan_kernel(int32_t* __restrict__ h
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
-// Every wavefront walks a quarter of the chunk 64 ids at a time; an id's place is its digit's first place, plus the equal digits of the
-// chunks, wavefronts and steps before, plus its rank among those of its step.
+// The place of this lane's id among the equal digits of its wavefront so far: `seen` counts them, and the highest lane of a digit
+// adds this step's.  (A wavefront's own counters: no barrier, and no atomics, which would queue on a digit that many ids share.)
+template <int BITS>
+__device__ __forceinline__ int32_t rank_in_wave(uint32_t d, bool live, int32_t* seen) {
+  const int lane = threadIdx.x % kWave;
+  const uint64_t match = same_digit<BITS>(d, live), below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
+  const int32_t before = live ? seen[d] : 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (live && (match >> lane) <= 1ull) seen[d] = before + __popcll(match);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  return before + __popcll(match & below);
+}
+
+// Every wavefront walks its part of the chunk 64 ids at a time; an id's place is its digit's first place, plus the equal digits of the
+// chunks and wavefronts before, plus its rank in its wavefront.
 template <bool FIRST>
-__global__ __launch_bounds__(kBlock) void id_scatter_kernel(const int32_t* __restrict__ keys_in, const int32_t* __restrict__ vals_in, int64_t n, uint32_t rows,
-                                                            int shift, int chunks, const int32_t* __restrict__ hist, const int32_t* __restrict__ totals,
-                                                            int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
-  constexpr int kWaves = kBlock / kWave, kSteps = kChunk / kBlock;
-  static_assert(kBins == 2 * kBlock, "two digits a thread");
+__global__ __launch_bounds__(kSort) void id_scatter_kernel(const int32_t* __restrict__ keys_in, const int32_t* __restrict__ vals_in, int64_t n, uint32_t rows,
+                                                           int shift, int chunks, const int32_t* __restrict__ hist, const int32_t* __restrict__ totals,
+                                                           int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
+  constexpr int kWaves = kSort / kWave, kSteps = kChunk / kSort;
+  static_assert(kBins == kSort, "a digit a thread");
   __shared__ int32_t off[kWaves][kBins];
   __shared__ int32_t wsum[kWaves];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) { off[w][threadIdx.x] = 0; off[w][threadIdx.x + kBlock] = 0; }
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, t = threadIdx.x;
   const int64_t first = (int64_t)blockIdx.x * kChunk + (int64_t)wave * kSteps * kWave + lane;
   uint32_t k[kSteps];
-  int32_t v[kSteps];
+  int32_t v[kSteps], rank[kSteps];
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
     const int64_t i = first + u * kWave;
@@ -147,51 +162,35 @@ __global__ __launch_bounds__(kBlock) void id_scatter_kernel(const int32_t* __res
       v[u] = FIRST ? (int32_t)i : vals_in[i];
     }
   }
-  // first places of the digits: thread t has 2 t and 2 t + 1
-  const int32_t a0 = totals[2 * threadIdx.x], a1 = totals[2 * threadIdx.x + 1];
-  int32_t inc = a0 + a1;
+  const int32_t total = totals[t], mine = hist[(int64_t)t * chunks + blockIdx.x];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) off[w][t] = 0;
+  int32_t inc = total;
   for (int d = 1; d < kWave; d <<= 1) {
-    const int32_t t = __shfl_up(inc, d);
-    if (lane >= d) inc += t;
+    const int32_t x = __shfl_up(inc, d);
+    if (lane >= d) inc += x;
   }
   if (lane == kWave - 1) wsum[wave] = inc;
   __syncthreads();
-  int32_t start = inc - a0 - a1;
-  for (int w = 0; w < wave; ++w) start += wsum[w];
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u)
-    if (first + u * kWave < n) atomicAdd(&off[wave][(k[u] >> shift) & (kBins - 1)], 1);
+  for (int u = 0; u < kSteps; ++u) rank[u] = rank_in_wave<kBits>((k[u] >> shift) & (kBins - 1), first + u * kWave < n, off[wave]);
+  int32_t at = inc - total + mine;
+  for (int w = 0; w < wave; ++w) at += wsum[w];
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int d = 2 * threadIdx.x + h;
-    int32_t at = start + (h ? a0 : 0) + hist[(int64_t)d * chunks + blockIdx.x];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const int32_t c = off[w][d];
-      off[w][d] = at;
-      at += c;
-    }
+  for (int w = 0; w < kWaves; ++w) {
+    const int32_t c = off[w][t];
+    off[w][t] = at;
+    at += c;
   }
   __syncthreads();
-  const uint64_t below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
-    const bool live = first + u * kWave < n;
-    const uint32_t d = (k[u] >> shift) & (kBins - 1);
-    const uint64_t match = same_digit<kBits>(d, live);
-    int32_t dst = 0;
-    if (live) dst = off[wave][d] + __popcll(match & below);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                 // (a wavefront's own offsets: no barrier)
-    __builtin_amdgcn_wave_barrier();
-    if (live && (match >> lane) <= 1ull) off[wave][d] += __popcll(match);  // the highest lane of its digit
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (live) {
+  for (int u = 0; u < kSteps; ++u)
+    if (first + u * kWave < n) {
+      const int32_t dst = off[wave][(k[u] >> shift) & (kBins - 1)] + rank[u];
       keys_out[dst] = (int32_t)k[u];
       vals_out[dst] = v[u];
     }
-  }
 }
 
 // The whole sort of up to kOneSort ids by one workgroup: 16 ids a thread in registers, which change places through LDS after every
@@ -212,18 +211,19 @@ __global__ __launch_bounds__(1024) void id_sort_one_kernel(const int32_t* __rest
     k[u] = u < steps && i < n ? id_key(ids[i], rows) : 0;
     v[u] = (uint32_t)i;
   }
-  const uint64_t below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
   for (int p = 0; p < passes; ++p) {
     const int shift = 8 * p;
     for (int i = threadIdx.x; i < 16 * kD; i += 1024) off[i / kD][i % kD] = 0;
     __syncthreads();
+    int32_t rank[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u)
-      if (u < steps && first + u * kWave < n) atomicAdd(&off[wave][(k[u] >> shift) & (kD - 1)], 1);
+      if (u < steps) rank[u] = rank_in_wave<8>((k[u] >> shift) & (kD - 1), first + u * kWave < n, off[wave]);
     __syncthreads();
-    int32_t total = 0, inc = 0;
+    int32_t c[16], total = 0, inc = 0;
     if (threadIdx.x < kD) {
-      for (int w = 0; w < 16; ++w) total += off[w][threadIdx.x];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) { c[w] = off[w][threadIdx.x]; total += c[w]; }
       inc = total;
       for (int d = 1; d < kWave; d <<= 1) {
         const int32_t t = __shfl_up(inc, d);
@@ -235,36 +235,20 @@ __global__ __launch_bounds__(1024) void id_sort_one_kernel(const int32_t* __rest
     if (threadIdx.x < kD) {
       int32_t at = inc - total;
       for (int w = 0; w < wave; ++w) at += wsum[w];
-      for (int w = 0; w < 16; ++w) {
-        const int32_t c = off[w][threadIdx.x];
-        off[w][threadIdx.x] = at;
-        at += c;
-      }
+#pragma unroll
+      for (int w = 0; w < 16; ++w) { off[w][threadIdx.x] = at; at += c[w]; }
     }
     __syncthreads();
-    int32_t dst[kSteps];
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-      if (u >= steps) continue;
-      const bool live = first + u * kWave < n;
-      const uint32_t d = (k[u] >> shift) & (kD - 1);
-      const uint64_t match = same_digit<8>(d, live);
-      dst[u] = live ? off[wave][d] + __popcll(match & below) : 0;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      if (live && (match >> lane) <= 1ull) off[wave][d] += __popcll(match);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
 #pragma unroll
     for (int u = 0; u < kSteps; ++u)
       if (u < steps && first + u * kWave < n) {
+        const int32_t dst = off[wave][(k[u] >> shift) & (kD - 1)] + rank[u];
         if (p + 1 == passes) {
-          keys_out[dst[u]] = (int32_t)k[u];
-          vals_out[dst[u]] = (int32_t)v[u];
+          keys_out[dst] = (int32_t)k[u];
+          vals_out[dst] = (int32_t)v[u];
         } else {
-          lk[dst[u]] = k[u];
-          lv[dst[u]] = (uint16_t)v[u];
+          lk[dst] = k[u];
+          lv[dst] = (uint16_t)v[u];
         }
       }
     if (p + 1 == passes) return;
@@ -318,30 +302,38 @@ __global__ __launch_bounds__(kBlock) void embed_runs_kernel(RunArgs a, int sh) {
   float s[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) s[j] = 0.0f;
-  int32_t key = a.sorted[p0];
-  bool open = p0 > 0 && a.sorted[p0 - 1] == key;       // the segment began in an earlier run
-  for (int64_t p = p0; p < p1 && key != none; p += 8) {
-    int32_t from[8], next[8];
-    float f[8][V];
+  int32_t from[8], next[8];
+  auto ask = [&](int64_t p) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int64_t q = p + u < p1 ? p + u : p1 - 1;
       from[u] = a.perm[q];
       next[u] = q + 1 < n ? a.sorted[q + 1] : -1;
     }
+  };
+  ask(p0);
+  int32_t key = a.sorted[p0];
+  bool open = p0 > 0 && a.sorted[p0 - 1] == key;       // the segment began in an earlier run
+  for (int64_t p = p0; p < p1 && key != none; p += 8) {
+    float f[8][V];
+    int32_t then[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) load_piece<TI, V>((const TI*)a.g.d_out + (int64_t)from[u] * a.g.ld_out + c, valid, f[u]);
+    for (int u = 0; u < 8; ++u) {
+      load_piece<TI, V>((const TI*)a.g.d_out + (int64_t)from[u] * a.g.ld_out + c, valid, f[u]);
+      then[u] = next[u];
+    }
+    if (p + 8 < p1) ask(p + 8);                         // the next places, while the rows are on their way
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (p + u >= p1 || key == none) break;
 #pragma unroll
       for (int j = 0; j < V; ++j) s[j] += f[u][j];
-      if (next[u] != key || p + u + 1 == p1) {
+      if (then[u] != key || p + u + 1 == p1) {
         // slot 0: a segment from before (through the whole run, perhaps); slot 1: one that begins here and goes on
-        if (open || next[u] == key) store_piece<float, V>(a.carry + (2 * run + (open ? 0 : 1)) * a.g.cols + c, valid, s);
+        if (open || then[u] == key) store_piece<float, V>(a.carry + (2 * run + (open ? 0 : 1)) * a.g.cols + c, valid, s);
         else write_row<TO, V, ADD>(a.g, key, c, valid, s);
         open = false;
-        key = next[u];
+        key = then[u];
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] = 0.0f;
       }
@@ -349,80 +341,151 @@ __global__ __launch_bounds__(kBlock) void embed_runs_kernel(RunArgs a, int sh) {
   }
 }
 
+// A load that depends on the one before costs most of a microsecond here (the sorted ids were written by other compute units), so a
+// whole wavefront looks at 64 places at a time.
 // First place of the sorted ids whose key is at least `key`.
-__device__ __forceinline__ int64_t lower_place(const int32_t* __restrict__ sorted, int64_t lo, int64_t hi, int32_t key) {
+__device__ __forceinline__ int64_t wave_lower(const int32_t* __restrict__ sorted, int64_t n, int64_t key) {
+  const int lane = threadIdx.x % kWave;
+  int64_t lo = 0, hi = n;
   while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (sorted[mid] < key) lo = mid + 1;
-    else hi = mid;
+    const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const int less = __popcll(__ballot(at < hi && sorted[at] < key));       // the keys rise: the first lanes
+    if (less == 0) return lo;
+    const int64_t end = lo + less * step;
+    lo = end - step + 1;
+    if (end < hi) hi = end;
+    if (step == 1) return lo;
   }
   return lo;
 }
+// Runs that the segment of `key` reaches which goes on behind run `run`: those that follow and begin with its key.
+__device__ __forceinline__ int32_t wave_span(const RunArgs& a, int64_t run, int32_t key) {
+  const int lane = threadIdx.x % kWave;
+  auto begins = [&](int64_t r) { return r < a.runs && a.sorted[r * a.run] == key; };
+  int64_t in = run + 1;                                 // run `in` begins with the key; so many runs of 64 of them behind it
+  int more = __popcll(__ballot(begins(in + 1 + lane)));
+  if (more < kWave) return (int32_t)(in + more - run + 1);
+  for (int64_t step = kWave * kWave; step >= 1; step /= kWave) {
+    do {
+      more = __popcll(__ballot(begins(in + (lane + 1) * step)));
+      in += more * step;
+    } while (more == kWave);
+  }
+  return (int32_t)(in - run + 1);
+}
 
-constexpr int kClearRows = 64;
+constexpr int kClearRows = 256, kJoin = 1024, kJoinRuns = 64, kShortSpan = 16;
 
-// Workgroup r < runs: if a segment begins in run r and goes on behind it, its carries are added, by 2^(8 - sh) groups of lanes that take
-// every so manieth of them and are then added in order.  The other workgroups zero the rows without ids (unless the caller
-// accumulates), kClearRows of them each.
+// Carries of runs from, from + by, .. last of a segment that begins in run `begin`, added to s, eight on their way at a time.
+template <int V>
+__device__ __forceinline__ void add_carries(const RunArgs& a, int64_t begin, int64_t from, int64_t by, int64_t last, int64_t c, int valid, float (&s)[V]) {
+  for (int64_t r = from; r <= last; r += 8 * by) {
+    float f[8][V];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t q = r + u * by;
+      load_piece<float, V>(a.carry + (2 * (q <= last ? q : begin) + (q == begin ? 1 : 0)) * a.g.cols + (valid > 0 ? c : 0), q <= last ? valid : 0, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] += f[u][j];
+  }
+}
+
+// The first workgroups look at kJoinRuns runs each: a segment that begins in one of them and goes on behind it is the sum of its
+// carries.  Up to kShortSpan of them are added by a group of 2^sh lanes, longer ones by all groups, each every so manieth, which are
+// then added in order.  The other workgroups zero the rows without ids (unless the caller accumulates), kClearRows of them each.
 template <class TO, bool ADD>
-__global__ __launch_bounds__(kBlock) void embed_join_kernel(RunArgs a, int sh) {
+__global__ __launch_bounds__(kJoin) void embed_join_kernel(RunArgs a, int sh, int64_t joins) {
   constexpr int V = 4;
   const int64_t n = a.g.n;
-  if ((int64_t)blockIdx.x >= a.runs) {
-    __shared__ uint8_t empty[kClearRows];
-    const int64_t v0 = ((int64_t)blockIdx.x - a.runs) * kClearRows;
-    if (threadIdx.x < kClearRows) {
-      const int64_t v = v0 + threadIdx.x;
-      uint8_t e = 0;
-      if (v < a.g.rows) {
-        const int64_t at = lower_place(a.sorted, 0, n, (int32_t)v);
-        e = at == n || a.sorted[at] != (int32_t)v;
+  const int lane = threadIdx.x & ((1 << sh) - 1), group = threadIdx.x >> sh, groups = kJoin >> sh;
+  if ((int64_t)blockIdx.x >= joins) {
+    __shared__ uint8_t full[kClearRows];
+    __shared__ int64_t ends[2];
+    const int64_t v0 = ((int64_t)blockIdx.x - joins) * kClearRows, v1 = v0 + kClearRows < a.g.rows ? v0 + kClearRows : a.g.rows;
+    if (threadIdx.x < kClearRows) full[threadIdx.x] = v0 + threadIdx.x >= v1;
+    if (threadIdx.x < 2 * kWave) {
+      const int64_t at = wave_lower(a.sorted, n, threadIdx.x < kWave ? v0 : v1);
+      if (threadIdx.x % kWave == 0) ends[threadIdx.x / kWave] = at;
+    }
+    __syncthreads();
+    const int64_t b = ends[0], e = ends[1];
+    if (e - b <= 16 * kJoin) {
+#pragma unroll 4
+      for (int64_t p = b + threadIdx.x; p < e; p += kJoin) full[a.sorted[p] - v0] = 1;
+    } else if (threadIdx.x < kClearRows && v0 + threadIdx.x < v1) {      // a row with many ids is among them: look for each
+      const int32_t v = (int32_t)(v0 + threadIdx.x);
+      int64_t lo = b, hi = e;
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (a.sorted[mid] < v) lo = mid + 1;
+        else hi = mid;
       }
-      empty[threadIdx.x] = e;
+      full[threadIdx.x] = lo < e && a.sorted[lo] == v;
     }
     __syncthreads();
     const float zero[V] = {0.f, 0.f, 0.f, 0.f};
-    const int lane = threadIdx.x & ((1 << sh) - 1);
-    for (int r = threadIdx.x >> sh; r < kClearRows; r += kBlock >> sh) {
-      if (!empty[r]) continue;
+    for (int r = group; r < kClearRows; r += groups) {
+      if (full[r]) continue;
       for (int64_t c = (int64_t)lane * V; c < a.g.cols; c += (int64_t)V << sh)
         store_piece<TO, V>((TO*)a.g.d_table + (v0 + r) * a.g.ld_table + c, (int)(a.g.cols - c < V ? a.g.cols - c : V), zero);
     }
     return;
   }
-  __shared__ float4 part[kBlock];
-  const int64_t run = blockIdx.x, p0 = run * a.run, p1 = p0 + a.run;
-  if (p1 >= n) return;
-  const int32_t key = a.sorted[p1 - 1];
-  if (key == (int32_t)a.g.rows || a.sorted[p1] != key) return;
-  if (p0 > 0 && a.sorted[p0 - 1] == key) return;       // it began before
-  const int64_t last = (lower_place(a.sorted, p1, n, key + 1) - 1) / a.run;       // the run that the segment ends in
-  const int lane = threadIdx.x & ((1 << sh) - 1), group = threadIdx.x >> sh, groups = kBlock >> sh;
-  const int64_t wide = (((a.g.cols + V - 1) / V + (1 << sh) - 1) >> sh << sh) * V;       // every lane makes the same number of turns
-  for (int64_t c = (int64_t)lane * V; c < wide; c += (int64_t)V << sh) {
-    const int valid = c < a.g.cols ? (int)(a.g.cols - c < V ? a.g.cols - c : V) : 0;
-    float s[V] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t r = run + group; r <= last; r += 8 * groups) {
-      float f[8][V];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int64_t q = r + u * groups;
-        load_piece<float, V>(a.carry + (2 * (q <= last ? q : run) + (q == run ? 1 : 0)) * a.g.cols + (valid > 0 ? c : 0), q <= last ? valid : 0, f[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] += f[u][j];
+  __shared__ float4 part[kJoin];
+  __shared__ int32_t keys[kJoinRuns], spans[kJoinRuns];     // runs that the segment reaches, 0 where there is none
+  const int64_t run0 = (int64_t)blockIdx.x * kJoinRuns;
+  if (threadIdx.x < kJoinRuns) {
+    const int64_t run = run0 + threadIdx.x, p0 = run * a.run, p1 = p0 + a.run;
+    int32_t key = 0, span = 0;
+    if (p1 < n) {
+      key = a.sorted[p1 - 1];
+      span = key != (int32_t)a.g.rows && a.sorted[p1] == key && !(p0 > 0 && a.sorted[p0 - 1] == key);
     }
-    __syncthreads();
-    part[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
-    __syncthreads();
-    if (group == 0 && valid > 0) {
-      for (int q = 1; q < groups; ++q) {
-        const float4 t = part[(q << sh) + lane];
-        s[0] += t.x; s[1] += t.y; s[2] += t.z; s[3] += t.w;
+    keys[threadIdx.x] = key;
+    spans[threadIdx.x] = span;
+  }
+  __syncthreads();
+  const int wave = threadIdx.x / kWave;
+#pragma unroll
+  for (int q = 0; q < kJoinRuns / (kJoin / kWave); ++q) {
+    const int r = wave + q * (kJoin / kWave);
+    if (spans[r] == 0) continue;
+    const int32_t span = wave_span(a, run0 + r, keys[r]);
+    if (threadIdx.x % kWave == 0) spans[r] = span;
+  }
+  __syncthreads();
+  for (int r = group; r < kJoinRuns; r += groups) {
+    if (spans[r] == 0 || spans[r] > kShortSpan) continue;
+    const int64_t run = run0 + r;
+    for (int64_t c = (int64_t)lane * V; c < a.g.cols; c += (int64_t)V << sh) {
+      const int valid = (int)(a.g.cols - c < V ? a.g.cols - c : V);
+      float s[V] = {0.f, 0.f, 0.f, 0.f};
+      add_carries<V>(a, run, run, 1, run + spans[r] - 1, c, valid, s);
+      write_row<TO, V, ADD>(a.g, keys[r], c, valid, s);
+    }
+  }
+  const int64_t wide = (((a.g.cols + V - 1) / V + (1 << sh) - 1) >> sh << sh) * V;       // every lane makes the same number of turns
+  static_assert(kJoinRuns == kWave, "a run a lane");
+  for (uint64_t left = __ballot(spans[threadIdx.x % kWave] > kShortSpan); left != 0; left &= left - 1) {
+    const int r = __builtin_ctzll(left);
+    const int64_t run = run0 + r;
+    for (int64_t c = (int64_t)lane * V; c < wide; c += (int64_t)V << sh) {
+      const int valid = c < a.g.cols ? (int)(a.g.cols - c < V ? a.g.cols - c : V) : 0;
+      float s[V] = {0.f, 0.f, 0.f, 0.f};
+      add_carries<V>(a, run, run + group, groups, run + spans[r] - 1, c, valid, s);
+      __syncthreads();
+      part[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
+      __syncthreads();
+      if (group == 0 && valid > 0) {
+        for (int q = 1; q < groups; ++q) {
+          const float4 t = part[(q << sh) + lane];
+          s[0] += t.x; s[1] += t.y; s[2] += t.z; s[3] += t.w;
+        }
+        write_row<TO, V, ADD>(a.g, keys[r], c, valid, s);
       }
-      write_row<TO, V, ADD>(a.g, key, c, valid, s);
     }
   }
 }
@@ -439,7 +502,7 @@ GradLayout grad_layout(int64_t n, int64_t cols) {
   // 1,000,000 ids, 128 columns: runs of 64 / 128 / 256; 9001 ids, 75 columns: runs of 8 / 16 / 64.
   const int64_t lanes = (cols + 7) / 8;
   l.run = 256;
-  while (l.run > 16 && n / l.run * lanes < 64 * 1024) l.run /= 2;
+  while (l.run > 16 && n / l.run * lanes < 256 * 1024) l.run /= 2;
   l.runs = (n + l.run - 1) / l.run;
   size_t at = 0;
   auto take = [&at](size_t bytes) { const size_t o = at; at += up256(bytes); return o; };
@@ -470,7 +533,8 @@ hipError_t grad_launch(const RunArgs& r, hipStream_t st) {
     embed_runs_kernel<TI, TO, ADD><<<dim3((unsigned)(((r.runs << sh) + kBlock - 1) / kBlock), slabs), kBlock, 0, st>>>(r, sh);
   }
   const int64_t clear = ADD ? 0 : (r.g.rows + kClearRows - 1) / kClearRows;
-  if (r.runs + clear > 0) embed_join_kernel<TO, ADD><<<(unsigned)(r.runs + clear), kBlock, 0, st>>>(r, lane_shift(r.g.cols, 4));
+  const int64_t joins = (r.runs + kJoinRuns - 1) / kJoinRuns;
+  if (joins + clear > 0) embed_join_kernel<TO, ADD><<<(unsigned)(joins + clear), kJoin, 0, st>>>(r, lane_shift(r.g.cols, 4), joins);
   return hipGetLastError();
 }
 
@@ -498,11 +562,11 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, hipStream_t st) {
     const int32_t *kin = a.ids, *vin = nullptr;
     for (int p = 0; p < passes; ++p) {
       int32_t *kout = (int32_t*)(ws + (p % 2 == 0 ? l.keys_a : l.keys_b)), *vout = (int32_t*)(ws + (p % 2 == 0 ? l.vals_a : l.vals_b));
-      if (p == 0) id_hist_kernel<true><<<chunks, kBlock, 0, st>>>(kin, a.n, rows, kBits * p, chunks, hist);
-      else id_hist_kernel<false><<<chunks, kBlock, 0, st>>>(kin, a.n, rows, kBits * p, chunks, hist);
+      if (p == 0) id_hist_kernel<true><<<chunks, kSort, 0, st>>>(kin, a.n, rows, kBits * p, chunks, hist);
+      else id_hist_kernel<false><<<chunks, kSort, 0, st>>>(kin, a.n, rows, kBits * p, chunks, hist);
       id_scan_kernel<<<kBins, kBlock, 0, st>>>(hist, chunks, totals);
-      if (p == 0) id_scatter_kernel<true><<<chunks, kBlock, 0, st>>>(kin, vin, a.n, rows, kBits * p, chunks, hist, totals, kout, vout);
-      else id_scatter_kernel<false><<<chunks, kBlock, 0, st>>>(kin, vin, a.n, rows, kBits * p, chunks, hist, totals, kout, vout);
+      if (p == 0) id_scatter_kernel<true><<<chunks, kSort, 0, st>>>(kin, vin, a.n, rows, kBits * p, chunks, hist, totals, kout, vout);
+      else id_scatter_kernel<false><<<chunks, kSort, 0, st>>>(kin, vin, a.n, rows, kBits * p, chunks, hist, totals, kout, vout);
       kin = kout;
       vin = vout;
     }
