@@ -62,7 +62,7 @@ size_t shares_bytes(bool h, int64_t M, int64_t N, int64_t K) {
 LayerLayout layer_layout(const ilargi_layer_t& y) {
   LayerLayout l;
   const bool h = y.type == ILARGI_TYPE_BF16;
-  l.forward = shares_bytes(h, y.n, y.m, y.k);
+  l.forward = mm_rows_takes(y.n, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k);
   l.dz = 0;
   l.partial = up256((size_t)y.n * (size_t)((y.m + 7) / 8 * 8) * (h ? 2 : 4));
   l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
@@ -143,6 +143,7 @@ ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_
   p.epi.bias = bias; p.epi.src = residual; p.epi.ld_src = ld_res; p.epi.src_bf16 = h;
   p.epi.pre = pre; p.epi.ld_pre = ld_pre; p.epi.act = y.act;
   p.epi.out = out; p.epi.ld_out = ld_out; p.epi.out_bf16 = h;
+  if (mm_rows_takes(y.n, h)) return done("linear", launch_mm_rows(p, mm_rows_plan(y.n, y.m, y.k), (float*)workspace, (hipStream_t)stream));
   return done("linear", product(p, (float*)workspace, (hipStream_t)stream));
 }
 

@@ -65,7 +65,7 @@ def _slope(z, act):
 # rows, inputs, outputs: single rows, single columns, odd, ragged against every tile, aligned
 SHAPES = [(0, 5, 3), (1, 1, 1), (1, 64, 96), (1, 1000, 333), (2, 72, 40), (3, 2048, 64), (5, 40, 8), (7, 16, 1030), (16, 136, 520), (17, 129, 131),
           (33, 250, 24), (64, 512, 256), (65, 63, 129), (127, 8, 200), (128, 128, 128), (130, 264, 136), (200, 1, 7), (257, 96, 264), (300, 777, 1),
-          (512, 320, 512), (1003, 333, 517), (1024, 64, 4096)]
+          (512, 320, 512), (1003, 333, 517), (1024, 64, 4096), (2, 9001, 70), (1, 20000, 9)]
 
 
 @pytest.mark.parametrize("n,k,m", SHAPES)
