@@ -186,8 +186,8 @@ hipError_t launch_mm_rows(const Product& a, const MmPlan& plan, float* partial, 
 // Adds the shares in their order: `partial` holds splits x batches matrices of M x (N to a multiple of 4).
 hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, const Epilogue& epi, int splits, const float* partial, hipStream_t st);
 
-// The same for 16-bit operands on the 16-bit matrix cores, with sums in float32.  An operand may be the sum of two planes,
-// hi + 2^-11 lo (`plane` elements apart, float16): then lo hi + hi lo + hi hi is formed, three products in place of one.
+// The same for 16-bit operands on the 16-bit matrix cores, with sums in float32.  Operands of pairs are the sum of two planes,
+// hi + lo (`plane` elements apart, float16): lo hi + hi lo + hi hi is formed, three products in place of one.
 // Rows and columns lie at 16-byte addresses and whole pieces of 8 elements may be read: `across` rows or columns (of i or j), and
 // along k up to the next multiple of 8, zeros behind K.
 struct Operand16 {

@@ -187,11 +187,58 @@ __device__ __forceinline__ void second_half(bool fetching, const TileP& tp, cons
   }(std::make_integer_sequence<int, FM>());
 }
 
+// The sums of a wavefront go through LDS, 64 rows of 64 columns at a time, so that stores run along the result's rows.
+template <int KIND, int TM, int FN>
+__device__ __forceinline__ void store_sums(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t b, int64_t i0,
+                                           int64_t j0, bool mirrored) {
+  const int lane = threadIdx.x % 64;
+  float* mine = (float*)lds + threadIdx.x / 64 * 64 * kOutPad;
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < TM / 64; ++h) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int y = 0; y < FN; ++y)
+        *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[4 * h + x][y];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int64_t ri = i0 + 64 * h;
+    const float none[4] = {0.f, 0.f, 0.f, 0.f};
+    const int c = (lane & 15) * 4;                     // a row of 64 columns takes 16 lanes
+    if (partial != nullptr) {
+      const int64_t ldp = (a.N + 3) / 4 * 4;
+      float* part = partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp;
+#pragma unroll 4
+      for (int q = 0; q < 16; ++q) {
+        const int r = 4 * q + (lane >> 4);
+        if (ri + r < a.M && j0 + c < a.N) *reinterpret_cast<f32x4*>(part + (ri + r) * ldp + j0 + c) = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
+      }
+    } else {
+      if (!a.epi.flip) {
+        float bias[4];
+        epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
+#pragma unroll 2
+        for (int q = 0; q < 16; ++q) {
+          const int r = 4 * q + (lane >> 4);
+          emit4<KIND>(a.epi, b, ri + r, j0 + c, a.M, a.N, false, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
+        }
+      }
+      if (a.epi.flip || mirrored) {                    // written along j's rows, which run over i
+#pragma unroll 2
+        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, j0 + 4 * q, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // blockIdx: block, matrix of the batch, share of k.  With several shares the sums go to `partial`, one M x (N to a multiple of 4)
 // matrix after the other.
-template <int KIND, bool PK, bool QK, int BM, int BN, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64)) void mm16_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
-  constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+template <bool PK, bool QK, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
+  constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16, STAGES = 2, KIND = kMm16Bf16;
   using TileP = Tile<PK, BM, NT>;
   using TileQ = Tile<QK, BN, NT>;
   static_assert(TN == 64 && TM % 64 == 0, "wavefronts of 64 columns and whole 64 rows");
@@ -199,8 +246,7 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
   __shared__ __attribute__((aligned(1024))) char lds_all[kTiles > kOut ? kTiles : kOut];
   char(*lds)[TileP::kBytes + TileQ::kBytes] = reinterpret_cast<char(*)[TileP::kBytes + TileQ::kBytes]>(lds_all);
   int ti, tj;
-  if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
-  else block_of(blockIdx.x, tm, tn, &ti, &tj);
+  block_of(blockIdx.x, tm, tn, &ti, &tj);
   const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN, b = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wi = (wave / WN) * TM, wj = (wave % WN) * TN;
   const int64_t step_p = PK ? kBK * a.P.ld * 2 : kBK * 2, step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
@@ -215,21 +261,13 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
   Fragments<QK, BN, FN> fq;
   fp.plan(wi);
   fq.plan(wj);
-  const int steps = KIND == kMm16Pairs ? 3 * ks : ks;
+  const int steps = ks;
   const bool whole = a.K % kBK == 0 || first + ks < ks_all;
   // Where step t's pieces come from, and the k that its last step has.
   auto source = [&](int t, const char** p, const char** q) {
-    int k = t;
-    *p = P; *q = Q;
-    if constexpr (KIND == kMm16Pairs) {
-      const int part = t / ks;                       // lo hi, hi lo, hi hi
-      k = t - part * ks;
-      if (part == 0) *p += 2 * a.P.plane;
-      if (part == 1) *q += 2 * a.Q.plane;
-    }
-    *p += k * step_p;
-    *q += k * step_q;
-    return k + 1 < ks || whole ? kBK : (int)(a.K - (int64_t)(first + k) * kBK);
+    *p = P + t * step_p;
+    *q = Q + t * step_q;
+    return t + 1 < ks || whole ? kBK : (int)(a.K - (int64_t)(first + t) * kBK);
   };
   auto fetch = [&](int t) {
     const char *p, *q;
@@ -259,14 +297,6 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
   for (int x = 0; x < FM; ++x) p0[x] = fp.read(lds_address(lds[0]), 0, x);
   for (int t = 0; t < steps; ++t) {
     const uint32_t here = lds_address(lds[t % STAGES]), next = lds_address(lds[(t + 1) % STAGES]);
-    if constexpr (KIND == kMm16Pairs) {
-      if (t == 2 * ks) {
-#pragma unroll
-        for (int x = 0; x < FM; ++x)
-#pragma unroll
-          for (int y = 0; y < FN; ++y) acc[x][y] *= 0x1p-11f;
-      }
-    }
     // A wavefront issues in order: the reads of the second half stand between the products of the first, else the matrix cores
     // would wait for their issue.
     q1[0] = fq.read(here + TileP::kBytes, 1, 0);
@@ -288,49 +318,116 @@ __global__ __launch_bounds__(WM* WN * 64, STAGES > 2 ? 1 : 512 / (WM * WN * 64))
     if (left > 0 && left < kBK) fetch(t + STAGES);
     second_half<TileP, TileQ, KIND, FM, FN>(left == kBK, tp, tq, from_p, from_q, here, fp, fq, next, p0, q0, p1, q1, acc);
   }
-  // The sums go through LDS, 64 rows of a wavefront at a time, so that stores run along the result's rows.
-  const int lane = threadIdx.x % 64;
-  float* mine = (float*)(&lds[0][0]) + wave * 64 * kOutPad;
-  __syncthreads();
-#pragma unroll
-  for (int h = 0; h < TM / 64; ++h) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int y = 0; y < FN; ++y)
-        *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[4 * h + x][y];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int64_t ri = i0 + wi + 64 * h, cj = j0 + wj;
-    float none[4] = {0.f, 0.f, 0.f, 0.f};
-    if (partial != nullptr) {
-      const int64_t ldp = (a.N + 3) / 4 * 4;
-      float* part = partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp;
-#pragma unroll 1
-      for (int q = 0; q < 16; ++q) {
-        const int r = 4 * q + (lane >> 4), c = (lane & 15) * 4;
-        if (ri + r < a.M && cj + c < a.N) *reinterpret_cast<f32x4*>(part + (ri + r) * ldp + cj + c) = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
-      }
+  store_sums<KIND, TM, FN>(a, partial, lds_all, acc, b, i0 + wi, j0 + wj, false);
+}
+
+// Pairs: a step's four tiles (both planes of both operands) lie in LDS together, and three products are formed from the fragments
+// read once: 64 KB fetched for 96 matrix instructions a wavefront, where the planes one after the other would take 96 KB.  Blocks of
+// 128, a wavefront to a SIMD; as above, reads and fetches stand between the products.  Q's rows run over k (QK) or its columns do.
+// (LDS is asked for at the launch: told of it, the compiler would take the accumulators to the other half of a lone wavefront's
+// registers, and move them to and fro.)
+constexpr int kPairsLds = 2 * 4 * 128 * kBK * 2;
+template <bool QK>
+__global__ __launch_bounds__(256, 2) void mm16_pairs_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
+  constexpr int NT = 256, FM = 4, FN = 4, kB = 128;
+  using TileP = Tile<false, kB, NT>;
+  using TileQ = Tile<QK, kB, NT>;
+  constexpr int kP = TileP::kBytes, kQ = TileQ::kBytes, kStage = 2 * (kP + kQ), kEach = TileP::kLoads;
+  static_assert(TileP::kLoads == FM && TileQ::kLoads == FM, "a piece of each tile between the products of a row of blocks");
+  static_assert(2 * kStage == kPairsLds && NT * kOutPad * 4 <= kPairsLds, "the sums fit too");
+  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+  int ti, tj;
+  if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
+  else block_of(blockIdx.x, tm, tn, &ti, &tj);
+  const int64_t i0 = (int64_t)ti * kB, j0 = (int64_t)tj * kB, b = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wi = (wave / 2) * 64, wj = (wave % 2) * 64;
+  const int64_t step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
+  const int first = (int)blockIdx.z * share, ks_all = (int)((a.K + kBK - 1) / kBK), steps = ks_all - first < share ? ks_all - first : share;
+  const char* P = (const char*)a.P.p + 2 * (b * a.P.batch + i0 * a.P.ld) + (int64_t)first * kBK * 2;
+  const char* Q = (const char*)a.Q.p + 2 * (b * a.Q.batch + (QK ? j0 : j0 * a.Q.ld)) + first * step_q;
+  const int64_t lo_p = 2 * a.P.plane, lo_q = 2 * a.Q.plane;
+  TileP tp;
+  TileQ tq;
+  tp.plan(a.P.ld, a.P.across - i0);
+  tq.plan(a.Q.ld, a.Q.across - j0);
+  Fragments<false, kB, FM> fp;
+  Fragments<QK, kB, FN> fq;
+  fp.plan(wi);
+  fq.plan(wj);
+  const uint32_t base = lds_address(lds_all);
+  auto left_of = [&](int t) { const int64_t left = a.K - (int64_t)(first + t) * kBK; return left < kBK ? (int)left : kBK; };
+  auto fetch = [&](int t) {
+    const char *p = P + (int64_t)t * kBK * 2, *q = Q + t * step_q;
+    const uint32_t to = base + (t & 1) * kStage;
+    if (left_of(t) == kBK) {
+      tp.template fetch_some<0, kEach>(p, to);
+      tp.template fetch_some<0, kEach>(p + lo_p, to + kP);
+      tq.template fetch_some<0, kEach>(q, to + 2 * kP);
+      tq.template fetch_some<0, kEach>(q + lo_q, to + 2 * kP + kQ);
     } else {
-      // a row of 64 columns takes 16 lanes; a flipped result is written along its own rows, which run over i
-      if (!a.epi.flip) {
-        const int c = (lane & 15) * 4;
-        float bias[4];
-        epilogue_bias(a.epi, cj + c, (int)(a.N - cj - c < 4 ? a.N - cj - c : 4), bias);
-#pragma unroll 2
-        for (int q = 0; q < 16; ++q) {
-          const int r = 4 * q + (lane >> 4);
-          emit4<KIND>(a.epi, b, ri + r, cj + c, a.M, a.N, false, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
-        }
-      }
-      if (a.epi.flip || (a.symmetric && ti != tj)) {
-#pragma unroll 1
-        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, cj + 4 * q, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
-      }
+      tp.fetch_last(p, to, left_of(t));
+      tp.fetch_last(p + lo_p, to + kP, left_of(t));
+      tq.fetch_last(q, to + 2 * kP, left_of(t));
+      tq.fetch_last(q + lo_q, to + 2 * kP + kQ, left_of(t));
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+  };
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int x = 0; x < FM; ++x)
+#pragma unroll
+    for (int y = 0; y < FN; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  s16x8 ph[2][FM], pl[2][FM], qh[2][FN], ql[2][FN];
+  // the x-th fragments of both planes and operands for a half step
+  auto read = [&](auto set, uint32_t at, auto xs) {
+    constexpr int S = decltype(set)::value, X = decltype(xs)::value;
+    ph[S][X] = fp.read(at, S, X);
+    pl[S][X] = fp.read(at + kP, S, X);
+    qh[S][X] = fq.read(at + 2 * kP, S, X);
+    ql[S][X] = fq.read(at + 2 * kP + kQ, S, X);
+  };
+  auto products = [&](auto set, auto xs) {
+    constexpr int S = decltype(set)::value, X = decltype(xs)::value;
+#pragma unroll
+    for (int y = 0; y < FN; ++y) acc[X][y] = mfma16<kMm16Pairs>(ql[S][y], ph[S][X], acc[X][y]);
+#pragma unroll
+    for (int y = 0; y < FN; ++y) acc[X][y] = mfma16<kMm16Pairs>(qh[S][y], pl[S][X], acc[X][y]);
+#pragma unroll
+    for (int y = 0; y < FN; ++y) acc[X][y] = mfma16<kMm16Pairs>(qh[S][y], ph[S][X], acc[X][y]);
+  };
+  using H0 = std::integral_constant<int, 0>;
+  using H1 = std::integral_constant<int, 1>;
+  auto each = [](auto f) { [&]<int... X>(std::integer_sequence<int, X...>) { (f(std::integral_constant<int, X>()), ...); }(std::make_integer_sequence<int, FM>()); };
+  for (int t = 0; t < 2 && t < steps; ++t) fetch(t);
+  if (steps >= 2) arrived_and_together<4 * kEach>();
+  else arrived_and_together<0>();
+  each([&](auto x) { read(H0(), base, x); });
+  for (int t = 0; t < steps; ++t) {
+    const uint32_t here = base + (t & 1) * kStage, next = base + ((t + 1) & 1) * kStage;
+    each([&](auto x) {
+      read(H1(), here, x);
+      __builtin_amdgcn_sched_barrier(0);
+      products(H0(), x);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    arrived_and_together<0>();                         // step t is in registers, step t + 1 in LDS
+    const bool more = t + 2 < steps, whole = more && left_of(t + 2) == kBK;
+    const char *p = P + (int64_t)(t + 2) * kBK * 2, *q = Q + (t + 2) * step_q;
+    if (more && !whole) fetch(t + 2);
+    each([&](auto x) {
+      constexpr int X = decltype(x)::value;
+      read(H0(), next, x);                             // (behind the last step: of an old one, for nothing)
+      if (whole) {
+        tp.template fetch_some<X, 1>(p, here);
+        tp.template fetch_some<X, 1>(p + lo_p, here + kP);
+        tq.template fetch_some<X, 1>(q, here + 2 * kP);
+        tq.template fetch_some<X, 1>(q + lo_q, here + 2 * kP + kQ);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      products(H1(), x);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
+  store_sums<kMm16Pairs, 64, FN>(a, partial, lds_all, acc, b, i0 + wi, j0 + wj, a.symmetric && ti != tj);
 }
 
 struct Join {
@@ -400,16 +497,32 @@ int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {
   return symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-template <int KIND, bool PK, bool QK>
+hipError_t finish_shares(const Product16& a, const MmPlan& plan, float* part, hipStream_t st) {
+  if (part != nullptr) return launch_mm_join(a.M, a.N, a.batches, a.symmetric, a.epi, plan.splits, part, st);
+  return hipGetLastError();
+}
+
+template <bool PK, bool QK>
 hipError_t mm16_order(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   const int tm = (int)((a.M + plan.tile - 1) / plan.tile), tn = (int)((a.N + plan.tile - 1) / plan.tile);
   const int ks = (int)((a.K + kBK - 1) / kBK), share = (ks + plan.splits - 1) / plan.splits;
-  const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, a.symmetric), (unsigned)a.batches, (unsigned)plan.splits);
+  const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, 0), (unsigned)a.batches, (unsigned)plan.splits);
   float* part = plan.splits > 1 ? partial : nullptr;
-  if (plan.tile == 256) mm16_kernel<KIND, PK, QK, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a, tm, tn, share, part);
-  else mm16_kernel<KIND, PK, QK, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a, tm, tn, share, part);
-  if (part != nullptr) return launch_mm_join(a.M, a.N, a.batches, a.symmetric, a.epi, plan.splits, part, st);
-  return hipGetLastError();
+  if (plan.tile == 256) mm16_kernel<PK, QK, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a, tm, tn, share, part);
+  else mm16_kernel<PK, QK, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a, tm, tn, share, part);
+  return finish_shares(a, plan, part, st);
+}
+
+hipError_t mm16_pairs(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
+  const int tm = (int)((a.M + 127) / 128), tn = (int)((a.N + 127) / 128);
+  const int ks = (int)((a.K + kBK - 1) / kBK), share = (ks + plan.splits - 1) / plan.splits;
+  const dim3 grid((unsigned)blocks_of(a.M, a.N, 128, a.symmetric), (unsigned)a.batches, (unsigned)plan.splits);
+  float* part = plan.splits > 1 ? partial : nullptr;
+  const void* kernel = a.Q.k_rows ? (const void*)mm16_pairs_kernel<true> : (const void*)mm16_pairs_kernel<false>;
+  if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kPairsLds); e != hipSuccess) return e;
+  if (a.Q.k_rows) mm16_pairs_kernel<true><<<grid, 256, kPairsLds, st>>>(a, tm, tn, share, part);
+  else mm16_pairs_kernel<false><<<grid, 256, kPairsLds, st>>>(a, tm, tn, share, part);
+  return finish_shares(a, plan, part, st);
 }
 
 }  // namespace
@@ -428,23 +541,24 @@ hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, 
 }
 
 // Blocks of 256 or 128 and the shares of k, by what they cost in microseconds: a step of a 256-block takes 1.7 (one workgroup fits a
-// compute unit), of a 128-block 0.75 alone on its unit and 1.08 beside another; shares are written and added at 8 TB/s, in a launch
-// of 3.  Measured: 2048 x 2048 x 2048 in pairs, 128-blocks: 84 us in one share, 62 in two, 72 in four; 1024 x 1024 x 4096, bfloat16:
-// 50, 27 (four), 32 (eight); 4096 x 4096 x 4096, bfloat16: 117 in 256-blocks.
+// compute unit), of a 128-block 0.75 alone on its unit and 1.08 beside another, of a 128-block of pairs (one to a unit) 0.9; shares
+// are written and added at 8 TB/s, in a launch of 3.  Measured: 1024 x 1024 x 4096, bfloat16, 128-blocks: 50 us in one share, 27 in
+// four, 32 in eight; 2048 x 2048 x 2048, bfloat16: 31; 4096 x 4096 x 4096, bfloat16: 117 in 256-blocks.
 MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric) {
-  MmPlan best{256, 1, 0};
+  MmPlan best{128, 1, 0};
   double least = 1e300;
-  const int64_t ks = (K + kBK - 1) / kBK, parts = kind == kMm16Pairs ? 3 : 1;
-  for (int tile = 256; tile >= 128; tile /= 2) {
+  const int64_t ks = (K + kBK - 1) / kBK;
+  for (int tile = kind == kMm16Pairs ? 128 : 256; tile >= 128; tile /= 2) {
     const int64_t blocks = blocks_of(M, N, tile, symmetric) * batches;
     for (int64_t splits = 1; splits <= 32 && splits <= (ks > 0 ? ks : 1); ++splits) {
       const int64_t share = (ks + splits - 1) / splits;
-      if (splits > 1 && ((ks + share - 1) / share != splits || share * parts < 4 || blocks * splits > 1024)) continue;   // no empty shares, no tiny ones
+      if (splits > 1 && ((ks + share - 1) / share != splits || share < (kind == kMm16Pairs ? 2 : 4) || blocks * splits > 1024)) continue;   // no empty shares, no tiny ones
       const int64_t groups = blocks * splits;
       double step;
-      if (tile == 256) step = 1.7 * (double)((groups + 255) / 256);
+      if (kind == kMm16Pairs) step = 0.9 * (double)((groups + 255) / 256);
+      else if (tile == 256) step = 1.7 * (double)((groups + 255) / 256);
       else step = 1.08 * (double)(groups / 512) + (groups % 512 == 0 ? 0.0 : groups % 512 <= 256 ? 0.75 : 1.08);
-      double cost = (double)(share * parts) * step;
+      double cost = (double)share * step;
       const double bytes = (double)splits * (double)batches * (double)M * (double)((N + 3) / 4 * 4) * 4.0;
       if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;
       if (cost < least) {
@@ -465,11 +579,11 @@ bool mm16_takes(const Operand& x, int64_t across, int64_t K) {
 hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.kind == kMm16Bf16) {
-    if (a.P.k_rows) return a.Q.k_rows ? mm16_order<kMm16Bf16, true, true>(a, plan, partial, st) : hipErrorInvalidValue;
-    return a.Q.k_rows ? mm16_order<kMm16Bf16, false, true>(a, plan, partial, st) : mm16_order<kMm16Bf16, false, false>(a, plan, partial, st);
+    if (a.symmetric) return hipErrorInvalidValue;
+    if (a.P.k_rows) return a.Q.k_rows ? mm16_order<true, true>(a, plan, partial, st) : hipErrorInvalidValue;
+    return a.Q.k_rows ? mm16_order<false, true>(a, plan, partial, st) : mm16_order<false, false>(a, plan, partial, st);
   }
-  if (a.P.k_rows) return hipErrorInvalidValue;
-  return a.Q.k_rows ? mm16_order<kMm16Pairs, false, true>(a, plan, partial, st) : mm16_order<kMm16Pairs, false, false>(a, plan, partial, st);
+  return a.P.k_rows ? hipErrorInvalidValue : mm16_pairs(a, plan, partial, st);
 }
 
 }  // namespace ilargi

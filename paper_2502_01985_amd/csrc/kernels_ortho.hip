@@ -7,8 +7,9 @@ namespace {
 
 constexpr int kNormParts = 256;
 
-// The pairs hold kUnit X, kUnit A and kUnit B: float16 keeps all eleven bits of its plane from 2.4e-7 to 255 then.
-constexpr float kUnit = 256.0f;
+// The pairs hold kUnit X and kUnit A, and B times a power of two that brings it to at most 60000 (float16 ends at 65504): their low
+// planes then count in 1.5e-11 of X and A.
+constexpr float kUnit = 4096.0f;
 
 // Sums of squares of a share of one matrix's rows, in 64 bits: the norm neither overflows nor loses small entries.
 template <class T>
@@ -68,23 +69,28 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Whether the iteration stays where pairs of float16 hold it: some interval [0, R] that holds the first singular values (at
-// most 1) is mapped into [-R, R] by s (a + b s^2 + c s^4), and the entries of B, at most |b| R^2 + |c| R^4, are below 200.
-bool stays_bounded(const float* coef) {
+// Whether the iteration stays where pairs of float16 hold it: some interval [0, R], R <= 2, that holds the first singular values (at
+// most 1) is mapped into [-R, R] by s (a + b s^2 + c s^4).  Then the entries of X are at most R, of A R^2, and of B |b| R^2 + |c| R^4,
+// which gives B's unit; 0: it does not stay.
+float unit_of_b(const float* coef) {
   const double a = coef[0], b = coef[1], c = coef[2];
   for (int q = 0; q <= 40; ++q) {
     const double R = 1.0 + 0.025 * q;
     double top = 0.0;
     bool number = true;
-    for (int k = 0; k <= 1000; ++k) {
-      const double s = R * k / 1000.0, v = s * (a + b * s * s + c * s * s * s * s);
+    for (int k = 0; k <= 500; ++k) {
+      const double s = R * k / 500.0, v = s * (a + b * s * s + c * s * s * s * s);
       if (!(v == v)) number = false;
       if (v > top) top = v;
       if (-v > top) top = -v;
     }
-    if (number && top <= R && (b < 0 ? -b : b) * R * R + (c < 0 ? -c : c) * R * R * R * R < 200.0) return true;
+    if (!number || top > R) continue;
+    const double most = (b < 0 ? -b : b) * R * R + (c < 0 ? -c : c) * R * R * R * R;
+    double unit = 4096.0;
+    while (unit > 1.0 && unit * most > 60000.0) unit /= 2.0;
+    return unit * most <= 60000.0 ? (float)unit : 0.0f;
   }
-  return false;
+  return 0.0f;
 }
 
 struct OrthoLayout {
@@ -125,7 +131,7 @@ void finish(const OrthoArgs& a, float unit, Epilogue* e) {
   e->flip = a.rows > a.cols;
 }
 
-hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipStream_t st) {
+hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, float unit_b, char* ws, hipStream_t st) {
   float* partial = (float*)(ws + o.partial);
   const int64_t px = a.batch * o.sp * o.lp, pa = a.batch * o.sp * o.sp;
   void *A = ws + o.A, *B = ws + o.B;
@@ -144,14 +150,14 @@ hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, char* ws, hip
     p.K = o.sp;
     p.P = {A, o.sp, 0, o.sp * o.sp, pa, o.sp};
     p.Q = p.P;
-    p.epi.s0 = a.coef[2] / kUnit; p.epi.s1 = a.coef[1];
+    p.epi.s0 = a.coef[2] * unit_b / (kUnit * kUnit); p.epi.s1 = a.coef[1] * unit_b / kUnit;
     p.epi.src = A; p.epi.ld_src = o.sp; p.epi.batch_src = o.sp * o.sp; p.epi.src_plane = pa;
     p.epi.out = B;
     if (hipError_t e = launch_mm16(p, o.square, partial, st); e != hipSuccess) return e;
     p.N = o.lp; p.symmetric = 0;
     p.P.p = B;
     p.Q = {x, o.lp, 1, o.sp * o.lp, px, o.lp};
-    p.epi.s0 = 1.0f / kUnit; p.epi.s1 = a.coef[0];
+    p.epi.s0 = 1.0f / unit_b; p.epi.s1 = a.coef[0];
     p.epi.src = x; p.epi.ld_src = o.lp; p.epi.batch_src = o.sp * o.lp; p.epi.src_plane = px;
     p.epi.out = next; p.epi.ld_out = o.lp; p.epi.batch_out = o.sp * o.lp; p.epi.out_plane = px;
     if (t + 1 == a.steps) {
@@ -198,7 +204,8 @@ template <class T>
 hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   const OrthoLayout o = ortho_layout(a.batch, a.rows, a.cols);
   double* parts = (double*)ws;
-  const bool pairs = stays_bounded(a.coef);
+  const float unit_b = unit_of_b(a.coef);
+  const bool pairs = unit_b > 0.0f;
   const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;
   const int tc = (int)((ld_x + 31) / 32);
   const dim3 tiles((unsigned)((rows_x + 31) / 32 * tc), (unsigned)a.batch), norms(kNormParts, (unsigned)a.batch);
@@ -206,7 +213,7 @@ hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   if (pairs) ortho_load_kernel<T, true><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
   else ortho_load_kernel<T, false><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return pairs ? iterate_pairs(a, o, ws, st) : iterate_f32(a, o, ws, st);
+  return pairs ? iterate_pairs(a, o, unit_b, ws, st) : iterate_f32(a, o, ws, st);
 }
 
 }  // namespace

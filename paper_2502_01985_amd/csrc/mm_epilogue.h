@@ -15,12 +15,12 @@ __device__ __forceinline__ void store4_any(void* p, int64_t at, int bf16, int va
   else store_piece<float, 4>((float*)p + at, valid, f);
 }
 
-// A pair of float16 planes: x = hi + 2^-11 lo, 22 bits.
-__device__ __forceinline__ float pair_value(const _Float16* p, int64_t at, int64_t plane) { return fmaf((float)p[at + plane], 0x1p-11f, (float)p[at]); }
+// A pair of float16 planes: x = hi + lo, 22 bits of entries that are not small against the largest (lo counts in 2^-24).
+__device__ __forceinline__ float pair_value(const _Float16* p, int64_t at, int64_t plane) { return (float)p[at] + (float)p[at + plane]; }
 __device__ __forceinline__ void pair_store(_Float16* p, int64_t at, int64_t plane, float x) {
   const _Float16 hi = (_Float16)x;
   p[at] = hi;
-  p[at + plane] = (_Float16)((x - (float)hi) * 0x1p11f);
+  p[at + plane] = (_Float16)(x - (float)hi);
 }
 
 // out(i, j) = s0 v + s1 src(i, j) in pairs, columns j .. j + valid.
@@ -32,13 +32,13 @@ __device__ __forceinline__ void epilogue4_pairs(const Epilogue& e, int64_t b, in
     load_piece<_Float16, 4>(src, valid, hi);
     load_piece<_Float16, 4>(src + e.src_plane, valid, lo);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) t[q] = fmaf(lo[q], 0x1p-11f, hi[q]);
+    for (int q = 0; q < 4; ++q) t[q] = hi[q] + lo[q];
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const float x = fmaf(e.s0, v[q], e.s1 * t[q]);
     hi[q] = (float)(_Float16)x;
-    lo[q] = (x - hi[q]) * 0x1p11f;
+    lo[q] = x - hi[q];
   }
   store_piece<_Float16, 4>(out, valid, hi);
   store_piece<_Float16, 4>(out + e.out_plane, valid, lo);
