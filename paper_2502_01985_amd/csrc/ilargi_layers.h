@@ -238,6 +238,9 @@ struct OrthoArgs {
 };
 size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st);
+// Small matrices, whose iteration stays in pairs of float16 times these units.
+bool ortho_one_takes(int64_t rows, int64_t cols);
+hipError_t launch_ortho_one(const OrthoArgs& a, float unit, float unit_b, hipStream_t st);
 
 }  // namespace ilargi
 #endif

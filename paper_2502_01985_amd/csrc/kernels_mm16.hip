@@ -145,16 +145,15 @@ __device__ __forceinline__ void upper_block(int id, int tn, int* ti, int* tj) {
   *tj = r + id;
 }
 
-// What is done with four neighbouring sums of row i; `mirrored`: of a symmetric result, at their places below the diagonal.
+// What is done with four neighbouring sums of row i.
 template <int KIND>
-__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, bool mirrored, const float (&bias)[4], f32x4 t) {
+__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, const float (&bias)[4], f32x4 t) {
   if (i >= M || j >= N) return;
   const int valid = (int)(N - j < 4 ? N - j : 4);
   float v[4] = {t[0], t[1], t[2], t[3]};
   if constexpr (KIND != kMm16Bf16) {
     if (e.out_plane != 0) {
-      if (mirrored) epilogue4_pairs_mirrored(e, b, i, j, valid, v);
-      else epilogue4_pairs(e, b, i, j, valid, v);
+      epilogue4_pairs(e, b, i, j, valid, v);
       return;
     }
   }
@@ -221,12 +220,22 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
 #pragma unroll 2
         for (int q = 0; q < 16; ++q) {
           const int r = 4 * q + (lane >> 4);
-          emit4<KIND>(a.epi, b, ri + r, j0 + c, a.M, a.N, false, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
+          emit4<KIND>(a.epi, b, ri + r, j0 + c, a.M, a.N, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
         }
       }
-      if (a.epi.flip || mirrored) {                    // written along j's rows, which run over i
+      if (a.epi.flip) {                                // written along j's rows, which run over i
 #pragma unroll 2
-        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, j0 + 4 * q, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
+        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, j0 + 4 * q, a.M, a.N, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
+      }
+      if constexpr (KIND == kMm16Pairs) {
+        if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
+#pragma unroll 2
+          for (int q = 0; q < 16; ++q) {
+            const int r = 4 * q + (lane >> 4);
+            const f32x4 v = {mine[c * kOutPad + r], mine[(c + 1) * kOutPad + r], mine[(c + 2) * kOutPad + r], mine[(c + 3) * kOutPad + r]};
+            emit4<KIND>(a.epi, b, j0 + r, ri + c, a.N, a.M, none, v);
+          }
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -484,12 +493,16 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits
   const bool turned = a.epi.flip || (a.symmetric && ti != tj);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (i0 + r < a.M && j0 + c < a.N) s = add_shares(partial + (b * a.M + i0 + r) * ldp + j0 + c, a.batches * a.M * ldp, splits);
-  if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, false, none, s);
+  if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, none, s);
   if (!turned) return;
   *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
   __syncthreads();
-  const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
-  emit4<KIND>(a.epi, b, i0 + x, j0 + y, a.M, a.N, true, none, *reinterpret_cast<const f32x4*>(&tile[x][y]));
+  if (a.epi.flip) {
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
+    emit4<KIND>(a.epi, b, i0 + x, j0 + y, a.M, a.N, none, *reinterpret_cast<const f32x4*>(&tile[x][y]));
+  } else {
+    emit4<KIND>(a.epi, b, j0 + r, i0 + c, a.N, a.M, none, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
+  }
 }
 
 int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {

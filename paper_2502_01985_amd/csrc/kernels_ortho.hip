@@ -206,6 +206,7 @@ hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   double* parts = (double*)ws;
   const float unit_b = unit_of_b(a.coef);
   const bool pairs = unit_b > 0.0f;
+  if (pairs && ortho_one_takes(a.rows, a.cols)) return launch_ortho_one(a, kUnit, unit_b, st);
   const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;
   const int tc = (int)((ld_x + 31) / 32);
   const dim3 tiles((unsigned)((rows_x + 31) / 32 * tc), (unsigned)a.batch), norms(kNormParts, (unsigned)a.batch);

@@ -43,14 +43,6 @@ __device__ __forceinline__ void epilogue4_pairs(const Epilogue& e, int64_t b, in
   store_piece<_Float16, 4>(out, valid, hi);
   store_piece<_Float16, 4>(out + e.out_plane, valid, lo);
 }
-// The same values at (j .. j + valid, i), for a symmetric src: lanes next to each other hold neighbouring i.
-__device__ __forceinline__ void epilogue4_pairs_mirrored(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&v)[4]) {
-  for (int q = 0; q < valid && q < 4; ++q) {
-    const float t = e.src != nullptr ? pair_value((const _Float16*)e.src, b * e.batch_src + (j + q) * e.ld_src + i, e.src_plane) : 0.0f;
-    pair_store((_Float16*)e.out, b * e.batch_out + (j + q) * e.ld_out + i, e.out_plane, fmaf(e.s0, v[q], e.s1 * t));
-  }
-}
-
 // The bias of columns j .. j + valid, zeros where there is none.
 __device__ __forceinline__ void epilogue_bias(const Epilogue& e, int64_t j, int valid, float (&bias)[4]) {
 #pragma unroll
