@@ -205,7 +205,8 @@ struct Product16 {
   Epilogue epi;
 };
 MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric);
-bool mm16_takes(const Operand& x, int64_t across, int64_t K);
+// A bfloat16 matrix laid out for launch_mm16: rows of (cols to a multiple of 8) elements.
+hipError_t launch_pack16(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, hipStream_t st);
 hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st);
 
 struct LayerGradArgs {

@@ -51,38 +51,81 @@ ilargi_status_t check_layer(const char* what, const ilargi_layer_t* y) {
   return ILARGI_OK;
 }
 
-struct LayerLayout {
-  size_t forward = 0;                                         // bytes of the forward call
-  size_t dz = 0, partial = 0, shares = 0, gradient = 0;       // offsets and bytes of the gradient call
-};
 size_t shares_bytes(bool h, int64_t M, int64_t N, int64_t K) {
   const size_t f = mm_f32_plan(M, N, K, 1).partial_bytes, m = h ? mm16_plan(M, N, K, 1, kMm16Bf16, 0).partial_bytes : 0;
   return up256(f > m ? f : m);
 }
+
+// Products of so many operations are formed on the 16-bit matrix cores also where an operand has to be laid out for them first: a
+// launch of about 3 us and a pass over each operand, against 50 to 100 TFLOP/s on the float32 cores.  bfloat16 with odd rows, forward:
+// 1003 x 701 x 1001 (1.4e9 operations) 31 us in float32; 2001 x 701 x 603 (1.7e9) 29 laid out; 4001 x 999 x 1001 (8e9) 36 laid out, 98
+// in float32.
+constexpr double kPackOps = 1.5e9;
+bool worth_packing(int64_t n, int64_t k, int64_t m) { return 2.0 * (double)n * (double)k * (double)m >= kPackOps; }
+int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
+
+struct LayerLayout {
+  size_t x = 0, w = 0;                          // X and W laid out (bfloat16), in both calls
+  size_t forward_shares = 0, forward = 0;       // the forward call's shares of k, and its bytes
+  size_t dz = 0, partial = 0, shares = 0, gradient = 0;
+};
 LayerLayout layer_layout(const ilargi_layer_t& y) {
   LayerLayout l;
   const bool h = y.type == ILARGI_TYPE_BF16;
-  l.forward = mm_rows_takes(y.n, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k);
-  l.dz = 0;
-  l.partial = up256((size_t)y.n * (size_t)((y.m + 7) / 8 * 8) * (h ? 2 : 4));
+  if (h && worth_packing(y.n, y.k, y.m)) {
+    l.w = up256(2 * (size_t)y.n * (size_t)up8(y.k));
+    l.forward_shares = l.w + up256(2 * (size_t)y.k * (size_t)up8(y.m));
+  }
+  l.forward = l.forward_shares + (mm_rows_takes(y.n, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k));
+  l.dz = l.forward_shares;
+  l.partial = l.dz + up256((size_t)y.n * (size_t)up8(y.m) * (h ? 2 : 4));
   l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
   const size_t x = shares_bytes(h, y.n, y.k, y.m), w = shares_bytes(h, y.k, y.m, y.n);
   l.gradient = l.shares + (x > w ? x : w);
   return l;
 }
 
-// A product of the layer's matrices: bfloat16 operands that lie in whole 16-byte pieces on the 16-bit matrix cores, others in float32.
-hipError_t product(const Product& p, float* partial, hipStream_t st) {
-  if (p.P.bf16 && mm16_takes(p.P, p.M, p.K) && mm16_takes(p.Q, p.N, p.K)) {
+// A matrix of the layer as it lies, or laid out in whole 16-byte pieces.
+struct Matrix {
+  const void* p;
+  int64_t ld, rows, cols;
+};
+bool in_pieces(const Matrix& m) { return reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld % 8 == 0 && m.ld < (1 << 22) && m.ld >= up8(m.cols); }
+
+// C = P Q (or with one of them transposed) for two matrices of the layer; `padded` of each: zeros stand behind its rows.
+struct Factor {
+  Matrix m;
+  int k_rows;
+  bool padded;
+};
+hipError_t product(const Factor& P, const Factor& Q, int64_t M, int64_t N, int64_t K, bool h, const Epilogue& epi, float* partial, hipStream_t st) {
+  auto ready = [&](const Factor& f) { return in_pieces(f.m) && (f.padded || f.m.cols % 8 == 0); };
+  if (h && ready(P) && ready(Q)) {
     Product16 a{};
-    a.P = {p.P.p, p.P.ld, p.P.k_rows, 0, 0, p.M};
-    a.Q = {p.Q.p, p.Q.ld, p.Q.k_rows, 0, 0, p.N};
-    a.M = p.M; a.N = p.N; a.K = p.K; a.batches = 1;
+    auto operand = [&](const Factor& f, int64_t across) { return Operand16{f.m.p, f.m.ld, f.k_rows, 0, 0, f.k_rows ? up8(f.m.cols) : across}; };
+    a.P = operand(P, M);
+    a.Q = operand(Q, N);
+    a.M = M; a.N = N; a.K = K; a.batches = 1;
     a.kind = kMm16Bf16;
-    a.epi = p.epi;
-    return launch_mm16(a, mm16_plan(p.M, p.N, p.K, 1, kMm16Bf16, 0), partial, st);
+    a.epi = epi;
+    return launch_mm16(a, mm16_plan(M, N, K, 1, kMm16Bf16, 0), partial, st);
   }
-  return launch_mm_f32(p, mm_f32_plan(p.M, p.N, p.K, 1), partial, st);
+  Product a{};
+  a.P = {P.m.p, P.m.ld, P.k_rows, h, 0};
+  a.Q = {Q.m.p, Q.m.ld, Q.k_rows, h, 0};
+  a.M = M; a.N = N; a.K = K; a.batches = 1;
+  a.epi = epi;
+  return launch_mm_f32(a, mm_f32_plan(M, N, K, 1), partial, st);
+}
+
+// The matrix laid out at `at` if the layer's products are worth it and it does not lie so already.
+hipError_t lay_out(const ilargi_layer_t& y, Factor* f, char* at, hipStream_t st) {
+  if (y.type != ILARGI_TYPE_BF16 || !worth_packing(y.n, y.k, y.m) || (in_pieces(f->m) && f->m.cols % 8 == 0)) return hipSuccess;
+  const hipError_t e = launch_pack16(f->m.p, f->m.ld, f->m.rows, f->m.cols, at, st);
+  f->m.p = at;
+  f->m.ld = up8(f->m.cols);
+  f->padded = true;
+  return e;
 }
 
 }  // namespace
@@ -133,18 +176,28 @@ ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_
     return refuse(ILARGI_ERR_SHAPE, "linear: a leading dimension below the matrix's columns");
   if (y.n == 0) return ILARGI_OK;
   if (X == nullptr || W == nullptr || out == nullptr) return refuse(ILARGI_ERR_NULL, "linear: X, W or out is NULL");
-  if (ilargi_status_t e = check_workspace("linear", workspace, workspace_bytes, layer_layout(y).forward); e != ILARGI_OK) return e;
+  const LayerLayout l = layer_layout(y);
+  if (ilargi_status_t e = check_workspace("linear", workspace, workspace_bytes, l.forward); e != ILARGI_OK) return e;
   const int h = y.type == ILARGI_TYPE_BF16;
-  Product p{};
-  p.M = y.n; p.N = y.m; p.K = y.k; p.batches = 1;
-  p.P = {X, ld_x, 0, h, 0};
-  p.Q = {W, ld_w, 1, h, 0};
-  p.epi.mode = kEpiLinear;
-  p.epi.bias = bias; p.epi.src = residual; p.epi.ld_src = ld_res; p.epi.src_bf16 = h;
-  p.epi.pre = pre; p.epi.ld_pre = ld_pre; p.epi.act = y.act;
-  p.epi.out = out; p.epi.ld_out = ld_out; p.epi.out_bf16 = h;
-  if (mm_rows_takes(y.n, h)) return done("linear", launch_mm_rows(p, mm_rows_plan(y.n, y.m, y.k), (float*)workspace, (hipStream_t)stream));
-  return done("linear", product(p, (float*)workspace, (hipStream_t)stream));
+  hipStream_t st = (hipStream_t)stream;
+  char* ws = (char*)workspace;
+  Epilogue epi{};
+  epi.mode = kEpiLinear;
+  epi.bias = bias; epi.src = residual; epi.ld_src = ld_res; epi.src_bf16 = h;
+  epi.pre = pre; epi.ld_pre = ld_pre; epi.act = y.act;
+  epi.out = out; epi.ld_out = ld_out; epi.out_bf16 = h;
+  if (mm_rows_takes(y.n, h)) {
+    Product p{};
+    p.M = y.n; p.N = y.m; p.K = y.k; p.batches = 1;
+    p.P = {X, ld_x, 0, h, 0};
+    p.Q = {W, ld_w, 1, h, 0};
+    p.epi = epi;
+    return done("linear", launch_mm_rows(p, mm_rows_plan(y.n, y.m, y.k), (float*)(ws + l.forward_shares), st));
+  }
+  Factor x{{X, ld_x, y.n, y.k}, 0, false}, w{{W, ld_w, y.k, y.m}, 1, false};
+  if (hipError_t e = lay_out(y, &x, ws + l.x, st); e != hipSuccess) return done("linear", e);
+  if (hipError_t e = lay_out(y, &w, ws + l.w, st); e != hipSuccess) return done("linear", e);
+  return done("linear", product(x, w, y.n, y.m, y.k, h, epi, (float*)(ws + l.forward_shares), st));
 }
 
 ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_out, int64_t ld_out, const void* pre, int64_t ld_pre,
@@ -162,30 +215,33 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
   const int h = y.type == ILARGI_TYPE_BF16;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
+  float* shares = (float*)(ws + l.shares);
   const bool products = d_X != nullptr || d_W != nullptr;
-  void* dz = bent && products ? ws + l.dz : nullptr;
-  LayerGradArgs g{y.n, y.m, d_out, ld_out, pre, ld_pre, y.act, h, dz, y.m, d_bias, accumulate};
+  Factor z{{d_out, ld_out, y.n, y.m}, 0, false};
+  // g, where it is not d_out itself, or d_out does not lie in pieces and the products are worth it
+  if (products && (bent || (h && worth_packing(y.n, y.k, y.m) && !(in_pieces(z.m) && y.m % 8 == 0)))) {
+    z.m.p = ws + l.dz;
+    z.m.ld = up8(y.m);
+    z.padded = true;
+  }
+  LayerGradArgs g{y.n, y.m, d_out, ld_out, pre, ld_pre, y.act, h, z.padded ? ws + l.dz : nullptr, up8(y.m), d_bias, accumulate};
   if (hipError_t e = launch_layer_grad(g, (float*)(ws + l.partial), st); e != hipSuccess) return done("linear_grad", e);
-  const Operand z = {bent ? dz : d_out, bent ? y.m : ld_out, 0, h, 0};
-  Product p{};
-  p.batches = 1;
-  p.epi.mode = kEpiScale;
-  p.epi.s0 = 1.0f; p.epi.out_bf16 = h;
+  Epilogue epi{};
+  epi.mode = kEpiScale;
+  epi.s0 = 1.0f; epi.out_bf16 = h;
   if (d_X != nullptr) {
-    p.M = y.n; p.N = y.k; p.K = y.m;
-    p.P = z;
-    p.Q = {W, ld_w, 0, h, 0};
-    p.epi.out = d_X; p.epi.ld_out = ld_dx;
-    if (hipError_t e = product(p, (float*)(ws + l.shares), st); e != hipSuccess) return done("linear_grad", e);
+    Factor w{{W, ld_w, y.k, y.m}, 0, false};
+    if (hipError_t e = lay_out(y, &w, ws + l.w, st); e != hipSuccess) return done("linear_grad", e);
+    epi.out = d_X; epi.ld_out = ld_dx;
+    if (hipError_t e = product(z, w, y.n, y.k, y.m, h, epi, shares, st); e != hipSuccess) return done("linear_grad", e);
   }
   if (d_W != nullptr) {
-    p.M = y.k; p.N = y.m; p.K = y.n;
-    p.P = {X, ld_x, 1, h, 0};
-    p.Q = z;
-    p.Q.k_rows = 1;
-    p.epi.out = d_W; p.epi.ld_out = ld_dw;
-    if (accumulate) { p.epi.base = d_W; p.epi.s2 = 1.0f; }
-    if (hipError_t e = product(p, (float*)(ws + l.shares), st); e != hipSuccess) return done("linear_grad", e);
+    Factor x{{X, ld_x, y.n, y.k}, 1, false};
+    if (hipError_t e = lay_out(y, &x, ws + l.x, st); e != hipSuccess) return done("linear_grad", e);
+    z.k_rows = 1;
+    epi.out = d_W; epi.ld_out = ld_dw;
+    if (accumulate) { epi.base = d_W; epi.s2 = 1.0f; }
+    if (hipError_t e = product(x, z, y.k, y.m, y.n, h, epi, shares, st); e != hipSuccess) return done("linear_grad", e);
   }
   return ILARGI_OK;
 }

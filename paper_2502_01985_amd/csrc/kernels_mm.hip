@@ -171,19 +171,20 @@ __global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_
   const int cl = threadIdx.x % 32, rl = threadIdx.x / 32;
   const int64_t j = ((int64_t)blockIdx.x * 32 + cl) * 4;
   const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < a.n ? r0 + rows_per : a.n;
-  const int valid = (int)(a.m - j < 4 ? a.m - j : 4);
+  const int valid = (int)(a.m - j < 0 ? 0 : a.m - j < 4 ? a.m - j : 4);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (valid > 0) {
+  if (valid > 0 || (a.dz != nullptr && j < a.ld_dz)) {
     for (int64_t i = r0 + rl; i < r1; i += 8) {
       float g[4];
-      load_piece<T, 4>((const T*)a.d_out + i * a.ld_out + j, valid, g);
+      load_piece<T, 4>((const T*)a.d_out + i * a.ld_out + (valid > 0 ? j : 0), valid, g);
       if (a.act != ILARGI_ACT_NONE) {
         float z[4];
-        load_piece<T, 4>((const T*)a.pre + i * a.ld_pre + j, valid, z);
+        load_piece<T, 4>((const T*)a.pre + i * a.ld_pre + (valid > 0 ? j : 0), valid, z);
 #pragma unroll
         for (int q = 0; q < 4; ++q) g[q] *= act_slope(z[q], a.act);
       }
-      if (a.dz != nullptr) store_piece<T, 4>((T*)a.dz + i * a.ld_dz + j, valid, g);
+      // (rows of dz are whole pieces of eight, with zeros behind their end)
+      if (a.dz != nullptr) store_piece<T, 4>((T*)a.dz + i * a.ld_dz + j, 4, g);
 #pragma unroll
       for (int q = 0; q < 4; ++q) s[q] += g[q];
     }
@@ -234,7 +235,7 @@ hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t
   const int64_t per = bias_rows(a.n), chunks = (a.n + per - 1) / per;
   if (a.d_bias == nullptr) partial = nullptr;
   if (chunks > 0 && (a.dz != nullptr || partial != nullptr)) {
-    const dim3 grid((unsigned)((a.m + 127) / 128), (unsigned)chunks);
+    const dim3 grid((unsigned)(((a.dz != nullptr ? a.ld_dz : a.m) + 127) / 128), (unsigned)chunks);
     if (a.bf16) layer_grad_kernel<bf16_t><<<grid, 256, 0, st>>>(a, per, partial);
     else layer_grad_kernel<float><<<grid, 256, 0, st>>>(a, per, partial);
   }

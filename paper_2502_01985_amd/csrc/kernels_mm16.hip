@@ -583,10 +583,33 @@ MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int
   return best;
 }
 
-// Whether the kernel reads this operand as it lies: 16-byte pieces that begin at 16-byte addresses and end with the matrix,
-// offsets within a tile of 32 bits.
-bool mm16_takes(const Operand& x, int64_t across, int64_t K) {
-  return reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld % 8 == 0 && x.ld < (1 << 22) && (x.k_rows ? across : K) % 8 == 0;
+namespace {
+
+// Rows of bfloat16 at any address, laid out in whole 16-byte pieces with zeros behind their end; 2^sh lanes a row.
+__global__ __launch_bounds__(256) void pack16_kernel(const bf16_t* __restrict__ src, int64_t ld, int64_t rows, int64_t cols, bf16_t* __restrict__ dst, int sh) {
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> sh, ldp = (cols + 7) / 8 * 8;
+  if (r >= rows) return;
+  for (int64_t c = (int64_t)(threadIdx.x & ((1 << sh) - 1)) * 8; c < cols; c += 8ll << sh) {
+    const bf16_t* p = src + r * ld + c;
+    Piece<bf16_t, 8> t;
+    if (cols - c >= 8) {
+      t = *reinterpret_cast<const Piece<bf16_t, 8>*>(p);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) t.v[q] = q < cols - c ? p[q] : (bf16_t)0.0f;
+    }
+    *reinterpret_cast<uint4*>(dst + r * ldp + c) = __builtin_bit_cast(uint4, t);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pack16(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, hipStream_t st) {
+  if (rows == 0) return hipSuccess;
+  int sh = ilog2_ceil((cols + 7) / 8);
+  if (sh > 6) sh = 6;
+  pack16_kernel<<<(unsigned)(((rows << sh) + 255) / 256), 256, 0, st>>>((const bf16_t*)src, ld, rows, cols, (bf16_t*)dst, sh);
+  return hipGetLastError();
 }
 
 hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {

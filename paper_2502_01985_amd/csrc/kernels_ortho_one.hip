@@ -16,7 +16,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kS = 64, kLdA = kS + 8, kMostLong = 448, kThreads = 1024;
+constexpr int kS = 64, kLdA = kS + 8, kMostLong = 448, kThreads = 1024, kSide = kThreads / 256;     // blocks of a row side by side
 
 struct OneArgs {
   OrthoArgs o;
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
   extern __shared__ __attribute__((aligned(16))) _Float16 lds[];
   __shared__ double wsum[kThreads / 64];
   const OrthoArgs& o = a.o;
-  const int ldx = a.lp + 8, t = threadIdx.x, lane = t % 64, wave = t / 64, r16 = lane & 15, g4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  const int ldx = a.lp + 8, t = threadIdx.x, lane = t % 64, wave = t / 64, g4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   _Float16 *xh = lds, *xl = xh + kS * ldx, *ah = xl + kS * ldx, *al = ah + kS * kLdA, *bh = al + kS * kLdA, *bl = bh + kS * kLdA;
   const T* G = (const T*)o.G + blockIdx.x * o.batch_g;
   const int rows = (int)o.rows, cols = (int)o.cols;
@@ -96,10 +96,15 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
       xl[at] = (_Float16)(v - (float)h);
     }
   __syncthreads();
-  const int bi = (wave % 4) * 16, bj = (wave / 4) * 16;       // this wavefront's block of A and B; its rows of X
-  const int blocks = a.lp / 16;                               // it forms blocks wave / 4, + 4, .. of X
+  const int bi = (wave % 4) * 16;                             // this wavefront's rows of A, B and X
+  const int blocks = a.lp / 16;                               // it forms blocks wave / 4, + kSide, .. of them
   for (int step = 0; step < o.steps; ++step) {
-    {
+    // (the places in LDS are worked out anew in every step: kept from one to the next they do not fit the registers)
+    int r16 = lane & 15;
+    asm volatile("" : "+v"(r16));
+#pragma unroll
+    for (int u = 0; u < 4 / kSide; ++u) {
+      const int bj = (wave / 4 + kSide * u) * 16;
       Three f;
       for (int k = 0; k < a.lp; k += 32)
         f.add(row_piece(xh + (bj + r16) * ldx + k + g8), row_piece(xl + (bj + r16) * ldx + k + g8), row_piece(xh + (bi + r16) * ldx + k + g8),
@@ -108,7 +113,9 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
       put_pair(ah + at, al + at, f.sum() * (1.0f / a.unit));
     }
     __syncthreads();
-    {
+#pragma unroll
+    for (int u = 0; u < 4 / kSide; ++u) {
+      const int bj = (wave / 4 + kSide * u) * 16;
       Three f;
 #pragma unroll
       for (int k = 0; k < kS; k += 32)
@@ -128,12 +135,12 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
       ph[k] = row_piece(bh + (bi + r16) * kLdA + 32 * k + g8);
       pl[k] = row_piece(bl + (bi + r16) * kLdA + 32 * k + g8);
     }
-    constexpr int kMost = kMostLong / 64;
+    constexpr int kMost = kMostLong / 16 / kSide;
     f32x4 next[kMost];
 #pragma unroll
     for (int u = 0; u < kMost; ++u) {
-      const int c = (wave / 4 + 4 * u) * 16;
-      if (wave / 4 + 4 * u >= blocks) continue;
+      const int c = (wave / 4 + kSide * u) * 16;
+      if (wave / 4 + kSide * u >= blocks) continue;
       Three f;
 #pragma unroll
       for (int k = 0; k < 2; ++k) f.add(column_piece(xh, ldx, 32 * k, c), column_piece(xl, ldx, 32 * k, c), ph[k], pl[k]);
@@ -147,27 +154,38 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
       __syncthreads();                                        // X is read: the next one takes its place
 #pragma unroll
       for (int u = 0; u < kMost; ++u) {
-        const int c = (wave / 4 + 4 * u) * 16;
-        if (wave / 4 + 4 * u >= blocks) continue;
+        const int c = (wave / 4 + kSide * u) * 16;
+        if (wave / 4 + kSide * u >= blocks) continue;
         const int at = (bi + r16) * ldx + c + g4;
         put_pair(xh + at, xl + at, next[u]);
       }
       __syncthreads();
       continue;
     }
-    const int S = flip ? cols : rows, L = flip ? rows : cols, i = bi + r16;
-    Epilogue e{};
-    e.mode = kEpiScale;
-    e.s0 = o.alpha / a.unit; e.s2 = o.beta; e.base = o.beta != 0.0f ? o.base : nullptr;
-    e.out = o.out; e.ld_out = o.ld_out; e.batch_out = o.batch_out; e.out_bf16 = o.out_bf16; e.flip = flip;
-    const float none[4] = {0.f, 0.f, 0.f, 0.f};
+    // the result, in float32 where X was, and from there along its rows
+    float* last = reinterpret_cast<float*>(lds);
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMost; ++u) {
-      const int j = (wave / 4 + 4 * u) * 16 + g4;
-      if (wave / 4 + 4 * u >= blocks || i >= S || j >= L) continue;
-      float v[4] = {next[u][0], next[u][1], next[u][2], next[u][3]};
-      epilogue4(e, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, v);
+      const int c = (wave / 4 + kSide * u) * 16;
+      if (wave / 4 + kSide * u >= blocks) continue;
+      *reinterpret_cast<f32x4*>(last + (bi + r16) * ldx + c + g4) = next[u];
     }
+  }
+  __syncthreads();
+  const float* last = reinterpret_cast<const float*>(lds);
+  const int S = flip ? cols : rows, L = flip ? rows : cols, quads = (L + 3) / 4;
+  Epilogue e{};
+  e.mode = kEpiScale;
+  e.s0 = o.alpha / a.unit; e.s2 = o.beta; e.base = o.beta != 0.0f ? o.base : nullptr;
+  e.out = o.out; e.ld_out = o.ld_out; e.batch_out = o.batch_out; e.out_bf16 = o.out_bf16; e.flip = flip;
+  const float none[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int q = t; q < kS * quads; q += kThreads) {
+    const int i = flip ? q % kS : q / quads, j = (flip ? q / kS : q % quads) * 4;
+    if (i >= S) continue;
+    const f32x4 w = *reinterpret_cast<const f32x4*>(last + i * ldx + j);
+    float v[4] = {w[0], w[1], w[2], w[3]};
+    epilogue4(e, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, v);
   }
 }
 

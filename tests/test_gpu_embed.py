@@ -173,6 +173,30 @@ def test_in_a_graph(il):
         assert torch.equal(out, want)
 
 
+def test_workspace_is_enough_and_no_more_is_touched(il):
+    gen = _gen(10)
+    for n, rows, cols in ((1, 1, 1), (700, 33, 20), (16384, 500, 24), (16385, 500, 24), (60_000, 70_000, 9), (200_000, 3, 40)):
+        ids, d = _ids(n, rows, "holes", gen), torch.randn(n, cols, generator=gen, device="cuda")
+        nbytes = il.ilargi_embed_grad_workspace_bytes(n, rows, cols)
+        store = torch.full((nbytes + 512,), 171, dtype=torch.uint8, device="cuda")
+        got = il.ilargi_embed_grad(d, ids, rows, workspace=store[256: 256 + nbytes])
+        assert torch.equal(got, il.ilargi_embed_grad(d, ids, rows))
+        assert bool((store[:256] == 171).all()) and bool((store[256 + nbytes:] == 171).all())
+
+
+# every range of the sorts and sums: one workgroup's sort and its border, one to four digits, a row that holds nearly all ids
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 1023, 1025, 4096, 16383, 16384, 16385, 40_961])
+@pytest.mark.parametrize("rows", [1, 2, 255, 256, 511, 512, 70_000, 300_001])
+def test_counts(il, n, rows):
+    """Sums of ones are counts: exact."""
+    gen = _gen(n + rows)
+    for kind in ("uniform", "skew", "one", "holes"):
+        ids = _ids(n, rows, kind, gen)
+        got = il.ilargi_embed_grad(torch.ones(n, 5, device="cuda"), ids, rows)
+        want = torch.bincount(ids[_live(ids, rows)].long(), minlength=rows).float()
+        assert torch.equal(got, want[:, None].expand(rows, 5))
+
+
 def test_refusals(il):
     t = torch.zeros(10, 8, device="cuda")
     ids = torch.zeros(4, dtype=torch.int32, device="cuda")

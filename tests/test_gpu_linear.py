@@ -130,6 +130,31 @@ def test_gradient(il, n, k, m, dtype, pad, shift):
     assert torch.equal(again[0], dX) and torch.equal(again[1], dW) and torch.equal(again[2], db)
 
 
+# products that are laid out first: odd rows, aligned rows in a wider matrix, one odd operand
+@pytest.mark.parametrize("n,k,m", [(1999, 701, 603), (2048, 704, 601), (1500, 1001, 512), (517, 1300, 1203), (16, 6999, 7001)])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 8), (3, 1), (8, 4)])
+def test_large_and_odd(il, n, k, m, pad, shift):
+    test_forward(il, n, k, m, BF16, pad, shift)
+    test_gradient(il, n, k, m, BF16, pad, shift)
+
+
+def test_workspace_is_enough_and_no_more_is_touched(il):
+    """Every path in a workspace of exactly the reported size, between guards."""
+    gen = _gen(21)
+    for dtype in (F32, BF16):
+        for n, k, m in ((1, 4099, 70), (2, 512, 512), (9, 40, 24), (300, 64, 72), (2001, 601, 701), (4000, 24, 16), (2048, 1024, 512)):
+            X, W, D, Z = _matrix(n, k, dtype, gen), _matrix(k, m, dtype, gen, scale=0.05), _matrix(n, m, dtype, gen), _matrix(n, m, dtype, gen)
+            for which, nbytes in enumerate(il.ilargi_linear_workspace_bytes(n, k, m, dtype)):
+                store = torch.full((nbytes + 512,), 171, dtype=torch.uint8, device="cuda")
+                ws = store[256: 256 + nbytes]
+                if which == 0:
+                    got, want = [il.ilargi_linear(X, W, act="gelu", workspace=ws)], [il.ilargi_linear(X, W, act="gelu")]
+                else:
+                    got, want = il.ilargi_linear_grad(D, X, W, pre=Z, act="silu", workspace=ws), il.ilargi_linear_grad(D, X, W, pre=Z, act="silu")
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
+                assert bool((store[:256] == 171).all()) and bool((store[256 + nbytes:] == 171).all())
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gradient_against_differences(il, act):
     """L = sum(Y o layer(X, W, b)): central differences of L in 64 bits along random directions against the kernels' gradients.

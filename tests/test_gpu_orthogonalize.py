@@ -149,6 +149,20 @@ def test_on_another_stream_and_in_a_graph(il):
             assert torch.equal(out, want)
 
 
+def test_workspace_is_enough_and_no_more_is_touched(il):
+    gen = _gen(9)
+    for shape in ((2, 40, 300), (3, 65, 65), (1, 500, 1100), (1, 1030, 520), (5, 130, 130)):
+        for dtype in (F32, BF16):
+            G = torch.randn(shape, generator=gen, device="cuda").to(dtype)
+            nbytes = il.ilargi_orthogonalize_workspace_bytes(*shape, dtype)
+            store = torch.full((nbytes + 512,), 171, dtype=torch.uint8, device="cuda")
+            for coef in (None, (2.0, -3.0, 9.0)):           # in pairs, and where the iteration leaves them
+                steps = 5 if coef is None else 2
+                got = il.ilargi_orthogonalize(G, steps=steps, coef=coef, workspace=store[256: 256 + nbytes])
+                assert _far(got, _exact(G, steps, coef or COEF)) <= 1e-2
+                assert bool((store[:256] == 171).all()) and bool((store[256 + nbytes:] == 171).all())
+
+
 def test_refusals(il):
     G = torch.zeros(8, 6, device="cuda")
     with pytest.raises(TypeError):
