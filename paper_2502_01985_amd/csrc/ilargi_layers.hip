@@ -240,7 +240,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     if (hipError_t e = lay_out(y, &x, ws + l.x, st); e != hipSuccess) return done("linear_grad", e);
     z.k_rows = 1;
     epi.out = d_W; epi.ld_out = ld_dw;
-    if (accumulate) { epi.base = d_W; epi.s2 = 1.0f; }
+    if (accumulate) { epi.src = d_W; epi.ld_src = ld_dw; epi.src_bf16 = h; epi.s1 = 1.0f; }
     if (hipError_t e = product(x, z, y.k, y.m, y.n, h, epi, shares, st); e != hipSuccess) return done("linear_grad", e);
   }
   return ILARGI_OK;

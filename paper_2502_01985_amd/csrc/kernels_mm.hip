@@ -92,21 +92,32 @@ __global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n, int
     const int64_t i = i0 + wi + 32 * x + r;
     if (i >= a.M) continue;
 #pragma unroll
-    for (int y = 0; y < F; ++y)
+    for (int y = 0; y < F; ++y) {
+      auto column = [&](int g) { return j0 + wj + 32 * y + 8 * g + 4 * h; };
+      auto sums = [&](int g) { return make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]); };
+      if (part != nullptr) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          if (column(g) < a.N) *reinterpret_cast<float4*>(part + i * ldp + column(g)) = sums(g);
+        continue;
+      }
+      SrcQuad raw[4];
+      float bias[4][4];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int64_t j = j0 + wj + 32 * y + 8 * g + 4 * h;
-        if (j >= a.N) continue;
-        float v[4] = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-        if (part != nullptr) {
-          *reinterpret_cast<float4*>(part + i * ldp + j) = make_float4(v[0], v[1], v[2], v[3]);
-          continue;
-        }
-        const int valid = (int)(a.N - j < 4 ? a.N - j : 4);
-        float bias[4];
-        epilogue_bias(a.epi, j, valid, bias);
-        epilogue4(a.epi, b, i, j, valid, bias, v);
+        const int valid = quad_valid(i, column(g), a.M, a.N);
+        raw[g] = epilogue_ask(a.epi, b, i, column(g), valid);
+        epilogue_bias(a.epi, column(g), valid, bias[g]);
       }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int valid = quad_valid(i, column(g), a.M, a.N);
+        if (valid == 0) continue;
+        const float4 t = sums(g);
+        float v[4] = {t.x, t.y, t.z, t.w};
+        epilogue4(a.epi, b, i, column(g), valid, bias[g], raw[g], v);
+      }
+    }
   }
 }
 

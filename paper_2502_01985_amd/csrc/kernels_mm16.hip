@@ -145,21 +145,6 @@ __device__ __forceinline__ void upper_block(int id, int tn, int* ti, int* tj) {
   *tj = r + id;
 }
 
-// What is done with four neighbouring sums of row i.
-template <int KIND>
-__device__ __forceinline__ void emit4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int64_t M, int64_t N, const float (&bias)[4], f32x4 t) {
-  if (i >= M || j >= N) return;
-  const int valid = (int)(N - j < 4 ? N - j : 4);
-  float v[4] = {t[0], t[1], t[2], t[3]};
-  if constexpr (KIND != kMm16Bf16) {
-    if (e.out_plane != 0) {
-      epilogue4_pairs(e, b, i, j, valid, v);
-      return;
-    }
-  }
-  epilogue4(e, b, i, j, valid, bias, v);
-}
-
 // The products of the second half of a step, between them the fetches of a later step into the buffer that has become free
 // and the reads of the next step's first half.
 template <class TileP, class TileQ, int KIND, int FM, int FN, class FragP, class FragQ>
@@ -214,27 +199,40 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
         if (ri + r < a.M && j0 + c < a.N) *reinterpret_cast<f32x4*>(part + (ri + r) * ldp + j0 + c) = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
       }
     } else {
+      auto row = [&](int r, int at) { return *reinterpret_cast<const float4*>(mine + r * kOutPad + at); };
       if (!a.epi.flip) {
         float bias[4];
         epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
+        if (a.epi.src == nullptr) {
 #pragma unroll 2
-        for (int q = 0; q < 16; ++q) {
-          const int r = 4 * q + (lane >> 4);
-          emit4<KIND>(a.epi, b, ri + r, j0 + c, a.M, a.N, bias, *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c));
+          for (int q = 0; q < 16; ++q) {
+            const int r = 4 * q + (lane >> 4), valid = quad_valid(ri + r, j0 + c, a.M, a.N);
+            if (valid == 0) continue;
+            const float4 t = row(r, c);
+            float v[4] = {t.x, t.y, t.z, t.w};
+            epilogue4<false>(a.epi, b, ri + r, j0 + c, valid, bias, SrcQuad{}, v);
+          }
+        } else {
+#pragma unroll 1
+          for (int q = 0; q < 16; q += 4)
+            epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
+                              [&](int u) { return row(4 * (q + u) + (lane >> 4), c); });
         }
-      }
-      if (a.epi.flip) {                                // written along j's rows, which run over i
-#pragma unroll 2
-        for (int q = 0; q < 16; ++q) emit4<KIND>(a.epi, b, ri + lane, j0 + 4 * q, a.M, a.N, none, *reinterpret_cast<const f32x4*>(mine + lane * kOutPad + 4 * q));
+      } else {                                         // written along j's rows, which run over i
+#pragma unroll 1
+        for (int q = 0; q < 16; q += 4)
+          epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + lane; *j = j0 + 4 * (q + u); },
+                            [&](int u) { return row(lane, 4 * (q + u)); });
       }
       if constexpr (KIND == kMm16Pairs) {
         if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
-#pragma unroll 2
-          for (int q = 0; q < 16; ++q) {
-            const int r = 4 * q + (lane >> 4);
-            const f32x4 v = {mine[c * kOutPad + r], mine[(c + 1) * kOutPad + r], mine[(c + 2) * kOutPad + r], mine[(c + 3) * kOutPad + r]};
-            emit4<KIND>(a.epi, b, j0 + r, ri + c, a.N, a.M, none, v);
-          }
+#pragma unroll 1
+          for (int q = 0; q < 16; q += 4)
+            epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + 4 * (q + u) + (lane >> 4); *j = ri + c; },
+                              [&](int u) {
+                                const float* m = mine + c * kOutPad + 4 * (q + u) + (lane >> 4);
+                                return make_float4(m[0], m[kOutPad], m[2 * kOutPad], m[3 * kOutPad]);
+                              });
         }
       }
     }
@@ -471,17 +469,17 @@ __global__ __launch_bounds__(256) void mm_join_rows_kernel(Join a, int splits, c
   const int64_t quads = (a.N + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x, i = at / quads, j = (at - i * quads) * 4, b = blockIdx.y;
   if (i >= a.M) return;
   const int64_t ldp = quads * 4;
-  const f32x4 s = add_shares(partial + (b * a.M + i) * ldp + j, a.batches * a.M * ldp, splits);
-  const int valid = (int)(a.N - j < 4 ? a.N - j : 4);
-  float bias[4], v[4] = {s[0], s[1], s[2], s[3]};
+  const int valid = quad_valid(i, j, a.M, a.N);
+  const SrcQuad raw = epilogue_ask(a.epi, b, i, j, valid);
+  float bias[4];
   epilogue_bias(a.epi, j, valid, bias);
-  if (a.epi.out_plane != 0) epilogue4_pairs(a.epi, b, i, j, valid, v);
-  else epilogue4(a.epi, b, i, j, valid, bias, v);
+  const f32x4 s = add_shares(partial + (b * a.M + i) * ldp + j, a.batches * a.M * ldp, splits);
+  float v[4] = {s[0], s[1], s[2], s[3]};
+  epilogue4(a.epi, b, i, j, valid, bias, raw, v);
 }
 
 // The same for results that are written along j too, 32 x 32 sums a workgroup: those on and above the diagonal of a symmetric
 // result, or all of a flipped one.
-template <int KIND>
 __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits, const float* __restrict__ partial) {
   __shared__ __attribute__((aligned(16))) float tile[32][36];
   int ti, tj;
@@ -491,18 +489,25 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits
   const int r = threadIdx.x / 8, c = (threadIdx.x % 8) * 4;
   const float none[4] = {0.f, 0.f, 0.f, 0.f};
   const bool turned = a.epi.flip || (a.symmetric && ti != tj);
+  // where this thread's quad goes, and where that of the turned tile does
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
+  const int64_t ti_row = a.epi.flip ? i0 + x : j0 + r, ti_col = a.epi.flip ? j0 + y : i0 + c;
+  const int valid = quad_valid(i0 + r, j0 + c, a.M, a.N), turned_valid = quad_valid(ti_row, ti_col, a.epi.flip ? a.M : a.N, a.epi.flip ? a.N : a.M);
+  const SrcQuad raw = epilogue_ask(a.epi, b, i0 + r, j0 + c, a.epi.flip ? 0 : valid), turned_raw = epilogue_ask(a.epi, b, ti_row, ti_col, turned ? turned_valid : 0);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  if (i0 + r < a.M && j0 + c < a.N) s = add_shares(partial + (b * a.M + i0 + r) * ldp + j0 + c, a.batches * a.M * ldp, splits);
-  if (!a.epi.flip) emit4<KIND>(a.epi, b, i0 + r, j0 + c, a.M, a.N, none, s);
+  if (valid > 0) s = add_shares(partial + (b * a.M + i0 + r) * ldp + j0 + c, a.batches * a.M * ldp, splits);
+  if (!a.epi.flip && valid > 0) {
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    epilogue4(a.epi, b, i0 + r, j0 + c, valid, none, raw, v);
+  }
   if (!turned) return;
   *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
   __syncthreads();
-  if (a.epi.flip) {
-    const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
-    emit4<KIND>(a.epi, b, i0 + x, j0 + y, a.M, a.N, none, *reinterpret_cast<const f32x4*>(&tile[x][y]));
-  } else {
-    emit4<KIND>(a.epi, b, j0 + r, i0 + c, a.N, a.M, none, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
-  }
+  if (turned_valid == 0) return;
+  float v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = a.epi.flip ? tile[x][y + q] : tile[c + q][r];
+  epilogue4(a.epi, b, ti_row, ti_col, turned_valid, none, turned_raw, v);
 }
 
 int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {
@@ -548,8 +553,7 @@ hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, 
     return hipGetLastError();
   }
   const dim3 grid((unsigned)blocks_of(M, N, 32, symmetric), (unsigned)batches);
-  if (epi.out_plane != 0) mm_join_kernel<kMm16Pairs><<<grid, 256, 0, st>>>(a, (int)((N + 31) / 32), splits, partial);
-  else mm_join_kernel<kMm16Bf16><<<grid, 256, 0, st>>>(a, (int)((N + 31) / 32), splits, partial);
+  mm_join_kernel<<<grid, 256, 0, st>>>(a, (int)((N + 31) / 32), splits, partial);
   return hipGetLastError();
 }
 

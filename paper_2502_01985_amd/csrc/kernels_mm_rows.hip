@@ -88,6 +88,8 @@ __global__ __launch_bounds__(kThreads) void mm_rows_kernel(Product a, int64_t sh
   const int r = threadIdx.x / (kCols / 4), c = threadIdx.x % (kCols / 4) * 4;
   const int64_t col = (int64_t)blockIdx.x * kCols + c;
   if (r >= n || col >= a.N) return;
+  const int left = (int)(a.N - col < 4 ? a.N - col : 4);
+  const SrcQuad raw = epilogue_ask(a.epi, 0, r, col, left);
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int w2 = 0; w2 < kWaves; ++w2)
@@ -97,10 +99,9 @@ __global__ __launch_bounds__(kThreads) void mm_rows_kernel(Product a, int64_t sh
     *reinterpret_cast<float4*>(partial + (blockIdx.y * a.M + r) * ldp + col) = make_float4(v[0], v[1], v[2], v[3]);
     return;
   }
-  const int left = (int)(a.N - col < 4 ? a.N - col : 4);
   float bias[4];
   epilogue_bias(a.epi, col, left, bias);
-  epilogue4(a.epi, 0, r, col, left, bias, v);
+  epilogue4(a.epi, 0, r, col, left, bias, raw, v);
 }
 
 template <class T>

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
     if (i >= S) continue;
     const f32x4 w = *reinterpret_cast<const f32x4*>(last + i * ldx + j);
     float v[4] = {w[0], w[1], w[2], w[3]};
-    epilogue4(e, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, v);
+    epilogue4(e, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, SrcQuad{}, v);
   }
 }
 

@@ -23,26 +23,6 @@ __device__ __forceinline__ void pair_store(_Float16* p, int64_t at, int64_t plan
   p[at + plane] = (_Float16)(x - (float)hi);
 }
 
-// out(i, j) = s0 v + s1 src(i, j) in pairs, columns j .. j + valid.
-__device__ __forceinline__ void epilogue4_pairs(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, float (&v)[4]) {
-  const _Float16* src = (const _Float16*)e.src + b * e.batch_src + i * e.ld_src + j;
-  _Float16* out = (_Float16*)e.out + b * e.batch_out + i * e.ld_out + j;
-  float t[4] = {0.f, 0.f, 0.f, 0.f}, hi[4], lo[4];
-  if (e.src != nullptr) {
-    load_piece<_Float16, 4>(src, valid, hi);
-    load_piece<_Float16, 4>(src + e.src_plane, valid, lo);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) t[q] = hi[q] + lo[q];
-  }
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const float x = fmaf(e.s0, v[q], e.s1 * t[q]);
-    hi[q] = (float)(_Float16)x;
-    lo[q] = x - hi[q];
-  }
-  store_piece<_Float16, 4>(out, valid, hi);
-  store_piece<_Float16, 4>(out + e.out_plane, valid, lo);
-}
 // The bias of columns j .. j + valid, zeros where there is none.
 __device__ __forceinline__ void epilogue_bias(const Epilogue& e, int64_t j, int valid, float (&bias)[4]) {
 #pragma unroll
@@ -50,8 +30,59 @@ __device__ __forceinline__ void epilogue_bias(const Epilogue& e, int64_t j, int 
   if (e.mode == kEpiLinear && e.bias != nullptr && valid > 0) load4_any(e.bias, j, e.out_bf16, valid, bias);
 }
 
-// Columns j .. j + valid of row i of matrix b of the batch.
-__device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&bias)[4], float (&v)[4]) {
+// Four columns of `src` as they lie: asked for early, turned into numbers when the sums are finished, so that the loads of many rows
+// are on their way together.  (A row at a time, every one waits for its own: 1 us each where another compute unit wrote it.)
+struct SrcQuad {
+  uint2 a, b;
+};
+__device__ __forceinline__ SrcQuad epilogue_ask(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid) {
+  SrcQuad r = {make_uint2(0, 0), make_uint2(0, 0)};
+  if (e.src == nullptr || valid <= 0) return r;
+  const int64_t at = b * e.batch_src + i * e.ld_src + j;
+  if (e.src_plane == 0 && !e.src_bf16) {
+    const uint32_t* p = (const uint32_t*)e.src + at;
+    if (valid >= 4) {
+      const Piece<uint32_t, 4> t = *reinterpret_cast<const Piece<uint32_t, 4>*>(p);
+      return {make_uint2(t.v[0], t.v[1]), make_uint2(t.v[2], t.v[3])};
+    }
+    r.a.x = p[0];
+    if (valid > 1) r.a.y = p[1];
+    if (valid > 2) r.b.x = p[2];
+    return r;
+  }
+  const uint16_t* p = (const uint16_t*)e.src + at;
+  auto four = [valid](const uint16_t* q) {
+    if (valid >= 4) return __builtin_bit_cast(uint2, *reinterpret_cast<const Piece<uint16_t, 4>*>(q));
+    uint2 t = make_uint2(q[0], 0);
+    if (valid > 1) t.x |= (uint32_t)q[1] << 16;
+    if (valid > 2) t.y = q[2];
+    return t;
+  };
+  r.a = four(p);
+  if (e.src_plane != 0) r.b = four(p + e.src_plane);
+  return r;
+}
+__device__ __forceinline__ void epilogue_src(const Epilogue& e, const SrcQuad& r, float (&t)[4]) {
+  if (e.src_plane != 0) {
+    const Piece<_Float16, 4> hi = __builtin_bit_cast(Piece<_Float16, 4>, r.a), lo = __builtin_bit_cast(Piece<_Float16, 4>, r.b);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = (float)hi.v[q] + (float)lo.v[q];
+  } else if (e.src_bf16) {
+    t[0] = __uint_as_float(r.a.x << 16); t[1] = __uint_as_float(r.a.x & 0xffff0000u);
+    t[2] = __uint_as_float(r.a.y << 16); t[3] = __uint_as_float(r.a.y & 0xffff0000u);
+  } else {
+    t[0] = __uint_as_float(r.a.x); t[1] = __uint_as_float(r.a.y);
+    t[2] = __uint_as_float(r.b.x); t[3] = __uint_as_float(r.b.y);
+  }
+}
+
+// Columns j .. j + valid of row i of matrix b of the batch: `v` are the sums, `raw` what epilogue_ask gave.
+// (SRC false: the caller knows that there is no src.)
+template <bool SRC = true>
+__device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&bias)[4], const SrcQuad& raw,
+                                          float (&v)[4]) {
+  float t[4] = {0.f, 0.f, 0.f, 0.f};
+  if (SRC && e.src != nullptr) epilogue_src(e, raw, t);
   if (e.mode == kEpiLinear) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += bias[q];
@@ -60,9 +91,7 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = act_value(v[q], e.act);
     }
-    if (e.src != nullptr) {
-      float t[4];
-      load4_any(e.src, i * e.ld_src + j, e.src_bf16, valid, t);
+    if constexpr (SRC) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] += t[q];
     }
@@ -70,19 +99,7 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
     return;
   }
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] *= e.s0;
-  if (e.src != nullptr) {
-    float t[4];
-    const int64_t from = b * e.batch_src + i * e.ld_src + j;
-    if (e.src_plane != 0) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) t[q] = q < valid ? pair_value((const _Float16*)e.src, from + q, e.src_plane) : 0.0f;
-    } else {
-      load4_any(e.src, from, e.src_bf16, valid, t);
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = fmaf(e.s1, t[q], v[q]);
-  }
+  for (int q = 0; q < 4; ++q) v[q] = SRC && e.src != nullptr ? fmaf(e.s1, t[q], e.s0 * v[q]) : e.s0 * v[q];
   if (e.flip) {
     for (int q = 0; q < valid && q < 4; ++q) {
       const int64_t at = b * e.batch_out + (j + q) * e.ld_out + i;
@@ -94,13 +111,47 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
     return;
   }
   const int64_t at = b * e.batch_out + i * e.ld_out + j;
-  if (e.base != nullptr) {
-    float t[4];
-    load4_any(e.base, at, e.out_bf16, valid, t);
+  if (e.out_plane != 0) {
+    float hi[4], lo[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = fmaf(e.s2, t[q], v[q]);
+    for (int q = 0; q < 4; ++q) {
+      hi[q] = (float)(_Float16)v[q];
+      lo[q] = v[q] - hi[q];
+    }
+    store_piece<_Float16, 4>((_Float16*)e.out + at, valid, hi);
+    store_piece<_Float16, 4>((_Float16*)e.out + at + e.out_plane, valid, lo);
+    return;
+  }
+  if (e.base != nullptr) {
+    float o[4];
+    load4_any(e.base, at, e.out_bf16, valid, o);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = fmaf(e.s2, o[q], v[q]);
   }
   store4_any(e.out, at, e.out_bf16, valid, v);
+}
+
+__device__ __forceinline__ int quad_valid(int64_t i, int64_t j, int64_t M, int64_t N) { return i >= M || j >= N ? 0 : N - j < 4 ? (int)(N - j) : 4; }
+
+// U quads of one column block: place(q, &i, &j) says where the q-th lies, sum(q) gives its four sums.
+template <int U, class Place, class Sum>
+__device__ __forceinline__ void epilogue_quads(const Epilogue& e, int64_t b, int64_t M, int64_t N, const float (&bias)[4], Place place, Sum sum) {
+  SrcQuad raw[U];
+  int64_t i, j;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    place(u, &i, &j);
+    raw[u] = epilogue_ask(e, b, i, j, quad_valid(i, j, M, N));
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    place(u, &i, &j);
+    const int valid = quad_valid(i, j, M, N);
+    if (valid == 0) continue;
+    const float4 t = sum(u);
+    float v[4] = {t.x, t.y, t.z, t.w};
+    epilogue4(e, b, i, j, valid, bias, raw[u], v);
+  }
 }
 
 }  // namespace ilargi
