@@ -171,30 +171,31 @@ __device__ __forceinline__ void second_half(bool fetching, const TileP& tp, cons
   }(std::make_integer_sequence<int, FM>());
 }
 
-// The sums of a wavefront go through LDS, 64 rows of 64 columns at a time, so that stores run along the result's rows.
+// The sums of a wavefront (TM x 64) go through LDS, up to 64 rows at a time, so that stores run along the result's rows.
 template <int KIND, int TM, int FN>
 __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t b, int64_t i0,
                                            int64_t j0, bool mirrored) {
+  constexpr int kRows = TM < 64 ? TM : 64, kQ = kRows / 4;      // rows of a pass, and its turns of 64 quads
   const int lane = threadIdx.x % 64;
-  float* mine = (float*)lds + threadIdx.x / 64 * 64 * kOutPad;
+  float* mine = (float*)lds + threadIdx.x / 64 * kRows * kOutPad;
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < TM / 64; ++h) {
+  for (int h = 0; h < TM / kRows; ++h) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < kRows / 16; ++x)
 #pragma unroll
       for (int y = 0; y < FN; ++y)
-        *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[4 * h + x][y];
+        *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[kRows / 16 * h + x][y];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int64_t ri = i0 + 64 * h;
+    const int64_t ri = i0 + kRows * h;
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
     const int c = (lane & 15) * 4;                     // a row of 64 columns takes 16 lanes
     if (partial != nullptr) {
       const int64_t ldp = (a.N + 3) / 4 * 4;
       float* part = partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp;
 #pragma unroll 4
-      for (int q = 0; q < 16; ++q) {
+      for (int q = 0; q < kQ; ++q) {
         const int r = 4 * q + (lane >> 4);
         if (ri + r < a.M && j0 + c < a.N) *reinterpret_cast<f32x4*>(part + (ri + r) * ldp + j0 + c) = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c);
       }
@@ -205,7 +206,7 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
         epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
         if (a.epi.src == nullptr) {
 #pragma unroll 2
-          for (int q = 0; q < 16; ++q) {
+          for (int q = 0; q < kQ; ++q) {
             const int r = 4 * q + (lane >> 4), valid = quad_valid(ri + r, j0 + c, a.M, a.N);
             if (valid == 0) continue;
             const float4 t = row(r, c);
@@ -214,23 +215,27 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
           }
         } else {
 #pragma unroll 1
-          for (int q = 0; q < 16; q += 4)
+          for (int q = 0; q < kQ; q += 4)
             epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
                               [&](int u) { return row(4 * (q + u) + (lane >> 4), c); });
         }
       } else {                                         // written along j's rows, which run over i
+        constexpr int kSide = 64 / kRows;              // quads side by side
+        const int r = lane % kRows, s = lane / kRows;
 #pragma unroll 1
-        for (int q = 0; q < 16; q += 4)
-          epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + lane; *j = j0 + 4 * (q + u); },
-                            [&](int u) { return row(lane, 4 * (q + u)); });
+        for (int q = 0; q < kQ; q += 4)
+          epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + r; *j = j0 + 4 * ((q + u) * kSide + s); },
+                            [&](int u) { return row(r, 4 * ((q + u) * kSide + s)); });
       }
       if constexpr (KIND == kMm16Pairs) {
         if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
+          constexpr int kAcross = kRows / 4, kDown = 64 / kAcross;
+          const int ci = lane % kAcross * 4, rj = lane / kAcross;
 #pragma unroll 1
-          for (int q = 0; q < 16; q += 4)
-            epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + 4 * (q + u) + (lane >> 4); *j = ri + c; },
+          for (int q = 0; q < kQ; q += 4)
+            epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + kDown * (q + u) + rj; *j = ri + ci; },
                               [&](int u) {
-                                const float* m = mine + c * kOutPad + 4 * (q + u) + (lane >> 4);
+                                const float* m = mine + ci * kOutPad + kDown * (q + u) + rj;
                                 return make_float4(m[0], m[kOutPad], m[2 * kOutPad], m[3 * kOutPad]);
                               });
         }
@@ -329,25 +334,28 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel
 }
 
 // Pairs: a step's four tiles (both planes of both operands) lie in LDS together, and three products are formed from the fragments
-// read once: 64 KB fetched for 96 matrix instructions a wavefront, where the planes one after the other would take 96 KB.  Blocks of
-// 128, a wavefront to a SIMD; as above, reads and fetches stand between the products.  Q's rows run over k (QK) or its columns do.
-// (LDS is asked for at the launch: told of it, the compiler would take the accumulators to the other half of a lone wavefront's
+// read once: 64 KB fetched for 96 matrix instructions where the planes one after the other would take 96 KB.  Blocks of 128 in
+// eight wavefronts: four have 64 x 64 sums of the first half of every step, four the same sums of the second half, and they exchange
+// halves of their sums at the end.  So two wavefronts share a SIMD, and one's products run while the other's reads and fetches are
+// issued (four wavefronts with both halves: 2048 x 2048 x 2048 takes 55 us, of which the products alone 33).  Q's rows run over k
+// (QK) or its columns do.
+// (LDS is asked for at the launch: told of it, the compiler would take the accumulators to the other half of a wavefront's
 // registers, and move them to and fro.)
 constexpr int kPairsLds = 2 * 4 * 128 * kBK * 2;
 template <bool QK>
-__global__ __launch_bounds__(256, 2) void mm16_pairs_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
-  constexpr int NT = 256, FM = 4, FN = 4, kB = 128;
+__global__ __launch_bounds__(512, 1) void mm16_pairs_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
+  constexpr int NT = 512, FM = 4, FN = 4, kB = 128;
   using TileP = Tile<false, kB, NT>;
   using TileQ = Tile<QK, kB, NT>;
   constexpr int kP = TileP::kBytes, kQ = TileQ::kBytes, kStage = 2 * (kP + kQ), kEach = TileP::kLoads;
-  static_assert(TileP::kLoads == FM && TileQ::kLoads == FM, "a piece of each tile between the products of a row of blocks");
-  static_assert(2 * kStage == kPairsLds && NT * kOutPad * 4 <= kPairsLds, "the sums fit too");
+  static_assert(kEach == 2 && TileQ::kLoads == 2, "a piece of two tiles between the products of a row of blocks");
+  static_assert(2 * kStage == kPairsLds && 8 * 32 * kOutPad * 4 <= kPairsLds, "the sums fit too");
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   int ti, tj;
   if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
   else block_of(blockIdx.x, tm, tn, &ti, &tj);
   const int64_t i0 = (int64_t)ti * kB, j0 = (int64_t)tj * kB, b = blockIdx.y;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wi = (wave / 2) * 64, wj = (wave % 2) * 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4, wi = (wave % 4 / 2) * 64, wj = (wave % 2) * 64;
   const int64_t step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
   const int first = (int)blockIdx.z * share, ks_all = (int)((a.K + kBK - 1) / kBK), steps = ks_all - first < share ? ks_all - first : share;
   const char* P = (const char*)a.P.p + 2 * (b * a.P.batch + i0 * a.P.ld) + (int64_t)first * kBK * 2;
@@ -383,14 +391,13 @@ __global__ __launch_bounds__(256, 2) void mm16_pairs_kernel(Product16 a, int tm,
   for (int x = 0; x < FM; ++x)
 #pragma unroll
     for (int y = 0; y < FN; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  s16x8 ph[2][FM], pl[2][FM], qh[2][FN], ql[2][FN];
-  // the x-th fragments of both planes and operands for a half step
+  s16x8 ph[2][FM], pl[2][FM], qh[2][FN], ql[2][FN];      // of this step and the next
   auto read = [&](auto set, uint32_t at, auto xs) {
     constexpr int S = decltype(set)::value, X = decltype(xs)::value;
-    ph[S][X] = fp.read(at, S, X);
-    pl[S][X] = fp.read(at + kP, S, X);
-    qh[S][X] = fq.read(at + 2 * kP, S, X);
-    ql[S][X] = fq.read(at + 2 * kP + kQ, S, X);
+    ph[S][X] = fp.read(at, half, X);
+    pl[S][X] = fp.read(at + kP, half, X);
+    qh[S][X] = fq.read(at + 2 * kP, half, X);
+    ql[S][X] = fq.read(at + 2 * kP + kQ, half, X);
   };
   auto products = [&](auto set, auto xs) {
     constexpr int S = decltype(set)::value, X = decltype(xs)::value;
@@ -401,40 +408,59 @@ __global__ __launch_bounds__(256, 2) void mm16_pairs_kernel(Product16 a, int tm,
 #pragma unroll
     for (int y = 0; y < FN; ++y) acc[X][y] = mfma16<kMm16Pairs>(qh[S][y], ph[S][X], acc[X][y]);
   };
-  using H0 = std::integral_constant<int, 0>;
-  using H1 = std::integral_constant<int, 1>;
   auto each = [](auto f) { [&]<int... X>(std::integer_sequence<int, X...>) { (f(std::integral_constant<int, X>()), ...); }(std::make_integer_sequence<int, FM>()); };
   for (int t = 0; t < 2 && t < steps; ++t) fetch(t);
   if (steps >= 2) arrived_and_together<4 * kEach>();
   else arrived_and_together<0>();
-  each([&](auto x) { read(H0(), base, x); });
-  for (int t = 0; t < steps; ++t) {
-    const uint32_t here = base + (t & 1) * kStage, next = base + ((t + 1) & 1) * kStage;
-    each([&](auto x) {
-      read(H1(), here, x);
-      __builtin_amdgcn_sched_barrier(0);
-      products(H0(), x);
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    arrived_and_together<0>();                         // step t is in registers, step t + 1 in LDS
+  each([&](auto x) { read(std::integral_constant<int, 0>(), base, x); });
+  // a step: its fragments are in registers, and so its half of LDS is free for the step after the next
+  auto step = [&](int t, auto set) {
+    constexpr int S = decltype(set)::value;
+    const uint32_t here = base + S * kStage, next = base + (1 - S) * kStage;
+    arrived_and_together<0>();                           // step t + 1 is in LDS
     const bool more = t + 2 < steps, whole = more && left_of(t + 2) == kBK;
     const char *p = P + (int64_t)(t + 2) * kBK * 2, *q = Q + (t + 2) * step_q;
     if (more && !whole) fetch(t + 2);
     each([&](auto x) {
       constexpr int X = decltype(x)::value;
-      read(H0(), next, x);                             // (behind the last step: of an old one, for nothing)
+      read(std::integral_constant<int, 1 - S>(), next, x);      // (behind the last step: of an old one, for nothing)
       if (whole) {
-        tp.template fetch_some<X, 1>(p, here);
-        tp.template fetch_some<X, 1>(p + lo_p, here + kP);
-        tq.template fetch_some<X, 1>(q, here + 2 * kP);
-        tq.template fetch_some<X, 1>(q + lo_q, here + 2 * kP + kQ);
+        if constexpr (X == 0) tp.template fetch_some<0, kEach>(p, here);
+        if constexpr (X == 1) tp.template fetch_some<0, kEach>(p + lo_p, here + kP);
+        if constexpr (X == 2) tq.template fetch_some<0, kEach>(q, here + 2 * kP);
+        if constexpr (X == 3) tq.template fetch_some<0, kEach>(q + lo_q, here + 2 * kP + kQ);
       }
       __builtin_amdgcn_sched_barrier(0);
-      products(H1(), x);
+      products(set, x);
       __builtin_amdgcn_sched_barrier(0);
     });
+  };
+  int t = 0;
+  for (; t + 2 <= steps; t += 2) {
+    step(t, std::integral_constant<int, 0>());
+    step(t + 1, std::integral_constant<int, 1>());
   }
-  store_sums<kMm16Pairs, 64, FN>(a, partial, lds_all, acc, b, i0 + wi, j0 + wj, a.symmetric && ti != tj);
+  if (t < steps) step(t, std::integral_constant<int, 0>());
+  // Both halves' sums: this wavefront keeps rows 32 half .. of its 64 x 64 and hands the others over.
+  __syncthreads();
+  float* given = (float*)lds_all + (wave ^ 4) * 32 * kOutPad;
+  const int lane = threadIdx.x % 64;
+  const auto at = [&](int x, int y) { return (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4; };
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int y = 0; y < FN; ++y) *reinterpret_cast<f32x4*>(given + at(x, y)) = half ? acc[x][y] : acc[2 + x][y];
+  __syncthreads();
+  const float* taken = (const float*)lds_all + wave * 32 * kOutPad;
+  f32x4 sum[2][FN];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int y = 0; y < FN; ++y) {
+      const f32x4 other = *reinterpret_cast<const f32x4*>(taken + at(x, y));
+      sum[x][y] = half ? acc[2 + x][y] + other : acc[x][y] + other;
+    }
+  store_sums<kMm16Pairs, 32, FN>(a, partial, lds_all, sum, b, i0 + wi + 32 * half, j0 + wj, a.symmetric && ti != tj);
 }
 
 struct Join {
@@ -538,8 +564,8 @@ hipError_t mm16_pairs(const Product16& a, const MmPlan& plan, float* partial, hi
   float* part = plan.splits > 1 ? partial : nullptr;
   const void* kernel = a.Q.k_rows ? (const void*)mm16_pairs_kernel<true> : (const void*)mm16_pairs_kernel<false>;
   if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kPairsLds); e != hipSuccess) return e;
-  if (a.Q.k_rows) mm16_pairs_kernel<true><<<grid, 256, kPairsLds, st>>>(a, tm, tn, share, part);
-  else mm16_pairs_kernel<false><<<grid, 256, kPairsLds, st>>>(a, tm, tn, share, part);
+  if (a.Q.k_rows) mm16_pairs_kernel<true><<<grid, 512, kPairsLds, st>>>(a, tm, tn, share, part);
+  else mm16_pairs_kernel<false><<<grid, 512, kPairsLds, st>>>(a, tm, tn, share, part);
   return finish_shares(a, plan, part, st);
 }
 
