@@ -16,7 +16,19 @@ __device__ __forceinline__ void fetch(const T* __restrict__ p, int64_t ld, int64
   const int64_t outer = KROWS ? k0 + t / (TILE / 8) : r0 + t / (STEP / 8), inner = KROWS ? r0 + t % (TILE / 8) * 8 : k0 + t % (STEP / 8) * 8;
   const int64_t n_outer = KROWS ? K : R, n_inner = KROWS ? R : K;
   const int64_t left = outer < n_outer ? n_inner - inner : 0;
-  load_piece<T, 8>(p + (left > 0 ? outer * ld + inner : 0), (int)(left < 0 ? 0 : left > 8 ? 8 : left), f);
+  const T* at = p + (left > 0 ? outer * ld + inner : 0);
+  if (left >= 8) {
+    const Piece<T, 8> t = *reinterpret_cast<const Piece<T, 8>*>(at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (float)t.v[j];
+  } else {
+    // (places before the end alone are read: the last of them in place of those behind it)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = left > 0 ? (float)at[j < left ? j : 0] : 0.0f;
+      f[j] = j < left ? v : 0.0f;
+    }
+  }
 }
 
 template <bool KROWS, int TILE, int STEP>
@@ -36,11 +48,17 @@ __device__ __forceinline__ void put(float (*lds)[TILE + 4], const float (&f)[8])
 // fetched.  The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
 // blockIdx: block, matrix of the batch, share.  With several shares the sums go to `partial`, as in kernels_mm16.hip.
 template <class TP, class TQ, bool PK, bool QK, int TILE, int STEP>
-__global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n, int64_t share, float* __restrict__ partial) {
+__global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tm, int tn, int64_t share, float* __restrict__ partial) {
   constexpr int F = TILE / 64;        // 32 x 32 pieces of a wavefront, each way
-  __shared__ __attribute__((aligned(16))) float lp[2][STEP][TILE + 4], lq[2][STEP][TILE + 4];
+  __shared__ __attribute__((aligned(16))) struct {
+    float p[3][STEP][TILE + 4], q[3][STEP][TILE + 4];
+  } lds;
+  auto& lp = lds.p;
+  auto& lq = lds.q;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t i0 = (int64_t)(blockIdx.x / tiles_n) * TILE, j0 = (int64_t)(blockIdx.x % tiles_n) * TILE, b = blockIdx.y;
+  int ti, tj;
+  block_of(blockIdx.x, tm, tn, &ti, &tj);
+  const int64_t i0 = (int64_t)ti * TILE, j0 = (int64_t)tj * TILE, b = blockIdx.y;
   const int64_t first = blockIdx.z * share, K = a.K < first + share ? a.K : first + share;
   const TP* P = (const TP*)a.P.p + b * a.P.batch;
   const TQ* Q = (const TQ*)a.Q.p + b * a.Q.batch;
@@ -52,72 +70,94 @@ __global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tiles_n, int
     for (int y = 0; y < F; ++y)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.0f;
+  // Three tiles of each operand: at the start of a step its own and the next lie in LDS, and the one behind is fetched, to be put
+  // where the last step's was.  So the first fragments of the next step are read before the barrier, and the products go on behind it.
   float fp[8], fq[8];
+  auto bring = [&](int64_t k) {
+    fetch<TP, PK, TILE, STEP>(P, a.P.ld, i0, a.M, k, K, fp);
+    fetch<TQ, QK, TILE, STEP>(Q, a.Q.ld, j0, a.N, k, K, fq);
+  };
+  auto lay = [&](int to) {
+    put<PK, TILE, STEP>(lp[to], fp);
+    put<QK, TILE, STEP>(lq[to], fq);
+  };
+  float p[2][F], q[2][F];
+  auto read = [&](int of, int k, int set) {
+#pragma unroll
+    for (int x = 0; x < F; ++x) p[set][x] = lp[of][k + h][wi + 32 * x + r];
+#pragma unroll
+    for (int y = 0; y < F; ++y) q[set][y] = lq[of][k + h][wj + 32 * y + r];
+  };
   if (first < K) {
-    fetch<TP, PK, TILE, STEP>(P, a.P.ld, i0, a.M, first, K, fp);
-    fetch<TQ, QK, TILE, STEP>(Q, a.Q.ld, j0, a.N, first, K, fq);
-    put<PK, TILE, STEP>(lp[0], fp);
-    put<QK, TILE, STEP>(lq[0], fq);
+    bring(first);
+    lay(0);
+    if (first + STEP < K) {
+      bring(first + STEP);
+      lay(1);
+    }
   }
   __syncthreads();
   int cur = 0;
-  for (int64_t k0 = first; k0 < K; k0 += STEP, cur ^= 1) {
-    const bool more = k0 + STEP < K;
-    if (more) {
-      fetch<TP, PK, TILE, STEP>(P, a.P.ld, i0, a.M, k0 + STEP, K, fp);
-      fetch<TQ, QK, TILE, STEP>(Q, a.Q.ld, j0, a.N, k0 + STEP, K, fq);
-    }
+  if (first < K) read(0, 0, 0);
+  for (int64_t k0 = first; k0 < K; k0 += STEP) {
+    const int next = cur == 2 ? 0 : cur + 1, last = cur == 0 ? 2 : cur - 1;
+    const bool more = k0 + 2 * STEP < K;
+    if (more) bring(k0 + 2 * STEP);
 #pragma unroll
     for (int k = 0; k < STEP; k += 2) {
-      float p[F], q[F];
-#pragma unroll
-      for (int x = 0; x < F; ++x) p[x] = lp[cur][k + h][wi + 32 * x + r];
-#pragma unroll
-      for (int y = 0; y < F; ++y) q[y] = lq[cur][k + h][wj + 32 * y + r];
+      const int set = k / 2 % 2;
+      if (k + 2 < STEP) read(cur, k + 2, set ^ 1);
+      else read(next, 0, set ^ 1);                     // (behind the last step: of an old one, for nothing)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < F; ++x)
 #pragma unroll
-        for (int y = 0; y < F; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[y], p[x], acc[x][y], 0, 0, 0);
+        for (int y = 0; y < F; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[set][y], p[set][x], acc[x][y], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (more) {
-      put<PK, TILE, STEP>(lp[cur ^ 1], fp);
-      put<QK, TILE, STEP>(lq[cur ^ 1], fq);
-    }
+    static_assert(STEP / 2 % 2 == 0, "the next step begins with the first set");
+    if (more) lay(last);
+    cur = next;
     __syncthreads();
   }
+  // The sums go through LDS, 32 rows of a wavefront at a time, so that stores run along the result's rows.
+  constexpr int kPad = 32 * F + 4, kLanes = 8 * F, kRows = 64 / kLanes;      // quads of a row, rows of a turn
+  static_assert(4 * 32 * kPad * 4 <= sizeof(lds), "the sums fit where the tiles were");
+  float* mine = reinterpret_cast<float*>(&lds) + wave * 32 * kPad;
   const int64_t ldp = (a.N + 3) / 4 * 4;
   float* part = partial != nullptr ? partial + ((int64_t)blockIdx.z * a.batches + b) * a.M * ldp : nullptr;
+  const int rr = lane / kLanes, cc = lane % kLanes * 4;
+  const int64_t j = j0 + wj + cc;
+  float bias[4];
+  epilogue_bias(a.epi, j, (int)(a.N - j < 4 ? a.N - j : 4), bias);
 #pragma unroll
   for (int x = 0; x < F; ++x) {
-    const int64_t i = i0 + wi + 32 * x + r;
-    if (i >= a.M) continue;
 #pragma unroll
-    for (int y = 0; y < F; ++y) {
-      auto column = [&](int g) { return j0 + wj + 32 * y + 8 * g + 4 * h; };
-      auto sums = [&](int g) { return make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]); };
-      if (part != nullptr) {
+    for (int y = 0; y < F; ++y)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          if (column(g) < a.N) *reinterpret_cast<float4*>(part + i * ldp + column(g)) = sums(g);
-        continue;
-      }
-      SrcQuad raw[4];
-      float bias[4][4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int valid = quad_valid(i, column(g), a.M, a.N);
-        raw[g] = epilogue_ask(a.epi, b, i, column(g), valid);
-        epilogue_bias(a.epi, column(g), valid, bias[g]);
-      }
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int valid = quad_valid(i, column(g), a.M, a.N);
-        if (valid == 0) continue;
-        const float4 t = sums(g);
-        float v[4] = {t.x, t.y, t.z, t.w};
-        epilogue4(a.epi, b, i, column(g), valid, bias[g], raw[g], v);
-      }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(mine + r * kPad + 32 * y + 8 * g + 4 * h) =
+            make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int64_t ri = i0 + wi + 32 * x;
+    auto sums = [&](int q) { return *reinterpret_cast<const float4*>(mine + (q * kRows + rr) * kPad + cc); };
+    if (part != nullptr) {
+#pragma unroll 4
+      for (int q = 0; q < 32 / kRows; ++q)
+        if (ri + q * kRows + rr < a.M && j < a.N) *reinterpret_cast<float4*>(part + (ri + q * kRows + rr) * ldp + j) = sums(q);
+    } else if (!a.epi.flip) {
+#pragma unroll 1
+      for (int q = 0; q < 32 / kRows; q += 4)
+        epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + (q + u) * kRows + rr; *jj = j; }, [&](int u) { return sums(q + u); });
+    } else {                                           // written along j's rows, which run over i
+#pragma unroll 1
+      for (int q = 0; q < 4 * F; q += 4)
+        epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + r; *jj = j0 + wj + 8 * (q + u) + 4 * h; },
+                          [&](int u) { return *reinterpret_cast<const float4*>(mine + r * kPad + 8 * (q + u) + 4 * h); });
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -127,8 +167,8 @@ hipError_t mm_f32_order(const Product& a, const MmPlan& plan, float* partial, hi
   const dim3 grid((unsigned)(tm * tn), (unsigned)a.batches, (unsigned)plan.splits);
   const int64_t step = plan.tile == 64 ? 32 : 16, steps = (a.K + step - 1) / step, share = (steps + plan.splits - 1) / plan.splits * step;
   float* part = plan.splits > 1 ? partial : nullptr;
-  if (plan.tile == 64) mm_f32_kernel<TP, TQ, PK, QK, 64, 32><<<grid, 256, 0, st>>>(a, (int)tn, share, part);
-  else mm_f32_kernel<TP, TQ, PK, QK, 128, 16><<<grid, 256, 0, st>>>(a, (int)tn, share, part);
+  if (plan.tile == 64) mm_f32_kernel<TP, TQ, PK, QK, 64, 32><<<grid, 256, 0, st>>>(a, (int)tm, (int)tn, share, part);
+  else mm_f32_kernel<TP, TQ, PK, QK, 128, 16><<<grid, 256, 0, st>>>(a, (int)tm, (int)tn, share, part);
   if (part != nullptr) return launch_mm_join(a.M, a.N, a.batches, 0, a.epi, plan.splits, part, st);
   return hipGetLastError();
 }
@@ -141,6 +181,10 @@ hipError_t mm_f32_typed(const Product& a, const MmPlan& plan, float* partial, hi
 
 }  // namespace
 
+// Blocks of 128 or 64 and the shares of k, by what they cost in microseconds: a step (16 k of a 128-block, 32 of a 64-block) keeps a
+// compute unit's matrix cores busy for 0.95 or 0.55 and takes 1.1 or 0.8 alone; shares as in kernels_mm16.hip.  Measured: 8192 x 2048
+// x 2048, 128-blocks 570 us (121 TFLOP/s, the library's product 468), 64-blocks 617; 512 x 2048 x 2048 50 (library 36); 1003 x 333 x 517
+// 16 (library 18).
 MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
   MmPlan best{128, 1, 0};
   double least = 1e300;
@@ -150,7 +194,7 @@ MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
     for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
       const int64_t share = (steps + splits - 1) / splits, groups = blocks * splits;
       if (splits > 1 && ((steps + share - 1) / share != splits || groups > 2048)) continue;
-      const double rounds = (double)((groups + 255) / 256), work = tile == 64 ? 0.47 : 0.95, alone = tile == 64 ? 0.8 : 1.1;
+      const double rounds = (double)((groups + 255) / 256), work = tile == 64 ? 0.55 : 0.95, alone = tile == 64 ? 0.8 : 1.1;
       double cost = (double)share * (rounds * work > alone ? rounds * work : alone);
       const double bytes = (double)groups / (double)blocks * (double)batches * (double)M * (double)((N + 3) / 4 * 4) * 4.0;
       if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;

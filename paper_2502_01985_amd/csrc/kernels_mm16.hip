@@ -126,17 +126,6 @@ __device__ __forceinline__ void arrived_and_together() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring blocks, walked eight rows of blocks at a time,
-// so that its L2 keeps the operand tiles they share.
-__device__ __forceinline__ void block_of(int id, int tm, int tn, int* ti, int* tj) {
-  const int total = tm * tn, q = total / 8, r = total % 8, x = id % 8, l = id / 8;
-  id = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + l;
-  constexpr int kGroup = 8;
-  const int g = id / (kGroup * tn), first = g * kGroup, rows = tm - first < kGroup ? tm - first : kGroup, in = id % (kGroup * tn);
-  *ti = first + in % rows;
-  *tj = in / rows;
-}
-
 // The n-th block on or above the diagonal of tn x tn blocks, row by row.
 __device__ __forceinline__ void upper_block(int id, int tn, int* ti, int* tj) {
   int r = 0;

@@ -131,6 +131,17 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
   store4_any(e.out, at, e.out_bf16, valid, v);
 }
 
+// Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring blocks, walked eight rows of blocks at a time,
+// so that its L2 keeps the operand tiles they share.
+__device__ __forceinline__ void block_of(int id, int tm, int tn, int* ti, int* tj) {
+  const int total = tm * tn, q = total / 8, r = total % 8, x = id % 8, l = id / 8;
+  id = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + l;
+  constexpr int kGroup = 8;
+  const int g = id / (kGroup * tn), first = g * kGroup, rows = tm - first < kGroup ? tm - first : kGroup, in = id % (kGroup * tn);
+  *ti = first + in % rows;
+  *tj = in / rows;
+}
+
 __device__ __forceinline__ int quad_valid(int64_t i, int64_t j, int64_t M, int64_t N) { return i >= M || j >= N ? 0 : N - j < 4 ? (int)(N - j) : 4; }
 
 // U quads of one column block: place(q, &i, &j) says where the q-th lies, sum(q) gives its four sums.
