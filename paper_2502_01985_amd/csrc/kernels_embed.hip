@@ -5,8 +5,21 @@ namespace ilargi {
 
 namespace {
 
-// A group of 2^sh lanes shares a row; every lane takes 16-byte pieces of it.
-template <class TI, class TO, bool ADD>
+constexpr int64_t kStreamBytes = 128ll << 20;     // half of the last-level cache
+
+// Sixteen aligned bytes written past the caches.
+template <class TO, int V>
+__device__ __forceinline__ void store_streaming(TO* p, const float (&f)[V]) {
+  typedef uint32_t words __attribute__((ext_vector_type(V * sizeof(TO) / 4)));
+  Piece<TO, V> t;
+#pragma unroll
+  for (int j = 0; j < V; ++j) t.v[j] = (TO)f[j];
+  __builtin_nontemporal_store(__builtin_bit_cast(words, t), reinterpret_cast<words*>(p));
+}
+
+// A group of 2^sh lanes shares a row; every lane takes 16-byte pieces of it.  STREAM: the output is larger than the caches and in aligned
+// pieces, and is written past them, which leaves them to the table.
+template <class TI, class TO, bool ADD, bool STREAM>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int sh) {
   constexpr int V = ElemOf<TI>::kVec < ElemOf<TO>::kVec ? ElemOf<TI>::kVec : ElemOf<TO>::kVec;
   const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> sh;
@@ -29,7 +42,8 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int sh) {
 #pragma unroll
       for (int j = 0; j < V; ++j) f[j] += o[j];
     }
-    store_piece<TO, V>(dst + c, valid, f);
+    if constexpr (STREAM) store_streaming<TO, V>(dst + c, f);
+    else store_piece<TO, V>(dst + c, valid, f);
   }
 }
 
@@ -39,8 +53,10 @@ hipError_t embed_typed(const EmbedArgs& a, hipStream_t st) {
   int sh = ilog2_ceil((a.cols + V - 1) / V);
   if (sh > 6) sh = 6;
   const int64_t blocks = ((a.n << sh) + kBlock - 1) / kBlock;
-  if (a.accumulate) embed_kernel<TI, TO, true><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
-  else embed_kernel<TI, TO, false><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
+  const bool whole = a.cols % V == 0 && a.ld_out * sizeof(TO) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && V * sizeof(TO) >= 8;
+  if (a.accumulate) embed_kernel<TI, TO, true, false><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
+  else if (whole && a.n * a.cols * (int64_t)sizeof(TO) >= kStreamBytes) embed_kernel<TI, TO, false, true><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
+  else embed_kernel<TI, TO, false, false><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
   return hipGetLastError();
 }
 

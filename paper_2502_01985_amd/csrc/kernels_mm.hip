@@ -182,7 +182,7 @@ hipError_t mm_f32_typed(const Product& a, const MmPlan& plan, float* partial, hi
 }  // namespace
 
 // Blocks of 128 or 64 and the shares of k, by what they cost in microseconds: a step (16 k of a 128-block, 32 of a 64-block) keeps a
-// compute unit's matrix cores busy for 0.95 or 0.55 and takes 1.1 or 0.8 alone; shares as in kernels_mm16.hip.  Measured: 8192 x 2048
+// compute unit's matrix cores busy for 0.8 or 0.47 and takes 1.1 or 0.8 alone; shares as in kernels_mm16.hip.  Measured: 8192 x 2048
 // x 2048, 128-blocks 570 us (121 TFLOP/s, the library's product 468), 64-blocks 617; 512 x 2048 x 2048 50 (library 36); 1003 x 333 x 517
 // 16 (library 18).
 MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
@@ -194,7 +194,7 @@ MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
     for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
       const int64_t share = (steps + splits - 1) / splits, groups = blocks * splits;
       if (splits > 1 && ((steps + share - 1) / share != splits || groups > 2048)) continue;
-      const double rounds = (double)((groups + 255) / 256), work = tile == 64 ? 0.55 : 0.95, alone = tile == 64 ? 0.8 : 1.1;
+      const double rounds = (double)((groups + 255) / 256), work = tile == 64 ? 0.47 : 0.8, alone = tile == 64 ? 0.8 : 1.1;
       double cost = (double)share * (rounds * work > alone ? rounds * work : alone);
       const double bytes = (double)groups / (double)blocks * (double)batches * (double)M * (double)((N + 3) / 4 * 4) * 4.0;
       if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;
