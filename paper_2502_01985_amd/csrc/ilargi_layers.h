@@ -180,7 +180,7 @@ struct MmPlan {
 };
 MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches);
 hipError_t launch_mm_f32(const Product& a, const MmPlan& plan, float* partial, hipStream_t st);
-bool mm_rows_takes(int64_t M, bool bf16);
+bool mm_rows_takes(int64_t M, int64_t K, bool bf16);
 MmPlan mm_rows_plan(int64_t M, int64_t N, int64_t K);
 hipError_t launch_mm_rows(const Product& a, const MmPlan& plan, float* partial, hipStream_t st);
 // Adds the shares in their order: `partial` holds splits x batches matrices of M x (N to a multiple of 4).

@@ -76,7 +76,7 @@ LayerLayout layer_layout(const ilargi_layer_t& y) {
     l.w = up256(2 * (size_t)y.n * (size_t)up8(y.k));
     l.forward_shares = l.w + up256(2 * (size_t)y.k * (size_t)up8(y.m));
   }
-  l.forward = l.forward_shares + (mm_rows_takes(y.n, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k));
+  l.forward = l.forward_shares + (mm_rows_takes(y.n, y.k, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k));
   l.dz = l.forward_shares;
   l.partial = l.dz + up256((size_t)y.n * (size_t)up8(y.m) * (h ? 2 : 4));
   l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
@@ -186,7 +186,7 @@ ilargi_status_t ilargi_linear(const ilargi_layer_t* layer, const void* X, int64_
   epi.bias = bias; epi.src = residual; epi.ld_src = ld_res; epi.src_bf16 = h;
   epi.pre = pre; epi.ld_pre = ld_pre; epi.act = y.act;
   epi.out = out; epi.ld_out = ld_out; epi.out_bf16 = h;
-  if (mm_rows_takes(y.n, h)) {
+  if (mm_rows_takes(y.n, y.k, h)) {
     Product p{};
     p.M = y.n; p.N = y.m; p.K = y.k; p.batches = 1;
     p.P = {X, ld_x, 0, h, 0};

@@ -17,8 +17,10 @@ __device__ __forceinline__ void store_streaming(TO* p, const float (&f)[V]) {
   __builtin_nontemporal_store(__builtin_bit_cast(words, t), reinterpret_cast<words*>(p));
 }
 
-// A group of 2^sh lanes shares a row; every lane takes 16-byte pieces of it.  STREAM: the output is larger than the caches and in aligned
-// pieces, and is written past them, which leaves them to the table.
+// out[i, :] = scale table[ids[i], :] (+ out[i, :]): bound by the bytes of the output and of the table's distinct rows.  A group of 2^sh
+// lanes shares a row; every lane takes 16-byte pieces of it.  STREAM: the output is larger than the caches and in aligned pieces, and
+// is written past them, which leaves them to the table: 1,000,000 rows of 256 from 100,000, bfloat16, skewed keys, 93 us = 6.1 TB/s
+// of its 563 MB, and 176 us through the caches; outputs of 15 to 102 MB take the same either way.
 template <class TI, class TO, bool ADD, bool STREAM>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int sh) {
   constexpr int V = ElemOf<TI>::kVec < ElemOf<TO>::kVec ? ElemOf<TI>::kVec : ElemOf<TO>::kVec;
@@ -74,6 +76,10 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
 // walk runs of equal length of the sorted ids and sum the rows of d_out that they stand for: a row of the table whose ids all lie
 // in one run is written there, and the sums of the others are carried to a second pass.  So one row that holds a large part of the
 // ids is spread over as many groups as it has runs, and every sum has a fixed order.
+//
+// Bound by the rows of d_out, gathered 256 bytes at a time, and the launches of the sort.  1,000,000 ids of 100,000 x 128, bfloat16,
+// skewed: 158 us, of which the sort 50, the runs 70 (256 MB: 3.7 TB/s), the carries and rows without ids 31; one row holds 13 % of
+// the ids.  9001 ids of 6040 x 75, float32: 40 us, of which the sort 22.
 namespace {
 
 constexpr int kBits = 9, kBins = 1 << kBits;      // two passes for tables of up to 262,143 rows

@@ -9,6 +9,10 @@
 //     transposing LDS read gives each lane its four k of one column.
 // LDS is filled in lane order, so the places are permuted by the addresses that the lanes fetch from.
 // The columns of the result are the first operand of the matrix instruction: a lane then holds four neighbouring columns.
+//
+// Bound by the matrix cores and, in blocks of 256, by the power they take (the clock falls to 2.0 GHz).  256-blocks: 8192 x 8192 x 4096
+// 1240 TFLOP/s with K contiguous on both sides, 1245 with one and 1250 with both operands' rows over k; the library's product 1210.
+// 128-blocks, two to a compute unit, for results of fewer than 256 large blocks: 2048 x 2048 x 2048 545 TFLOP/s.
 #include <utility>
 
 #include "mm_epilogue.h"
@@ -326,7 +330,8 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel
 // read once: 64 KB fetched for 96 matrix instructions where the planes one after the other would take 96 KB.  Blocks of 128 in
 // eight wavefronts: four have 64 x 64 sums of the first half of every step, four the same sums of the second half, and they exchange
 // halves of their sums at the end.  So two wavefronts share a SIMD, and one's products run while the other's reads and fetches are
-// issued (four wavefronts with both halves: 2048 x 2048 x 2048 takes 55 us, of which the products alone 33).  Q's rows run over k
+// issued (four wavefronts with both halves: 2048 x 2048 x 2048 takes 55 us, of which the products alone are 33; the fifteen products of
+// an orthogonalised 2048 x 2048 took 840 us so, and 750 with eight wavefronts).  Q's rows run over k
 // (QK) or its columns do.
 // (LDS is asked for at the launch: told of it, the compiler would take the accumulators to the other half of a wavefront's
 // registers, and move them to and fro.)

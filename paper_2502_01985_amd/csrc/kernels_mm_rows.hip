@@ -5,6 +5,7 @@
 // its share of k, and a second launch adds the shares, where there are several.  Longer shares in fewer launches are slower where W
 // comes from memory: 1 x 4096 x 4096, bfloat16, 15.3 us with shares of 1024 rows and 27.9 with one share; 1 x 8192 x 1000 14.1
 // and 45.3.  Blocks on the matrix cores take 17.5 and 13.4 for the same.
+// With W in the last-level cache the 4096 x 4096 call takes 13 us.
 #include "mm_epilogue.h"
 
 namespace ilargi {
@@ -121,7 +122,7 @@ hipError_t mm_rows_typed(const Product& a, const MmPlan& plan, float* partial, h
 
 // Up to two rows of bfloat16, four of float32: with more the vector units take longer than blocks on the matrix cores do (4096 x
 // 4096, bfloat16, 4 rows: 30.6 us against 17.7 in blocks; float32, 4 rows: 26.5 against 32, 8 rows: 37.8).
-bool mm_rows_takes(int64_t M, bool bf16) { return M <= (bf16 ? 2 : 4); }
+bool mm_rows_takes(int64_t M, int64_t K, bool bf16) { return M <= (bf16 ? 2 : 4) && K <= 65535 * (int64_t)kMostShare; }
 
 MmPlan mm_rows_plan(int64_t M, int64_t N, int64_t K) {
   MmPlan p{0, 1, 0};
@@ -133,7 +134,7 @@ MmPlan mm_rows_plan(int64_t M, int64_t N, int64_t K) {
 
 hipError_t launch_mm_rows(const Product& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  if (!mm_rows_takes(a.M, a.P.bf16) || a.P.k_rows || !a.Q.k_rows || a.batches != 1 || a.K < 1 || a.P.bf16 != a.Q.bf16 || plan.splits > 65535)
+  if (!mm_rows_takes(a.M, a.K, a.P.bf16) || a.P.k_rows || !a.Q.k_rows || a.batches != 1 || a.K < 1 || a.P.bf16 != a.Q.bf16)
     return hipErrorInvalidValue;
   return a.P.bf16 ? mm_rows_typed<bf16_t>(a, plan, partial, st) : mm_rows_typed<float>(a, plan, partial, st);
 }
