@@ -87,10 +87,7 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += bias[q];
     if (e.pre != nullptr) store4_any(e.pre, i * e.ld_pre + j, e.out_bf16, valid, v);
-    if (e.act != ILARGI_ACT_NONE) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = act_value(v[q], e.act);
-    }
+    act_values(v, e.act);
     if constexpr (SRC) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] += t[q];
