@@ -129,6 +129,9 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   }
 }
 
+// Outputs of so many bytes are written past the caches: half of the last-level cache.
+constexpr int64_t kStreamBytes = 128ll << 20;
+
 // ------------------------------------------------------------------------------------------------- embedding rows
 struct EmbedArgs {
   const void* table;
@@ -222,6 +225,7 @@ struct Product16 {
   int kind;
   int symmetric;            // C = C^T: blocks above the diagonal are formed, and written twice
   Epilogue epi;
+  bool past;                // a layer's outputs are written past the caches
 };
 MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric);
 // A bfloat16 matrix laid out for launch_mm16: rows of (cols to a multiple of 8) elements.

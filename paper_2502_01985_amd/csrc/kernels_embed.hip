@@ -5,8 +5,6 @@ namespace ilargi {
 
 namespace {
 
-constexpr int64_t kStreamBytes = 128ll << 20;     // half of the last-level cache
-
 // Sixteen aligned bytes written past the caches.
 template <class TO, int V>
 __device__ __forceinline__ void store_streaming(TO* p, const float (&f)[V]) {

@@ -286,3 +286,26 @@ def test_refusals(il):
         il.ilargi_linear_grad(torch.zeros(4, 6, device="cuda"), X, W, pre=torch.zeros(4, 6, device="cuda"), act="relu",
                               workspace=torch.empty(256, dtype=torch.uint8, device="cuda")[:0])
     assert e.value.status in (il.ERR_WORKSPACE, il.ERR_NULL)
+
+
+@pytest.mark.parametrize("n,m,act,keep", [(4099, 8200, "gelu", True), (8209, 8193, "silu", False)])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
+def test_forward_outputs_larger_than_the_caches(il, n, m, act, keep, pad, shift):
+    """bfloat16 outputs of 128 MiB and more, rows at any address; what lies between the rows stays as it was."""
+    k, gen = 72, _gen(n + m + pad)
+    X, W = _matrix(n, k, BF16, gen), _matrix(k, m, BF16, gen, 0, 0, 1 / math.sqrt(k))
+    bias = torch.randn(m, generator=gen, device="cuda").to(BF16)
+    stores = [torch.full((n * (m + pad) + shift + 8,), 7.0, dtype=BF16, device="cuda") for _ in range(2)]
+    out, pre = (s[shift: shift + n * (m + pad)].view(n, m + pad) for s in stores)
+    il.ilargi_linear(X, W, bias=bias, act=act, out=out[:, :m], pre=pre[:, :m] if keep else None)
+    for a in range(0, n, 1024):
+        x = X[a: a + 1024].double()
+        z = x @ W.double() + bias.double()
+        ez = (k + 3) * E32 * (x.abs() @ W.double().abs() + bias.double().abs())
+        want = _f(z, act)
+        err = 1.13 * ez + 16 * E32 * (1 + z.abs()) + 2 * E32 * want.abs()
+        assert bool(((out[a: a + 1024, :m].double() - want).abs() <= err + U[BF16] * (want.abs() + err)).all())
+        if keep:
+            assert bool(((pre[a: a + 1024, :m].double() - z).abs() <= ez + U[BF16] * (z.abs() + ez)).all())
+    for s, v in zip(stores, (out, pre)):
+        assert bool((v[:, m:] == 7.0).all()) and bool((s[:shift] == 7.0).all()) and bool((s[shift + v.numel():] == 7.0).all())
