@@ -227,8 +227,8 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
   LayerGradArgs g{y.n, y.m, d_out, ld_out, pre, ld_pre, y.act, h, z.padded ? ws + l.dz : nullptr, up8(y.m), d_bias, accumulate};
   if (hipError_t e = launch_layer_grad(g, (float*)(ws + l.partial), st); e != hipSuccess) return done("linear_grad", e);
   Epilogue epi{};
-  epi.mode = kEpiScale;
-  epi.s0 = 1.0f; epi.out_bf16 = h;
+  epi.mode = kEpiLinear;
+  epi.out_bf16 = h;
   if (d_X != nullptr) {
     Factor w{{W, ld_w, y.k, y.m}, 0, false};
     if (hipError_t e = lay_out(y, &w, ws + l.w, st); e != hipSuccess) return done("linear_grad", e);
@@ -240,7 +240,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
     if (hipError_t e = lay_out(y, &x, ws + l.x, st); e != hipSuccess) return done("linear_grad", e);
     z.k_rows = 1;
     epi.out = d_W; epi.ld_out = ld_dw;
-    if (accumulate) { epi.src = d_W; epi.ld_src = ld_dw; epi.src_bf16 = h; epi.s1 = 1.0f; }
+    if (accumulate) { epi.src = d_W; epi.ld_src = ld_dw; epi.src_bf16 = h; }
     if (hipError_t e = product(x, z, y.k, y.m, y.n, h, epi, shares, st); e != hipSuccess) return done("linear_grad", e);
   }
   return ILARGI_OK;

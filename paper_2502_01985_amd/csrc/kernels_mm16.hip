@@ -177,10 +177,12 @@ __device__ __forceinline__ void store8(bf16_t* p, int valid, bool past, const fl
   }
 }
 
-// The sums of a wavefront (TM x 64) of a layer without a residual, in bfloat16: as store_sums, with nothing else in it and 16 bytes a lane.
-// 16384 x 2048 x 8192, gelu, z kept: the general one 628 us, this one 597, past the caches (whose lines the operands then keep) 562.
+// The sums of a wavefront (TM x 64) of a bfloat16 layer go through LDS, 64 rows at a time, so that stores run along the result's rows,
+// 16 bytes a lane.  The residual is added in a pass of its own, in which the loads of four rows are on their way together (with a residual 16384 x 2048 x 8192 takes 720 us, 785 in one pass of 8 bytes a
+// lane).  16384 x 2048 x 8192, gelu, z kept: 628 us with the epilogue of all products, 597 with this, 562 past the caches (whose lines the
+// operands then keep).
 template <int TM, int FN>
-__device__ __forceinline__ void store_layer(const Product16& a, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t i0, int64_t j0) {
+__device__ __forceinline__ void store_layer(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t i0, int64_t j0) {
   const int lane = threadIdx.x % 64, c = (lane & 7) * 8;
   float* mine = (float*)lds + threadIdx.x / 64 * 64 * kOutPad;
   const Epilogue& e = a.epi;
@@ -190,6 +192,7 @@ __device__ __forceinline__ void store_layer(const Product16& a, char* lds, const
 #pragma unroll
   for (int q = 0; q < 8; ++q) bias[q] = 0.0f;
   if (e.bias != nullptr && valid > 0) load_piece<bf16_t, 8>((const bf16_t*)e.bias + j, valid, bias);
+  const bool added = e.src != nullptr;
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < TM / 64; ++h) {
@@ -200,24 +203,63 @@ __device__ __forceinline__ void store_layer(const Product16& a, char* lds, const
         *reinterpret_cast<f32x4*>(mine + (16 * x + (lane & 15)) * kOutPad + 16 * y + (lane >> 4) * 4) = acc[4 * h + x][y];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    const int64_t ih = i0 + 64 * h + (lane >> 3);
+    float* const at = mine + (lane >> 3) * kOutPad + c;
+    if (partial != nullptr) {
+      const int64_t ldp = (a.N + 3) / 4 * 4;
+      float* part = partial + (int64_t)blockIdx.z * a.M * ldp + j;
+#pragma unroll 2
+      for (int q = 0; q < 8; ++q) {
+        const int64_t i = ih + 8 * q;
+        if (i >= a.M) continue;
+        if (valid > 0) *reinterpret_cast<f32x4*>(part + i * ldp) = *reinterpret_cast<const f32x4*>(at + 8 * q * kOutPad);
+        if (valid > 4) *reinterpret_cast<f32x4*>(part + i * ldp + 4) = *reinterpret_cast<const f32x4*>(at + 8 * q * kOutPad + 4);
+      }
+    } else {
 #pragma unroll 1
-    for (int q = 0; q < 8; ++q) {
-      const int r = 8 * q + (lane >> 3);
-      const int64_t i = i0 + 64 * h + r;
-      if (i >= a.M || valid == 0) continue;
-      const f32x4 s0 = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c), s1 = *reinterpret_cast<const f32x4*>(mine + r * kOutPad + c + 4);
-      float v[8] = {s0[0] + bias[0], s0[1] + bias[1], s0[2] + bias[2], s0[3] + bias[3], s1[0] + bias[4], s1[1] + bias[5], s1[2] + bias[6], s1[3] + bias[7]};
-      if (e.pre != nullptr) store8((bf16_t*)e.pre + i * e.ld_pre + j, valid, a.past, v);
-      act_values(v, e.act);
-      store8((bf16_t*)e.out + i * e.ld_out + j, valid, a.past, v);
+      for (int q = 0; q < 8; ++q) {
+        const int64_t i = ih + 8 * q;
+        if (i >= a.M || valid == 0) continue;
+        f32x4* const sums = reinterpret_cast<f32x4*>(at + 8 * q * kOutPad);
+        const f32x4 s0 = sums[0], s1 = sums[1];
+        float v[8] = {s0[0] + bias[0], s0[1] + bias[1], s0[2] + bias[2], s0[3] + bias[3], s1[0] + bias[4], s1[1] + bias[5], s1[2] + bias[6], s1[3] + bias[7]};
+        if (e.pre != nullptr) store8((bf16_t*)e.pre + i * e.ld_pre + j, valid, a.past, v);
+        act_values(v, e.act);
+        if (added) {
+          sums[0] = f32x4{v[0], v[1], v[2], v[3]};
+          sums[1] = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+          store8((bf16_t*)e.out + i * e.ld_out + j, valid, a.past, v);
+        }
+      }
+      if (added) {
+#pragma unroll 1
+        for (int q = 0; q < 8; q += 4) {
+          float r[4][8];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int64_t i = ih + 8 * (q + u);
+            load_piece<bf16_t, 8>((const bf16_t*)e.src + i * e.ld_src + j, i < a.M ? valid : 0, r[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int64_t i = ih + 8 * (q + u);
+            if (i >= a.M || valid == 0) continue;
+            const f32x4* const sums = reinterpret_cast<const f32x4*>(at + 8 * (q + u) * kOutPad);
+#pragma unroll
+            for (int w = 0; w < 8; ++w) r[u][w] += sums[w / 4][w % 4];
+            store8((bf16_t*)e.out + i * e.ld_out + j, valid, a.past, r[u]);
+          }
+        }
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-// The sums of a wavefront (TM x 64) go through LDS, up to 64 rows at a time, so that stores run along the result's rows.
-template <int KIND, int TM, int FN>
+// The same of a product of pairs, scaled and added to `src`, into planes, float32 or bfloat16.
+template <int TM, int FN>
 __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t b, int64_t i0,
                                            int64_t j0, bool mirrored) {
   constexpr int kRows = TM < 64 ? TM : 64, kQ = kRows / 4;      // rows of a pass, and its turns of 64 quads
@@ -247,8 +289,6 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
     } else {
       auto row = [&](int r, int at) { return *reinterpret_cast<const float4*>(mine + r * kOutPad + at); };
       if (!a.epi.flip) {
-        float bias[4];
-        epilogue_bias(a.epi, j0 + c, (int)(a.N - j0 - c < 4 ? a.N - j0 - c : 4), bias);
         if (a.epi.src == nullptr) {
 #pragma unroll 2
           for (int q = 0; q < kQ; ++q) {
@@ -256,12 +296,12 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
             if (valid == 0) continue;
             const float4 t = row(r, c);
             float v[4] = {t.x, t.y, t.z, t.w};
-            epilogue4<false>(a.epi, b, ri + r, j0 + c, valid, bias, SrcQuad{}, v);
+            epilogue4<false>(a.epi, b, ri + r, j0 + c, valid, none, SrcQuad{}, v);
           }
         } else {
 #pragma unroll 1
           for (int q = 0; q < kQ; q += 4)
-            epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
+            epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
                               [&](int u) { return row(4 * (q + u) + (lane >> 4), c); });
         }
       } else {                                         // written along j's rows, which run over i
@@ -272,18 +312,16 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
           epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + r; *j = j0 + 4 * ((q + u) * kSide + s); },
                             [&](int u) { return row(r, 4 * ((q + u) * kSide + s)); });
       }
-      if constexpr (KIND == kMm16Pairs) {
-        if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
-          constexpr int kAcross = kRows / 4, kDown = 64 / kAcross;
-          const int ci = lane % kAcross * 4, rj = lane / kAcross;
+      if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
+        constexpr int kAcross = kRows / 4, kDown = 64 / kAcross;
+        const int ci = lane % kAcross * 4, rj = lane / kAcross;
 #pragma unroll 1
-          for (int q = 0; q < kQ; q += 4)
-            epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + kDown * (q + u) + rj; *j = ri + ci; },
-                              [&](int u) {
-                                const float* m = mine + ci * kOutPad + kDown * (q + u) + rj;
-                                return make_float4(m[0], m[kOutPad], m[2 * kOutPad], m[3 * kOutPad]);
-                              });
-        }
+        for (int q = 0; q < kQ; q += 4)
+          epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + kDown * (q + u) + rj; *j = ri + ci; },
+                            [&](int u) {
+                              const float* m = mine + ci * kOutPad + kDown * (q + u) + rj;
+                              return make_float4(m[0], m[kOutPad], m[2 * kOutPad], m[3 * kOutPad]);
+                            });
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -291,10 +329,9 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
   }
 }
 
-// blockIdx: block, matrix of the batch, share of k.  With several shares the sums go to `partial`, one M x (N to a multiple of 4)
-// matrix after the other.
-// LAYER: a layer without a residual, in one share.
-template <bool PK, bool QK, int BM, int BN, int WM, int WN, bool LAYER>
+// blockIdx: block, none, share of k.  With several shares the sums go to `partial`, one M x (N to a multiple of 4) matrix after the
+// other.
+template <bool PK, bool QK, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel(Product16 a, int tm, int tn, int share, float* __restrict__ partial) {
   constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16, STAGES = 2, KIND = kMm16Bf16;
   using TileP = Tile<PK, BM, NT>;
@@ -305,12 +342,12 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel
   char(*lds)[TileP::kBytes + TileQ::kBytes] = reinterpret_cast<char(*)[TileP::kBytes + TileQ::kBytes]>(lds_all);
   int ti, tj;
   block_of(blockIdx.x, tm, tn, &ti, &tj);
-  const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN, b = blockIdx.y;
+  const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wi = (wave / WN) * TM, wj = (wave % WN) * TN;
   const int64_t step_p = PK ? kBK * a.P.ld * 2 : kBK * 2, step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
   const int first = (int)blockIdx.z * share, ks_all = (int)((a.K + kBK - 1) / kBK), ks = ks_all - first < share ? ks_all - first : share;
-  const char* P = (const char*)a.P.p + 2 * (b * a.P.batch + (PK ? i0 : i0 * a.P.ld)) + first * step_p;
-  const char* Q = (const char*)a.Q.p + 2 * (b * a.Q.batch + (QK ? j0 : j0 * a.Q.ld)) + first * step_q;
+  const char* P = (const char*)a.P.p + 2 * (PK ? i0 : i0 * a.P.ld) + first * step_p;
+  const char* Q = (const char*)a.Q.p + 2 * (QK ? j0 : j0 * a.Q.ld) + first * step_q;
   TileP tp;
   TileQ tq;
   tp.plan(a.P.ld, a.P.across - i0);
@@ -376,8 +413,7 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void mm16_kernel
     if (left > 0 && left < kBK) fetch(t + STAGES);
     second_half<TileP, TileQ, KIND, FM, FN>(left == kBK, tp, tq, from_p, from_q, here, fp, fq, next, p0, q0, p1, q1, acc);
   }
-  if constexpr (LAYER) store_layer<TM, FN>(a, lds_all, acc, i0 + wi, j0 + wj);
-  else store_sums<KIND, TM, FN>(a, partial, lds_all, acc, b, i0 + wi, j0 + wj, false);
+  store_layer<TM, FN>(a, partial, lds_all, acc, i0 + wi, j0 + wj);
 }
 
 // Pairs: a step's four tiles (both planes of both operands) lie in LDS together, and three products are formed from the fragments
@@ -508,7 +544,7 @@ __global__ __launch_bounds__(512, 1) void mm16_pairs_kernel(Product16 a, int tm,
       const f32x4 other = *reinterpret_cast<const f32x4*>(taken + at(x, y));
       sum[x][y] = half ? acc[2 + x][y] + other : acc[x][y] + other;
     }
-  store_sums<kMm16Pairs, 32, FN>(a, partial, lds_all, sum, b, i0 + wi + 32 * half, j0 + wj, a.symmetric && ti != tj);
+  store_sums<32, FN>(a, partial, lds_all, sum, b, i0 + wi + 32 * half, j0 + wj, a.symmetric && ti != tj);
 }
 
 struct Join {
@@ -598,20 +634,12 @@ template <bool PK, bool QK>
 hipError_t mm16_order(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   const int tm = (int)((a.M + plan.tile - 1) / plan.tile), tn = (int)((a.N + plan.tile - 1) / plan.tile);
   const int ks = (int)((a.K + kBK - 1) / kBK), share = (ks + plan.splits - 1) / plan.splits;
-  const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, 0), (unsigned)a.batches, (unsigned)plan.splits);
+  const dim3 grid((unsigned)blocks_of(a.M, a.N, plan.tile, 0), 1, (unsigned)plan.splits);
   float* part = plan.splits > 1 ? partial : nullptr;
-  const Epilogue& e = a.epi;
-  if constexpr (!PK && QK) {
-    if (part == nullptr && e.mode == kEpiLinear && e.src == nullptr && e.out_bf16 && a.batches == 1) {
-      Product16 l = a;
-      l.past = (e.pre != nullptr ? 4 : 2) * a.M * a.N >= kStreamBytes;
-      if (plan.tile == 256) mm16_kernel<PK, QK, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(l, tm, tn, share, part);
-      else mm16_kernel<PK, QK, 128, 128, 2, 2, true><<<grid, 256, 0, st>>>(l, tm, tn, share, part);
-      return hipGetLastError();
-    }
-  }
-  if (plan.tile == 256) mm16_kernel<PK, QK, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(a, tm, tn, share, part);
-  else mm16_kernel<PK, QK, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, tm, tn, share, part);
+  Product16 l = a;
+  l.past = part == nullptr && (a.epi.pre != nullptr ? 4 : 2) * a.M * a.N >= kStreamBytes;
+  if (plan.tile == 256) mm16_kernel<PK, QK, 256, 256, 2, 4><<<grid, 512, 0, st>>>(l, tm, tn, share, part);
+  else mm16_kernel<PK, QK, 128, 128, 2, 2><<<grid, 256, 0, st>>>(l, tm, tn, share, part);
   return finish_shares(a, plan, part, st);
 }
 
@@ -703,7 +731,7 @@ hipError_t launch_pack16(const void* src, int64_t ld, int64_t rows, int64_t cols
 hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.kind == kMm16Bf16) {
-    if (a.symmetric) return hipErrorInvalidValue;
+    if (a.symmetric || a.batches != 1 || a.epi.mode != kEpiLinear || !a.epi.out_bf16) return hipErrorInvalidValue;
     if (a.P.k_rows) return a.Q.k_rows ? mm16_order<true, true>(a, plan, partial, st) : hipErrorInvalidValue;
     return a.Q.k_rows ? mm16_order<false, true>(a, plan, partial, st) : mm16_order<false, false>(a, plan, partial, st);
   }
