@@ -178,9 +178,9 @@ __device__ __forceinline__ void store8(bf16_t* p, int valid, bool past, const fl
 }
 
 // The sums of a wavefront (TM x 64) of a bfloat16 layer go through LDS, 64 rows at a time, so that stores run along the result's rows,
-// 16 bytes a lane.  The residual is added in a pass of its own, in which the loads of four rows are on their way together (with a residual 16384 x 2048 x 8192 takes 720 us, 785 in one pass of 8 bytes a
-// lane).  16384 x 2048 x 8192, gelu, z kept: 628 us with the epilogue of all products, 597 with this, 562 past the caches (whose lines the
-// operands then keep).
+// 16 bytes a lane.  The residual is added in a pass of its own, in which the loads of four rows are on their way together.
+// 16384 x 2048 x 8192, gelu, z kept: 628 us in one pass of 8 bytes a lane for every kind of result, 597 with this, 562 to 571 past the
+// caches (whose lines the operands then keep); with a residual 785 and 720.
 template <int TM, int FN>
 __device__ __forceinline__ void store_layer(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t i0, int64_t j0) {
   const int lane = threadIdx.x % 64, c = (lane & 7) * 8;
