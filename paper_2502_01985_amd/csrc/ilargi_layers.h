@@ -132,6 +132,17 @@ __device__ __forceinline__ float act_slope(float z, int act) {
 // Outputs of so many bytes are written past the caches: half of the last-level cache.
 constexpr int64_t kStreamBytes = 128ll << 20;
 
+// The threads of a launch along an axis are counted in 32 bits: one of 2^32 and more forms the wrong number of workgroups, with no
+// error.  So `groups` workgroups of `threads` go in parts: launch(first, count) forms workgroups first .. first + count.
+constexpr int64_t kMostThreads = 1ll << 31;
+constexpr int64_t kMostAcross = 32768;       // workgroups along the second axis: devices promise 65,535
+template <class F>
+hipError_t in_parts(int64_t groups, int threads, F launch) {
+  const int64_t most = kMostThreads / threads;
+  for (int64_t first = 0; first < groups; first += most) launch(first, (unsigned)(groups - first < most ? groups - first : most));
+  return hipGetLastError();
+}
+
 // ------------------------------------------------------------------------------------------------- embedding rows
 struct EmbedArgs {
   const void* table;

@@ -52,12 +52,18 @@ hipError_t embed_typed(const EmbedArgs& a, hipStream_t st) {
   constexpr int V = ElemOf<TI>::kVec < ElemOf<TO>::kVec ? ElemOf<TI>::kVec : ElemOf<TO>::kVec;
   int sh = ilog2_ceil((a.cols + V - 1) / V);
   if (sh > 6) sh = 6;
-  const int64_t blocks = ((a.n << sh) + kBlock - 1) / kBlock;
   const bool whole = a.cols % V == 0 && a.ld_out * sizeof(TO) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && V * sizeof(TO) >= 8;
-  if (a.accumulate) embed_kernel<TI, TO, true, false><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
-  else if (whole && a.n * a.cols * (int64_t)sizeof(TO) >= kStreamBytes) embed_kernel<TI, TO, false, true><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
-  else embed_kernel<TI, TO, false, false><<<(unsigned)blocks, kBlock, 0, st>>>(a, sh);
-  return hipGetLastError();
+  const bool past = whole && a.n * a.cols * (int64_t)sizeof(TO) >= kStreamBytes;
+  return in_parts(((a.n << sh) + kBlock - 1) / kBlock, kBlock, [&](int64_t first, unsigned blocks) {
+    const int64_t row = first * (kBlock >> sh), rows = (int64_t)blocks * (kBlock >> sh);
+    EmbedArgs b = a;
+    b.ids += row;
+    b.out = (TO*)a.out + row * a.ld_out;
+    b.n = a.n - row < rows ? a.n - row : rows;
+    if (a.accumulate) embed_kernel<TI, TO, true, false><<<blocks, kBlock, 0, st>>>(b, sh);
+    else if (past) embed_kernel<TI, TO, false, true><<<blocks, kBlock, 0, st>>>(b, sh);
+    else embed_kernel<TI, TO, false, false><<<blocks, kBlock, 0, st>>>(b, sh);
+  });
 }
 
 }  // namespace
@@ -308,13 +314,13 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& g, int64_t v, int
   store_piece<TO, V>(dst, valid, r);
 }
 
-// A group of 2^sh lanes walks a run over columns [blockIdx.y V 2^sh, ...), eight rows of d_out on their way at a time.
+// A group of 2^sh lanes walks a run over columns [(slab + blockIdx.y) V 2^sh, ...), eight rows of d_out on their way at a time.
 template <class TI, class TO, bool ADD>
-__global__ __launch_bounds__(kBlock) void embed_runs_kernel(RunArgs a, int sh) {
+__global__ __launch_bounds__(kBlock) void embed_runs_kernel(RunArgs a, int sh, int64_t slab) {
   constexpr int V = ElemOf<TI>::kVec;
   const int64_t run = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> sh;
   const int lane = threadIdx.x & ((1 << sh) - 1);
-  const int64_t c = ((int64_t)blockIdx.y << sh) * V + (int64_t)lane * V;
+  const int64_t c = ((slab + blockIdx.y) << sh) * V + (int64_t)lane * V;
   if (run >= a.runs || c >= a.g.cols) return;
   const int valid = (int)(a.g.cols - c < V ? a.g.cols - c : V);
   const int64_t n = a.g.n, p0 = run * a.run, p1 = p0 + a.run < n ? p0 + a.run : n;
@@ -416,15 +422,17 @@ __device__ __forceinline__ void add_carries(const RunArgs& a, int64_t begin, int
 // The first workgroups look at kJoinRuns runs each: a segment that begins in one of them and goes on behind it is the sum of its
 // carries.  Up to kShortSpan of them are added by a group of 2^sh lanes, longer ones by all groups, each every so manieth, which are
 // then added in order.  The other workgroups zero the rows without ids (unless the caller accumulates), kClearRows of them each.
+// `first`: workgroups of this call in earlier launches.
 template <class TO, bool ADD>
-__global__ __launch_bounds__(kJoin) void embed_join_kernel(RunArgs a, int sh, int64_t joins) {
+__global__ __launch_bounds__(kJoin) void embed_join_kernel(RunArgs a, int sh, int64_t joins, int64_t first) {
   constexpr int V = 4;
+  const int64_t id = first + blockIdx.x;
   const int64_t n = a.g.n;
   const int lane = threadIdx.x & ((1 << sh) - 1), group = threadIdx.x >> sh, groups = kJoin >> sh;
-  if ((int64_t)blockIdx.x >= joins) {
+  if (id >= joins) {
     __shared__ uint8_t full[kClearRows];
     __shared__ int64_t ends[2];
-    const int64_t v0 = ((int64_t)blockIdx.x - joins) * kClearRows, v1 = v0 + kClearRows < a.g.rows ? v0 + kClearRows : a.g.rows;
+    const int64_t v0 = (id - joins) * kClearRows, v1 = v0 + kClearRows < a.g.rows ? v0 + kClearRows : a.g.rows;
     if (threadIdx.x < kClearRows) full[threadIdx.x] = v0 + threadIdx.x >= v1;
     if (threadIdx.x < 2 * kWave) {
       const int64_t at = wave_lower(a.sorted, n, threadIdx.x < kWave ? v0 : v1);
@@ -456,7 +464,7 @@ __global__ __launch_bounds__(kJoin) void embed_join_kernel(RunArgs a, int sh, in
   }
   __shared__ float4 part[kJoin];
   __shared__ int32_t keys[kJoinRuns], spans[kJoinRuns];     // runs that the segment reaches, 0 where there is none
-  const int64_t run0 = (int64_t)blockIdx.x * kJoinRuns;
+  const int64_t run0 = id * kJoinRuns;
   if (threadIdx.x < kJoinRuns) {
     const int64_t run = run0 + threadIdx.x, p0 = run * a.run, p1 = p0 + a.run;
     int32_t key = 0, span = 0;
@@ -547,15 +555,19 @@ int lane_shift(int64_t cols, int vec) {
 template <class TI, class TO, bool ADD>
 hipError_t grad_launch(const RunArgs& r, hipStream_t st) {
   constexpr int V = ElemOf<TI>::kVec;
-  if (r.runs > 0) {
+  if (r.runs > 0) {                                      // (at most 2^23 runs of 64 lanes: in one launch)
     const int sh = lane_shift(r.g.cols, V);
-    const unsigned slabs = (unsigned)((r.g.cols + ((int64_t)V << sh) - 1) / ((int64_t)V << sh));
-    embed_runs_kernel<TI, TO, ADD><<<dim3((unsigned)(((r.runs << sh) + kBlock - 1) / kBlock), slabs), kBlock, 0, st>>>(r, sh);
+    const int64_t slabs = (r.g.cols + ((int64_t)V << sh) - 1) / ((int64_t)V << sh);
+    for (int64_t slab = 0; slab < slabs; slab += kMostAcross) {
+      const unsigned across = (unsigned)(slabs - slab < kMostAcross ? slabs - slab : kMostAcross);
+      embed_runs_kernel<TI, TO, ADD><<<dim3((unsigned)(((r.runs << sh) + kBlock - 1) / kBlock), across), kBlock, 0, st>>>(r, sh, slab);
+    }
   }
   const int64_t clear = ADD ? 0 : (r.g.rows + kClearRows - 1) / kClearRows;
   const int64_t joins = (r.runs + kJoinRuns - 1) / kJoinRuns;
-  if (joins + clear > 0) embed_join_kernel<TO, ADD><<<(unsigned)(joins + clear), kJoin, 0, st>>>(r, lane_shift(r.g.cols, 4), joins);
-  return hipGetLastError();
+  return in_parts(joins + clear, kJoin, [&](int64_t first, unsigned blocks) {
+    embed_join_kernel<TO, ADD><<<blocks, kJoin, 0, st>>>(r, lane_shift(r.g.cols, 4), joins, first);
+  });
 }
 
 template <class TI, class TO>
