@@ -229,6 +229,11 @@ struct Operand16 {
   int k_rows;
   int64_t batch, plane, across;
 };
+inline void shift_operand(Operand* o, int64_t by) { o->p = (const char*)o->p + (o->k_rows ? by : by * o->ld) * (o->bf16 ? 2 : 4); }
+inline void shift_operand(Operand16* o, int64_t by) {
+  o->p = (const char*)o->p + (o->k_rows ? by : by * o->ld) * 2;
+  o->across -= by;
+}
 enum { kMm16Bf16 = 0, kMm16Pairs = 1 };     // bfloat16; pairs of float16 planes
 struct Product16 {
   Operand16 P, Q;
@@ -257,6 +262,32 @@ struct LayerGradArgs {
 };
 size_t layer_grad_partial_bytes(int64_t n, int64_t m);
 hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t st);
+
+// A product of a layer in blocks of tile_m x tile_n sums, a workgroup of `threads` each: whole, or in parts of whole blocks where they are
+// too many for one launch.
+template <class P, class F>
+hipError_t in_blocks(const P& a, int64_t tile_m, int64_t tile_n, int threads, F launch) {
+  const int64_t tm = (a.M + tile_m - 1) / tile_m, tn = (a.N + tile_n - 1) / tile_n, most = kMostThreads / threads;
+  if (tm * tn <= most) return launch(a);
+  if (a.batches != 1 || a.epi.mode != kEpiLinear) return hipErrorInvalidValue;
+  const int64_t across = tn < most ? tn : most, down = most / across;
+  for (int64_t ti = 0; ti < tm; ti += down)
+    for (int64_t tj = 0; tj < tn; tj += across) {
+      const int64_t i = ti * tile_m, j = tj * tile_n;
+      P b = a;
+      b.M = a.M - i < down * tile_m ? a.M - i : down * tile_m;
+      b.N = a.N - j < across * tile_n ? a.N - j : across * tile_n;
+      shift_operand(&b.P, i);
+      shift_operand(&b.Q, j);
+      auto shift = [](const void* p, int64_t by, int bf16) { return p != nullptr ? (const void*)((const char*)p + by * (bf16 ? 2 : 4)) : p; };
+      b.epi.bias = shift(a.epi.bias, j, a.epi.out_bf16);
+      b.epi.src = shift(a.epi.src, i * a.epi.ld_src + j, a.epi.src_bf16);
+      b.epi.pre = (void*)shift(a.epi.pre, i * a.epi.ld_pre + j, a.epi.out_bf16);
+      b.epi.out = (void*)shift(a.epi.out, i * a.epi.ld_out + j, a.epi.out_bf16);
+      if (hipError_t e = launch(b); e != hipSuccess) return e;
+    }
+  return hipSuccess;
+}
 
 // ------------------------------------------------------------------------------------------------- orthogonal updates
 struct OrthoArgs {

@@ -210,7 +210,9 @@ MmPlan mm_f32_plan(int64_t M, int64_t N, int64_t K, int64_t batches) {
 hipError_t launch_mm_f32(const Product& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.P.bf16 != a.Q.bf16) return hipErrorInvalidValue;
-  return a.P.bf16 ? mm_f32_typed<bf16_t, bf16_t>(a, plan, partial, st) : mm_f32_typed<float, float>(a, plan, partial, st);
+  return in_blocks(a, plan.tile, plan.tile, 256, [&](const Product& b) {
+    return b.P.bf16 ? mm_f32_typed<bf16_t, bf16_t>(b, plan, partial, st) : mm_f32_typed<float, float>(b, plan, partial, st);
+  });
 }
 
 // --------------------------------------------------------------------------------------- elementwise pass of a gradient
@@ -219,12 +221,12 @@ namespace {
 constexpr int kBiasChunks = 256;
 
 // g = d_out f'(pre), written in the layer's type; column sums of the unrounded g over this workgroup's rows.
-// 32 lanes of four columns, eight rows at a time.  Bound by memory: 8192 x 4096, bfloat16, gelu 51 us for 201 MB (3.9 TB/s).
+// 32 lanes of four columns (`first` workgroups of them in earlier launches), eight rows at a time.  Bound by memory: 8192 x 4096, bfloat16, gelu 51 us for 201 MB (3.9 TB/s).
 template <class T>
-__global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_t rows_per, float* __restrict__ partial) {
+__global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_t first, int64_t rows_per, float* __restrict__ partial) {
   __shared__ float4 part[8][32];
   const int cl = threadIdx.x % 32, rl = threadIdx.x / 32;
-  const int64_t j = ((int64_t)blockIdx.x * 32 + cl) * 4;
+  const int64_t j = ((first + blockIdx.x) * 32 + cl) * 4;
   const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < a.n ? r0 + rows_per : a.n;
   const int valid = (int)(a.m - j < 0 ? 0 : a.m - j < 4 ? a.m - j : 4);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -257,10 +259,10 @@ __global__ __launch_bounds__(256) void layer_grad_kernel(LayerGradArgs a, int64_
 
 // Sixteen threads share a column: each adds every sixteenth chunk, then they are added in order.
 template <class T>
-__global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, int chunks, int64_t m, int accumulate, T* __restrict__ out) {
+__global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, int chunks, int64_t m, int64_t first, int accumulate, T* __restrict__ out) {
   __shared__ float part[16][17];
   const int c = threadIdx.x % 16, q = threadIdx.x / 16;
-  const int64_t j = (int64_t)blockIdx.x * 16 + c;
+  const int64_t j = (first + blockIdx.x) * 16 + c;
   float s = 0.0f;
   if (j < m) {
 #pragma unroll
@@ -290,16 +292,18 @@ hipError_t launch_layer_grad(const LayerGradArgs& a, float* partial, hipStream_t
   const int64_t per = bias_rows(a.n), chunks = (a.n + per - 1) / per;
   if (a.d_bias == nullptr) partial = nullptr;
   if (chunks > 0 && (a.dz != nullptr || partial != nullptr)) {
-    const dim3 grid((unsigned)(((a.dz != nullptr ? a.ld_dz : a.m) + 127) / 128), (unsigned)chunks);
-    if (a.bf16) layer_grad_kernel<bf16_t><<<grid, 256, 0, st>>>(a, per, partial);
-    else layer_grad_kernel<float><<<grid, 256, 0, st>>>(a, per, partial);
+    const hipError_t e = in_parts(((a.dz != nullptr ? a.ld_dz : a.m) + 127) / 128, 256, [&](int64_t first, unsigned blocks) {
+      const dim3 grid(blocks, (unsigned)chunks);
+      if (a.bf16) layer_grad_kernel<bf16_t><<<grid, 256, 0, st>>>(a, first, per, partial);
+      else layer_grad_kernel<float><<<grid, 256, 0, st>>>(a, first, per, partial);
+    });
+    if (e != hipSuccess) return e;
   }
-  if (a.d_bias != nullptr) {
-    const unsigned grid = (unsigned)((a.m + 15) / 16);
-    if (a.bf16) bias_sum_kernel<bf16_t><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (bf16_t*)a.d_bias);
-    else bias_sum_kernel<float><<<grid, 256, 0, st>>>(partial, (int)chunks, a.m, a.accumulate, (float*)a.d_bias);
-  }
-  return hipGetLastError();
+  if (a.d_bias == nullptr) return hipGetLastError();
+  return in_parts((a.m + 15) / 16, 256, [&](int64_t first, unsigned blocks) {
+    if (a.bf16) bias_sum_kernel<bf16_t><<<blocks, 256, 0, st>>>(partial, (int)chunks, a.m, first, a.accumulate, (bf16_t*)a.d_bias);
+    else bias_sum_kernel<float><<<blocks, 256, 0, st>>>(partial, (int)chunks, a.m, first, a.accumulate, (float*)a.d_bias);
+  });
 }
 
 }  // namespace ilargi

@@ -724,16 +724,21 @@ hipError_t launch_pack16(const void* src, int64_t ld, int64_t rows, int64_t cols
   if (rows == 0) return hipSuccess;
   int sh = ilog2_ceil((cols + 7) / 8);
   if (sh > 6) sh = 6;
-  pack16_kernel<<<(unsigned)(((rows << sh) + 255) / 256), 256, 0, st>>>((const bf16_t*)src, ld, rows, cols, (bf16_t*)dst, sh);
-  return hipGetLastError();
+  const int64_t ldp = (cols + 7) / 8 * 8;
+  return in_parts(((rows << sh) + 255) / 256, 256, [&](int64_t first, unsigned blocks) {
+    const int64_t row = first * (256 >> sh), some = (int64_t)blocks * (256 >> sh);
+    pack16_kernel<<<blocks, 256, 0, st>>>((const bf16_t*)src + row * ld, ld, rows - row < some ? rows - row : some, cols, (bf16_t*)dst + row * ldp, sh);
+  });
 }
 
 hipError_t launch_mm16(const Product16& a, const MmPlan& plan, float* partial, hipStream_t st) {
   if (a.M == 0 || a.N == 0 || a.batches == 0) return hipSuccess;
   if (a.kind == kMm16Bf16) {
     if (a.symmetric || a.batches != 1 || a.epi.mode != kEpiLinear || !a.epi.out_bf16) return hipErrorInvalidValue;
-    if (a.P.k_rows) return a.Q.k_rows ? mm16_order<true, true>(a, plan, partial, st) : hipErrorInvalidValue;
-    return a.Q.k_rows ? mm16_order<false, true>(a, plan, partial, st) : mm16_order<false, false>(a, plan, partial, st);
+    return in_blocks(a, plan.tile, plan.tile, plan.tile * 2, [&](const Product16& b) {
+      if (b.P.k_rows) return b.Q.k_rows ? mm16_order<true, true>(b, plan, partial, st) : hipErrorInvalidValue;
+      return b.Q.k_rows ? mm16_order<false, true>(b, plan, partial, st) : mm16_order<false, false>(b, plan, partial, st);
+    });
   }
   return a.P.k_rows ? hipErrorInvalidValue : mm16_pairs(a, plan, partial, st);
 }

@@ -136,7 +136,10 @@ hipError_t launch_mm_rows(const Product& a, const MmPlan& plan, float* partial, 
   if (a.M == 0 || a.N == 0) return hipSuccess;
   if (!mm_rows_takes(a.M, a.K, a.P.bf16) || a.P.k_rows || !a.Q.k_rows || a.batches != 1 || a.K < 1 || a.P.bf16 != a.Q.bf16)
     return hipErrorInvalidValue;
-  return a.P.bf16 ? mm_rows_typed<bf16_t>(a, plan, partial, st) : mm_rows_typed<float>(a, plan, partial, st);
+  const int64_t cols = kLanes * (a.P.bf16 ? ElemOf<bf16_t>::kVec : ElemOf<float>::kVec);
+  return in_blocks(a, a.M, cols, kThreads, [&](const Product& b) {
+    return b.P.bf16 ? mm_rows_typed<bf16_t>(b, plan, partial, st) : mm_rows_typed<float>(b, plan, partial, st);
+  });
 }
 
 }  // namespace ilargi

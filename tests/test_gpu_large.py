@@ -77,3 +77,49 @@ def test_rows_of_very_many_columns(il, accumulate):
     want = torch.stack([d[1] + d[4], torch.zeros_like(d[0]), d[0] + d[2]]) + (old if accumulate else 0.0)
     assert torch.equal(got, want)
     assert torch.equal(il.ilargi_embed(got, ids, 1.0)[:3], got[[2, 0, 2]])
+
+
+@pytest.mark.parametrize("n,k,m,dtype,gib", [
+    ((1 << 26) + 9, 257, 1, BF16, 80),        # operands laid out first, 64 lanes a row
+    ((1 << 30) + 3, 17, 1, F32, 90),          # blocks of 64 rows
+    ((1 << 31) - 1, 8, 8, BF16, 120),          # blocks of 128 rows on the 16-bit matrix cores
+])
+def test_layers_of_many_rows(il, n, k, m, dtype, gib):
+    """The same rows again and again: every chunk of the result is the first one."""
+    _room(gib)
+    chunk = 1 << 22
+    X = torch.empty(n, k, dtype=dtype, device="cuda")
+    first, W, bias = _ints((chunk, k), 6, 3).to(dtype), _ints((k, m), 7, 3).to(dtype), _ints((m,), 8, 3).to(dtype)
+    for a in range(0, n, chunk):
+        X[a: a + chunk] = first[: n - a]
+    out = torch.empty(n, m, dtype=dtype, device="cuda")
+    il.ilargi_linear(X, W, bias=bias, act="relu", out=out)
+    want = (first.float() @ W.float() + bias.float()).clamp(min=0).to(dtype)
+    for a in range(0, n, chunk):
+        assert torch.equal(out[a: a + chunk], want[: n - a]), a
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_row_of_many_outputs(il, dtype):
+    """2^28 + 3 columns of W, two of X; the gradient of the bias and of the inputs."""
+    _room(16)
+    k, m = 2, (1 << 28) + 3
+    X, W, bias = _ints((1, k), 9).to(dtype), _ints((k, m), 10).to(dtype), _ints((m,), 11).to(dtype)
+    out = il.ilargi_linear(X, W, bias=bias)
+    want = (X[0, 0].float() * W[0].float() + X[0, 1].float() * W[1].float() + bias.float()).to(dtype)
+    assert torch.equal(out[0], want)
+    d_bias = il.ilargi_linear_grad(W, torch.zeros(k, 1, dtype=dtype, device="cuda"), W[:1], d_X=None, d_W=None)[2]
+    assert torch.equal(d_bias, (W[0].float() + W[1].float()).to(dtype))
+
+
+def test_many_outputs_of_several_rows(il):
+    """2^30 + 1 columns for five rows: blocks of 64 side by side."""
+    _room(110)
+    n, k, m, chunk = 5, 17, (1 << 30) + 1, 1 << 22
+    X, first, W = _ints((n, k), 12, 3).float(), _ints((k, chunk), 13, 3).float(), torch.empty(k, m, device="cuda")
+    for a in range(0, m, chunk):
+        W[:, a: a + chunk] = first[:, : m - a]
+    out = il.ilargi_linear(X, W)
+    want = X @ first
+    for a in range(0, m, chunk):
+        assert torch.equal(out[:, a: a + chunk], want[:, : m - a]), a
