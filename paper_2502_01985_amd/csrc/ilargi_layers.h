@@ -304,6 +304,18 @@ struct OrthoArgs {
 };
 size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_ortho(const OrthoArgs& a, char* ws, hipStream_t st);
+// x times a factor that may be no float32 number, as the reciprocal of a norm may: a power of two first, then what is left of it.
+struct Factor2 {
+  float mantissa;
+  int exponent;
+};
+__device__ __forceinline__ Factor2 factor2(double f) {
+  int e;
+  const double m = frexp(f, &e);
+  return {(float)m, e};
+}
+__device__ __forceinline__ float times(float x, const Factor2& f) { return ldexpf(x, f.exponent) * f.mantissa; }
+
 // Small matrices, whose iteration stays in pairs of float16 times these units.
 bool ortho_one_takes(int64_t rows, int64_t cols);
 hipError_t launch_ortho_one(const OrthoArgs& a, float unit, float unit_b, hipStream_t st);

@@ -47,13 +47,13 @@ template <class T, bool PAIRS>
 __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const double* __restrict__ parts, void* __restrict__ out, int64_t rows_x, int64_t ld_x,
                                                          int tiles_c) {
   __shared__ float tile[32][33];
-  __shared__ float scale;
+  __shared__ Factor2 scale;
   const int64_t b = blockIdx.y;
   if (threadIdx.x < 64) {
     const double* p = parts + b * kNormParts + threadIdx.x;
     double s = (p[0] + p[64]) + (p[128] + p[192]);
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
-    if (threadIdx.x == 0) scale = (float)(1.0 / (sqrt(s) + (double)a.eps));
+    if (threadIdx.x == 0) scale = factor2((PAIRS ? (double)kUnit : 1.0) / (sqrt(s) + (double)a.eps));
   }
   const T* G = (const T*)a.G + b * a.batch_g;
   const bool flip = a.rows > a.cols;
@@ -70,8 +70,8 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
   for (int q = 0; q < 32; q += 8) {
     if (y0 + y + q >= rows_x || x0 + x >= ld_x) continue;
     const int64_t at = (b * rows_x + y0 + y + q) * ld_x + x0 + x;
-    const float v = (flip ? tile[x][y + q] : tile[y + q][x]) * scale;
-    if constexpr (PAIRS) pair_store((_Float16*)out, at, a.batch * rows_x * ld_x, v * kUnit);
+    const float v = times(flip ? tile[x][y + q] : tile[y + q][x], scale);
+    if constexpr (PAIRS) pair_store((_Float16*)out, at, a.batch * rows_x * ld_x, v);
     else ((float*)out)[at] = v;
   }
 }

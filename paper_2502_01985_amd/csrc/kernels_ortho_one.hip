@@ -88,10 +88,10 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
   __syncthreads();
   s = 0.0;
   for (int w = 0; w < kThreads / 64; ++w) s += wsum[w];
-  const float scale = (float)((double)a.unit / (sqrt(s) + (double)o.eps));
+  const Factor2 scale = factor2((double)a.unit / (sqrt(s) + (double)o.eps));
   for (int r = wave; r < rows; r += kThreads / 64)
     for (int c = lane; c < cols; c += 64) {
-      const float v = (float)G[r * o.ld_g + c] * scale;
+      const float v = times((float)G[r * o.ld_g + c], scale);
       const int at = flip ? c * ldx + r : r * ldx + c;
       const _Float16 h = (_Float16)v;
       xh[at] = h;
