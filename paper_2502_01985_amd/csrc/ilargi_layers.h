@@ -185,8 +185,9 @@ enum { kEpiLinear = 0, kEpiScale = 1 };
 struct Epilogue {
   int mode;
   // kEpiLinear: z = acc + bias[j] kept in `pre`, out = f(z) + src
-  // kEpiScale: out = s0 acc + s1 src + s2 base; `flip` writes out(j, i), with `base` laid out as `out`
+  // kEpiScale: out = (s0 acc + s1 src) by[b] + s2 base (by: NULL for 1); `flip` writes out(j, i), with `base` laid out as `out`
   float s0, s1, s2;
+  const float* by;
   const void* base;
   const void* bias;
   const void* src;
@@ -317,8 +318,19 @@ __device__ __forceinline__ Factor2 factor2(double f) {
 __device__ __forceinline__ float times(float x, const Factor2& f) { return ldexpf(x, f.exponent) * f.mantissa; }
 
 // Small matrices, whose iteration stays in pairs of float16 times these units.
+// X_t of step t is held times 2^e besides, the largest e from 0 to 126 for which grow^t |X_0| 2^e <= 1 (`grow`: most that a step
+// multiplies a singular value by): X is as small as |G| / eps where the norm is far below eps.  Logarithms to base 2, of
+// |X_0| = norm / (norm + eps) and of grow; 126 where a logarithm is no number.
+__device__ __forceinline__ float lg_of(double v) {
+  int e;
+  const float m = (float)frexp(v, &e);
+  return (float)e + __builtin_amdgcn_logf(m);
+}
+__device__ __forceinline__ int ortho_exponent(float lg_norm, float lg_grow, int t) {
+  return (int)fmaxf(0.0f, fminf(126.0f, floorf(-fmaf((float)t, lg_grow, lg_norm))));
+}
 bool ortho_one_takes(int64_t rows, int64_t cols);
-hipError_t launch_ortho_one(const OrthoArgs& a, float unit, float unit_b, hipStream_t st);
+hipError_t launch_ortho_one(const OrthoArgs& a, float unit, float unit_b, float lg_grow, hipStream_t st);
 
 }  // namespace ilargi
 #endif

@@ -149,11 +149,11 @@ __global__ __launch_bounds__(256) void mm_f32_kernel(Product a, int tm, int tn, 
     } else if (!a.epi.flip) {
 #pragma unroll 1
       for (int q = 0; q < 32 / kRows; q += 4)
-        epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + (q + u) * kRows + rr; *jj = j; }, [&](int u) { return sums(q + u); });
+        epilogue_quads<4>(a.epi, 1.0f, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + (q + u) * kRows + rr; *jj = j; }, [&](int u) { return sums(q + u); });
     } else {                                           // written along j's rows, which run over i
 #pragma unroll 1
       for (int q = 0; q < 4 * F; q += 4)
-        epilogue_quads<4>(a.epi, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + r; *jj = j0 + wj + 8 * (q + u) + 4 * h; },
+        epilogue_quads<4>(a.epi, 1.0f, b, a.M, a.N, bias, [&](int u, int64_t* i, int64_t* jj) { *i = ri + r; *jj = j0 + wj + 8 * (q + u) + 4 * h; },
                           [&](int u) { return *reinterpret_cast<const float4*>(mine + r * kPad + 8 * (q + u) + 4 * h); });
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -260,8 +260,8 @@ __device__ __forceinline__ void store_layer(const Product16& a, float* __restric
 
 // The same of a product of pairs, scaled and added to `src`, into planes, float32 or bfloat16.
 template <int TM, int FN>
-__device__ __forceinline__ void store_sums(const Product16& a, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t b, int64_t i0,
-                                           int64_t j0, bool mirrored) {
+__device__ __forceinline__ void store_sums(const Product16& a, float by, float* __restrict__ partial, char* lds, const f32x4 (&acc)[TM / 16][FN], int64_t b,
+                                           int64_t i0, int64_t j0, bool mirrored) {
   constexpr int kRows = TM < 64 ? TM : 64, kQ = kRows / 4;      // rows of a pass, and its turns of 64 quads
   const int lane = threadIdx.x % 64;
   float* mine = (float*)lds + threadIdx.x / 64 * kRows * kOutPad;
@@ -296,12 +296,12 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
             if (valid == 0) continue;
             const float4 t = row(r, c);
             float v[4] = {t.x, t.y, t.z, t.w};
-            epilogue4<false>(a.epi, b, ri + r, j0 + c, valid, none, SrcQuad{}, v);
+            epilogue4<false>(a.epi, by, b, ri + r, j0 + c, valid, none, SrcQuad{}, v);
           }
         } else {
 #pragma unroll 1
           for (int q = 0; q < kQ; q += 4)
-            epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
+            epilogue_quads<4>(a.epi, by, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + 4 * (q + u) + (lane >> 4); *j = j0 + c; },
                               [&](int u) { return row(4 * (q + u) + (lane >> 4), c); });
         }
       } else {                                         // written along j's rows, which run over i
@@ -309,7 +309,7 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
         const int r = lane % kRows, s = lane / kRows;
 #pragma unroll 1
         for (int q = 0; q < kQ; q += 4)
-          epilogue_quads<4>(a.epi, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + r; *j = j0 + 4 * ((q + u) * kSide + s); },
+          epilogue_quads<4>(a.epi, by, b, a.M, a.N, none, [&](int u, int64_t* i, int64_t* j) { *i = ri + r; *j = j0 + 4 * ((q + u) * kSide + s); },
                             [&](int u) { return row(r, 4 * ((q + u) * kSide + s)); });
       }
       if (mirrored) {                                // the sums of a symmetric result at their places below the diagonal
@@ -317,7 +317,7 @@ __device__ __forceinline__ void store_sums(const Product16& a, float* __restrict
         const int ci = lane % kAcross * 4, rj = lane / kAcross;
 #pragma unroll 1
         for (int q = 0; q < kQ; q += 4)
-          epilogue_quads<4>(a.epi, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + kDown * (q + u) + rj; *j = ri + ci; },
+          epilogue_quads<4>(a.epi, by, b, a.N, a.M, none, [&](int u, int64_t* i, int64_t* j) { *i = j0 + kDown * (q + u) + rj; *j = ri + ci; },
                             [&](int u) {
                               const float* m = mine + ci * kOutPad + kDown * (q + u) + rj;
                               return make_float4(m[0], m[kOutPad], m[2 * kOutPad], m[3 * kOutPad]);
@@ -439,6 +439,7 @@ __global__ __launch_bounds__(512, 1) void mm16_pairs_kernel(Product16 a, int tm,
   if (a.symmetric) upper_block(blockIdx.x, tn, &ti, &tj);
   else block_of(blockIdx.x, tm, tn, &ti, &tj);
   const int64_t i0 = (int64_t)ti * kB, j0 = (int64_t)tj * kB, b = blockIdx.y;
+  const float by = a.epi.by != nullptr ? a.epi.by[b] : 1.0f;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4, wi = (wave % 4 / 2) * 64, wj = (wave % 2) * 64;
   const int64_t step_q = QK ? kBK * a.Q.ld * 2 : kBK * 2;
   const int first = (int)blockIdx.z * share, ks_all = (int)((a.K + kBK - 1) / kBK), steps = ks_all - first < share ? ks_all - first : share;
@@ -544,7 +545,7 @@ __global__ __launch_bounds__(512, 1) void mm16_pairs_kernel(Product16 a, int tm,
       const f32x4 other = *reinterpret_cast<const f32x4*>(taken + at(x, y));
       sum[x][y] = half ? acc[2 + x][y] + other : acc[x][y] + other;
     }
-  store_sums<32, FN>(a, partial, lds_all, sum, b, i0 + wi + 32 * half, j0 + wj, a.symmetric && ti != tj);
+  store_sums<32, FN>(a, by, partial, lds_all, sum, b, i0 + wi + 32 * half, j0 + wj, a.symmetric && ti != tj);
 }
 
 struct Join {
@@ -580,12 +581,13 @@ __global__ __launch_bounds__(256) void mm_join_rows_kernel(Join a, int splits, c
   if (i >= a.M) return;
   const int64_t ldp = quads * 4;
   const int valid = quad_valid(i, j, a.M, a.N);
+  const float by = a.epi.by != nullptr ? a.epi.by[b] : 1.0f;
   const SrcQuad raw = epilogue_ask(a.epi, b, i, j, valid);
   float bias[4];
   epilogue_bias(a.epi, j, valid, bias);
   const f32x4 s = add_shares(partial + (b * a.M + i) * ldp + j, a.batches * a.M * ldp, splits);
   float v[4] = {s[0], s[1], s[2], s[3]};
-  epilogue4(a.epi, b, i, j, valid, bias, raw, v);
+  epilogue4(a.epi, by, b, i, j, valid, bias, raw, v);
 }
 
 // The same for results that are written along j too, 32 x 32 sums a workgroup: those on and above the diagonal of a symmetric
@@ -597,7 +599,7 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits
   else { ti = blockIdx.x / tn; tj = blockIdx.x % tn; }
   const int64_t b = blockIdx.y, i0 = (int64_t)ti * 32, j0 = (int64_t)tj * 32, ldp = (a.N + 3) / 4 * 4;
   const int r = threadIdx.x / 8, c = (threadIdx.x % 8) * 4;
-  const float none[4] = {0.f, 0.f, 0.f, 0.f};
+  const float none[4] = {0.f, 0.f, 0.f, 0.f}, by = a.epi.by != nullptr ? a.epi.by[b] : 1.0f;
   const bool turned = a.epi.flip || (a.symmetric && ti != tj);
   // where this thread's quad goes, and where that of the turned tile does
   const int x = threadIdx.x % 32, y = threadIdx.x / 32 * 4;
@@ -608,7 +610,7 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits
   if (valid > 0) s = add_shares(partial + (b * a.M + i0 + r) * ldp + j0 + c, a.batches * a.M * ldp, splits);
   if (!a.epi.flip && valid > 0) {
     float v[4] = {s[0], s[1], s[2], s[3]};
-    epilogue4(a.epi, b, i0 + r, j0 + c, valid, none, raw, v);
+    epilogue4(a.epi, by, b, i0 + r, j0 + c, valid, none, raw, v);
   }
   if (!turned) return;
   *reinterpret_cast<f32x4*>(&tile[r][c]) = s;
@@ -617,7 +619,7 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Join a, int tn, int splits
   float v[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) v[q] = a.epi.flip ? tile[x][y + q] : tile[c + q][r];
-  epilogue4(a.epi, b, ti_row, ti_col, turned_valid, none, turned_raw, v);
+  epilogue4(a.epi, by, b, ti_row, ti_col, turned_valid, none, turned_raw, v);
 }
 
 int64_t blocks_of(int64_t M, int64_t N, int tile, int symmetric) {

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void mm_rows_kernel(Product a, int64_t sh
   }
   float bias[4];
   epilogue_bias(a.epi, col, left, bias);
-  epilogue4(a.epi, 0, r, col, left, bias, raw, v);
+  epilogue4(a.epi, 1.0f, 0, r, col, left, bias, raw, v);
 }
 
 template <class T>

@@ -8,16 +8,19 @@
 // which with bfloat16's own 1.7e-3 is too much.  Bound by the matrix cores and, below about 1000, by the chain of launches: 2048 x
 // 2048, float32, 778 us (221 TFLOP/s of the formula's operations, those of symmetric products counted once, and three times that in
 // products); 1024 x 4096, bfloat16, 400 us.
+#include <math.h>
+
 #include "mm_epilogue.h"
 
 namespace ilargi {
 
 namespace {
 
-constexpr int kNormParts = 256;
+constexpr int kNormParts = 256, kMostSteps = 100;
 
-// The pairs hold kUnit X and kUnit A, and B times a power of two that brings it to at most 60000 (float16 ends at 65504): their low
-// planes then count in 1.5e-11 of X and A.
+// The pairs hold kUnit 2^e X (ortho_exponent) and kUnit A, and B times a power of two that brings it to at most 60000 (float16 ends at
+// 65504): their low planes then count in 1.5e-11 of A and of an X of norm 1.  (What A and B lose of a small X is small against the
+// identity that a X stands for.)
 constexpr float kUnit = 4096.0f;
 
 // Sums of squares of a share of one matrix's rows, in 64 bits: the norm neither overflows nor loses small entries.
@@ -42,10 +45,11 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a, double* __
 }
 
 // X (short side x long side) = G or its transpose over the norm, 32 x 32 tiles through LDS; zeros up to `rows_x` x `ld_x`.
-// In pairs of float16 planes, X is held times kUnit.
+// In pairs of float16 planes, X is held times kUnit 2^e; then `by` receives, for every step and matrix, 2^-2e of X X^T and behind them the
+// change of 2^e to the next step, of the last step to 1.
 template <class T, bool PAIRS>
 __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const double* __restrict__ parts, void* __restrict__ out, int64_t rows_x, int64_t ld_x,
-                                                         int tiles_c) {
+                                                         int tiles_c, float lg_grow, float* __restrict__ by) {
   __shared__ float tile[32][33];
   __shared__ Factor2 scale;
   const int64_t b = blockIdx.y;
@@ -53,7 +57,15 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
     const double* p = parts + b * kNormParts + threadIdx.x;
     double s = (p[0] + p[64]) + (p[128] + p[192]);
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
-    if (threadIdx.x == 0) scale = factor2((PAIRS ? (double)kUnit : 1.0) / (sqrt(s) + (double)a.eps));
+    const double norm = sqrt(s), one = 1.0 / (norm + (double)a.eps);
+    const float lg_norm = PAIRS ? lg_of(norm * one) : 0.0f;
+    if (threadIdx.x == 0) scale = factor2(PAIRS ? ldexp(one * (double)kUnit, ortho_exponent(lg_norm, lg_grow, 0)) : one);
+    if (PAIRS && blockIdx.x == 0)
+      for (int t = threadIdx.x; t < a.steps; t += 64) {
+        const int up = ortho_exponent(lg_norm, lg_grow, t), then = t + 1 < a.steps ? ortho_exponent(lg_norm, lg_grow, t + 1) : 0;
+        by[(2 * t) * a.batch + b] = ldexpf(1.0f, -2 * up);
+        by[(2 * t + 1) * a.batch + b] = ldexpf(1.0f, then - up);
+      }
   }
   const T* G = (const T*)a.G + b * a.batch_g;
   const bool flip = a.rows > a.cols;
@@ -79,33 +91,42 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoArgs a, const doub
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Whether the iteration stays where pairs of float16 hold it: some interval [0, R], R <= 2, that holds the first singular values (at
-// most 1) is mapped into [-R, R] by s (a + b s^2 + c s^4).  Then the entries of X are at most R, of A R^2, and of B |b| R^2 + |c| R^4,
-// which gives B's unit; 0: it does not stay.
-float unit_of_b(const float* coef) {
+// most 1) is mapped into [-R, R] by p(s) = s (a + b s^2 + c s^4).  Then the entries of X are at most R, of A R^2, and of B |b| R^2 +
+// |c| R^4, which gives B's unit (0: it does not stay); and a step multiplies a singular value by at most `grow`.
+struct PairRange {
+  float unit_b;
+  double grow;
+};
+PairRange pair_range(const float* coef) {
   const double a = coef[0], b = coef[1], c = coef[2];
+  auto size = [](double v) { return v < 0 ? -v : v; };
+  auto factor = [&](double x) { return a + b * x + c * x * x; };                  // p(s) / s at s^2 = x
+  // where p and p / s have their extremes besides the ends: 5 c x^2 + 3 b x + a = 0, 2 c x + b = 0
+  const double root = sqrt(9 * b * b - 20 * a * c);
+  const double turns[3] = {c != 0 ? (-3 * b + root) / (10 * c) : -a / (3 * b), c != 0 ? (-3 * b - root) / (10 * c) : 0.0, -b / (2 * c)};
   for (int q = 0; q <= 40; ++q) {
     const double R = 1.0 + 0.025 * q;
-    double top = 0.0;
-    bool number = true;
-    for (int k = 0; k <= 500; ++k) {
-      const double s = R * k / 500.0, v = s * (a + b * s * s + c * s * s * s * s);
-      if (!(v == v)) number = false;
-      if (v > top) top = v;
-      if (-v > top) top = -v;
+    double top = size(R * factor(R * R)), grow = size(factor(R * R));
+    if (!(grow >= size(a))) grow = size(a);
+    for (double x : turns) {
+      if (!(x > 0 && x < R * R)) continue;
+      const double f = size(factor(x));
+      if (sqrt(x) * f > top) top = sqrt(x) * f;
+      if (f > grow) grow = f;
     }
-    if (!number || top > R) continue;
-    const double most = (b < 0 ? -b : b) * R * R + (c < 0 ? -c : c) * R * R * R * R;
+    if (!(top <= R)) continue;
+    const double most = size(b) * R * R + size(c) * R * R * R * R;
     double unit = 4096.0;
     while (unit > 1.0 && unit * most > 60000.0) unit /= 2.0;
-    return unit * most <= 60000.0 ? (float)unit : 0.0f;
+    return {unit * most <= 60000.0 ? (float)unit : 0.0f, grow};
   }
-  return 0.0f;
+  return {0.0f, 0.0};
 }
 
 struct OrthoLayout {
   int64_t s, l, sp, lp;                 // short and long side, and the same up to a multiple of 8
   MmPlan gram, square, apply;
-  size_t x[2], A, B, partial, total;
+  size_t by, x[2], A, B, partial, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
   OrthoLayout o{};
@@ -118,6 +139,7 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
   o.apply = mm16_plan(o.sp, o.lp, o.sp, batch, kMm16Pairs, 0);
   size_t at = up256((size_t)batch * kNormParts * 8);
   auto take = [&at](size_t bytes) { const size_t p = at; at += up256(bytes); return p; };
+  o.by = take(4 * 2 * (size_t)kMostSteps * (size_t)batch);
   o.x[0] = take(4 * (size_t)(batch * o.sp * o.lp));
   o.x[1] = take(4 * (size_t)(batch * o.sp * o.lp));
   o.A = take(4 * (size_t)(batch * o.sp * o.sp));
@@ -154,6 +176,7 @@ hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, float unit_b,
     p.Q = p.P;
     p.epi.mode = kEpiScale;
     p.epi.s0 = 1.0f / kUnit;
+    p.epi.by = (const float*)(ws + o.by) + 2 * t * a.batch;
     p.epi.out = A; p.epi.ld_out = o.sp; p.epi.batch_out = o.sp * o.sp; p.epi.out_plane = pa;
     if (hipError_t e = launch_mm16(p, o.gram, partial, st); e != hipSuccess) return e;
     p.K = o.sp;
@@ -161,6 +184,7 @@ hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, float unit_b,
     p.Q = p.P;
     p.epi.s0 = a.coef[2] * unit_b / (kUnit * kUnit); p.epi.s1 = a.coef[1] * unit_b / kUnit;
     p.epi.src = A; p.epi.ld_src = o.sp; p.epi.batch_src = o.sp * o.sp; p.epi.src_plane = pa;
+    p.epi.by = nullptr;
     p.epi.out = B;
     if (hipError_t e = launch_mm16(p, o.square, partial, st); e != hipSuccess) return e;
     p.N = o.lp; p.symmetric = 0;
@@ -168,6 +192,7 @@ hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, float unit_b,
     p.Q = {x, o.lp, 1, o.sp * o.lp, px, o.lp};
     p.epi.s0 = 1.0f / unit_b; p.epi.s1 = a.coef[0];
     p.epi.src = x; p.epi.ld_src = o.lp; p.epi.batch_src = o.sp * o.lp; p.epi.src_plane = px;
+    p.epi.by = (const float*)(ws + o.by) + (2 * t + 1) * a.batch;
     p.epi.out = next; p.epi.ld_out = o.lp; p.epi.batch_out = o.sp * o.lp; p.epi.out_plane = px;
     if (t + 1 == a.steps) {
       finish(a, kUnit, &p.epi);
@@ -213,17 +238,18 @@ template <class T>
 hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   const OrthoLayout o = ortho_layout(a.batch, a.rows, a.cols);
   double* parts = (double*)ws;
-  const float unit_b = unit_of_b(a.coef);
-  const bool pairs = unit_b > 0.0f;
-  if (pairs && ortho_one_takes(a.rows, a.cols)) return launch_ortho_one(a, kUnit, unit_b, st);
+  const PairRange range = pair_range(a.coef);
+  const bool pairs = range.unit_b > 0.0f;
+  const float lg_grow = pairs && range.grow > 1e-38 ? (float)log2(range.grow) : -126.0f;
+  if (pairs && ortho_one_takes(a.rows, a.cols)) return launch_ortho_one(a, kUnit, range.unit_b, lg_grow, st);
   const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;
   const int tc = (int)((ld_x + 31) / 32);
   const dim3 tiles((unsigned)((rows_x + 31) / 32 * tc), (unsigned)a.batch), norms(kNormParts, (unsigned)a.batch);
   ortho_norm_kernel<T><<<norms, 256, 0, st>>>(a, parts);
-  if (pairs) ortho_load_kernel<T, true><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
-  else ortho_load_kernel<T, false><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc);
+  if (pairs) ortho_load_kernel<T, true><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc, lg_grow, (float*)(ws + o.by));
+  else ortho_load_kernel<T, false><<<tiles, 256, 0, st>>>(a, parts, ws + o.x[0], rows_x, ld_x, tc, 0.0f, nullptr);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return pairs ? iterate_pairs(a, o, unit_b, ws, st) : iterate_f32(a, o, ws, st);
+  return pairs ? iterate_pairs(a, o, range.unit_b, ws, st) : iterate_f32(a, o, ws, st);
 }
 
 }  // namespace

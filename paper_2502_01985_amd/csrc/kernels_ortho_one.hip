@@ -22,7 +22,7 @@ constexpr int kS = 64, kLdA = kS + 8, kMostLong = 448, kThreads = 1024, kSide = 
 
 struct OneArgs {
   OrthoArgs o;
-  float unit, unit_b;
+  float unit, unit_b, lg_grow;
   int lp;              // long side up to a multiple of 32
 };
 
@@ -88,7 +88,10 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
   __syncthreads();
   s = 0.0;
   for (int w = 0; w < kThreads / 64; ++w) s += wsum[w];
-  const Factor2 scale = factor2((double)a.unit / (sqrt(s) + (double)o.eps));
+  const double norm = sqrt(s), one = 1.0 / (norm + (double)o.eps);
+  const float lg_norm = lg_of(norm * one);
+  int up = ortho_exponent(lg_norm, a.lg_grow, 0);             // X is held times unit 2^up
+  const Factor2 scale = factor2(ldexp(one * (double)a.unit, up));
   for (int r = wave; r < rows; r += kThreads / 64)
     for (int c = lane; c < cols; c += 64) {
       const float v = times((float)G[r * o.ld_g + c], scale);
@@ -104,6 +107,9 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
     // (the places in LDS are worked out anew in every step: kept from one to the next they do not fit the registers)
     int r16 = lane & 15;
     asm volatile("" : "+v"(r16));
+    const int then = step + 1 < o.steps ? ortho_exponent(lg_norm, a.lg_grow, step + 1) : 0;
+    const float by_a = ldexpf(1.0f / a.unit, -2 * up), by_x = ldexpf(1.0f, then - up);
+    up = then;
 #pragma unroll
     for (int u = 0; u < 4 / kSide; ++u) {
       const int bj = (wave / 4 + kSide * u) * 16;
@@ -112,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
         f.add(row_piece(xh + (bj + r16) * ldx + k + g8), row_piece(xl + (bj + r16) * ldx + k + g8), row_piece(xh + (bi + r16) * ldx + k + g8),
               row_piece(xl + (bi + r16) * ldx + k + g8));
       const int at = (bi + r16) * kLdA + bj + g4;
-      put_pair(ah + at, al + at, f.sum() * (1.0f / a.unit));
+      put_pair(ah + at, al + at, f.sum() * by_a);
     }
     __syncthreads();
 #pragma unroll
@@ -149,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
       const int at = (bi + r16) * ldx + c + g4;
       const f32x4 v = get_pair(xh + at, xl + at), w = f.sum();
 #pragma unroll
-      for (int q = 0; q < 4; ++q) next[u][q] = fmaf(1.0f / a.unit_b, w[q], o.coef[0] * v[q]);
+      for (int q = 0; q < 4; ++q) next[u][q] = fmaf(1.0f / a.unit_b, w[q], o.coef[0] * v[q]) * by_x;
       __builtin_amdgcn_sched_barrier(0);                      // (all blocks' reads at once do not fit the registers)
     }
     if (step + 1 < o.steps) {
@@ -187,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void ortho_one_kernel(OneArgs a) {
     if (i >= S) continue;
     const f32x4 w = *reinterpret_cast<const f32x4*>(last + i * ldx + j);
     float v[4] = {w[0], w[1], w[2], w[3]};
-    epilogue4(e, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, SrcQuad{}, v);
+    epilogue4(e, 1.0f, blockIdx.x, i, j, L - j < 4 ? L - j : 4, none, SrcQuad{}, v);
   }
 }
 
@@ -199,10 +205,10 @@ bool ortho_one_takes(int64_t rows, int64_t cols) {
   return s <= kS && l <= kMostLong;
 }
 
-hipError_t launch_ortho_one(const OrthoArgs& o, float unit, float unit_b, hipStream_t st) {
+hipError_t launch_ortho_one(const OrthoArgs& o, float unit, float unit_b, float lg_grow, hipStream_t st) {
   if (!ortho_one_takes(o.rows, o.cols)) return hipErrorInvalidValue;
   const int64_t l = o.rows < o.cols ? o.cols : o.rows;
-  const OneArgs a{o, unit, unit_b, (int)((l + 31) / 32 * 32)};
+  const OneArgs a{o, unit, unit_b, lg_grow, (int)((l + 31) / 32 * 32)};
   const size_t bytes = 2 * (2 * (size_t)kS * (size_t)(a.lp + 8) + 4 * (size_t)kS * kLdA);
   const void* kernel = o.g_bf16 ? (const void*)ortho_one_kernel<bf16_t> : (const void*)ortho_one_kernel<float>;
   if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); e != hipSuccess) return e;

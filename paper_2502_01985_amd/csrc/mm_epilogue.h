@@ -77,9 +77,9 @@ __device__ __forceinline__ void epilogue_src(const Epilogue& e, const SrcQuad& r
 }
 
 // Columns j .. j + valid of row i of matrix b of the batch: `v` are the sums, `raw` what epilogue_ask gave.
-// (SRC false: the caller knows that there is no src.)
+// `by` is by[b], which kernels that have one ask for at their start.  (SRC false: the caller knows that there is no src.)
 template <bool SRC = true>
-__device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t i, int64_t j, int valid, const float (&bias)[4], const SrcQuad& raw,
+__device__ __forceinline__ void epilogue4(const Epilogue& e, float by, int64_t b, int64_t i, int64_t j, int valid, const float (&bias)[4], const SrcQuad& raw,
                                           float (&v)[4]) {
   float t[4] = {0.f, 0.f, 0.f, 0.f};
   if (SRC && e.src != nullptr) epilogue_src(e, raw, t);
@@ -96,7 +96,7 @@ __device__ __forceinline__ void epilogue4(const Epilogue& e, int64_t b, int64_t 
     return;
   }
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = SRC && e.src != nullptr ? fmaf(e.s1, t[q], e.s0 * v[q]) : e.s0 * v[q];
+  for (int q = 0; q < 4; ++q) v[q] = (SRC && e.src != nullptr ? fmaf(e.s1, t[q], e.s0 * v[q]) : e.s0 * v[q]) * by;
   if (e.flip) {
     for (int q = 0; q < valid && q < 4; ++q) {
       const int64_t at = b * e.batch_out + (j + q) * e.ld_out + i;
@@ -143,7 +143,7 @@ __device__ __forceinline__ int quad_valid(int64_t i, int64_t j, int64_t M, int64
 
 // U quads of one column block: place(q, &i, &j) says where the q-th lies, sum(q) gives its four sums.
 template <int U, class Place, class Sum>
-__device__ __forceinline__ void epilogue_quads(const Epilogue& e, int64_t b, int64_t M, int64_t N, const float (&bias)[4], Place place, Sum sum) {
+__device__ __forceinline__ void epilogue_quads(const Epilogue& e, float by, int64_t b, int64_t M, int64_t N, const float (&bias)[4], Place place, Sum sum) {
   SrcQuad raw[U];
   int64_t i, j;
 #pragma unroll
@@ -158,7 +158,7 @@ __device__ __forceinline__ void epilogue_quads(const Epilogue& e, int64_t b, int
     if (valid == 0) continue;
     const float4 t = sum(u);
     float v[4] = {t.x, t.y, t.z, t.w};
-    epilogue4(e, b, i, j, valid, bias, raw[u], v);
+    epilogue4(e, by, b, i, j, valid, bias, raw[u], v);
   }
 }
 

@@ -66,3 +66,47 @@ def test_norms_at_the_ends_of_float32(il, shape, norm):
     assert bool(torch.isfinite(G).all())
     for steps in (1, 5):
         assert _far(il.ilargi_orthogonalize(G, steps=steps, eps=0.0), _exact(G, steps, eps=0.0)) <= _tol(*shape, steps)
+
+
+@pytest.mark.parametrize("shape", [(64, 220), (220, 60), (1, 1), (512, 512), (300, 1000), (777, 130), (130, 2500)])
+@pytest.mark.parametrize("norm,eps", [(1e-7, 1e-7), (1e-9, 1e-7), (1e-11, 1e-7), (1e-13, 1e-7), (1e-16, 1e-7), (1e-25, 1e-7), (1e-8, 1e-3), (1.0, 1.0),
+                                      (1e-3, 1e3), (1e-30, 1.0)])
+def test_norms_below_eps(il, shape, norm, eps):
+    """X = G / (|G| + eps) is as small as |G| / eps, and the result a^T times that: not less exact for it."""
+    G = _of_norm((1, *shape), norm, _gen(shape[0]))
+    for steps in (1, 2, 5):
+        assert _far(il.ilargi_orthogonalize(G, steps=steps, eps=eps), _exact(G, steps, eps=eps)) <= _tol(*shape, steps)
+    assert _far(il.ilargi_orthogonalize(G, eps=eps, out_dtype=BF16), _exact(G, 5, eps=eps)) <= _tol(*shape, 5, BF16)
+    assert _far(il.ilargi_orthogonalize(G.bfloat16(), eps=eps, out_dtype=F32), _exact(G.bfloat16(), 5, eps=eps)) <= _tol(*shape, 5)
+
+
+@pytest.mark.parametrize("shape", [(64, 220), (220, 60), (130, 257), (512, 300)])
+def test_a_batch_of_very_different_norms(il, shape):
+    """Every matrix by its own norm; a zero one among them, and weights that are updated in place."""
+    norms = (1.0, 1e-12, 0.0, 1e-7, 1e-20, 1e5)
+    G = torch.cat([_of_norm((1, *shape), v, _gen(q)) for q, v in enumerate(norms)])
+    G[2] = 0.0
+    out, want = il.ilargi_orthogonalize(G), _exact(G, 5)
+    for q, v in enumerate(norms):
+        assert bool((out[q] == 0).all()) if v == 0.0 else _far(out[q], want[q]) <= _tol(*shape, 5)
+    W = torch.randn(G.shape, generator=_gen(9), device="cuda") * want.float().abs().amax((1, 2), keepdim=True)
+    far = 0.99 * W.double() - 0.3 * want
+    il.ilargi_orthogonalize(G, out=W, base=W, alpha=-0.3, beta=0.99)
+    for q, v in enumerate(norms):
+        assert bool((W[q] == 0).all()) if v == 0.0 else _far(W[q], far[q]) <= _tol(*shape, 5)
+
+
+@pytest.mark.parametrize("coef", [(1.5, -0.5, 0.0), (0.1, 0.0, 0.0), (0.5, 0.25, 0.0)])
+def test_other_coefficients_below_eps(il, coef):
+    """Iterations that grow slowly, or shrink what they are given: T roundings, none of them amplified beyond the result."""
+    for shape in ((60, 220), (300, 200)):
+        for norm in (1e-12, 1e-4, 1.0):
+            G = _of_norm((1, *shape), norm, _gen(5))
+            for steps in (3, 12):
+                want = _exact(G, steps, coef)
+                assert _far(il.ilargi_orthogonalize(G, steps=steps, coef=coef), want) <= 2 * steps * 3 * (math.sqrt(max(shape)) + 4) * U32
+
+
+def test_coefficients_that_leave_nothing(il):
+    for shape in ((60, 40), (200, 300)):
+        assert bool((il.ilargi_orthogonalize(torch.randn(shape, generator=_gen(6), device="cuda"), steps=3, coef=(0.0, 0.0, 0.0)) == 0).all())
