@@ -239,7 +239,7 @@ hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   const OrthoLayout o = ortho_layout(a.batch, a.rows, a.cols);
   double* parts = (double*)ws;
   const PairRange range = pair_range(a.coef);
-  const bool pairs = range.unit_b > 0.0f;
+  const bool pairs = range.unit_b > 0.0f && a.eps >= 0.0f;       // (below 0, the first singular values may be beyond 1)
   const float lg_grow = pairs && range.grow > 1e-38 ? (float)log2(range.grow) : -126.0f;
   if (pairs && ortho_one_takes(a.rows, a.cols)) return launch_ortho_one(a, kUnit, range.unit_b, lg_grow, st);
   const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;

@@ -110,3 +110,13 @@ def test_other_coefficients_below_eps(il, coef):
 def test_coefficients_that_leave_nothing(il):
     for shape in ((60, 40), (200, 300)):
         assert bool((il.ilargi_orthogonalize(torch.randn(shape, generator=_gen(6), device="cuda"), steps=3, coef=(0.0, 0.0, 0.0)) == 0).all())
+
+
+def test_negative_eps(il):
+    """eps < 0 brings X beyond norm 1: |G| = 1, eps = -0.98 gives X of norm 50."""
+    for shape in ((1, 1), (40, 64), (100, 130)):
+        G = _of_norm((1, *shape), 1.0, _gen(shape[0]))
+        eps = -0.98
+        for steps in (1, 3):
+            want = _exact(G, steps, (0.1, 0.0, 0.0), eps=float(torch.tensor(eps)))
+            assert _far(il.ilargi_orthogonalize(G, steps=steps, coef=(0.1, 0.0, 0.0), eps=eps), want) <= 50 * _tol(*shape, steps)
