@@ -126,7 +126,7 @@ PairRange pair_range(const float* coef) {
 struct OrthoLayout {
   int64_t s, l, sp, lp;                 // short and long side, and the same up to a multiple of 8
   MmPlan gram, square, apply;
-  size_t by, x[2], A, B, partial, total;
+  size_t by, x[2], A, B, partial, most, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
   OrthoLayout o{};
@@ -144,10 +144,10 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
   o.x[1] = take(4 * (size_t)(batch * o.sp * o.lp));
   o.A = take(4 * (size_t)(batch * o.sp * o.sp));
   o.B = take(4 * (size_t)(batch * o.sp * o.sp));
-  size_t most = o.gram.partial_bytes;
-  if (o.square.partial_bytes > most) most = o.square.partial_bytes;
-  if (o.apply.partial_bytes > most) most = o.apply.partial_bytes;
-  o.partial = take(most);
+  o.most = o.gram.partial_bytes;
+  if (o.square.partial_bytes > o.most) o.most = o.square.partial_bytes;
+  if (o.apply.partial_bytes > o.most) o.most = o.apply.partial_bytes;
+  o.partial = take(o.most);
   o.total = at;
   return o;
 }
@@ -206,6 +206,11 @@ hipError_t iterate_pairs(const OrthoArgs& a, const OrthoLayout& o, float unit_b,
 hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipStream_t st) {
   float *A = (float*)(ws + o.A), *B = (float*)(ws + o.B);
   const int64_t s = o.s, l = o.l;
+  auto form = [&](const Product& p) {
+    MmPlan plan = mm_f32_plan(p.M, p.N, p.K, p.batches);
+    if (plan.partial_bytes > o.most) plan = {128, 1, 0};         // (the workspace is as large as the products of pairs have it)
+    return launch_mm_f32(p, plan, (float*)(ws + o.partial), st);
+  };
   for (int t = 0; t < a.steps; ++t) {
     float *x = (float*)(ws + o.x[t & 1]), *next = (float*)(ws + o.x[(t & 1) ^ 1]);
     Product p{};
@@ -214,14 +219,14 @@ hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipSt
     p.Q = p.P;
     p.epi.mode = kEpiScale;
     p.epi.s0 = 1.0f; p.epi.out = A; p.epi.ld_out = s; p.epi.batch_out = s * s;
-    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
+    if (hipError_t e = form(p); e != hipSuccess) return e;
     p.K = s;
     p.P = {A, s, 0, 0, s * s};
     p.Q = p.P;
     p.epi.s0 = a.coef[2]; p.epi.s1 = a.coef[1];
     p.epi.src = A; p.epi.ld_src = s; p.epi.batch_src = s * s;
     p.epi.out = B;
-    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
+    if (hipError_t e = form(p); e != hipSuccess) return e;
     p.N = l;
     p.P.p = B;
     p.Q = {x, l, 1, 0, s * l};
@@ -229,7 +234,7 @@ hipError_t iterate_f32(const OrthoArgs& a, const OrthoLayout& o, char* ws, hipSt
     p.epi.src = x; p.epi.ld_src = l; p.epi.batch_src = s * l;
     p.epi.out = next; p.epi.ld_out = l; p.epi.batch_out = s * l;
     if (t + 1 == a.steps) finish(a, 1.0f, &p.epi);
-    if (hipError_t e = launch_mm_f32(p, MmPlan{128, 1, 0}, nullptr, st); e != hipSuccess) return e;
+    if (hipError_t e = form(p); e != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -239,8 +244,13 @@ hipError_t ortho_typed(const OrthoArgs& a, char* ws, hipStream_t st) {
   const OrthoLayout o = ortho_layout(a.batch, a.rows, a.cols);
   double* parts = (double*)ws;
   const PairRange range = pair_range(a.coef);
-  const bool pairs = range.unit_b > 0.0f && a.eps >= 0.0f;       // (below 0, the first singular values may be beyond 1)
-  const float lg_grow = pairs && range.grow > 1e-38 ? (float)log2(range.grow) : -126.0f;
+  const float lg_grow = range.grow > 1e-38 ? (float)log2(range.grow) : -126.0f;
+  // Pairs, where the iteration stays in their range (with eps below 0 the first singular values may be beyond 1), and what they lose of
+  // an entry, 2^-37 of the norm in a step, grows to no more than 2^-25 by the last: six steps of the usual coefficients, twenty of a = 1.5.
+  // Parts of G that are small against the norm and grow near 1 in more steps keep their bits in float32 products alone (the first
+  // steps in float32 and the last six in pairs: a part that is still small at the end is off by 1e-4 of itself).  Seven steps in float32
+  // and in pairs: 2048 x 2048 3868 and 1088 us, 1024 x 4096 3367 and 569, four of 220 x 64 299 and 46.
+  const bool pairs = range.unit_b > 0.0f && a.eps >= 0.0f && (float)a.steps * lg_grow <= 12.0f;
   if (pairs && ortho_one_takes(a.rows, a.cols)) return launch_ortho_one(a, kUnit, range.unit_b, lg_grow, st);
   const int64_t rows_x = pairs ? o.sp : o.s, ld_x = pairs ? o.lp : o.l;
   const int tc = (int)((ld_x + 31) / 32);

@@ -120,3 +120,44 @@ def test_negative_eps(il):
         for steps in (1, 3):
             want = _exact(G, steps, (0.1, 0.0, 0.0), eps=float(torch.tensor(eps)))
             assert _far(il.ilargi_orthogonalize(G, steps=steps, coef=(0.1, 0.0, 0.0), eps=eps), want) <= 50 * _tol(*shape, steps)
+
+
+def _orbit(s, steps):
+    """Singular values s_0 .. s_T of one direction, and a bound of the relative error of s_T for errors e in every step: an error of the
+    value itself is passed on by p'(s) s / p(s), one of its vectors (all values of a part are equal) as it is."""
+    a, b, c = COEF
+    values = [s]
+    for _ in range(steps):
+        x = values[-1]
+        values.append(x * (a + b * x * x + c * x ** 4))
+    total = 0.0
+    for j in range(steps):
+        k = 1.0
+        for x in values[j:steps]:
+            k *= abs((a + 3 * b * x * x + 5 * c * x ** 4) / (a + b * x * x + c * x ** 4))
+        total += max(1.0, k)
+    return total
+
+
+@pytest.mark.parametrize("rows,cols", [(32, 64), (64, 400), (96, 256), (512, 300)])
+@pytest.mark.parametrize("steps", [7, 8, 10, 15, 20])
+@pytest.mark.parametrize("part", [1e-4, 1e-6, 1e-8, 1e-10])
+def test_parts_of_very_different_size(il, rows, cols, steps, part):
+    """Two parts on rows and columns of their own, each with orthonormal rows, the second scaled far down: they do not mix, and many steps
+    bring the second near 1 too.  Each part is good to what float32 products leave of it."""
+    gen = _gen(rows + steps)
+    G = torch.zeros(rows, cols, device="cuda", dtype=torch.float64)
+    r, c = rows // 2, cols // 2
+    for q, size in enumerate((1.0, part)):
+        m = torch.randn(max(r, c), min(r, c), generator=gen, device="cuda", dtype=torch.float64)
+        Q = torch.linalg.qr(m)[0]
+        G[q * r: (q + 1) * r, q * c: (q + 1) * c] = (Q if r > c else Q.t()) * size
+    G = G.float()
+    got, want = il.ilargi_orthogonalize(G, steps=steps), _exact(G, steps)
+    e = 3 * (math.sqrt(max(rows, cols)) + 4) * U32
+    for q, size in enumerate((1.0, part)):
+        rr, cc = slice(q * r, (q + 1) * r), slice(q * c, (q + 1) * c)
+        s0 = size / math.sqrt(min(r, c) * (1 + part * part))
+        # (the factors of G are orthonormal to a rounding of float32: one more e at the start)
+        assert _far(got[rr, cc], want[rr, cc]) <= e * (_orbit(s0, steps) + 1)
+    assert bool((got[:r, c:] == 0).all()) and bool((got[r:, :c] == 0).all())
