@@ -71,13 +71,15 @@ struct LayerLayout {
 };
 LayerLayout layer_layout(const ilargi_layer_t& y) {
   LayerLayout l;
-  const bool h = y.type == ILARGI_TYPE_BF16;
+  const bool h = y.type == ILARGI_TYPE_BF16, few = mm_rows_takes(y.n, y.k, h);       // (few rows: W is read where it lies)
+  size_t copies = 0;
   if (h && worth_packing(y.n, y.k, y.m)) {
     l.w = up256(2 * (size_t)y.n * (size_t)up8(y.k));
-    l.forward_shares = l.w + up256(2 * (size_t)y.k * (size_t)up8(y.m));
+    copies = l.w + up256(2 * (size_t)y.k * (size_t)up8(y.m));
   }
-  l.forward = l.forward_shares + (mm_rows_takes(y.n, y.k, h) ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k));
-  l.dz = l.forward_shares;
+  l.forward_shares = few ? 0 : copies;
+  l.forward = l.forward_shares + (few ? up256(mm_rows_plan(y.n, y.m, y.k).partial_bytes) : shares_bytes(h, y.n, y.m, y.k));
+  l.dz = copies;
   l.partial = l.dz + up256((size_t)y.n * (size_t)up8(y.m) * (h ? 2 : 4));
   l.shares = l.partial + up256(layer_grad_partial_bytes(y.n, y.m));
   const size_t x = shares_bytes(h, y.n, y.k, y.m), w = shares_bytes(h, y.k, y.m, y.n);
