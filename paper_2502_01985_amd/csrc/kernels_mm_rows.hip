@@ -1,8 +1,8 @@
 // Products of a few rows with a whole matrix: serving.  W is read once, and every element of it multiplies the few rows' values in
 // vector registers.
 //
-// A workgroup takes a line (128 bytes) of every row of W, 128 rows at a time, eight turns of which are on their way at once; that is
-// its share of k, and a second launch adds the shares, where there are several.  Longer shares in fewer launches are slower where W
+// A workgroup takes a line (128 bytes) of every row of W, 128 rows at a time, eight turns of which (four of two rows of bfloat16) are on
+// their way at once; its share of k is at most 1024 rows, and a second launch adds the shares, where there are several.  Longer shares in fewer launches are slower where W
 // comes from memory: 1 x 4096 x 4096, bfloat16, 15.3 us with shares of 1024 rows and 27.9 with one share; 1 x 8192 x 1000 14.1
 // and 45.3.  Blocks on the matrix cores take 17.5 and 13.4 for the same.
 // With W in the last-level cache the 4096 x 4096 call takes 13 us.
@@ -14,14 +14,14 @@ namespace {
 
 constexpr int kThreads = 1024, kLanes = 8, kSubs = kThreads / kLanes;     // lanes of 16 bytes side by side, rows of W at a time
 constexpr int kWaves = kThreads / kWave;
-constexpr int kPart = 1024, kMostShare = 1024;                            // rows of W whose factors lie in LDS; of a workgroup
+constexpr int kMostShare = 1024;                                          // rows of W of a workgroup
 
 // blockIdx: columns kLanes V wide, share of k.  N: rows of X that the registers have room for.
 template <class T, int N>
 __global__ __launch_bounds__(kThreads) void mm_rows_kernel(Product a, int64_t share, float* __restrict__ partial) {
   constexpr int V = ElemOf<T>::kVec, kCols = kLanes * V, U = N * V > 8 && V == 8 ? 4 : 8;       // (128 registers a lane)
   __shared__ union {
-    float x[N][kPart];
+    float x[N][kMostShare];
     float sums[kWaves][N][kCols];
   } lds;
   const int lane = threadIdx.x % kLanes, sub = threadIdx.x / kLanes, wave = threadIdx.x / kWave;
@@ -42,36 +42,35 @@ __global__ __launch_bounds__(kThreads) void mm_rows_kernel(Product a, int64_t sh
       }
     }
   };
+  // The rows of X first: what is asked for first arrives first, and goes into LDS while W is on its way.
+  static_assert(kMostShare == kThreads, "a k a thread");
+  const int k = threadIdx.x;
+  T f[N];
+#pragma unroll
+  for (int x = 0; x < N; ++x) f[x] = x < n && k < rows ? ((const T*)a.P.p)[x * a.P.ld + k0 + k] : (T)0.0f;
   ask(sub);
   float s[N][V];
 #pragma unroll
   for (int r = 0; r < N; ++r)
 #pragma unroll
     for (int v = 0; v < V; ++v) s[r][v] = 0.0f;
-  for (int p0 = 0; p0 < rows; p0 += kPart) {
-    const int p1 = rows - p0 < kPart ? rows : p0 + kPart;
-    __syncthreads();
 #pragma unroll
-    for (int x = 0; x < N; ++x)
-      for (int k = p0 + threadIdx.x; k < p1; k += kThreads) lds.x[x][k - p0] = x < n ? (float)((const T*)a.P.p)[x * a.P.ld + k0 + k] : 0.0f;
-    __syncthreads();
-    for (int r = p0 + sub; r < p1; r += U * kSubs) {
+  for (int x = 0; x < N; ++x) lds.x[x][k] = (float)f[x];
+  __syncthreads();
+  for (int r = sub; r < rows; r += U * kSubs) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int q = r + u * kSubs;
-        if (q >= p1) continue;
+    for (int u = 0; u < U; ++u) {
+      const int q = r + u * kSubs;
+      if (q >= rows) continue;
 #pragma unroll
-        for (int x = 0; x < N; ++x) {
-          const float f = lds.x[x][q - p0];
+      for (int x = 0; x < N; ++x) {
+        const float f = lds.x[x][q];
 #pragma unroll
-          for (int v = 0; v < V; ++v) s[x][v] = fmaf(f, (float)w[u].v[v], s[x][v]);
-        }
+        for (int v = 0; v < V; ++v) s[x][v] = fmaf(f, (float)w[u].v[v], s[x][v]);
       }
-      // (kPart is a multiple of U kSubs: the next rows begin where these end, in this part or the next)
-      if (r + U * kSubs < rows) ask(r + U * kSubs);
     }
+    if (r + U * kSubs < rows) ask(r + U * kSubs);
   }
-  static_assert(kPart % (8 * kSubs) == 0, "whole turns");
   __syncthreads();
   // the eight rows of W that a wavefront holds side by side, then the wavefronts in order
 #pragma unroll
