@@ -818,7 +818,9 @@ def ilargi_orthogonalize(G, out=None, alpha: float = 1.0, beta: float = 0.0, bas
     o3 = out if out.dim() == 3 else out.unsqueeze(0)
     ldo, faro = _batch_of(o3, "out", G3.shape)
     if beta != 0.0:
-        if base is None or base.dtype != out.dtype or base.shape != shape or base.stride() != out.stride() or not base.is_cuda:
+        # (the stride along a side of 1 says nothing of the layout)
+        alike = base is not None and base.shape == shape and all(p == q for p, q, v in zip(base.stride(), out.stride(), shape) if v > 1)
+        if not alike or base.dtype != out.dtype or not base.is_cuda:
             raise ValueError("base must have the type, shape and strides of out")
     batch, rows, cols = G3.shape
     need = ilargi_orthogonalize_workspace_bytes(batch, rows, cols, G.dtype) if workspace is None else 0

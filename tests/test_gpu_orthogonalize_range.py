@@ -161,3 +161,15 @@ def test_parts_of_very_different_size(il, rows, cols, steps, part):
         # (the factors of G are orthonormal to a rounding of float32: one more e at the start)
         assert _far(got[rr, cc], want[rr, cc]) <= e * (_orbit(s0, steps) + 1)
     assert bool((got[:r, c:] == 0).all()) and bool((got[r:, :c] == 0).all())
+
+
+def test_a_base_with_a_side_of_one(il):
+    """The stride along a side of length 1 says nothing of the layout: a row, or one matrix, cut from wider weights is read as it lies."""
+    wide = torch.randn(8, 96, generator=_gen(3), device="cuda")
+    store = torch.empty(8, 96, device="cuda")
+    for base, out in ((wide[2:3, :40], torch.empty(1, 40, device="cuda")), (wide[None, :, :40], store.as_strided((1, 8, 40), (7, 96, 1)))):
+        G = torch.randn(base.shape, generator=_gen(4), device="cuda")
+        want = -0.5 * _exact(G, 5) + base.double()
+        assert _far(il.ilargi_orthogonalize(G, out=out, base=base, alpha=-0.5, beta=1.0), want) <= _tol(8, 96, 5)
+    with pytest.raises(ValueError):
+        il.ilargi_orthogonalize(wide[:, :40], base=wide[:, :40], beta=1.0)      # (out is new, and its rows are shorter)
