@@ -99,3 +99,16 @@ def test_gradients_in_long_runs(il, n, rows, cols, dt, do, kind):
     old = torch.randint(-8, 9, (rows, cols), generator=gen, device="cuda", dtype=torch.int8).to(do)
     added = il.ilargi_embed_grad(d, ids, rows, scale=-1.0, d_table=old.clone(), accumulate=True)
     assert torch.equal(added, (old.float() - want).to(do))
+
+
+@pytest.mark.parametrize("k,m", [(8, 8), (64, 256), (264, 136)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_gradient_of_no_rows(il, k, m, dtype):
+    """Sums over nothing: zeros, or what was there."""
+    X, D = torch.empty(0, k, dtype=dtype, device="cuda"), torch.empty(0, m, dtype=dtype, device="cuda")
+    W = torch.randn(k, m, device="cuda").to(dtype)
+    d_X, d_W, d_b = il.ilargi_linear_grad(D, X, W, pre=D, act="gelu", d_W=torch.full_like(W, 3.0), d_bias=torch.full((m,), 3.0, dtype=dtype, device="cuda"))
+    assert d_X.shape == (0, k) and bool((d_W == 0).all()) and bool((d_b == 0).all())
+    old_W, old_b = W.clone(), W[0].clone()
+    il.ilargi_linear_grad(D, X, W, d_X=None, d_W=old_W, d_bias=old_b, accumulate=True)
+    assert torch.equal(old_W, W) and torch.equal(old_b, W[0])
