@@ -346,7 +346,8 @@ typedef struct {
   ilargi_activation_t act;
 } ilargi_layer_t;
 
-/* Bytes of workspace of ilargi_linear and ilargi_linear_grad for this layer (either pointer may be NULL).
+/* Bytes of workspace of ilargi_linear and ilargi_linear_grad for this layer (either pointer may be NULL).  In bfloat16, from 7.5e8
+ * multiplications on, they hold copies of X and W (and of g) whose rows are whole pieces of 16 bytes, for operands whose rows are not.
  * Errors: NULL (layer), SHAPE (n < 0, k or m < 1, any above 2^31 - 1), UNSUPPORTED (type, act). */
 ilargi_status_t ilargi_linear_workspace_bytes(const ilargi_layer_t* layer, size_t* forward, size_t* gradient);
 
@@ -380,7 +381,7 @@ ilargi_status_t ilargi_linear_grad(const ilargi_layer_t* layer, const void* d_ou
  * norm 1 (2^-37 |G| / (|G| + eps) of a small X), which float32 products of the whole lose too; parts of G on rows and columns of their
  * own, below about 1e-6 of the norm, keep fewer bits than those would.  With more steps, eps < 0, or coefficients that bring a
  * singular value beyond 2, all is float32, in four to seven times the time.
- * Errors: NULL, SHAPE (batch < 0, rows or cols < 1 or above 16384, steps outside [1, 100], leading dimensions or strides
+ * Errors: NULL, SHAPE (batch < 0 or above 65535, rows or cols < 1 or above 16384, steps outside [1, 100], leading dimensions or strides
  * that overlap), UNSUPPORTED (types), WORKSPACE, DEVICE. */
 ilargi_status_t ilargi_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, ilargi_type_t g_type,
                                                      size_t* bytes);

@@ -53,8 +53,8 @@ __device__ __forceinline__ void store_piece(T* __restrict__ p, int valid, const 
 __device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(x)); }
 
 // erfc(|z| / sqrt 2) / 2 = the upper tail of the normal distribution, and exp(-z^2 / 2).  With t = 1 / (1 + 0.3 x) the scaled function
-// exp(x^2) erfc(x) is a polynomial of t without a constant term, fitted here to 2.2e-8 of itself on [0, 12], so the tail keeps its
-// relative accuracy where 1 + erf cancels.  16384 x 2048 x 8192 with gelu, bfloat16: 739 microseconds with the device library's erf
+// exp(x^2) erfc(x) is a polynomial of t without a constant term, fitted here to 3.4e-8 of itself on [0, 12] (7.4e-8, its largest at
+// x = 0.07, with the constants as floats hold them), so the tail keeps its relative accuracy where 1 + erf cancels.  16384 x 2048 x 8192 with gelu, bfloat16: 739 microseconds with the device library's erf
 // where this took 661.
 __device__ __forceinline__ float normal_tail(float z, float& gauss) {
   const float x = 0.70710678118654752f * fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.3f, x, 1.0f));

@@ -527,7 +527,8 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 GradLayout grad_layout(int64_t n, int64_t cols) {
   GradLayout l{};
   // Long runs leave fewer carries, short ones more groups: enough groups of lanes to fill the chip eight times over come first.
-  // 1,000,000 ids, 128 columns: runs of 64 / 128 / 256; 9001 ids, 75 columns: runs of 8 / 16 / 64.
+  // Whole calls with runs of 8 / 16 / 32 / 64 / 128 / 256: 1,000,000 ids of 128 columns, bfloat16, skewed: 290 / 194 / 158 / 143 / 174 / 251 us
+  // (the rule takes 32); 9001 ids of 75 columns, float32: 38 / 39.6 / 44 / 54 / 70 / 109 (the rule takes 16).
   const int64_t lanes = (cols + 7) / 8;
   l.run = 256;
   while (l.run > 16 && n / l.run * lanes < 256 * 1024) l.run /= 2;

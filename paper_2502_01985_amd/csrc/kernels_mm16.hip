@@ -676,7 +676,9 @@ hipError_t launch_mm_join(int64_t M, int64_t N, int64_t batches, int symmetric, 
 
 // Blocks of 256 or 128 and the shares of k, by what they cost in microseconds: a step of a 256-block takes 1.7 (one workgroup fits a
 // compute unit), of a 128-block 0.75 alone on its unit and 1.08 beside another, of a 128-block of pairs (one to a unit) 0.9; shares
-// are written and added at 8 TB/s, in a launch of 3.  Measured: 1024 x 1024 x 4096, bfloat16, 128-blocks: 50 us in one share, 27 in
+// are written and added at 8 TB/s, in a launch of 3.  (What every block of pairs costs besides, its start and its sums, about 20 us, is
+// the same for every number of shares that is one round, and is not counted: of 2048 x 2048 x 2048 the sum is 28.8 and the kernel takes
+// 52, of 1024 x 4096 x 1024 14.4 and 31.)  Measured: 1024 x 1024 x 4096, bfloat16, 128-blocks: 50 us in one share, 27 in
 // four, 32 in eight; 2048 x 2048 x 2048, bfloat16: 31; 4096 x 4096 x 4096, bfloat16: 117 in 256-blocks.
 MmPlan mm16_plan(int64_t M, int64_t N, int64_t K, int64_t batches, int kind, int symmetric) {
   MmPlan best{128, 1, 0};

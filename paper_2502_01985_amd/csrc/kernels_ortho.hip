@@ -6,8 +6,8 @@
 // and every product is three on the 16-bit matrix cores.  The result is as near to 64 bits as float32 products bring it (2048 x
 // 2048: 1.1e-6, those 2.8e-6); single float16 planes are off by 1e-3 to 2e-2, single planes in the last step alone by up to 2e-3,
 // which with bfloat16's own 1.7e-3 is too much.  Bound by the matrix cores and, below about 1000, by the chain of launches: 2048 x
-// 2048, float32, 778 us (221 TFLOP/s of the formula's operations, those of symmetric products counted once, and three times that in
-// products); 1024 x 4096, bfloat16, 400 us.
+// 2048, float32, 786 us (218 TFLOP/s of the formula's operations, those of symmetric products counted once, and three times that in
+// products); 1024 x 4096, bfloat16, 401 us.
 #include <math.h>
 
 #include "mm_epilogue.h"

@@ -2,9 +2,10 @@
 //
 // X (up to 64 rows, zeros behind its own) and A, B (64 x 64) are pairs of float16 planes, as in kernels_ortho.hip; sixteen wavefronts
 // form blocks of 16 x 16 with three products each, on accumulators of their own that are added at the end: (lo hi + hi lo) + hi hi is
-// the same for (i, j) and (j, i), so A and B are symmetric to the bit.  What bounds it is the LDS reads of X X^T
-// (every block reads both its operands) and the chain of four barriers a step.  Four of 220 x 64, five steps: 35 us; seventeen
-// launches of the general kernels 190.
+// the same for (i, j) and (j, i), so A and B are symmetric to the bit.  Four of 220 x 64: 36.8 us for five steps, 5.0 of each more;
+// seventeen launches of the general kernels 190.  What bounds a step is the LDS reads of X X^T (every block reads both its operands) and
+// the chain of four barriers; the other 11.6 us are the launch, two passes over G with one load a lane on its way at a time, and the
+// result.
 #include <utility>
 
 #include "mm_epilogue.h"
