@@ -390,6 +390,101 @@ ilargi_status_t ilargi_orthogonalize(const void* G, ilargi_type_t g_type, int64_
                                      float beta, const void* base, void* out, ilargi_type_t out_type, int64_t ld_out,
                                      int64_t stride_out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The end of a block of a deeper model and the start of the next, in one pass:
+ *   u = N1(h);   r = x + scale f(gate) o u;   y = N2(r)
+ * N is one of
+ *   NONE     v o gain + bias
+ *   RMS      v / sqrt(mean v^2 + eps) o gain + bias
+ *   CENTRED  (v - mean v) / sqrt(mean (v - mean v)^2 + eps) o gain + bias
+ * over the m columns of a row; gains and biases are vectors of m, NULL for ones and zeros.  gate is n x m, one row of m for all rows
+ * (gate_rows = 0), or NULL for ones; x may be NULL for zeros.  With second = NONE there is no y (then gain2 and bias2 are NULL).
+ * All matrices and vectors are of one type; a row is held in float32 from its loads to its stores, each output is rounded once,
+ * and y follows from the r that was not rounded.  A mean of squares that no float32 holds gives what float32 arithmetic gives. */
+typedef enum { ILARGI_NORM_NONE = 0, ILARGI_NORM_RMS = 1, ILARGI_NORM_CENTRED = 2 } ilargi_norm_kind_t;
+
+typedef struct {
+  int64_t n, m;                     /* rows (may be 0), columns (1 .. 16384) */
+  ilargi_type_t type;
+  ilargi_norm_kind_t first, second;
+  ilargi_activation_t gate_act;     /* f */
+  int gate_rows;                    /* 1: a row of the gate for every row; 0: one for all */
+  float scale, eps;
+  const void *h, *gain1, *bias1, *gate, *x, *gain2, *bias2;
+  int64_t ld_h, ld_gate, ld_x;
+} ilargi_norm_t;
+
+/* r and y, either of which may be NULL where it is not wanted; r may be x or h itself, y may be h (not r).  No workspace.
+ * Errors: NULL (block, h with n > 0), SHAPE (n, m, leading dimensions, eps < 0 or no number), UNSUPPORTED (type, kinds, gate_act, y,
+ * gain2 or bias2 without a second norm), DEVICE. */
+ilargi_status_t ilargi_norm(const ilargi_norm_t* block, void* r, int64_t ld_r, void* y, int64_t ld_y, void* stream);
+
+/* Its gradients for d_r and d_y (each may be NULL for zeros; y's is refused without a second norm).  Each result is optional:
+ *   d_h, d_x: n x m; d_gate: n x m, or m sums over the rows where the gate is one row; d_gain*, d_bias*: m sums over the rows.
+ * With accumulate not 0 the sums over rows are added to what is there.  d_x may be d_r itself, d_h may be d_y.  Everything is worked
+ * out again from h, gate and x, in float32; sums over rows are added in an order that depends on n, m and the type only.
+ * d_x is wanted of a block without x too: it is the gradient of what is added to the gated u.
+ * Errors: as ilargi_norm, NULL (a workspace that is needed), UNSUPPORTED (d_gate without a gate, d_gain2 or d_bias2 without a second
+ * norm), WORKSPACE, DEVICE.  (d_gain and d_bias need no gain or bias: they are those at ones and zeros.) */
+typedef struct {
+  void *d_h, *d_x, *d_gate, *d_gain1, *d_bias1, *d_gain2, *d_bias2;
+  int64_t ld_h, ld_x, ld_gate;
+} ilargi_norm_grads_t;
+ilargi_status_t ilargi_norm_grad_workspace_bytes(int64_t n, int64_t m, ilargi_type_t type, size_t* bytes);
+ilargi_status_t ilargi_norm_grad(const ilargi_norm_t* block, const void* d_r, int64_t ld_dr, const void* d_y, int64_t ld_dy,
+                                 const ilargi_norm_grads_t* out, int accumulate, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* A layer of its own for every group of rows (ilargi_linear over ragged groups):
+ *   z[i, :] = X[i, :] W_g + bias_g,   out[i, :] = act(z[i, :]) + residual[i, :]   for offsets[g] <= i < offsets[g + 1].
+ * offsets: device int32[groups + 1], ascending, in [0, n]; the rowptr of ilargi_plan_inverse_index is of this form for rows
+ * brought together by its perm.  Rows of no group (before offsets[0], from offsets[groups] on) are not written.  The offsets are
+ * looked at on the device only: one outside [0, n] or below an earlier one counts as the nearest that is none of that.
+ * W: `groups` matrices k x m, stride_w elements apart (>= (k - 1) ld_w + m); bias groups x m (optional) with ld_bias.
+ * type, act, pre, residual and the sums are those of ilargi_linear; residual may be `out`.
+ * The gradient: g = d_out o act'(pre); d_X[i, :] = g[i, :] W_g^T (rows of no group are not written); d_W_g = X_g^T g_g and
+ * d_bias_g = column sums of g_g, zeros for groups without rows; with accumulate not 0 they are added to what is there.  Each
+ * result is optional; X is not read without d_W, nor W without d_X; pre is NULL if act is NONE.
+ * Errors: NULL, SHAPE (groups < 0 or above 65535, n < 0, k or m < 1, any above 2^31 - 1, leading dimensions, matrices of the groups
+ * that overlap, more than 2^31 - 1 blocks of 64 x 64 results), UNSUPPORTED (type, act), WORKSPACE, DEVICE. */
+typedef struct {
+  int64_t groups, n, k, m;
+  ilargi_type_t type;
+  ilargi_activation_t act;
+} ilargi_groups_t;
+
+ilargi_status_t ilargi_grouped_linear_workspace_bytes(const ilargi_groups_t* layer, size_t* forward, size_t* gradient);
+ilargi_status_t ilargi_grouped_linear(const ilargi_groups_t* layer, const int32_t* offsets, const void* X, int64_t ld_x,
+                                      const void* W, int64_t ld_w, int64_t stride_w, const void* bias, int64_t ld_bias,
+                                      const void* residual, int64_t ld_res, void* out, int64_t ld_out, void* pre,
+                                      int64_t ld_pre, void* workspace, size_t workspace_bytes, void* stream);
+ilargi_status_t ilargi_grouped_linear_grad(const ilargi_groups_t* layer, const int32_t* offsets, const void* d_out,
+                                           int64_t ld_out, const void* pre, int64_t ld_pre, const void* X, int64_t ld_x,
+                                           const void* W, int64_t ld_w, int64_t stride_w, void* d_X, int64_t ld_dx, void* d_W,
+                                           int64_t ld_dw, int64_t stride_dw, void* d_bias, int64_t ld_dbias, int accumulate,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm over all entries of `count` matrices together, and the matrices scaled so that it is at most max_norm:
+ *   norm = sqrt(sum of all squares);   out_t = in_t (max_norm / norm)  if norm > max_norm,  else in_t.
+ * A norm that is no finite number scales nothing: the outputs are the inputs, and `norm` says so.  Squares are summed in float64 in an
+ * order that depends on the sizes only, so no float32 or bfloat16 entries are too large or too small for it.
+ * tensors: host array, read during the call; a vector is a matrix of one row.  out NULL: the tensor counts and is not written; out may
+ * be `in` itself (with ld_out = ld_in: scaled in place, and not written where nothing is scaled).  Any other overlap of an out with an in or
+ * out of the call is refused, except that of column blocks of one matrix (equal leading dimensions).  norm: device float32 (optional).
+ * (It is stored in 32 bits: infinite beyond 3.4e38, where the tensors are scaled all the same.)
+ * max_norm may be infinite: outputs are copies.  count may be 0 (norm 0).
+ * Errors: NULL (tensors, an in, workspace), SHAPE (count outside [0, 65535], rows or cols < 0, a leading dimension below cols, a
+ * max_norm below 0 or no number, overlaps), UNSUPPORTED (type), WORKSPACE, DEVICE. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t rows, cols, ld_in, ld_out;
+  ilargi_type_t type;
+} ilargi_tensor_t;
+
+ilargi_status_t ilargi_clip_norm_workspace_bytes(const ilargi_tensor_t* tensors, int64_t count, size_t* bytes);
+ilargi_status_t ilargi_clip_norm(const ilargi_tensor_t* tensors, int64_t count, float max_norm, float* norm, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
 /* Message for the most recent failure on this thread ("" if none).  Static storage. */
 const char* ilargi_last_error(void);
 

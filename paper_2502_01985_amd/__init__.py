@@ -45,6 +45,8 @@ EXPORTED = [
     "ilargi_plan_trace_name", "ilargi_stream_probe",
     "ilargi_embed", "ilargi_embed_grad", "ilargi_embed_grad_workspace_bytes", "ilargi_linear", "ilargi_linear_grad",
     "ilargi_linear_workspace_bytes", "ilargi_orthogonalize", "ilargi_orthogonalize_workspace_bytes",
+    "ilargi_norm", "ilargi_norm_grad", "ilargi_norm_grad_workspace_bytes", "ilargi_grouped_linear", "ilargi_grouped_linear_grad",
+    "ilargi_grouped_linear_workspace_bytes", "ilargi_clip_norm", "ilargi_clip_norm_workspace_bytes",
     "ilargi_static_scratch_bytes",
     "ilargi_last_error",
     "ilargi_version",
@@ -61,6 +63,30 @@ class SourceStruct(ctypes.Structure):
 class LayerStruct(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("k", ctypes.c_int64), ("m", ctypes.c_int64), ("type", ctypes.c_int),
                 ("act", ctypes.c_int)]
+
+
+class NormStruct(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("m", ctypes.c_int64), ("type", ctypes.c_int), ("first", ctypes.c_int),
+                ("second", ctypes.c_int), ("gate_act", ctypes.c_int), ("gate_rows", ctypes.c_int), ("scale", ctypes.c_float),
+                ("eps", ctypes.c_float), ("h", ctypes.c_void_p), ("gain1", ctypes.c_void_p), ("bias1", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("x", ctypes.c_void_p), ("gain2", ctypes.c_void_p), ("bias2", ctypes.c_void_p),
+                ("ld_h", ctypes.c_int64), ("ld_gate", ctypes.c_int64), ("ld_x", ctypes.c_int64)]
+
+
+class NormGradsStruct(ctypes.Structure):
+    _fields_ = [("d_h", ctypes.c_void_p), ("d_x", ctypes.c_void_p), ("d_gate", ctypes.c_void_p), ("d_gain1", ctypes.c_void_p),
+                ("d_bias1", ctypes.c_void_p), ("d_gain2", ctypes.c_void_p), ("d_bias2", ctypes.c_void_p),
+                ("ld_h", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_gate", ctypes.c_int64)]
+
+
+class GroupsStruct(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64), ("m", ctypes.c_int64),
+                ("type", ctypes.c_int), ("act", ctypes.c_int)]
+
+
+class TensorStruct(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("type", ctypes.c_int)]
 
 
 _vp, _i64, _int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
@@ -103,6 +129,17 @@ lib.ilargi_linear_grad.argtypes = [ctypes.POINTER(LayerStruct), _vp, _i64, _vp, 
 lib.ilargi_orthogonalize_workspace_bytes.argtypes = [_i64, _i64, _i64, _int, ctypes.POINTER(_size)]
 lib.ilargi_orthogonalize.argtypes = [_vp, _int, _i64, _i64, _i64, _i64, _i64, _int, _vp, _f32, _f32, _f32, _vp, _vp, _int,
                                      _i64, _i64, _vp, _size, _vp]
+lib.ilargi_norm.argtypes = [ctypes.POINTER(NormStruct), _vp, _i64, _vp, _i64, _vp]
+lib.ilargi_norm_grad_workspace_bytes.argtypes = [_i64, _i64, _int, ctypes.POINTER(_size)]
+lib.ilargi_norm_grad.argtypes = [ctypes.POINTER(NormStruct), _vp, _i64, _vp, _i64, ctypes.POINTER(NormGradsStruct), _int, _vp,
+                                 _size, _vp]
+lib.ilargi_grouped_linear_workspace_bytes.argtypes = [ctypes.POINTER(GroupsStruct), ctypes.POINTER(_size), ctypes.POINTER(_size)]
+lib.ilargi_grouped_linear.argtypes = [ctypes.POINTER(GroupsStruct), _vp, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp,
+                                      _i64, _vp, _i64, _vp, _size, _vp]
+lib.ilargi_grouped_linear_grad.argtypes = [ctypes.POINTER(GroupsStruct), _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64,
+                                           _vp, _i64, _vp, _i64, _i64, _vp, _i64, _int, _vp, _size, _vp]
+lib.ilargi_clip_norm_workspace_bytes.argtypes = [ctypes.POINTER(TensorStruct), _i64, ctypes.POINTER(_size)]
+lib.ilargi_clip_norm.argtypes = [ctypes.POINTER(TensorStruct), _i64, _f32, _vp, _vp, _size, _vp]
 for _name in EXPORTED[:-3]:
     getattr(lib, _name).restype = _int
 lib.ilargi_static_scratch_bytes.restype = ctypes.c_size_t
@@ -830,6 +867,293 @@ def ilargi_orthogonalize(G, out=None, alpha: float = 1.0, beta: float = 0.0, bas
                                     base.data_ptr() if beta != 0.0 else None, out.data_ptr(), TYPES[out.dtype], ldo, faro, ws,
                                     ws_bytes, _stream_ptr(stream)), "ilargi_orthogonalize")
     return out
+
+
+# ------------------------------------------------------------------------------------ deeper models
+NORMS = {"none": 0, "rms": 1, "centred": 2}
+
+
+def _norm_code(kind) -> int:
+    if isinstance(kind, str):
+        if kind not in NORMS:
+            raise ValueError(f"a norm must be one of {sorted(NORMS)}")
+        return NORMS[kind]
+    return int(kind)
+
+
+def _call(fn, where: str, device, stream, *args) -> None:
+    """Calls ``fn(*args, stream)`` for tensors of ``device``, on its current stream unless one is given."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream belongs to {stream.device}, the tensors to {device}")
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream_ptr(stream)), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream_ptr(stream)), where)
+
+
+def _together(where: str, device, *tensors) -> None:
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.device != device:
+            raise ValueError(f"{where}: tensors of {t.device} and {device}")
+
+
+def _ptr(t) -> Optional[int]:
+    return t.data_ptr() or None if t is not None else None
+
+
+def _norm_block(where, h, first, gain1, bias1, gate, gate_act, scale, x, second, gain2, bias2, eps):
+    code = _typed(h, "h")
+    if h.dim() != 2:
+        raise ValueError("h must be 2-D")
+    n, m = h.shape
+    dtype, rows = h.dtype, gate is not None and gate.dim() == 2
+    _together(where, h.device, gain1, bias1, gate, x, gain2, bias2)
+    return NormStruct(n, m, code, _norm_code(first), _norm_code(second), _act_code(gate_act), int(rows), scale, eps, _ptr(h),
+                      _vector(gain1, "gain1", m, dtype) or None, _vector(bias1, "bias1", m, dtype) or None,
+                      _ptr(gate) if rows else _vector(gate, "gate", m, dtype) or None, _ptr(x),
+                      _vector(gain2, "gain2", m, dtype) or None, _vector(bias2, "bias2", m, dtype) or None,
+                      _rows_of(h, "h", n, m), _rows_of(gate, "gate", n, m, dtype) if rows else 0,
+                      _rows_of(x, "x", n, m, dtype) if x is not None else 0)
+
+
+def ilargi_norm(h, first="rms", gain1=None, bias1=None, gate=None, gate_act="none", scale: float = 1.0, x=None, second="none",
+                gain2=None, bias2=None, eps: float = 1e-6, r="new", y="new", stream=None):
+    """``r = x + scale * gate_act(gate) * N1(h)`` and ``y = N2(r)``: the end of a block and the norm before the next, in one pass.
+    ``first`` and ``second`` are ``"none"``, ``"rms"`` or ``"centred"``, with vectors ``gain`` and ``bias``; ``gate`` is a matrix like
+    ``h`` or one row (1-D) for all.  Returns ``(r, y)``: each a tensor to fill, ``"new"``, or ``None`` where it is not wanted (``y``
+    is ``None`` without a second norm).  ``r`` may be ``x`` or ``h``, ``y`` may be ``h``."""
+    block = _norm_block("ilargi_norm", h, first, gain1, bias1, gate, gate_act, scale, x, second, gain2, bias2, eps)
+    n, m = h.shape
+    if isinstance(r, str):
+        r = _new((n, m), h.dtype, h.device, stream)
+    if isinstance(y, str):
+        y = _new((n, m), h.dtype, h.device, stream) if block.second else None
+    _together("ilargi_norm", h.device, r, y)
+    ldr = _rows_of(r, "r", n, m, h.dtype) if r is not None else 0
+    ldy = _rows_of(y, "y", n, m, h.dtype) if y is not None else 0
+    _call(lib.ilargi_norm, "ilargi_norm", h.device, stream, ctypes.byref(block), _ptr(r), ldr, _ptr(y), ldy)
+    return r, y
+
+
+def ilargi_norm_grad_workspace_bytes(n: int, m: int, dtype) -> int:
+    nbytes = _size(0)
+    _check(lib.ilargi_norm_grad_workspace_bytes(n, m, TYPES[dtype], ctypes.byref(nbytes)), "ilargi_norm_grad_workspace_bytes")
+    return nbytes.value
+
+
+def ilargi_norm_grad(d_r, d_y, h, first="rms", gain1=None, bias1=None, gate=None, gate_act="none", scale: float = 1.0, x=None,
+                     second="none", gain2=None, bias2=None, eps: float = 1e-6, d_h="new", d_x="new", d_gate="new", d_gain1="new",
+                     d_bias1="new", d_gain2="new", d_bias2="new", accumulate: bool = False, workspace=None, stream=None):
+    """``(d_h, d_x, d_gate, d_gain1, d_bias1, d_gain2, d_bias2)`` of ``ilargi_norm`` for the gradients ``d_r`` and ``d_y`` of its
+    results (``None`` for zeros).  Each result is a tensor to fill, ``"new"`` (made where its operand is given), or ``None`` where
+    it is not wanted; ``accumulate`` adds to the given sums over rows: vectors, and ``d_gate`` of a gate of one row."""
+    where = "ilargi_norm_grad"
+    block = _norm_block(where, h, first, gain1, bias1, gate, gate_act, scale, x, second, gain2, bias2, eps)
+    n, m = h.shape
+    dtype = h.dtype
+    given = dict(d_h=(d_h, h), d_x=(d_x, x), d_gate=(d_gate, gate), d_gain1=(d_gain1, gain1), d_bias1=(d_bias1, bias1),
+                 d_gain2=(d_gain2, gain2), d_bias2=(d_bias2, bias2))
+    got = {}
+    for name, (t, of) in given.items():
+        if isinstance(t, str):
+            matrix = name in ("d_h", "d_x") or (name == "d_gate" and block.gate_rows)
+            if accumulate and of is not None and not matrix:
+                raise ValueError(f"accumulate needs {name} (or None)")
+            t = _new((n, m) if matrix else (m,), dtype, h.device, stream) if of is not None else None
+        got[name] = t
+    _together(where, h.device, d_r, d_y, *got.values())
+    lds = {}
+    for name, t in got.items():
+        if name in ("d_h", "d_x") or (name == "d_gate" and block.gate_rows):
+            lds[name] = _rows_of(t, name, n, m, dtype) if t is not None else 0
+        else:
+            _vector(t, name, m, dtype)
+    out = NormGradsStruct(*(_ptr(t) for t in got.values()), lds["d_h"], lds["d_x"], lds.get("d_gate", 0))
+    lddr = _rows_of(d_r, "d_r", n, m, dtype) if d_r is not None else 0
+    lddy = _rows_of(d_y, "d_y", n, m, dtype) if d_y is not None else 0
+    need = ilargi_norm_grad_workspace_bytes(n, m, dtype) if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, h.device, stream)
+    _together(where, h.device, workspace)
+    _call(lib.ilargi_norm_grad, where, h.device, stream, ctypes.byref(block), _ptr(d_r), lddr, _ptr(d_y), lddy, ctypes.byref(out),
+          int(accumulate), ws, ws_bytes)
+    return tuple(got.values())
+
+
+def ilargi_grouped_linear_workspace_bytes(groups: int, n: int, k: int, m: int, dtype) -> Tuple[int, int]:
+    """Bytes of workspace of ``ilargi_grouped_linear`` and of ``ilargi_grouped_linear_grad``."""
+    fwd, grad = _size(0), _size(0)
+    _check(lib.ilargi_grouped_linear_workspace_bytes(ctypes.byref(GroupsStruct(groups, n, k, m, TYPES[dtype], 0)), ctypes.byref(fwd),
+                                                     ctypes.byref(grad)), "ilargi_grouped_linear_workspace_bytes")
+    return fwd.value, grad.value
+
+
+def _groups_of(where, X, W, offsets, dtype):
+    code = _typed(X, "X")
+    if X.dim() != 2 or W.dim() != 3:
+        raise ValueError("X must be n x k and W groups x k x m")
+    n, k = X.shape
+    groups, m = W.shape[0], W.shape[2]
+    if X.dtype != dtype or W.dtype != dtype:
+        raise TypeError("X and W must be of one type")
+    if W.shape[1] != k:
+        raise ValueError(f"W must be groups x {k} x m")
+    _dev_i32(offsets, "offsets")
+    if offsets.numel() != groups + 1:
+        raise ValueError(f"offsets must hold {groups + 1} values")
+    _together(where, X.device, W, offsets)
+    return code, groups, n, k, m
+
+
+def _zeros(shape, dtype, device, stream):
+    """A new tensor of zeros that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.zeros(shape, dtype=dtype, device=device)
+
+
+def ilargi_grouped_linear(X, W, offsets, bias=None, residual=None, act="none", out=None, pre=None, workspace=None, stream=None):
+    """``act(X[i] W[g] + bias[g]) + residual[i]`` for the rows ``offsets[g] <= i < offsets[g + 1]`` of every group: ``X`` n x k, ``W``
+    groups x k x m, ``offsets`` int32[groups + 1] on the device, ``bias`` groups x m.  Rows of no group are not written (zeros in
+    a new ``out``).  ``pre`` (n x m, optional) receives the values before ``act``; ``residual`` may be ``out``."""
+    where, dtype = "ilargi_grouped_linear", X.dtype
+    code, groups, n, k, m = _groups_of(where, X, W, offsets, dtype)
+    ldx = _rows_of(X, "X", n, k, dtype)
+    ldw, farw = _batch_of(W, "W", W.shape)
+    if out is None:
+        out = _zeros((n, m), dtype, X.device, stream)
+    ldo = _rows_of(out, "out", n, m, dtype)
+    ldb = _rows_of(bias, "bias", groups, m, dtype) if bias is not None else 0
+    ldr = _rows_of(residual, "residual", n, m, dtype) if residual is not None else 0
+    ldp = _rows_of(pre, "pre", n, m, dtype) if pre is not None else 0
+    need = ilargi_grouped_linear_workspace_bytes(groups, n, k, m, dtype)[0] if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, X.device, stream)
+    _together(where, X.device, bias, residual, out, pre, workspace)
+    y = GroupsStruct(groups, n, k, m, code, _act_code(act))
+    _call(lib.ilargi_grouped_linear, where, X.device, stream, ctypes.byref(y), _ptr(offsets), _ptr(X), ldx, _ptr(W), ldw, farw,
+          _ptr(bias), ldb, _ptr(residual), ldr, _ptr(out), ldo, _ptr(pre), ldp, ws, ws_bytes)
+    return out
+
+
+def ilargi_grouped_linear_grad(d_out, X, W, offsets, pre=None, act="none", d_X="new", d_W="new", d_bias="new",
+                               accumulate: bool = False, workspace=None, stream=None):
+    """``(d_X, d_W, d_bias)`` of ``ilargi_grouped_linear`` (the residual's gradient is ``d_out``).  Each result is a tensor to fill,
+    ``"new"``, or ``None`` where it is not wanted; ``accumulate`` adds to the given ``d_W`` and ``d_bias``.  Rows of ``d_X`` of no
+    group are not written (zeros in a new one); ``d_W`` and ``d_bias`` of a group without rows are zeros."""
+    where, dtype = "ilargi_grouped_linear_grad", d_out.dtype
+    code, groups, n, k, m = _groups_of(where, X, W, offsets, dtype)
+    ldo = _rows_of(d_out, "d_out", n, m, dtype)
+    ldx = _rows_of(X, "X", n, k, dtype)
+    ldw, farw = _batch_of(W, "W", W.shape)
+    a = _act_code(act)
+    if a and pre is None:
+        raise ValueError("pre is needed unless act is none")
+    ldp = _rows_of(pre, "pre", n, m, dtype) if pre is not None else 0
+    if accumulate and (isinstance(d_W, str) or isinstance(d_bias, str)):
+        raise ValueError("accumulate needs d_W and d_bias (or None)")
+    if isinstance(d_X, str):
+        d_X = _zeros((n, k), dtype, X.device, stream)
+    if isinstance(d_W, str):
+        d_W = _new((groups, k, m), dtype, X.device, stream)
+    if isinstance(d_bias, str):
+        d_bias = _new((groups, m), dtype, X.device, stream)
+    lddx = _rows_of(d_X, "d_X", n, k, dtype) if d_X is not None else 0
+    lddw, fardw = (0, 0)
+    if d_W is not None:
+        if d_W.dtype != dtype:
+            raise TypeError(f"d_W must be a {dtype} CUDA tensor")
+        lddw, fardw = _batch_of(d_W, "d_W", (groups, k, m))
+    lddb = _rows_of(d_bias, "d_bias", groups, m, dtype) if d_bias is not None else 0
+    need = ilargi_grouped_linear_workspace_bytes(groups, n, k, m, dtype)[1] if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, X.device, stream)
+    _together(where, X.device, d_out, pre, d_X, d_W, d_bias, workspace)
+    y = GroupsStruct(groups, n, k, m, code, a)
+    _call(lib.ilargi_grouped_linear_grad, where, X.device, stream, ctypes.byref(y), _ptr(offsets), _ptr(d_out), ldo, _ptr(pre), ldp,
+          _ptr(X), ldx, _ptr(W), ldw, farw, _ptr(d_X), lddx, _ptr(d_W), lddw, fardw, _ptr(d_bias), lddb, int(accumulate), ws, ws_bytes)
+    return d_X, d_W, d_bias
+
+
+def _as_matrix(t, name: str):
+    """rows, columns and leading dimension of a tensor whose elements lie in rows."""
+    _typed(t, name)
+    if t.is_contiguous() or t.numel() == 0:
+        return 1, t.numel(), max(t.numel(), 1)
+    if t.dim() == 1:
+        shape, strides = [t.shape[0], 1], [t.stride(0), 1]
+    else:
+        shape, strides = list(t.shape), list(t.stride())
+    cols, unit = shape.pop(), strides.pop()
+    if unit != 1 and cols > 1:
+        raise TypeError(f"{name} must have unit column stride")
+    rows, ld = 1, None
+    for size, stride in reversed([(a, b) for a, b in zip(shape, strides) if a > 1]):
+        if ld is None:
+            ld = stride
+        elif stride != rows * ld:
+            raise TypeError(f"{name} must be rows of one distance")
+        rows *= size
+    if ld is not None and ld < cols:
+        raise TypeError(f"{name} must have rows that do not overlap")
+    return rows, cols, ld if ld is not None else cols
+
+
+class TensorList:
+    """Tensors for ``ilargi_clip_norm`` (float32 and bfloat16, of one device), and where they go: ``outs`` are tensors of the same
+    shapes and types, the tensors themselves to scale them in place, ``None`` entries where nothing is to be written, or ``None``
+    for no outputs at all.  Programs that clip the same gradients at every step keep the list."""
+
+    def __init__(self, tensors, outs=None):
+        self.tensors = list(tensors)
+        self.outs = list(outs) if outs is not None else [None] * len(self.tensors)
+        if len(self.outs) != len(self.tensors):
+            raise ValueError("as many outs as tensors")
+        self.array = (TensorStruct * max(len(self.tensors), 1))()
+        self.device = self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
+        for q, (t, o) in enumerate(zip(self.tensors, self.outs)):
+            rows, cols, ld = _as_matrix(t, f"tensor {q}")
+            out, ldo = None, 0
+            if o is not None:
+                if o.shape != t.shape or o.dtype != t.dtype:
+                    raise ValueError(f"out {q} must have the shape and type of its tensor")
+                o_rows, o_cols, ldo = _as_matrix(o, f"out {q}")
+                if (rows, cols) != (o_rows, o_cols):
+                    # one of them is contiguous: it is taken in the rows of the other
+                    if t.is_contiguous():
+                        rows, cols, ld = o_rows, o_cols, o_cols
+                    else:
+                        ldo = cols
+                out = o.data_ptr() or None
+            _together("TensorList", self.device, t, o)
+            self.array[q] = TensorStruct(t.data_ptr() or None, out, rows, cols, ld, ldo, TYPES[t.dtype])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def ilargi_clip_norm_workspace_bytes(tensors) -> int:
+    if not isinstance(tensors, TensorList):
+        tensors = TensorList(tensors, tensors)
+    nbytes = _size(0)
+    _check(lib.ilargi_clip_norm_workspace_bytes(tensors.array, len(tensors), ctypes.byref(nbytes)), "ilargi_clip_norm_workspace_bytes")
+    return nbytes.value
+
+
+def ilargi_clip_norm(tensors, max_norm: float, norm=None, workspace=None, stream=None):
+    """The norm over all entries of the tensors (float32[1] on the device), and the tensors scaled so that it is at most ``max_norm``:
+    in place where a plain sequence is given, else as the ``TensorList`` says.  A norm that is not finite scales nothing."""
+    if not isinstance(tensors, TensorList):
+        tensors = list(tensors)
+        tensors = TensorList(tensors, tensors)
+    if norm is None:
+        norm = _new((1,), torch.float32, tensors.device, stream)
+    _vector(norm, "norm", 1, torch.float32)
+    need = ilargi_clip_norm_workspace_bytes(tensors) if workspace is None else 0
+    workspace, ws, ws_bytes = _scratch(workspace, need, tensors.device, stream)
+    _together("ilargi_clip_norm", tensors.device, norm, workspace)
+    _call(lib.ilargi_clip_norm, "ilargi_clip_norm", tensors.device, stream, tensors.array, len(tensors), max_norm, _ptr(norm),
+          ws, ws_bytes)
+    return norm
 
 
 def schema_to_device(schema, device="cuda:0", sparse=False):

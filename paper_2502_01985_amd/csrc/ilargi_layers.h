@@ -332,5 +332,31 @@ __device__ __forceinline__ int ortho_exponent(float lg_norm, float lg_grow, int 
 bool ortho_one_takes(int64_t rows, int64_t cols);
 hipError_t launch_ortho_one(const OrthoArgs& a, float unit, float unit_b, float lg_grow, hipStream_t st);
 
+// ------------------------------------------------------------------------------------------------- norms around a residual sum
+constexpr int64_t kNormMostCols = 16384;
+hipError_t launch_norm(const ilargi_norm_t& a, void* r, int64_t ld_r, void* y, int64_t ld_y, hipStream_t st);
+size_t norm_grad_bytes(int64_t n, int64_t m, bool bf16);
+hipError_t launch_norm_grad(const ilargi_norm_t& a, const void* d_r, int64_t ld_dr, const void* d_y, int64_t ld_dy, const ilargi_norm_grads_t& out,
+                            int accumulate, float* partial, hipStream_t st);
+
+// ------------------------------------------------------------------------------------------------- layers by group of rows
+struct GroupedArgs {
+  ilargi_groups_t y;
+  const int32_t* offsets;
+  const void *d_out, *pre_in, *X, *W, *bias, *residual;
+  int64_t ld_dout, ld_pre, ld_x, ld_w, stride_w, ld_bias, ld_res;
+  void *out, *pre, *d_X, *d_W, *d_bias;
+  int64_t ld_out, ld_dx, ld_dw, stride_dw, ld_dbias;
+  int accumulate;
+};
+bool grouped_blocks_fit(const ilargi_groups_t& y);
+void grouped_bytes(const ilargi_groups_t& y, size_t* forward, size_t* gradient);
+hipError_t launch_grouped(const GroupedArgs& a, char* ws, hipStream_t st);
+hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st);
+
+// ------------------------------------------------------------------------------------------------- the norm over many tensors
+size_t clip_bytes(const ilargi_tensor_t* t, int64_t count);
+hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st);
+
 }  // namespace ilargi
 #endif

@@ -1,6 +1,10 @@
 // C ABI of the operators of models with learned features: checks of the arguments, workspaces, sequences of kernels.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+
+#include <algorithm>
+#include <vector>
 
 #include "ilargi_layers.h"
 
@@ -128,6 +132,91 @@ hipError_t lay_out(const ilargi_layer_t& y, Factor* f, char* at, hipStream_t st)
   f->m.ld = up8(f->m.cols);
   f->padded = true;
   return e;
+}
+
+bool is_act(int f) { return f >= ILARGI_ACT_NONE && f <= ILARGI_ACT_GELU; }
+bool is_norm(int k) { return k >= ILARGI_NORM_NONE && k <= ILARGI_NORM_CENTRED; }
+
+ilargi_status_t check_norm(const char* what, const ilargi_norm_t* a) {
+  if (a == nullptr) return refuse(ILARGI_ERR_NULL, "%s: block is NULL", what);
+  if (a->n < 0 || a->n > kMost || a->m < 1 || a->m > kNormMostCols)
+    return refuse(ILARGI_ERR_SHAPE, "%s: n = %lld, m = %lld", what, (long long)a->n, (long long)a->m);
+  if (!is_type(a->type)) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: no such element type", what);
+  if (!is_norm(a->first) || !is_norm(a->second)) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: no such norm", what);
+  if (!is_act(a->gate_act)) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: no such activation", what);
+  if (a->gate_rows != 0 && a->gate_rows != 1) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: gate_rows = %d", what, a->gate_rows);
+  if (a->second == ILARGI_NORM_NONE && (a->gain2 != nullptr || a->bias2 != nullptr))
+    return refuse(ILARGI_ERR_UNSUPPORTED, "%s: gain2 or bias2 without a second norm", what);
+  if (!(a->eps >= 0.0f)) return refuse(ILARGI_ERR_SHAPE, "%s: eps = %g", what, (double)a->eps);
+  if (a->ld_h < a->m || (a->gate != nullptr && a->gate_rows && a->ld_gate < a->m) || (a->x != nullptr && a->ld_x < a->m))
+    return refuse(ILARGI_ERR_SHAPE, "%s: a leading dimension below m = %lld", what, (long long)a->m);
+  if (a->n > 0 && a->h == nullptr) return refuse(ILARGI_ERR_NULL, "%s: h is NULL", what);
+  return ILARGI_OK;
+}
+
+ilargi_status_t check_groups(const char* what, const ilargi_groups_t* y) {
+  if (y == nullptr) return refuse(ILARGI_ERR_NULL, "%s: layer is NULL", what);
+  if (y->groups < 0 || y->groups > 65535 || y->n < 0 || y->n > kMost || y->k < 1 || y->k > kMost || y->m < 1 || y->m > kMost)
+    return refuse(ILARGI_ERR_SHAPE, "%s: groups = %lld, n = %lld, k = %lld, m = %lld", what, (long long)y->groups, (long long)y->n, (long long)y->k, (long long)y->m);
+  if (!is_type(y->type)) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: no such element type", what);
+  if (!is_act(y->act)) return refuse(ILARGI_ERR_UNSUPPORTED, "%s: no such activation", what);
+  if (!grouped_blocks_fit(*y)) return refuse(ILARGI_ERR_SHAPE, "%s: too many blocks of results", what);
+  return ILARGI_OK;
+}
+bool apart(const ilargi_groups_t& y, int64_t ld, int64_t stride) { return ld >= y.m && (y.groups <= 1 || stride >= (y.k - 1) * ld + y.m); }
+
+// Where the matrices of a call lie.
+struct Range {
+  const char *lo, *hi;
+  int64_t rows, cols, ld, size;
+  bool written;
+};
+Range range_of(const void* p, const ilargi_tensor_t& t, int64_t ld, bool written) {
+  const int64_t size = t.type == ILARGI_TYPE_BF16 ? 2 : 4;
+  return {(const char*)p, (const char*)p + ((t.rows - 1) * ld + t.cols) * size, t.rows, t.cols, ld, size, written};
+}
+// Column blocks of one matrix: they interleave and share no element.  (a begins first.)
+bool column_blocks(const Range& a, const Range& b) {
+  const int64_t ld = a.rows > 1 ? a.ld : b.ld, far = b.lo - a.lo;
+  if (a.size != b.size || far % a.size != 0 || (a.rows > 1 && b.rows > 1 && a.ld != b.ld)) return false;
+  const int64_t at = far / a.size % ld;
+  return a.cols <= at && at + b.cols <= ld;
+}
+bool overlapping(const ilargi_tensor_t* t, int64_t count) {
+  std::vector<Range> all, open;
+  for (int64_t q = 0; q < count; ++q) {
+    if (t[q].rows == 0 || t[q].cols == 0) continue;
+    if (t[q].out != t[q].in) all.push_back(range_of(t[q].in, t[q], t[q].ld_in, false));
+    if (t[q].out != nullptr) all.push_back(range_of(t[q].out, t[q], t[q].ld_out, true));
+  }
+  std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  for (const Range& r : all) {
+    size_t kept = 0;
+    for (const Range& o : open)
+      if (o.hi > r.lo) open[kept++] = o;
+    open.resize(kept);
+    for (const Range& o : open)
+      if ((o.written || r.written) && !column_blocks(o, r)) return true;
+    open.push_back(r);
+  }
+  return false;
+}
+
+ilargi_status_t check_tensors(const ilargi_tensor_t* t, int64_t count) {
+  if (count < 0 || count > 65535) return refuse(ILARGI_ERR_SHAPE, "clip_norm: count = %lld", (long long)count);
+  if (count > 0 && t == nullptr) return refuse(ILARGI_ERR_NULL, "clip_norm: tensors is NULL");
+  for (int64_t q = 0; q < count; ++q) {
+    if (!is_type(t[q].type)) return refuse(ILARGI_ERR_UNSUPPORTED, "clip_norm: tensor %lld is of no such element type", (long long)q);
+    if (t[q].rows < 0 || t[q].rows > kMost || t[q].cols < 0 || t[q].cols > (1ll << 40))
+      return refuse(ILARGI_ERR_SHAPE, "clip_norm: tensor %lld is %lld x %lld", (long long)q, (long long)t[q].rows, (long long)t[q].cols);
+    const int64_t most = 1ll << 40;
+    if (t[q].ld_in < t[q].cols || t[q].ld_in > most || (t[q].out != nullptr && (t[q].ld_out < t[q].cols || t[q].ld_out > most)))
+      return refuse(ILARGI_ERR_SHAPE, "clip_norm: a leading dimension of tensor %lld below its columns, or above 2^40", (long long)q);
+    if (t[q].rows > 0 && t[q].cols > 0 && t[q].in == nullptr) return refuse(ILARGI_ERR_NULL, "clip_norm: tensor %lld is NULL", (long long)q);
+    if (t[q].out == t[q].in && t[q].rows > 1 && t[q].ld_out != t[q].ld_in)
+      return refuse(ILARGI_ERR_SHAPE, "clip_norm: tensor %lld in place with another leading dimension", (long long)q);
+  }
+  return ILARGI_OK;
 }
 
 }  // namespace
@@ -280,6 +369,113 @@ ilargi_status_t ilargi_orthogonalize(const void* G, ilargi_type_t g_type, int64_
   a.eps = eps; a.alpha = alpha; a.beta = beta; a.base = base;
   a.out = out; a.ld_out = ld_out; a.batch_out = stride_out; a.out_bf16 = out_type == ILARGI_TYPE_BF16;
   return done("orthogonalize", launch_ortho(a, (char*)workspace, (hipStream_t)stream));
+}
+
+ilargi_status_t ilargi_norm(const ilargi_norm_t* block, void* r, int64_t ld_r, void* y, int64_t ld_y, void* stream) {
+  if (ilargi_status_t e = check_norm("norm", block); e != ILARGI_OK) return e;
+  if (y != nullptr && block->second == ILARGI_NORM_NONE) return refuse(ILARGI_ERR_UNSUPPORTED, "norm: y without a second norm");
+  if ((r != nullptr && ld_r < block->m) || (y != nullptr && ld_y < block->m))
+    return refuse(ILARGI_ERR_SHAPE, "norm: a leading dimension below m = %lld", (long long)block->m);
+  if (block->n == 0 || (r == nullptr && y == nullptr)) return ILARGI_OK;
+  return done("norm", launch_norm(*block, r, ld_r, y, ld_y, (hipStream_t)stream));
+}
+
+ilargi_status_t ilargi_norm_grad_workspace_bytes(int64_t n, int64_t m, ilargi_type_t type, size_t* bytes) {
+  if (bytes == nullptr) return refuse(ILARGI_ERR_NULL, "norm_grad: bytes is NULL");
+  if (n < 0 || n > kMost || m < 1 || m > kNormMostCols) return refuse(ILARGI_ERR_SHAPE, "norm_grad: n = %lld, m = %lld", (long long)n, (long long)m);
+  if (!is_type(type)) return refuse(ILARGI_ERR_UNSUPPORTED, "norm_grad: no such element type");
+  *bytes = norm_grad_bytes(n, m, type == ILARGI_TYPE_BF16);
+  return ILARGI_OK;
+}
+
+ilargi_status_t ilargi_norm_grad(const ilargi_norm_t* block, const void* d_r, int64_t ld_dr, const void* d_y, int64_t ld_dy,
+                                 const ilargi_norm_grads_t* out, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  if (ilargi_status_t e = check_norm("norm_grad", block); e != ILARGI_OK) return e;
+  if (out == nullptr) return refuse(ILARGI_ERR_NULL, "norm_grad: out is NULL");
+  const ilargi_norm_t& a = *block;
+  const bool second = a.second != ILARGI_NORM_NONE;
+  if (!second && (d_y != nullptr || out->d_gain2 != nullptr || out->d_bias2 != nullptr))
+    return refuse(ILARGI_ERR_UNSUPPORTED, "norm_grad: d_y, d_gain2 or d_bias2 without a second norm");
+  if (out->d_gate != nullptr && a.gate == nullptr) return refuse(ILARGI_ERR_UNSUPPORTED, "norm_grad: d_gate without a gate");
+  if ((d_r != nullptr && ld_dr < a.m) || (d_y != nullptr && ld_dy < a.m) || (out->d_h != nullptr && out->ld_h < a.m) ||
+      (out->d_x != nullptr && out->ld_x < a.m) || (out->d_gate != nullptr && a.gate_rows && out->ld_gate < a.m))
+    return refuse(ILARGI_ERR_SHAPE, "norm_grad: a leading dimension below m = %lld", (long long)a.m);
+  if ((out->d_gate != nullptr && !a.gate_rows) || out->d_gain1 != nullptr || out->d_bias1 != nullptr || out->d_gain2 != nullptr || out->d_bias2 != nullptr)
+    if (ilargi_status_t e = check_workspace("norm_grad", workspace, workspace_bytes, norm_grad_bytes(a.n, a.m, a.type == ILARGI_TYPE_BF16)); e != ILARGI_OK) return e;
+  return done("norm_grad", launch_norm_grad(a, d_r, ld_dr, d_y, ld_dy, *out, accumulate, (float*)workspace, (hipStream_t)stream));
+}
+
+ilargi_status_t ilargi_grouped_linear_workspace_bytes(const ilargi_groups_t* layer, size_t* forward, size_t* gradient) {
+  if (ilargi_status_t e = check_groups("grouped_linear", layer); e != ILARGI_OK) return e;
+  grouped_bytes(*layer, forward, gradient);
+  return ILARGI_OK;
+}
+
+ilargi_status_t ilargi_grouped_linear(const ilargi_groups_t* layer, const int32_t* offsets, const void* X, int64_t ld_x, const void* W, int64_t ld_w,
+                                      int64_t stride_w, const void* bias, int64_t ld_bias, const void* residual, int64_t ld_res, void* out,
+                                      int64_t ld_out, void* pre, int64_t ld_pre, void* workspace, size_t workspace_bytes, void* stream) {
+  if (ilargi_status_t e = check_groups("grouped_linear", layer); e != ILARGI_OK) return e;
+  const ilargi_groups_t& y = *layer;
+  if (ld_x < y.k || ld_out < y.m || (bias != nullptr && ld_bias < y.m) || (residual != nullptr && ld_res < y.m) || (pre != nullptr && ld_pre < y.m))
+    return refuse(ILARGI_ERR_SHAPE, "grouped_linear: a leading dimension below the matrix's columns");
+  if (!apart(y, ld_w, stride_w)) return refuse(ILARGI_ERR_SHAPE, "grouped_linear: matrices of the groups overlap");
+  if (y.n == 0 || y.groups == 0) return ILARGI_OK;
+  if (offsets == nullptr || X == nullptr || W == nullptr || out == nullptr) return refuse(ILARGI_ERR_NULL, "grouped_linear: offsets, X, W or out is NULL");
+  size_t need = 0;
+  grouped_bytes(y, &need, nullptr);
+  if (ilargi_status_t e = check_workspace("grouped_linear", workspace, workspace_bytes, need); e != ILARGI_OK) return e;
+  GroupedArgs a{};
+  a.y = y; a.offsets = offsets;
+  a.X = X; a.ld_x = ld_x; a.W = W; a.ld_w = ld_w; a.stride_w = y.groups > 1 ? stride_w : 0;
+  a.bias = bias; a.ld_bias = ld_bias; a.residual = residual; a.ld_res = ld_res;
+  a.out = out; a.ld_out = ld_out; a.pre = pre; a.ld_pre = ld_pre;
+  return done("grouped_linear", launch_grouped(a, (char*)workspace, (hipStream_t)stream));
+}
+
+ilargi_status_t ilargi_grouped_linear_grad(const ilargi_groups_t* layer, const int32_t* offsets, const void* d_out, int64_t ld_out, const void* pre,
+                                           int64_t ld_pre, const void* X, int64_t ld_x, const void* W, int64_t ld_w, int64_t stride_w, void* d_X,
+                                           int64_t ld_dx, void* d_W, int64_t ld_dw, int64_t stride_dw, void* d_bias, int64_t ld_dbias, int accumulate,
+                                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (ilargi_status_t e = check_groups("grouped_linear_grad", layer); e != ILARGI_OK) return e;
+  const ilargi_groups_t& y = *layer;
+  const bool bent = y.act != ILARGI_ACT_NONE;
+  if (ld_out < y.m || (bent && ld_pre < y.m) || (d_W != nullptr && ld_x < y.k) || (d_X != nullptr && ld_dx < y.k) || (d_bias != nullptr && ld_dbias < y.m))
+    return refuse(ILARGI_ERR_SHAPE, "grouped_linear_grad: a leading dimension below the matrix's columns");
+  if ((d_X != nullptr && !apart(y, ld_w, stride_w)) || (d_W != nullptr && !apart(y, ld_dw, stride_dw)))
+    return refuse(ILARGI_ERR_SHAPE, "grouped_linear_grad: matrices of the groups overlap");
+  if (y.groups == 0 || (d_X == nullptr && d_W == nullptr && d_bias == nullptr)) return ILARGI_OK;
+  if (offsets == nullptr || (y.n > 0 && (d_out == nullptr || (bent && pre == nullptr) || (d_W != nullptr && X == nullptr) || (d_X != nullptr && W == nullptr))))
+    return refuse(ILARGI_ERR_NULL, "grouped_linear_grad: offsets, d_out, pre, X or W is NULL");
+  size_t need = 0;
+  grouped_bytes(y, nullptr, &need);
+  if (ilargi_status_t e = check_workspace("grouped_linear_grad", workspace, workspace_bytes, need); e != ILARGI_OK) return e;
+  GroupedArgs a{};
+  a.y = y; a.offsets = offsets;
+  a.d_out = d_out; a.ld_dout = ld_out; a.pre_in = pre;
+  a.X = X; a.ld_x = ld_x; a.W = W; a.ld_w = ld_w; a.stride_w = y.groups > 1 ? stride_w : 0;
+  a.ld_pre = ld_pre; a.d_X = d_X; a.ld_dx = ld_dx; a.d_W = d_W; a.ld_dw = ld_dw; a.stride_dw = y.groups > 1 ? stride_dw : 0;
+  a.d_bias = d_bias; a.ld_dbias = ld_dbias; a.accumulate = accumulate;
+  return done("grouped_linear_grad", launch_grouped_grad(a, (char*)workspace, (hipStream_t)stream));
+}
+
+ilargi_status_t ilargi_clip_norm_workspace_bytes(const ilargi_tensor_t* tensors, int64_t count, size_t* bytes) {
+  if (bytes == nullptr) return refuse(ILARGI_ERR_NULL, "clip_norm: bytes is NULL");
+  if (ilargi_status_t e = check_tensors(tensors, count); e != ILARGI_OK) return e;
+  *bytes = clip_bytes(tensors, count);
+  return ILARGI_OK;
+}
+
+ilargi_status_t ilargi_clip_norm(const ilargi_tensor_t* tensors, int64_t count, float max_norm, float* norm, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  if (ilargi_status_t e = check_tensors(tensors, count); e != ILARGI_OK) return e;
+  if (!(max_norm >= 0.0f)) return refuse(ILARGI_ERR_SHAPE, "clip_norm: max_norm = %g", (double)max_norm);
+  try {
+    if (overlapping(tensors, count)) return refuse(ILARGI_ERR_SHAPE, "clip_norm: an output overlaps another tensor");
+  } catch (...) {
+    return refuse(ILARGI_ERR_DEVICE, "clip_norm: out of host memory");
+  }
+  if (ilargi_status_t e = check_workspace("clip_norm", workspace, workspace_bytes, clip_bytes(tensors, count)); e != ILARGI_OK) return e;
+  return done("clip_norm", launch_clip(tensors, count, max_norm, norm, (double*)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,182 @@
+// The norm over many tensors and the tensors scaled by it: every workgroup leaves the sum of the squares of its part, in float64; the
+// workgroups of the second pass add those sums up themselves, all in the same order, so no launch stands between the two.
+//
+// Tensors go sixty-four to a launch, in the launch's arguments: nothing is copied to the device before.  A workgroup takes a run of one
+// tensor's pieces of 16 bytes; a tensor whose rows follow each other counts as one row.  Bound by memory.
+#include "ilargi_layers.h"
+
+namespace ilargi {
+
+namespace {
+
+constexpr int kMostTensors = 64, kMostParts = 2048, kLoads = 4;
+constexpr int64_t kLeastPart = 2048;         // pieces
+
+struct Part {
+  const char* in;
+  char* out;
+  int64_t row_pieces, pieces;       // of a row, of all
+  int64_t cols, ld_in, ld_out;
+};
+struct Parts {
+  Part t[kMostTensors];
+  int first[kMostTensors + 1];      // its first workgroup
+  int count;
+  uint64_t bf16;                    // a bit a tensor
+  int64_t part;                     // pieces of a workgroup
+};
+
+// The tensor of a workgroup.
+__device__ __forceinline__ int tensor_of(const Parts& a) {
+  const int lane = threadIdx.x % kWave;
+  const bool before = lane < a.count && a.first[lane] <= (int)blockIdx.x;
+  return __popcll(__ballot(before)) - 1;
+}
+
+// use(piece, valid elements, offset in `out`) for the pieces of this workgroup's part; kLoads of them are asked for together.
+template <class T, class Use>
+__device__ __forceinline__ void pieces_of(const Part& t, int64_t first, int64_t last, Use use) {
+  constexpr int V = ElemOf<T>::kVec;
+  for (int64_t at = first + threadIdx.x; at < last; at += 256 * kLoads) {
+    int64_t in[kLoads], out[kLoads];
+    int valid[kLoads];
+    Piece<T, V> v[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int64_t p = at + 256 * u;
+      int64_t row = 0, c = p;
+      if (t.row_pieces != t.pieces) {
+        row = t.pieces < (1ll << 31) ? (int64_t)((uint32_t)p / (uint32_t)t.row_pieces) : p / t.row_pieces;
+        c = p - row * t.row_pieces;
+      }
+      const int64_t left = t.cols - c * V;
+      valid[u] = p >= last ? 0 : left < V ? (int)left : V;
+      in[u] = row * t.ld_in + c * V;
+      out[u] = row * t.ld_out + c * V;
+    }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      if (valid[u] == V) {
+        v[u] = *reinterpret_cast<const Piece<T, V>*>((const T*)t.in + in[u]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[u].v[j] = j < valid[u] ? ((const T*)t.in)[in[u] + j] : (T)0.0f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) use(v[u], valid[u], out[u]);
+  }
+}
+
+__device__ __forceinline__ double workgroup_sum(double s, double (&lds)[4]) {
+#pragma unroll
+  for (int q = kWave / 2; q >= 1; q /= 2) s += __shfl_xor(s, q);
+  if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = s;
+  __syncthreads();
+  return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+__global__ __launch_bounds__(256) void squares_kernel(Parts a, double* __restrict__ partial) {
+  __shared__ double lds[4];
+  const int q = tensor_of(a);
+  const Part& t = a.t[q];
+  const int64_t first = (int64_t)(blockIdx.x - a.first[q]) * a.part, last = first + a.part < t.pieces ? first + a.part : t.pieces;
+  double s = 0.0;
+  auto add = [&](auto piece) {
+#pragma unroll
+    for (auto x : piece.v) s = fma((double)(float)x, (double)(float)x, s);
+  };
+  if (a.bf16 >> q & 1) pieces_of<bf16_t>(t, first, last, [&](const Piece<bf16_t, 8>& v, int, int64_t) { add(v); });
+  else pieces_of<float>(t, first, last, [&](const Piece<float, 4>& v, int, int64_t) { add(v); });
+  s = workgroup_sum(s, lds);
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+// blockIdx: the part of a tensor; without tensors one workgroup that stores the norm.
+__global__ __launch_bounds__(256) void clip_kernel(Parts a, const double* __restrict__ partial, int sums, float max_norm, float* __restrict__ norm) {
+  __shared__ double lds[4];
+  double s = 0.0;
+#pragma unroll 8
+  for (int w = threadIdx.x; w < sums; w += 256) s += partial[w];
+  const double total = sqrt(workgroup_sum(s, lds));
+  if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+  if (a.count == 0) return;
+  const bool scaled = total > (double)max_norm && total <= 1.7976931348623157e308;      // (no for NaN and infinity)
+  const Factor2 factor = factor2(scaled ? (double)max_norm / total : 1.0);      // (a factor below 2^-126 keeps its bits)
+  const int q = tensor_of(a);
+  const Part& t = a.t[q];
+  if (!scaled && t.in == t.out) return;
+  const int64_t first = (int64_t)(blockIdx.x - a.first[q]) * a.part, last = first + a.part < t.pieces ? first + a.part : t.pieces;
+  auto put = [&](auto v, int valid, int64_t at) {
+    using P = decltype(v);
+    using T = std::remove_reference_t<decltype(v.v[0])>;
+    constexpr int V = sizeof(P) / sizeof(T);
+    if (scaled) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v.v[j] = (T)times((float)v.v[j], factor);
+    }
+    T* const to = (T*)t.out + at;
+    if (valid == V) {
+      *reinterpret_cast<P*>(to) = v;
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < valid) to[j] = v.v[j];
+    }
+  };
+  if (a.bf16 >> q & 1) pieces_of<bf16_t>(t, first, last, put);
+  else pieces_of<float>(t, first, last, put);
+}
+
+int64_t vec_of(const ilargi_tensor_t& t) { return t.type == ILARGI_TYPE_BF16 ? ElemOf<bf16_t>::kVec : ElemOf<float>::kVec; }
+bool in_one_row(const ilargi_tensor_t& t) { return t.rows <= 1 || (t.ld_in == t.cols && (t.out == nullptr || t.ld_out == t.cols)); }
+int64_t row_pieces(const ilargi_tensor_t& t) { return ((in_one_row(t) ? t.rows * t.cols : t.cols) + vec_of(t) - 1) / vec_of(t); }
+int64_t pieces_in(const ilargi_tensor_t& t) { return t.rows == 0 || t.cols == 0 ? 0 : row_pieces(t) * (in_one_row(t) ? 1 : t.rows); }
+
+struct ClipPlan {
+  int64_t part, groups;      // pieces of a workgroup, workgroups
+};
+ClipPlan clip_plan(const ilargi_tensor_t* t, int64_t count) {
+  int64_t all = 0;
+  for (int64_t q = 0; q < count; ++q) all += pieces_in(t[q]);
+  ClipPlan p{all / kMostParts, 0};
+  p.part = p.part < kLeastPart ? kLeastPart : (p.part + 255) / 256 * 256;
+  for (int64_t q = 0; q < count; ++q) p.groups += (pieces_in(t[q]) + p.part - 1) / p.part;
+  return p;
+}
+
+}  // namespace
+
+size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)clip_plan(t, count).groups * 8; }
+
+hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
+  const ClipPlan plan = clip_plan(t, count);
+  bool stored = false;
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t done = 0;
+    for (int64_t q = 0; q < count;) {
+      Parts a{};
+      a.part = plan.part;
+      for (; q < count && a.count < kMostTensors; ++q) {
+        const int64_t pieces = pieces_in(t[q]);
+        if (pieces == 0 || (pass == 1 && t[q].out == nullptr)) continue;
+        const bool one = in_one_row(t[q]);
+        a.t[a.count] = {(const char*)t[q].in, (char*)t[q].out, row_pieces(t[q]), pieces, one ? t[q].rows * t[q].cols : t[q].cols, t[q].ld_in, t[q].ld_out};
+        a.bf16 |= (uint64_t)(t[q].type == ILARGI_TYPE_BF16) << a.count;
+        a.first[a.count + 1] = a.first[a.count] + (int)((pieces + plan.part - 1) / plan.part);
+        ++a.count;
+      }
+      if (a.count == 0) break;
+      const unsigned groups = (unsigned)a.first[a.count];
+      if (pass == 0) squares_kernel<<<groups, 256, 0, st>>>(a, partial + done);
+      else clip_kernel<<<groups, 256, 0, st>>>(a, partial, (int)plan.groups, max_norm, stored ? nullptr : norm);
+      stored = pass == 1;
+      done += groups;
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+  }
+  if (!stored && norm != nullptr) clip_kernel<<<1, 256, 0, st>>>(Parts{}, partial, (int)plan.groups, max_norm, norm);
+  return hipGetLastError();
+}
+
+}  // namespace ilargi
