@@ -226,14 +226,15 @@ __global__ __launch_bounds__(256) void grouped_grad_kernel(GroupedGrad a, int64_
   }
 }
 
-// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order.  blockIdx: 16 columns
+// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in
+// float64: they cancel each other as the rows do.  blockIdx: 16 columns
 // (from `first` on), group.
 template <class T>
 __global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_t first) {
-  __shared__ float part[16][17];
+  __shared__ double part[16][17];
   const int c = threadIdx.x % 16, q = threadIdx.x / 16, g = blockIdx.y;
   const int64_t j = (first + blockIdx.x) * 16 + c, m = a.g.m;
-  float s = 0.0f;
+  double s = 0.0;
   if (j < m) {
 #pragma unroll 4
     for (int u = a.at.chunks[g] + q; u < a.at.chunks[g + 1]; u += 16) s += a.partial[(int64_t)u * m + j];
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_
   if (q != 0 || j >= m) return;
   for (int u = 1; u < 16; ++u) s += part[u][c];
   T* const out = (T*)a.g.d_bias + g * a.ld_dbias + j;
-  *out = (T)(a.g.accumulate ? (float)*out + s : s);
+  *out = (T)(float)(a.g.accumulate ? (double)(float)*out + s : s);
 }
 
 // Matrices of bfloat16 at any address, laid out in whole 16-byte pieces with zeros behind their rows' ends; 2^sh lanes a row.

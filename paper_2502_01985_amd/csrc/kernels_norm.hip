@@ -199,7 +199,7 @@ __device__ __forceinline__ void normalise_back(const L& row, int kind, float by,
   row_sums<W, L::R>(s, lds, turn);
   const float along = s[0] * share, mean = kind == ILARGI_NORM_CENTRED ? s[1] * share : 0.0f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) t[e] = by * (fmaf(-along, unit[e], t[e]) - mean);
+  for (int e = 0; e < E; ++e) t[e] = by * (fmaf(-along, unit[e], t[e]) - (row.live(e / L::V, e % L::V) ? mean : 0.0f));
 }
 
 struct NormGradIn {
@@ -334,15 +334,16 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_grad_kernel(ilargi_nor
   }
 }
 
-// Adds the workgroups' sums: sixteen threads share a column, each adds every sixteenth workgroup, then they are added in order.
+// Adds the workgroups' sums, in float64: they cancel each other as the rows' parts do.  Sixteen threads share a column, each adds every
+// sixteenth workgroup, then they are added in order.
 template <class T>
 __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict__ partial, int groups, int64_t m, ilargi_norm_grads_t o, int gate_sum, int accumulate) {
-  __shared__ float part[16][17];
+  __shared__ double part[16][17];
   const int c = threadIdx.x % 16, q = threadIdx.x / 16, which = blockIdx.y;
   T* const out = (T*)(which == kSumGain2 ? o.d_gain2 : which == kSumBias2 ? o.d_bias2 : which == kSumGate ? (gate_sum ? o.d_gate : nullptr) : which == kSumGain1 ? o.d_gain1 : o.d_bias1);
   if (out == nullptr) return;
   const int64_t j = (int64_t)blockIdx.x * 16 + c;
-  float s = 0.0f;
+  double s = 0.0;
   if (j < m) {
 #pragma unroll 8
     for (int w = q; w < groups; w += 16) s += partial[((int64_t)w * kSums + which) * m + j];
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict_
   __syncthreads();
   if (q != 0 || j >= m) return;
   for (int u = 1; u < 16; ++u) s += part[u][c];
-  out[j] = (T)(accumulate ? (float)out[j] + s : s);
+  out[j] = (T)(float)(accumulate ? (double)(float)out[j] + s : s);
 }
 
 // Threads of a row and pieces of a thread: the least that hold it.

@@ -221,6 +221,27 @@ def test_long_sums_over_rows(il):
             _close(into[k], (w + old[k].double(), e + E * (w.abs() + old[k].double().abs())), dtype, k)
 
 
+@pytest.mark.parametrize("kinds", [(a, b) for a in ("none", "rms", "centred") for b in ("none", "rms", "centred")])
+@pytest.mark.parametrize("act", ["none", "sigmoid", "gelu"])
+def test_every_pair_of_norms_where_rows_do_not_fill_their_threads(il, kinds, act):
+    """Threads that hold no columns of a row, or columns that their neighbours have too, add nothing to its means: with a gate whose value
+    at 0 is not 0, and without one."""
+    gen = _gen(14)
+    for dtype, n, m in ((F32, 40, 23), (F32, 9, 2369), (BF16, 30, 9), (BF16, 7, 1100)):
+        h, x, dr, dy = (_matrix(n, m, dtype, gen) for _ in range(4))
+        second = kinds[1] != "none"
+        for gate in (None, h[0].clone(), x):
+            args = dict(first=kinds[0], second=kinds[1], gate=gate, gate_act=act, x=x, scale=0.8)
+            want = _oracle(kinds, h, x, gate, None, None, None, None, act, 0.8, dr, dy if second else None)
+            for name, t in zip(("r", "y"), il.ilargi_norm(h, **args)):
+                if t is not None:
+                    _close(t, want[name], dtype, name)
+            more = dict(d_gain1=torch.empty_like(h[0]), d_bias1=torch.empty_like(h[0]))
+            for name, t in zip(GRADS, il.ilargi_norm_grad(dr, dy if second else None, h, **args, **more)):
+                if t is not None:
+                    _close(t, want[name], dtype, (name, gate is None))
+
+
 def test_no_rows(il):
     e = torch.empty(0, 12, device="cuda")
     v = torch.ones(12, device="cuda")
