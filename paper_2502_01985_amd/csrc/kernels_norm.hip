@@ -3,16 +3,26 @@
 //
 // W threads share a row; each holds P pieces of 16 bytes of it, W pieces apart.  A piece that would reach behind the row's end begins
 // earlier instead, so that every load is a whole one: the columns that the neighbour holds already count as zeros here and are not
-// stored ([lo, hi) is what a piece has of its own).  Bound by memory.
+// stored ([lo, hi) is what a piece has of its own).  Rows of whole pieces have only pieces of their own and others.  Bound by
+// memory.
 #include "ilargi_layers.h"
 
 namespace ilargi {
 
 namespace {
 
-template <class T, int W, int P>
+enum { kFull, kWhole, kRagged };       // rows that fill their threads; of whole pieces; of any length
+
+template <class T, int W, int P, int SHAPE>
 struct Row {
-  static constexpr int V = ElemOf<T>::kVec, E = V * P, NT = W < 256 ? 256 : W, R = NT / W, kWaves = W / kWave;
+  static constexpr int kW = W, kP = P, V = ElemOf<T>::kVec, E = V * P, NT = W < 256 ? 256 : W, R = NT / W;
+  static constexpr int kShape = SHAPE;
+  // which of the R rows side by side: the same for a whole wavefront, where it can be
+  static __device__ __forceinline__ int slot() {
+    if constexpr (R == 1) return 0;
+    else if constexpr (W >= kWave) return __builtin_amdgcn_readfirstlane(threadIdx.x / W);
+    else return threadIdx.x / W;
+  }
   using Raw = Piece<T, V>;
   int c[P], lo[P], hi[P], m;
 
@@ -27,10 +37,10 @@ struct Row {
       hi[p] = m < V ? m : V;
     }
   }
-  __device__ __forceinline__ bool live(int p, int j) const { return j >= lo[p] && j < hi[p]; }
+  __device__ __forceinline__ bool live(int p, int j) const { return SHAPE == kRagged ? j >= lo[p] && j < hi[p] : SHAPE == kFull || lo[p] == 0; }
   __device__ __forceinline__ void load(const void* row, Raw (&r)[P]) const {
     const T* at = (const T*)row;
-    if (m >= V) {
+    if (SHAPE != kRagged || m >= V) {
 #pragma unroll
       for (int p = 0; p < P; ++p) r[p] = *reinterpret_cast<const Raw*>(at + c[p]);
     } else {
@@ -50,12 +60,12 @@ struct Row {
     T* at = (T*)row;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      if (lo[p] == 0 && hi[p] == V) {
+      if (SHAPE == kFull || (lo[p] == 0 && (SHAPE == kWhole || hi[p] == V))) {
         Raw r;
 #pragma unroll
         for (int j = 0; j < V; ++j) r.v[j] = (T)f[p * V + j];
         *reinterpret_cast<Raw*>(at + c[p]) = r;
-      } else {
+      } else if (SHAPE == kRagged) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (live(p, j)) at[c[p] + j] = (T)f[p * V + j];
@@ -64,33 +74,50 @@ struct Row {
   }
 };
 
-// Sums over the threads of a row, the same for all of them.  `turn` alternates between two places in LDS, so one barrier a sum is enough.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
+// Sums over the threads of a row, the same for all of them: over sixteen lanes by lane permutations of the vector units (through LDS,
+// each of the six steps of a wavefront would wait a hundred cycles), then wavefronts through LDS.  `turn` alternates between two
+// places there, so one barrier a sum is enough.
+template <int W, int R>
+struct RowLds {
+  static constexpr int kWaves = W < kWave ? 1 : W / kWave;
+  float v[2][2][R * kWaves];
+};
 template <int W, int R, int K>
-__device__ __forceinline__ void row_sums(float (&v)[K], float (*lds)[R * (W < kWave ? 1 : W / kWave)][2], int& turn) {
+__device__ __forceinline__ void row_sums(float (&v)[K], RowLds<W, R>& lds, int& turn) {
 #pragma unroll
-  for (int s = (W < kWave ? W : kWave) / 2; s >= 1; s /= 2)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], s);
+  for (int k = 0; k < K; ++k) {
+    v[k] += from_lane<0xB1>(v[k]);       // lanes 1 away
+    v[k] += from_lane<0x4E>(v[k]);       // 2 away
+    v[k] += from_lane<0x141>(v[k]);      // mirrored in eight
+    v[k] += from_lane<0x140>(v[k]);      // mirrored in sixteen
+    if constexpr (W >= kWave) v[k] = (lane_value(v[k], 0) + lane_value(v[k], 16)) + (lane_value(v[k], 32) + lane_value(v[k], 48));
+  }
   if constexpr (W > kWave) {
     constexpr int kWaves = W / kWave;
     const int wave = threadIdx.x / kWave, first = threadIdx.x / W * kWaves;
     if (threadIdx.x % kWave == 0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) lds[turn][wave][k] = v[k];
+      for (int k = 0; k < K; ++k) lds.v[turn][k][wave] = v[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      v[k] = lds[turn][first][k];
+      v[k] = lds.v[turn][k][first];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v[k] += lds[turn][first + w][k];
+      for (int w = 1; w < kWaves; ++w) v[k] += lds.v[turn][k][first + w];
     }
     turn ^= 1;
   }
 }
 
 // v normalised in place, before gain and bias; returns what it was multiplied by.
-template <class L, int W, class Lds>
-__device__ __forceinline__ float normalise(const L& row, int kind, float eps, float (&v)[L::E], Lds lds, int& turn) {
+template <class L, int W>
+__device__ __forceinline__ float normalise(const L& row, int kind, float eps, float (&v)[L::E], RowLds<W, L::R>& lds, int& turn) {
   if (kind == ILARGI_NORM_NONE) return 1.0f;
   constexpr int V = L::V, E = L::E;
   const float share = 1.0f / (float)row.m;
@@ -116,6 +143,17 @@ __device__ __forceinline__ float normalise(const L& row, int kind, float eps, fl
 
 __device__ __forceinline__ const char* row_at(const void* p, int64_t i, int64_t ld, int size) { return (const char*)p + i * ld * size; }
 
+// Keeps the compiler from holding a vector's values in 32 bits, in twice the registers, from row to row.
+template <class Raw, int P>
+__device__ __forceinline__ void as_they_are(Raw (&r)[P]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    uint4 w = __builtin_bit_cast(uint4, r[p]);
+    asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w));
+    r[p] = __builtin_bit_cast(Raw, w);
+  }
+}
+
 template <class L, int P>
 __device__ __forceinline__ void times_gain(const L& row, const void* is, const typename L::Raw (&gain)[P], float (&v)[L::E]) {
   if (is == nullptr) return;
@@ -134,11 +172,11 @@ struct NormOut {
   int64_t ld_r, ld_y;
 };
 
-template <class T, int W, int P>
+template <class T, int W, int P, int SHAPE>
 __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a, NormOut o) {
-  using L = Row<T, W, P>;
+  using L = Row<T, W, P, SHAPE>;
   constexpr int E = L::E, R = L::R, S = sizeof(T);
-  __shared__ float lds[2][R * (W < kWave ? 1 : W / kWave)][2];
+  __shared__ __attribute__((aligned(16))) RowLds<W, R> lds;
   L row;
   row.plan(a.m);
   int turn = 0;
@@ -149,7 +187,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a
   if (a.gain2 != nullptr) row.load(a.gain2, g2);
   if (a.bias2 != nullptr) row.load(a.bias2, b2);
   for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < a.n; i0 += (int64_t)gridDim.x * R) {
-    const int64_t mine = i0 + threadIdx.x / W, i = mine < a.n ? mine : a.n - 1;
+    const int64_t mine = i0 + L::slot(), i = mine < a.n ? mine : a.n - 1;
     typename L::Raw h[P], x[P];
     row.load(row_at(a.h, i, a.ld_h, S), h);
     if (a.gate_rows) row.load(row_at(a.gate, i, a.ld_gate, S), gr);
@@ -185,113 +223,182 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a
 }
 
 // t becomes the gradient of what was normalised to `unit` by the factor `by`.
-template <class L, int W, class Lds>
-__device__ __forceinline__ void normalise_back(const L& row, int kind, float by, const float (&unit)[L::E], float (&t)[L::E], Lds lds, int& turn) {
+template <class L, int W>
+__device__ __forceinline__ void normalise_back(const L& row, int kind, float by, const float (&unit)[L::E], float (&t)[L::E], RowLds<W, L::R>& lds, int& turn) {
   if (kind == ILARGI_NORM_NONE) return;
   constexpr int E = L::E;
   const float share = 1.0f / (float)row.m;
-  float s[2] = {0.0f, 0.0f};
+  if (kind == ILARGI_NORM_CENTRED) {
+    float s[2] = {0.0f, 0.0f};
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    s[0] = fmaf(t[e], unit[e], s[0]);
-    s[1] += t[e];
+    for (int e = 0; e < E; ++e) {
+      s[0] = fmaf(t[e], unit[e], s[0]);
+      s[1] += t[e];
+    }
+    row_sums<W, L::R>(s, lds, turn);
+    const float along = s[0] * share, mean = s[1] * share;
+#pragma unroll
+    for (int e = 0; e < E; ++e) t[e] = by * (fmaf(-along, unit[e], t[e]) - (row.live(e / L::V, e % L::V) ? mean : 0.0f));
+  } else {
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[0] = fmaf(t[e], unit[e], s[0]);
+    row_sums<W, L::R>(s, lds, turn);
+    const float along = s[0] * share;
+#pragma unroll
+    for (int e = 0; e < E; ++e) t[e] = by * fmaf(-along, unit[e], t[e]);
   }
-  row_sums<W, L::R>(s, lds, turn);
-  const float along = s[0] * share, mean = kind == ILARGI_NORM_CENTRED ? s[1] * share : 0.0f;
+}
+
+// f(z) in place of z, and f'(z): one exponential for both.
+template <int N>
+__device__ __forceinline__ void act_both(float (&z)[N], float (&slope)[N], int act) {
+  switch (act) {
+    case ILARGI_ACT_SIGMOID:
+    case ILARGI_ACT_SILU:
 #pragma unroll
-  for (int e = 0; e < E; ++e) t[e] = by * (fmaf(-along, unit[e], t[e]) - (row.live(e / L::V, e % L::V) ? mean : 0.0f));
+      for (int j = 0; j < N; ++j) {
+        const float e = exp_minus(z[j]), q = __builtin_amdgcn_rcpf(1.0f + e), far = e * q;        // sigmoid(|z|), sigmoid(-|z|)
+        const float p = z[j] >= 0.0f ? q : far, both = far * q;
+        if (act == ILARGI_ACT_SIGMOID) {
+          slope[j] = both;
+          z[j] = p;
+        } else {                                         // (beyond 200 both factors are 0 or 1 already: no infinity meets a 0)
+          slope[j] = fmaf(fminf(fmaxf(z[j], -200.0f), 200.0f), both, p);
+          z[j] = fmaxf(z[j], -200.0f) * p;
+        }
+      }
+      break;
+    case ILARGI_ACT_NONE:
+#pragma unroll
+      for (int j = 0; j < N; ++j) slope[j] = 1.0f;
+      break;
+    default:
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        slope[j] = act_slope(z[j], act);
+        z[j] = act_value(z[j], act);
+      }
+  }
 }
 
 struct NormGradIn {
   const void *d_r, *d_y;
   int64_t ld_dr, ld_dy;
 };
-enum { kSumGain2, kSumBias2, kSumGate, kSumGain1, kSumBias1, kSums };
+#ifndef GW
+#define GW 2
+#endif
+constexpr int kGradWaves = GW;
+enum { kSumGain1, kSumGain2, kSumGate, kSumBias1, kSumBias2, kSums };
 
-// The sums over this workgroup's rows go to partial[workgroup][sum][column].
-template <class T, int W, int P>
-__global__ __launch_bounds__(W < 256 ? 256 : W) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial) {
-  using L = Row<T, W, P>;
-  constexpr int E = L::E, R = L::R, V = L::V, S = sizeof(T);
-  __shared__ float lds[2][R * (W < kWave ? 1 : W / kWave)][2];
+// The sums over this workgroup's rows go to partial[workgroup][sum][column].  FEW: there is no bias1, and those
+// of the gains alone are wanted.  A row's data are
+// asked for as soon as those of the row before have been taken out of their registers.
+template <class T, int W, int P, int SHAPE, bool FEW>
+__global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial) {
+  using L = Row<T, W, P, SHAPE>;
+  constexpr int E = L::E, R = L::R, V = L::V, S = sizeof(T), kHeld = FEW ? 2 : kSums;
+  __shared__ __attribute__((aligned(16))) RowLds<W, R> lds;
   __shared__ float rows_sums[R > 1 ? R : 1][R > 1 ? W * E : 1];
   L row;
   row.plan(a.m);
   int turn = 0;
-  typename L::Raw g1[P], b1[P], gr[P], g2[P];
+  const bool second = a.second != ILARGI_NORM_NONE && d.d_y != nullptr, with_x = second && a.x != nullptr, gate_sum = o.d_gate != nullptr && !a.gate_rows;
+  typename L::Raw g1[P], b1[P], gr[P], g2[P], h[P], x[P], dr[P], dy[P];
+  const int64_t first = (int64_t)blockIdx.x * R + L::slot(), step = (int64_t)gridDim.x * R;
+  auto at = [&](int64_t i) { return i < a.n ? i : a.n - 1; };
+  row.load(row_at(a.h, at(first), a.ld_h, S), h);
+  if (a.gate_rows) row.load(row_at(a.gate, at(first), a.ld_gate, S), gr);
+  if (with_x) row.load(row_at(a.x, at(first), a.ld_x, S), x);
+  if (second) row.load(row_at(d.d_y, at(first), d.ld_dy, S), dy);
+  if (d.d_r != nullptr) row.load(row_at(d.d_r, at(first), d.ld_dr, S), dr);
   if (a.gain1 != nullptr) row.load(a.gain1, g1);
-  if (a.bias1 != nullptr) row.load(a.bias1, b1);
+  if (!FEW && a.bias1 != nullptr) row.load(a.bias1, b1);
   if (a.gate != nullptr && !a.gate_rows) row.load(a.gate, gr);
   if (a.gain2 != nullptr) row.load(a.gain2, g2);
-  const bool second = a.second != ILARGI_NORM_NONE, gate_sum = o.d_gate != nullptr && !a.gate_rows;
-  float sums[kSums][E];
+  float sums[kHeld][E];
 #pragma unroll
-  for (int q = 0; q < kSums; ++q)
+  for (int q = 0; q < kHeld; ++q)
 #pragma unroll
     for (int e = 0; e < E; ++e) sums[q][e] = 0.0f;
-  for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < a.n; i0 += (int64_t)gridDim.x * R) {
-    const int64_t mine = i0 + threadIdx.x / W, i = mine < a.n ? mine : a.n - 1;
+  for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < a.n; i0 += step) {
+    const int64_t mine = i0 + L::slot(), i = at(mine), next = at(mine + step);
     const bool is = mine < a.n;
-    typename L::Raw h[P], x[P], dr[P], dy[P];
-    row.load(row_at(a.h, i, a.ld_h, S), h);
-    if (a.gate_rows) row.load(row_at(a.gate, i, a.ld_gate, S), gr);
-    if (second && a.x != nullptr) row.load(row_at(a.x, i, a.ld_x, S), x);
-    if (d.d_r != nullptr) row.load(row_at(d.d_r, i, d.ld_dr, S), dr);
-    if (d.d_y != nullptr) row.load(row_at(d.d_y, i, d.ld_dy, S), dy);
+    if constexpr (V == 8) {
+      as_they_are(g1);
+      if constexpr (!FEW) as_they_are(b1);
+      as_they_are(gr);
+      as_they_are(g2);
+    }
     float unit[E];                                       // h normalised
     row.values(h, unit);
+    row.load(row_at(a.h, next, a.ld_h, S), h);
     const float by1 = normalise<L, W>(row, a.first, a.eps, unit, lds, turn);
-    float u[E], f[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) u[e] = unit[e];
-    times_gain(row, a.gain1, g1, u);
-    plus_bias(row, a.bias1, b1, u);
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = 1.0f;
+    float f[E], slope[E];
     if (a.gate != nullptr) {
       row.values(gr, f);
-      act_values(f, a.gate_act);
+      if (a.gate_rows) row.load(row_at(a.gate, next, a.ld_gate, S), gr);
+      act_both(f, slope, a.gate_act);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = 1.0f;
     }
     float t[E];                                          // the gradient on its way back: of r first
-    if (d.d_r != nullptr) row.values(dr, t);
-    else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) t[e] = 0.0f;
-    }
-    if (second && d.d_y != nullptr) {
+    if (second) {
       float r[E], back[E];
-      if (a.x != nullptr) row.values(x, r);
 #pragma unroll
-      for (int e = 0; e < E; ++e) r[e] = a.x != nullptr ? fmaf(a.scale, f[e] * u[e], r[e]) : a.scale * (f[e] * u[e]);
+      for (int e = 0; e < E; ++e) r[e] = unit[e];
+      times_gain(row, a.gain1, g1, r);
+      if constexpr (!FEW) plus_bias(row, a.bias1, b1, r);
+      if (with_x) {
+        row.values(x, back);
+        row.load(row_at(a.x, next, a.ld_x, S), x);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) r[e] = with_x ? fmaf(a.scale, f[e] * r[e], back[e]) : a.scale * (f[e] * r[e]);
       const float by2 = normalise<L, W>(row, a.second, a.eps, r, lds, turn);
       row.values(dy, back);
+      row.load(row_at(d.d_y, next, d.ld_dy, S), dy);
       if (is) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           sums[kSumGain2][e] = fmaf(back[e], r[e], sums[kSumGain2][e]);
-          sums[kSumBias2][e] += back[e];
+          if constexpr (!FEW) sums[kSumBias2][e] += back[e];
         }
       }
       times_gain(row, a.gain2, g2, back);
       normalise_back<L, W>(row, a.second, by2, r, back, lds, turn);
 #pragma unroll
-      for (int e = 0; e < E; ++e) t[e] += back[e];
+      for (int e = 0; e < E; ++e) t[e] = back[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) t[e] = 0.0f;
+    }
+    if (d.d_r != nullptr) {
+      float v[E];
+      row.values(dr, v);
+      row.load(row_at(d.d_r, next, d.ld_dr, S), dr);
+#pragma unroll
+      for (int e = 0; e < E; ++e) t[e] += v[e];
     }
     if (o.d_x != nullptr && is) row.store((char*)o.d_x + i * o.ld_x * S, t);
 #pragma unroll
     for (int e = 0; e < E; ++e) t[e] *= a.scale;
     if (o.d_gate != nullptr) {
-      float slope[E];
-      row.values(gr, slope);
+      float u[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) slope[e] = act_slope(slope[e], a.gate_act) * u[e] * t[e];
-      if (gate_sum) {
-        if (is) {
+      for (int e = 0; e < E; ++e) u[e] = unit[e];
+      times_gain(row, a.gain1, g1, u);
+      if constexpr (!FEW) plus_bias(row, a.bias1, b1, u);
 #pragma unroll
-          for (int e = 0; e < E; ++e) sums[kSumGate][e] += slope[e];
-        }
-      } else if (is) {
-        row.store((char*)o.d_gate + i * o.ld_gate * S, slope);
+      for (int e = 0; e < E; ++e) u[e] *= slope[e] * t[e];
+      if (!is) {
+      } else if (a.gate_rows) {
+        row.store((char*)o.d_gate + i * o.ld_gate * S, u);
+      } else if constexpr (!FEW) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[kSumGate][e] += u[e];
       }
     }
 #pragma unroll
@@ -300,7 +407,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_grad_kernel(ilargi_nor
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         sums[kSumGain1][e] = fmaf(t[e], unit[e], sums[kSumGain1][e]);
-        sums[kSumBias1][e] += t[e];
+        if constexpr (!FEW) sums[kSumBias1][e] += t[e];
       }
     }
     if (o.d_h == nullptr) continue;
@@ -310,9 +417,9 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_grad_kernel(ilargi_nor
   }
   if (partial == nullptr) return;
   float* const to = partial + (int64_t)blockIdx.x * kSums * a.m;
-  const void* const wanted[kSums] = {o.d_gain2, o.d_bias2, gate_sum ? o.d_gate : nullptr, o.d_gain1, o.d_bias1};
+  const void* const wanted[kSums] = {o.d_gain1, o.d_gain2, gate_sum ? o.d_gate : nullptr, o.d_bias1, o.d_bias2};
 #pragma unroll
-  for (int q = 0; q < kSums; ++q) {
+  for (int q = 0; q < kHeld; ++q) {
     if (wanted[q] == nullptr) continue;
     if constexpr (R == 1) {
 #pragma unroll
@@ -340,7 +447,7 @@ template <class T>
 __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict__ partial, int groups, int64_t m, ilargi_norm_grads_t o, int gate_sum, int accumulate) {
   __shared__ double part[16][17];
   const int c = threadIdx.x % 16, q = threadIdx.x / 16, which = blockIdx.y;
-  T* const out = (T*)(which == kSumGain2 ? o.d_gain2 : which == kSumBias2 ? o.d_bias2 : which == kSumGate ? (gate_sum ? o.d_gate : nullptr) : which == kSumGain1 ? o.d_gain1 : o.d_bias1);
+  T* const out = (T*)(which == kSumGain1 ? o.d_gain1 : which == kSumGain2 ? o.d_gain2 : which == kSumGate ? (gate_sum ? o.d_gate : nullptr) : which == kSumBias1 ? o.d_bias1 : o.d_bias2);
   if (out == nullptr) return;
   const int64_t j = (int64_t)blockIdx.x * 16 + c;
   double s = 0.0;
@@ -355,21 +462,26 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict_
   out[j] = (T)(float)(accumulate ? (double)(float)out[j] + s : s);
 }
 
-// Threads of a row and pieces of a thread: the least that hold it.
+// f(row): threads of a row and pieces of a thread, the least that hold it.
 template <class T, class F>
 hipError_t by_columns(int64_t m, F f) {
-  const int64_t pieces = (m + ElemOf<T>::kVec - 1) / ElemOf<T>::kVec;
-  auto at = [&](auto w, auto p) { return f(w, p); };
+  constexpr int V = ElemOf<T>::kVec;
+  const int64_t pieces = (m + V - 1) / V;
+  auto with = [&](auto w, auto p) {
+    constexpr int W = decltype(w)::value, P = decltype(p)::value;
+    return m % V != 0 ? f(Row<T, W, P, kRagged>()) : m == W * P * V ? f(Row<T, W, P, kFull>()) : f(Row<T, W, P, kWhole>());
+  };
   using std::integral_constant;
-  if (pieces <= 16) return at(integral_constant<int, 16>(), integral_constant<int, 1>());
-  if (pieces <= 64) return at(integral_constant<int, 64>(), integral_constant<int, 1>());
-  if (pieces <= 128) return at(integral_constant<int, 128>(), integral_constant<int, 1>());
-  if (pieces <= 256) return at(integral_constant<int, 256>(), integral_constant<int, 1>());
-  if (pieces <= 512) return at(integral_constant<int, 512>(), integral_constant<int, 1>());
-  if (pieces <= 1024) return at(integral_constant<int, 1024>(), integral_constant<int, 1>());
-  if (pieces <= 2048) return at(integral_constant<int, 1024>(), integral_constant<int, 2>());
-  if constexpr (ElemOf<T>::kVec == 4)
-    if (pieces <= 4096) return at(integral_constant<int, 1024>(), integral_constant<int, 4>());
+  constexpr integral_constant<int, 1> one;
+  if (pieces <= 16) return with(integral_constant<int, 16>(), one);
+  if (pieces <= 64) return with(integral_constant<int, 64>(), one);
+  if (pieces <= 128) return with(integral_constant<int, 128>(), one);
+  if (pieces <= 256) return with(integral_constant<int, 256>(), one);
+  if (pieces <= 512) return with(integral_constant<int, 512>(), one);
+  if (pieces <= 1024) return with(integral_constant<int, 1024>(), one);
+  if (pieces <= 2048) return with(integral_constant<int, 1024>(), integral_constant<int, 2>());
+  if constexpr (V == 4)
+    if (pieces <= 4096) return with(integral_constant<int, 1024>(), integral_constant<int, 4>());
   return hipErrorInvalidValue;
 }
 
@@ -378,13 +490,13 @@ int64_t groups_of(int64_t n, int rows, int64_t most) {
   return g < most ? g : most;
 }
 
-// Workgroups of the gradient: at most two of the larger ones fit a compute unit, and each leaves its sums behind.
+// Workgroups of the gradient: as many as are on the card at once (two of 512 threads on a compute unit), as each leaves its sums behind.
 template <class T>
 int64_t grad_groups(int64_t n, int64_t m) {
   int64_t g = 0;
-  const hipError_t e = by_columns<T>(m, [&](auto w, auto p) {
-    using L = Row<T, decltype(w)::value, decltype(p)::value>;
-    g = groups_of(n, L::R, L::NT == 256 ? 1024 : 512);
+  const hipError_t e = by_columns<T>(m, [&](auto row) {
+    using L = decltype(row);
+    g = groups_of(n, L::R, 256 * 1024 / L::NT);
     return hipSuccess;
   });
   return e == hipSuccess ? g : 0;
@@ -392,10 +504,9 @@ int64_t grad_groups(int64_t n, int64_t m) {
 
 template <class T>
 hipError_t norm_typed(const ilargi_norm_t& a, const NormOut& o, hipStream_t st) {
-  return by_columns<T>(a.m, [&](auto w, auto p) {
-    constexpr int W = decltype(w)::value, P = decltype(p)::value;
-    using L = Row<T, W, P>;
-    norm_kernel<T, W, P><<<(unsigned)groups_of(a.n, L::R, 256 * (2048 / L::NT)), L::NT, 0, st>>>(a, o);
+  return by_columns<T>(a.m, [&](auto row) {
+    using L = decltype(row);
+    norm_kernel<T, L::kW, L::kP, L::kShape><<<(unsigned)groups_of(a.n, L::R, 256 * (2048 / L::NT)), L::NT, 0, st>>>(a, o);
     return hipGetLastError();
   });
 }
@@ -404,17 +515,19 @@ template <class T>
 hipError_t norm_grad_typed(const ilargi_norm_t& a, const NormGradIn& d, const ilargi_norm_grads_t& o, int accumulate, float* partial, hipStream_t st) {
   const bool gate_sum = o.d_gate != nullptr && !a.gate_rows;
   const bool sums = gate_sum || o.d_gain1 != nullptr || o.d_bias1 != nullptr || o.d_gain2 != nullptr || o.d_bias2 != nullptr;
+  const bool few = !gate_sum && a.bias1 == nullptr && o.d_bias1 == nullptr && o.d_bias2 == nullptr;
   if (!sums) partial = nullptr;
   const int64_t groups = grad_groups<T>(a.n, a.m);
   if (groups > 0) {
-    const hipError_t e = by_columns<T>(a.m, [&](auto w, auto p) {
-      constexpr int W = decltype(w)::value, P = decltype(p)::value;
-      norm_grad_kernel<T, W, P><<<(unsigned)groups, Row<T, W, P>::NT, 0, st>>>(a, d, o, partial);
+    const hipError_t e = by_columns<T>(a.m, [&](auto row) {
+      using L = decltype(row);
+      if (few) norm_grad_kernel<T, L::kW, L::kP, L::kShape, true><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial);
+      else norm_grad_kernel<T, L::kW, L::kP, L::kShape, false><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
   }
-  if (sums) norm_join_kernel<T><<<dim3((unsigned)((a.m + 15) / 16), kSums), 256, 0, st>>>(partial, (int)groups, a.m, o, gate_sum, accumulate);
+  if (sums) norm_join_kernel<T><<<dim3((unsigned)((a.m + 15) / 16), few ? 2 : kSums), 256, 0, st>>>(partial, (int)groups, a.m, o, gate_sum, accumulate);
   return hipGetLastError();
 }
 
