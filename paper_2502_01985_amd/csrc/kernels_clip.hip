@@ -1,16 +1,17 @@
 // The norm over many tensors and the tensors scaled by it: every workgroup leaves the sum of the squares of its part, in float64; the
-// workgroups of the second pass add those sums up themselves, all in the same order, so no launch stands between the two.
+// workgroups of the second pass add those sums up themselves, all in the same order, and where they are many a workgroup does it for all.
 //
 // Tensors go sixty-four to a launch, in the launch's arguments: nothing is copied to the device before.  A workgroup takes a run of one
-// tensor's pieces of 16 bytes; a tensor whose rows follow each other counts as one row.  Bound by memory.
+// tensor's pieces of 16 bytes; a tensor whose rows follow each other counts as one row.  The second pass goes through the parts from
+// the last to the first, whose data the caches still hold.  Bound by memory.
 #include "ilargi_layers.h"
 
 namespace ilargi {
 
 namespace {
 
-constexpr int kMostTensors = 64, kMostParts = 2048, kLoads = 4;
-constexpr int64_t kLeastPart = 2048;         // pieces
+constexpr int kMostTensors = 64, kMostSums = 1024, kLoads = 4;
+constexpr int64_t kLeastPart = 2048, kMostPart = 8192;         // pieces
 
 struct Part {
   const char* in;
@@ -27,9 +28,9 @@ struct Parts {
 };
 
 // The tensor of a workgroup.
-__device__ __forceinline__ int tensor_of(const Parts& a) {
+__device__ __forceinline__ int tensor_of(const Parts& a, int group) {
   const int lane = threadIdx.x % kWave;
-  const bool before = lane < a.count && a.first[lane] <= (int)blockIdx.x;
+  const bool before = lane < a.count && a.first[lane] <= group;
   return __popcll(__ballot(before)) - 1;
 }
 
@@ -78,7 +79,7 @@ __device__ __forceinline__ double workgroup_sum(double s, double (&lds)[4]) {
 
 __global__ __launch_bounds__(256) void squares_kernel(Parts a, double* __restrict__ partial) {
   __shared__ double lds[4];
-  const int q = tensor_of(a);
+  const int q = tensor_of(a, blockIdx.x);
   const Part& t = a.t[q];
   const int64_t first = (int64_t)(blockIdx.x - a.first[q]) * a.part, last = first + a.part < t.pieces ? first + a.part : t.pieces;
   double s = 0.0;
@@ -92,21 +93,32 @@ __global__ __launch_bounds__(256) void squares_kernel(Parts a, double* __restric
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-// blockIdx: the part of a tensor; without tensors one workgroup that stores the norm.
-__global__ __launch_bounds__(256) void clip_kernel(Parts a, const double* __restrict__ partial, int sums, float max_norm, float* __restrict__ norm) {
-  __shared__ double lds[4];
+__device__ __forceinline__ double add_sums(const double* __restrict__ partial, int sums, double (&lds)[4]) {
   double s = 0.0;
 #pragma unroll 8
   for (int w = threadIdx.x; w < sums; w += 256) s += partial[w];
-  const double total = sqrt(workgroup_sum(s, lds));
+  return workgroup_sum(s, lds);
+}
+
+__global__ __launch_bounds__(256) void add_sums_kernel(const double* __restrict__ partial, int sums, double* __restrict__ to) {
+  __shared__ double lds[4];
+  const double s = add_sums(partial, sums, lds);
+  if (threadIdx.x == 0) *to = s;
+}
+
+// blockIdx: the part of a tensor, each tensor's from its last on; without tensors one workgroup that stores the norm.  `past`: what is written is larger
+// than the caches.
+__global__ __launch_bounds__(256) void clip_kernel(Parts a, const double* __restrict__ partial, int sums, float max_norm, float* __restrict__ norm, bool past) {
+  __shared__ double lds[4];
+  const double total = sqrt(add_sums(partial, sums, lds));
   if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
   if (a.count == 0) return;
   const bool scaled = total > (double)max_norm && total <= 1.7976931348623157e308;      // (no for NaN and infinity)
   const Factor2 factor = factor2(scaled ? (double)max_norm / total : 1.0);      // (a factor below 2^-126 keeps its bits)
-  const int q = tensor_of(a);
+  const int q = tensor_of(a, blockIdx.x);
   const Part& t = a.t[q];
   if (!scaled && t.in == t.out) return;
-  const int64_t first = (int64_t)(blockIdx.x - a.first[q]) * a.part, last = first + a.part < t.pieces ? first + a.part : t.pieces;
+  const int64_t first = (int64_t)(a.first[q + 1] - 1 - (int)blockIdx.x) * a.part, last = first + a.part < t.pieces ? first + a.part : t.pieces;
   auto put = [&](auto v, int valid, int64_t at) {
     using P = decltype(v);
     using T = std::remove_reference_t<decltype(v.v[0])>;
@@ -116,7 +128,10 @@ __global__ __launch_bounds__(256) void clip_kernel(Parts a, const double* __rest
       for (int j = 0; j < V; ++j) v.v[j] = (T)times((float)v.v[j], factor);
     }
     T* const to = (T*)t.out + at;
-    if (valid == V) {
+    if (valid == V && past) {
+      typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+      __builtin_nontemporal_store(__builtin_bit_cast(words, v), reinterpret_cast<words*>(to));
+    } else if (valid == V) {
       *reinterpret_cast<P*>(to) = v;
     } else {
 #pragma unroll
@@ -139,43 +154,61 @@ struct ClipPlan {
 ClipPlan clip_plan(const ilargi_tensor_t* t, int64_t count) {
   int64_t all = 0;
   for (int64_t q = 0; q < count; ++q) all += pieces_in(t[q]);
-  ClipPlan p{all / kMostParts, 0};
-  p.part = p.part < kLeastPart ? kLeastPart : (p.part + 255) / 256 * 256;
+  ClipPlan p{all / kMostSums, 0};
+  p.part = p.part < kLeastPart ? kLeastPart : p.part > kMostPart ? kMostPart : (p.part + 255) / 256 * 256;
   for (int64_t q = 0; q < count; ++q) p.groups += (pieces_in(t[q]) + p.part - 1) / p.part;
   return p;
 }
 
 }  // namespace
 
-size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)clip_plan(t, count).groups * 8; }
+size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)(clip_plan(t, count).groups + 1) * 8; }
 
 hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
   const ClipPlan plan = clip_plan(t, count);
-  bool stored = false;
-  for (int pass = 0; pass < 2; ++pass) {
-    int64_t done = 0;
-    for (int64_t q = 0; q < count;) {
-      Parts a{};
-      a.part = plan.part;
-      for (; q < count && a.count < kMostTensors; ++q) {
-        const int64_t pieces = pieces_in(t[q]);
-        if (pieces == 0 || (pass == 1 && t[q].out == nullptr)) continue;
-        const bool one = in_one_row(t[q]);
-        a.t[a.count] = {(const char*)t[q].in, (char*)t[q].out, row_pieces(t[q]), pieces, one ? t[q].rows * t[q].cols : t[q].cols, t[q].ld_in, t[q].ld_out};
-        a.bf16 |= (uint64_t)(t[q].type == ILARGI_TYPE_BF16) << a.count;
-        a.first[a.count + 1] = a.first[a.count] + (int)((pieces + plan.part - 1) / plan.part);
-        ++a.count;
-      }
-      if (a.count == 0) break;
-      const unsigned groups = (unsigned)a.first[a.count];
-      if (pass == 0) squares_kernel<<<groups, 256, 0, st>>>(a, partial + done);
-      else clip_kernel<<<groups, 256, 0, st>>>(a, partial, (int)plan.groups, max_norm, stored ? nullptr : norm);
-      stored = pass == 1;
-      done += groups;
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (plan.groups > 2147483647ll) return hipErrorInvalidValue;
+  int64_t written = 0;
+  for (int64_t q = 0; q < count; ++q)
+    if (t[q].out != nullptr && t[q].out != t[q].in) written += pieces_in(t[q]) * 16;
+  const bool past = written >= kStreamBytes;
+  auto next = [&](int64_t& q, int step, bool outputs) {                  // tensors from q on, until a launch is full
+    Parts a{};
+    a.part = plan.part;
+    for (; q >= 0 && q < count && a.count < kMostTensors; q += step) {
+      const int64_t pieces = pieces_in(t[q]);
+      if (pieces == 0 || (outputs && t[q].out == nullptr)) continue;
+      const bool one = in_one_row(t[q]);
+      a.t[a.count] = {(const char*)t[q].in, (char*)t[q].out, row_pieces(t[q]), pieces, one ? t[q].rows * t[q].cols : t[q].cols, t[q].ld_in, t[q].ld_out};
+      a.bf16 |= (uint64_t)(t[q].type == ILARGI_TYPE_BF16) << a.count;
+      a.first[a.count + 1] = a.first[a.count] + (int)((pieces + plan.part - 1) / plan.part);
+      ++a.count;
     }
+    return a;
+  };
+  int64_t done = 0;
+  for (int64_t q = 0; q < count;) {
+    const Parts a = next(q, 1, false);
+    if (a.count == 0) break;
+    squares_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, partial + done);
+    done += a.first[a.count];
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  if (!stored && norm != nullptr) clip_kernel<<<1, 256, 0, st>>>(Parts{}, partial, (int)plan.groups, max_norm, norm);
+  int sums = (int)plan.groups;
+  const double* from = partial;
+  if (sums > kMostSums) {
+    add_sums_kernel<<<1, 256, 0, st>>>(partial, sums, partial + sums);
+    from = partial + sums;
+    sums = 1;
+  }
+  bool stored = norm == nullptr;
+  for (int64_t q = count - 1; q >= 0;) {
+    const Parts a = next(q, -1, true);
+    if (a.count == 0) break;
+    clip_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, from, sums, max_norm, stored ? nullptr : norm, past);
+    stored = true;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (!stored) clip_kernel<<<1, 256, 0, st>>>(Parts{}, from, sums, max_norm, norm, false);
   return hipGetLastError();
 }
 

@@ -56,7 +56,7 @@ struct Row {
 #pragma unroll
       for (int j = 0; j < V; ++j) f[p * V + j] = live(p, j) ? (float)r[p].v[j] : 0.0f;
   }
-  __device__ __forceinline__ void store(void* row, const float (&f)[E]) const {
+  __device__ __forceinline__ void store(void* row, const float (&f)[E], bool past) const {
     T* at = (T*)row;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -64,7 +64,12 @@ struct Row {
         Raw r;
 #pragma unroll
         for (int j = 0; j < V; ++j) r.v[j] = (T)f[p * V + j];
-        *reinterpret_cast<Raw*>(at + c[p]) = r;
+        if (past) {
+          typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+          __builtin_nontemporal_store(__builtin_bit_cast(words, r), reinterpret_cast<words*>(at + c[p]));
+        } else {
+          *reinterpret_cast<Raw*>(at + c[p]) = r;
+        }
       } else if (SHAPE == kRagged) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -173,7 +178,7 @@ struct NormOut {
 };
 
 template <class T, int W, int P, int SHAPE>
-__global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a, NormOut o) {
+__global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a, NormOut o, bool past) {
   using L = Row<T, W, P, SHAPE>;
   constexpr int E = L::E, R = L::R, S = sizeof(T);
   __shared__ __attribute__((aligned(16))) RowLds<W, R> lds;
@@ -213,12 +218,12 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] *= a.scale;
     }
-    if (o.r != nullptr && mine < a.n) row.store((char*)o.r + i * o.ld_r * S, v);
+    if (o.r != nullptr && mine < a.n) row.store((char*)o.r + i * o.ld_r * S, v, past);
     if (a.second == ILARGI_NORM_NONE) continue;
     normalise<L, W>(row, a.second, a.eps, v, lds, turn);
     times_gain(row, a.gain2, g2, v);
     plus_bias(row, a.bias2, b2, v);
-    if (o.y != nullptr && mine < a.n) row.store((char*)o.y + i * o.ld_y * S, v);
+    if (o.y != nullptr && mine < a.n) row.store((char*)o.y + i * o.ld_y * S, v, past);
   }
 }
 
@@ -286,17 +291,14 @@ struct NormGradIn {
   const void *d_r, *d_y;
   int64_t ld_dr, ld_dy;
 };
-#ifndef GW
-#define GW 2
-#endif
-constexpr int kGradWaves = GW;
+constexpr int kGradWaves = 2;        // of a SIMD, at least: with 128 registers (four) a thread's values did not fit, 173 us for 132 at 8192 x 4096
 enum { kSumGain1, kSumGain2, kSumGate, kSumBias1, kSumBias2, kSums };
 
 // The sums over this workgroup's rows go to partial[workgroup][sum][column].  FEW: there is no bias1, and those
 // of the gains alone are wanted.  A row's data are
 // asked for as soon as those of the row before have been taken out of their registers.
 template <class T, int W, int P, int SHAPE, bool FEW>
-__global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial) {
+__global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial, bool past) {
   using L = Row<T, W, P, SHAPE>;
   constexpr int E = L::E, R = L::R, V = L::V, S = sizeof(T), kHeld = FEW ? 2 : kSums;
   __shared__ __attribute__((aligned(16))) RowLds<W, R> lds;
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
 #pragma unroll
       for (int e = 0; e < E; ++e) t[e] += v[e];
     }
-    if (o.d_x != nullptr && is) row.store((char*)o.d_x + i * o.ld_x * S, t);
+    if (o.d_x != nullptr && is) row.store((char*)o.d_x + i * o.ld_x * S, t, past);
 #pragma unroll
     for (int e = 0; e < E; ++e) t[e] *= a.scale;
     if (o.d_gate != nullptr) {
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
       for (int e = 0; e < E; ++e) u[e] *= slope[e] * t[e];
       if (!is) {
       } else if (a.gate_rows) {
-        row.store((char*)o.d_gate + i * o.ld_gate * S, u);
+        row.store((char*)o.d_gate + i * o.ld_gate * S, u, past);
       } else if constexpr (!FEW) {
 #pragma unroll
         for (int e = 0; e < E; ++e) sums[kSumGate][e] += u[e];
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
     if (o.d_h == nullptr) continue;
     times_gain(row, a.gain1, g1, t);
     normalise_back<L, W>(row, a.first, by1, unit, t, lds, turn);
-    if (is) row.store((char*)o.d_h + i * o.ld_h * S, t);
+    if (is) row.store((char*)o.d_h + i * o.ld_h * S, t, past);
   }
   if (partial == nullptr) return;
   float* const to = partial + (int64_t)blockIdx.x * kSums * a.m;
@@ -490,13 +492,14 @@ int64_t groups_of(int64_t n, int rows, int64_t most) {
   return g < most ? g : most;
 }
 
-// Workgroups of the gradient: as many as are on the card at once (two of 512 threads on a compute unit), as each leaves its sums behind.
+// Workgroups of the gradient: as many as are on the card at once, three of 256 threads or one larger on a compute unit, as each leaves its
+// sums behind.  (8192 x 4096, bfloat16: 256 of them 125 us, 512 129, 1024 140; 100,000 x 220: 768 109, 1024 113, 2048 118.)
 template <class T>
 int64_t grad_groups(int64_t n, int64_t m) {
   int64_t g = 0;
   const hipError_t e = by_columns<T>(m, [&](auto row) {
     using L = decltype(row);
-    g = groups_of(n, L::R, 256 * 1024 / L::NT);
+    g = groups_of(n, L::R, L::NT == 256 ? 768 : 256);
     return hipSuccess;
   });
   return e == hipSuccess ? g : 0;
@@ -504,9 +507,10 @@ int64_t grad_groups(int64_t n, int64_t m) {
 
 template <class T>
 hipError_t norm_typed(const ilargi_norm_t& a, const NormOut& o, hipStream_t st) {
+  const bool past = (int64_t)sizeof(T) * a.n * a.m * ((o.r != nullptr) + (o.y != nullptr)) >= kStreamBytes;
   return by_columns<T>(a.m, [&](auto row) {
     using L = decltype(row);
-    norm_kernel<T, L::kW, L::kP, L::kShape><<<(unsigned)groups_of(a.n, L::R, 256 * (2048 / L::NT)), L::NT, 0, st>>>(a, o);
+    norm_kernel<T, L::kW, L::kP, L::kShape><<<(unsigned)groups_of(a.n, L::R, 256 * (2048 / L::NT)), L::NT, 0, st>>>(a, o, past);
     return hipGetLastError();
   });
 }
@@ -515,14 +519,15 @@ template <class T>
 hipError_t norm_grad_typed(const ilargi_norm_t& a, const NormGradIn& d, const ilargi_norm_grads_t& o, int accumulate, float* partial, hipStream_t st) {
   const bool gate_sum = o.d_gate != nullptr && !a.gate_rows;
   const bool sums = gate_sum || o.d_gain1 != nullptr || o.d_bias1 != nullptr || o.d_gain2 != nullptr || o.d_bias2 != nullptr;
+  const bool past = (int64_t)sizeof(T) * a.n * a.m * ((o.d_h != nullptr) + (o.d_x != nullptr) + (o.d_gate != nullptr && a.gate_rows)) >= kStreamBytes;
   const bool few = !gate_sum && a.bias1 == nullptr && o.d_bias1 == nullptr && o.d_bias2 == nullptr;
   if (!sums) partial = nullptr;
   const int64_t groups = grad_groups<T>(a.n, a.m);
   if (groups > 0) {
     const hipError_t e = by_columns<T>(a.m, [&](auto row) {
       using L = decltype(row);
-      if (few) norm_grad_kernel<T, L::kW, L::kP, L::kShape, true><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial);
-      else norm_grad_kernel<T, L::kW, L::kP, L::kShape, false><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial);
+      if (few) norm_grad_kernel<T, L::kW, L::kP, L::kShape, true><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial, past);
+      else norm_grad_kernel<T, L::kW, L::kP, L::kShape, false><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial, past);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
