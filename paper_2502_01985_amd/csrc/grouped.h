@@ -6,8 +6,11 @@
 
 namespace ilargi {
 
-// What one launch works out of the offsets for all others.  A prefix p has p[q] <= u < p[q + 1] for the units u of place q.
+// Up to 64 groups every wavefront works out of the offsets itself where they lie, a group a lane: no launch stands before the products
+// (it took 3 to 8 us).  With more, one launch does it for all others and leaves:
 struct GroupIndex {
+  const int32_t* offsets;
+  int groups, n;
   int* start;       // groups + 1: first rows, ascending, in [0, n]
   int* tiles;       // prefix of the blocks of rows of every group
   int* order;       // groups by their rows, the longest first (up to kMostSorted groups; else as they come)
@@ -15,14 +18,14 @@ struct GroupIndex {
   int* slots;       // prefix, in that order, of those of groups of several parts
   int* chunks;      // prefix of the chunks of rows of the column sums
 };
-constexpr int kMostSorted = 512;
+constexpr int kMostSorted = 512, kMostInLanes = kWave;
+// (a prefix p has p[q] <= u < p[q + 1] for the units u of place q)
 
 // Products of the rows of every group with its own matrix.  P's rows and the result's are the groups'; Q's matrices are far_q elements apart.
 template <class Prod>
 struct GroupedRows {
   Prod p;                     // M = n
   GroupIndex at;
-  int groups;
   int64_t far_q, far_bias;    // elements
   int64_t share;              // of k, in the block's units
   float* partial;             // shares of n x (N to a multiple of 4) where k is split
@@ -32,11 +35,26 @@ template <class Prod>
 struct GroupedSums {
   Prod p;                     // K = n
   GroupIndex at;
-  int groups;
   int64_t far_out;
   int part;                   // rows
   float* partial;             // M x (N to a multiple of 4) a slot
 };
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+// Over the lanes up to this one, of values that are not negative: their sum or the largest.
+template <bool MOST>
+__device__ __forceinline__ int scan_lanes(int v) {
+  auto take = [&](int o) { v = MOST ? (v > o ? v : o) : v + o; };
+  take(from_lane<0x111, 0xf>(v));       // 1, 2, 4 and 8 lanes before, in sixteen
+  take(from_lane<0x112, 0xf>(v));
+  take(from_lane<0x114, 0xf>(v));
+  take(from_lane<0x118, 0xf>(v));
+  take(from_lane<0x142, 0xa>(v));       // the last of the sixteen before
+  take(from_lane<0x143, 0xc>(v));       // ... of the thirty-two before
+  return v;
+}
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
 // The place of unit u in a prefix of n places: the last one that begins at or before it.  A wavefront looks at 64 places at a time.
 __device__ __forceinline__ int place_of(const int* __restrict__ prefix, int n, int u) {
@@ -50,6 +68,99 @@ __device__ __forceinline__ int place_of(const int* __restrict__ prefix, int n, i
   }
   return __builtin_amdgcn_readfirstlane(lo);
 }
+
+// The groups' first rows and their ends, a group a lane.
+struct Lanes {
+  int start, end;
+  __device__ __forceinline__ explicit Lanes(const GroupIndex& at) {
+    const int lane = threadIdx.x % kWave;
+    auto inside = [&](int v) { return v < 0 ? 0 : v > at.n ? at.n : v; };
+    const bool is = lane < at.groups;
+    const int v = is ? inside(at.offsets[lane]) : 0, next = is ? inside(at.offsets[lane + 1]) : 0;
+    start = scan_lanes<true>(v);                  // (an offset below an earlier one counts as that)
+    end = next > start ? next : start;
+  }
+};
+__device__ __forceinline__ bool in_lanes(const GroupIndex& at) { return at.groups <= kMostInLanes; }
+__device__ __forceinline__ int blocks_of_rows(int rows, int size) { return (int)(((uint32_t)rows + (uint32_t)size - 1) / (uint32_t)size); }
+
+// Where unit u of a launch lies: its group, the group's rows, and which of the group's units it is.
+struct Unit {
+  int group, first, rows, number;
+};
+// Blocks of `size` rows of every group; `prefix` where the groups are not in lanes.
+struct Blocks {
+  const GroupIndex& at;
+  const int* prefix;
+  int start, end, before, total;
+  __device__ __forceinline__ Blocks(const GroupIndex& at, const int* prefix, int size) : at(at), prefix(prefix) {
+    if (in_lanes(at)) {
+      const Lanes l(at);
+      const int mine = blocks_of_rows(l.end - l.start, size), upto = scan_lanes<false>(mine);
+      start = l.start; end = l.end; before = upto - mine;
+      total = lane_value(upto, kWave - 1);
+    } else {
+      start = end = before = 0;
+      total = prefix[at.groups];
+    }
+  }
+  __device__ __forceinline__ Unit find(int u) const {
+    if (in_lanes(at)) {
+      const int g = __popcll(__ballot((int)(threadIdx.x % kWave) < at.groups && before <= u)) - 1, first = lane_value(start, g);
+      return {g, first, lane_value(end, g) - first, u - lane_value(before, g)};
+    }
+    const int g = place_of(prefix, at.groups, u), first = at.start[g];
+    return {g, first, at.start[g + 1] - first, u - prefix[g]};
+  }
+  // the first unit of a group, and that of the next
+  __device__ __forceinline__ void of_group(int g, int* first, int* end) const {
+    *first = in_lanes(at) ? lane_value(before, g) : prefix[g];
+    *end = !in_lanes(at) ? prefix[g + 1] : g + 1 < at.groups ? lane_value(before, g + 1) : total;
+  }
+};
+
+// Parts of `size` rows, the longest groups first, one at least of every group; those of groups of several have a slot each.
+struct Parts {
+  const GroupIndex& at;
+  int start, end, group, before, slot, total;       // of the place that is this lane
+  __device__ __forceinline__ Parts(const GroupIndex& at, int size) : at(at) {
+    if (in_lanes(at)) {
+      const Lanes l(at);
+      const int lane = threadIdx.x % kWave, mine = l.end - l.start;
+      int place = 0;
+      for (int o = 0; o < at.groups; ++o) {
+        const int other = lane_value(mine, o);
+        place += other > mine || (other == mine && o < lane);
+      }
+      if (lane >= at.groups) place = lane;
+      group = __builtin_amdgcn_ds_permute(place * 4, lane);
+      start = __shfl(l.start, group);
+      end = __shfl(l.end, group);
+      const int b = blocks_of_rows(end - start, size), parts = lane < at.groups ? (b > 1 ? b : 1) : 0, held = parts > 1 ? parts : 0;
+      const int upto = scan_lanes<false>(parts);
+      before = upto - parts;
+      slot = scan_lanes<false>(held) - held;
+      total = lane_value(upto, kWave - 1);
+    } else {
+      start = end = group = before = slot = 0;
+      total = at.parts[at.groups];
+    }
+  }
+  struct Place {
+    int group, first, end, parts, slot, number;
+  };
+  __device__ __forceinline__ Place place(int q, int u) const {
+    if (in_lanes(at)) {
+      const int b = lane_value(before, q), next = q + 1 < at.groups ? lane_value(before, q + 1) : total;
+      return {lane_value(group, q), lane_value(start, q), lane_value(end, q), next - b, lane_value(slot, q), u - b};
+    }
+    const int g = at.order[q], b = at.parts[q];
+    return {g, at.start[g], at.start[g + 1], at.parts[q + 1] - b, at.slots[q], u - b};
+  }
+  __device__ __forceinline__ Place find(int u) const {
+    return place(in_lanes(at) ? __popcll(__ballot((int)(threadIdx.x % kWave) < at.groups && before <= u)) - 1 : place_of(at.parts, at.groups, u), u);
+  }
+};
 
 template <class T>
 __device__ __forceinline__ void move_to(T*& p, int64_t elements, int size) {
@@ -82,27 +193,27 @@ __device__ __forceinline__ Prod sums_of(const GroupedSums<Prod>& a, int g, int64
 
 // run(product, block of rows, block of columns, sums_to) for block `id` of a launch of rows, `tn` blocks of columns.
 template <int SIZE, class Prod, class F>
-__device__ __forceinline__ void grouped_rows_block(const GroupedRows<Prod>& a, int id, int tn, F run) {
-  const int tm = a.at.tiles[a.groups];
-  if (id >= tm * tn) return;
+__device__ __forceinline__ void grouped_rows_block(const GroupedRows<Prod>& a, int id, int tile, int tn, F run) {
+  const Blocks blocks(a.at, a.at.tiles, tile);
+  if (id >= blocks.total * tn) return;
   int u, tj;
-  block_of(id, tm, tn, &u, &tj);
-  const int g = place_of(a.at.tiles, a.groups, u);
-  const int64_t r0 = a.at.start[g], rows = a.at.start[g + 1] - r0;
-  float* to = a.partial != nullptr ? a.partial + ((int64_t)blockIdx.z * a.p.M + r0) * ((a.p.N + 3) / 4 * 4) : nullptr;
-  run(rows_of(a, g, r0, rows, SIZE), u - a.at.tiles[g], tj, to);
+  block_of(id, blocks.total, tn, &u, &tj);
+  const Unit b = blocks.find(u);
+  float* to = a.partial != nullptr ? a.partial + ((int64_t)blockIdx.z * a.p.M + b.first) * ((a.p.N + 3) / 4 * 4) : nullptr;
+  run(rows_of(a, b.group, b.first, b.rows, SIZE), b.number, tj, to);
 }
 template <int SIZE, class Prod, class F>
 __device__ __forceinline__ void grouped_sums_block(const GroupedSums<Prod>& a, int id, int tm, int tn, F run) {
+  const Parts parts(a.at, a.part);
   const int u = id / (tm * tn);
-  if (u >= a.at.parts[a.groups]) return;
+  if (u >= parts.total) return;
   int ti, tj;
   block_of(id - u * (tm * tn), tm, tn, &ti, &tj);
-  const int q = place_of(a.at.parts, a.groups, u), g = a.at.order[q], c = u - a.at.parts[q];
-  const int64_t r0 = a.at.start[g] + (int64_t)c * a.part, end = a.at.start[g + 1], rows = end - r0 < a.part ? end - r0 : a.part;
+  const Parts::Place q = parts.find(u);
+  const int64_t r0 = q.first + (int64_t)q.number * a.part, rows = q.end - r0 < a.part ? q.end - r0 : a.part;
   if (rows == 0 && a.p.epi.src != nullptr) return;         // nothing to add
-  float* to = a.at.parts[q + 1] - a.at.parts[q] > 1 ? a.partial + (int64_t)(a.at.slots[q] + c) * a.p.M * ((a.p.N + 3) / 4 * 4) : nullptr;
-  run(sums_of(a, g, r0, rows, SIZE), ti, tj, to);
+  float* to = q.parts > 1 ? a.partial + (int64_t)(q.slot + q.number) * a.p.M * ((a.p.N + 3) / 4 * 4) : nullptr;
+  run(sums_of(a, q.group, r0, rows, SIZE), ti, tj, to);
 }
 
 hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int64_t tiles, int splits, hipStream_t st);

@@ -1,6 +1,12 @@
 // Layers by group of rows: the index of the groups, products in float32, the elementwise pass of the gradient, the sums of parts, and
 // what runs where.
 #include "grouped.h"
+#ifndef AIM
+#define AIM 256
+#endif
+#ifndef FEWAIM
+#define FEWAIM 256
+#endif
 #include "mm_f32_block.h"
 
 namespace ilargi {
@@ -50,13 +56,14 @@ __device__ __forceinline__ void write_prefix(int* __restrict__ to, int n, Scan& 
 }
 
 // One workgroup.  tile, part, chunk: rows of a block, a part, a chunk; 0 where the call has no use for them.
-__global__ __launch_bounds__(kIndexThreads) void group_index_kernel(const int32_t* __restrict__ offsets, int groups, int n, GroupIndex at, int tile, int part, int chunk) {
+__global__ __launch_bounds__(kIndexThreads) void group_index_kernel(GroupIndex at, int tile, int part, int chunk) {
+  const int groups = at.groups, n = at.n;
   __shared__ Scan lds;
   __shared__ int sizes[kMostSorted];
   int most = 0;                                // the largest offset so far: a later one below it counts as that
   for (int q0 = 0; q0 <= groups; q0 += kIndexThreads) {
     const int q = q0 + threadIdx.x;
-    int v = q <= groups ? offsets[q] : 0;
+    int v = q <= groups ? at.offsets[q] : 0;
     v = v < 0 ? 0 : v > n ? n : v;
     int all;
     v = scan_of<true>(v, lds, &all);
@@ -92,7 +99,7 @@ __global__ __launch_bounds__(kIndexThreads) void group_index_kernel(const int32_
 template <class T, bool QK, int TILE, int STEP>
 __global__ __launch_bounds__(256) void grouped_rows_kernel(GroupedRows<Product> a, int first, int tn) {
   __shared__ __attribute__((aligned(16))) MmF32Lds<TILE, STEP> lds;
-  grouped_rows_block<sizeof(T)>(a, first + blockIdx.x, tn, [&](const Product& b, int ti, int tj, float* to) {
+  grouped_rows_block<sizeof(T)>(a, first + blockIdx.x, TILE, tn, [&](const Product& b, int ti, int tj, float* to) {
     mm_f32_block<T, T, false, QK, TILE, STEP>(b, ti, tj, 0, blockIdx.z, a.share, to, lds);
   });
 }
@@ -130,16 +137,26 @@ hipError_t sums_f32(const GroupedSums<Product>& a, int tile, int64_t parts, hipS
 
 // ------------------------------------------------------------------------------------------------------------ sums of parts
 // Adds the shares of k and finishes, a thread for four sums of a row (from workgroup `first` on); rows of no group are left alone.
-__global__ __launch_bounds__(256) void grouped_rows_join_kernel(Epilogue epi, int64_t N, int64_t n, const int* __restrict__ start, int groups, int64_t far_bias, int64_t first,
-                                                                int splits, const float* __restrict__ partial) {
-  const int64_t quads = (N + 3) / 4, at = (first + blockIdx.x) * 256 + threadIdx.x, i = at / quads, j = (at - i * quads) * 4;
-  if (i < start[0] || i >= start[groups]) return;
-  int lo = 0, hi = groups;                       // start[lo] <= i < start[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (start[mid] <= i) lo = mid;
-    else hi = mid;
+__global__ __launch_bounds__(256) void grouped_rows_join_kernel(Epilogue epi, int64_t N, GroupIndex at, int64_t far_bias, int64_t first, int splits, const float* __restrict__ partial) {
+  const int64_t quads = (N + 3) / 4, e = (first + blockIdx.x) * 256 + threadIdx.x, i = e / quads, j = (e - i * quads) * 4;
+  int lo = 0, hi = at.groups;                    // start[lo] <= i < start[hi]
+  bool is;
+  if (in_lanes(at)) {
+    const Lanes l(at);
+    is = i >= lane_value(l.start, 0) && i < lane_value(l.end, at.groups - 1);
+    for (int s = kWave / 2; s > 0; s /= 2) {
+      const int mid = lo + s, from = __shfl(l.start, mid);       // (lo is below 64 - s)
+      if (mid < at.groups && from <= i) lo = mid;
+    }
+  } else {
+    is = i >= at.start[0] && i < at.start[at.groups];
+    while (is && hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (at.start[mid] <= i) lo = mid;
+      else hi = mid;
+    }
   }
+  if (!is) return;
   move_to(epi.bias, lo * far_bias, epi.out_bf16 ? 2 : 4);
   const int valid = N - j < 4 ? (int)(N - j) : 4;
   const SrcQuad raw = epilogue_ask(epi, 0, i, j, valid);
@@ -148,23 +165,23 @@ __global__ __launch_bounds__(256) void grouped_rows_join_kernel(Epilogue epi, in
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int z = 0; z < splits; ++z) {
-    const float4 t = *reinterpret_cast<const float4*>(partial + ((int64_t)z * n + i) * quads * 4 + j);
+    const float4 t = *reinterpret_cast<const float4*>(partial + ((int64_t)z * at.n + i) * quads * 4 + j);
     v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
   }
   epilogue4(epi, 1.0f, 0, i, j, valid, bias, raw, v);
 }
 
 // blockIdx: four sums a thread (from workgroup `first` on), place of the group.
-__global__ __launch_bounds__(256) void grouped_sums_join_kernel(Epilogue epi, int64_t M, int64_t N, GroupIndex at, int64_t far_out, int64_t first, const float* __restrict__ partial) {
-  const int q = blockIdx.y, parts = at.parts[q + 1] - at.parts[q];
+__global__ __launch_bounds__(256) void grouped_sums_join_kernel(Epilogue epi, int64_t M, int64_t N, GroupIndex at, int part, int64_t far_out, int64_t first, const float* __restrict__ partial) {
+  const Parts::Place q = Parts(at, part).place(blockIdx.y, 0);
+  const int parts = q.parts, size = epi.out_bf16 ? 2 : 4;
   const int64_t quads = (N + 3) / 4, e = (first + blockIdx.x) * 256 + threadIdx.x, i = e / quads, j = (e - i * quads) * 4;
   if (parts < 2 || i >= M) return;
-  const int g = at.order[q], size = epi.out_bf16 ? 2 : 4;
-  move_to(epi.src, g * far_out, size);
-  move_to(epi.out, g * far_out, size);
+  move_to(epi.src, q.group * far_out, size);
+  move_to(epi.out, q.group * far_out, size);
   const int valid = N - j < 4 ? (int)(N - j) : 4;
   const SrcQuad raw = epilogue_ask(epi, 0, i, j, valid);
-  const float* p = partial + ((int64_t)at.slots[q] * M + i) * quads * 4 + j;
+  const float* p = partial + ((int64_t)q.slot * M + i) * quads * 4 + j;
   const float none[4] = {0.f, 0.f, 0.f, 0.f};
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -179,7 +196,7 @@ __global__ __launch_bounds__(256) void grouped_sums_join_kernel(Epilogue epi, in
 struct GroupedGrad {
   LayerGradArgs g;
   GroupIndex at;
-  int groups, chunk;
+  int chunk;
   int64_t ld_dbias;
   float* partial;        // m sums a chunk
 };
@@ -190,12 +207,13 @@ template <class T>
 __global__ __launch_bounds__(256) void grouped_grad_kernel(GroupedGrad a, int64_t first, int first_chunk) {
   __shared__ float4 part[8][32];
   const int u = first_chunk + blockIdx.y;
-  if (u >= a.at.chunks[a.groups]) return;
+  const Blocks chunks(a.at, a.at.chunks, a.chunk);
+  if (u >= chunks.total) return;
   const LayerGradArgs& y = a.g;
-  const int g = place_of(a.at.chunks, a.groups, u);
+  const Unit b = chunks.find(u);
   const int cl = threadIdx.x % 32, rl = threadIdx.x / 32;
   const int64_t j = ((first + blockIdx.x) * 32 + cl) * 4;
-  const int64_t r0 = a.at.start[g] + (int64_t)(u - a.at.chunks[g]) * a.chunk, end = a.at.start[g + 1], r1 = end - r0 < a.chunk ? end : r0 + a.chunk;
+  const int64_t r0 = b.first + (int64_t)b.number * a.chunk, end = (int64_t)b.first + b.rows, r1 = end - r0 < a.chunk ? end : r0 + a.chunk;
   const int valid = (int)(y.m - j < 0 ? 0 : y.m - j < 4 ? y.m - j : 4);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   if (valid > 0 || (y.dz != nullptr && j < y.ld_dz)) {
@@ -235,9 +253,11 @@ __global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_
   const int c = threadIdx.x % 16, q = threadIdx.x / 16, g = blockIdx.y;
   const int64_t j = (first + blockIdx.x) * 16 + c, m = a.g.m;
   double s = 0.0;
+  int first_chunk, end_chunk;
+  Blocks(a.at, a.at.chunks, a.chunk).of_group(g, &first_chunk, &end_chunk);
   if (j < m) {
 #pragma unroll 4
-    for (int u = a.at.chunks[g] + q; u < a.at.chunks[g + 1]; u += 16) s += a.partial[(int64_t)u * m + j];
+    for (int u = first_chunk + q; u < end_chunk; u += 16) s += a.partial[(int64_t)u * m + j];
   }
   part[q][c] = s;
   __syncthreads();
@@ -291,6 +311,15 @@ RowsPlan rows_plan(const ilargi_groups_t& y, int64_t N, int64_t K, bool h) {
   RowsPlan best{};
   double least = 1e300;
   const double some = (double)filled(y), each = (double)y.n / (some > 0 ? some : 1.0);
+  if (h && each <= 24.0) {
+    const int64_t blocks = filled(y) * blocks_in(N, 64), steps = K > 64 ? blocks_in(K, 64) : 1;
+    int64_t splits = blocks > 0 ? FEWAIM / blocks : 1;
+    if (splits > steps / 8) splits = steps / 8;
+    if (splits < 1) splits = 1;
+    const int64_t share = blocks_in(steps, splits);
+    splits = blocks_in(steps, share);
+    return {32, (int)splits, share, y.n / 32 + filled(y), splits > 1 ? (size_t)splits * (size_t)y.n * (size_t)up4(N) * 4 : 0};
+  }
   for (int tile = h ? 256 : 128; tile >= (h ? 128 : 64); tile /= 2) {
     const double rows = some * (each > 0.5 * tile ? each / tile + 0.5 : 1.0), blocks = rows * (double)blocks_in(N, tile);
     const int64_t step = h ? 64 : tile == 64 ? 32 : 16, steps = K > step ? blocks_in(K, step) : 1;
@@ -332,7 +361,7 @@ SumsPlan sums_plan(const ilargi_groups_t& y, bool h) {
   auto blocks = [&](int t) { return blocks_in(y.k, t) * blocks_in(y.m, t); };
   if (blocks(tile) * filled(y) < 512) tile = least;
   p.tile = tile;
-  const int64_t aim = 1024 / blocks(tile);       // parts that fill it
+  const int64_t aim = AIM / blocks(tile);       // parts that fill it
   int64_t rows = aim > 1 ? blocks_in(y.n, aim) : y.n;
   rows = rows < 256 ? 256 : (rows + 63) / 64 * 64;
   p.part = (int)(rows < (1 << 30) ? rows : 1 << 30);
@@ -377,10 +406,16 @@ GroupedLayout grouped_layout(const ilargi_groups_t& y) {
   l.gradient = l.shares + (dx > dw ? dx : dw);
   return l;
 }
-GroupIndex index_in(char* ws, int64_t groups) {
+GroupIndex index_in(char* ws, const ilargi_groups_t& y, const int32_t* offsets) {
   int* p = (int*)ws;
-  const int64_t far = groups + 1;
-  return {p, p + far, p + 2 * far, p + 3 * far, p + 4 * far, p + 5 * far};
+  const int64_t far = y.groups + 1;
+  return {offsets, (int)y.groups, (int)y.n, p, p + far, p + 2 * far, p + 3 * far, p + 4 * far, p + 5 * far};
+}
+
+hipError_t find_groups(const GroupIndex& at, int tile, int part, int chunk, hipStream_t st) {
+  if (at.groups <= kMostInLanes) return hipSuccess;
+  group_index_kernel<<<1, kIndexThreads, 0, st>>>(at, tile, part, chunk);
+  return hipGetLastError();
 }
 
 // A matrix, or the matrices of all groups, as they lie or laid out in whole pieces (then with zeros behind their rows).
@@ -412,7 +447,7 @@ hipError_t rows_product(const ilargi_groups_t& y, const Held& P, const Held& Q, 
     a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1; a.p.kind = kMm16Bf16;
     a.p.epi = epi;
     a.p.past = part == nullptr && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
-    a.at = at; a.groups = (int)y.groups; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
+    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
     e = launch_grouped16_rows(a, plan.tile, plan.tiles, plan.splits, st);
   } else {
     GroupedRows<Product> a{};
@@ -420,12 +455,12 @@ hipError_t rows_product(const ilargi_groups_t& y, const Held& P, const Held& Q, 
     a.p.Q = {Q.p, Q.ld, q_rows, bf16, 0};
     a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1;
     a.p.epi = epi;
-    a.at = at; a.groups = (int)y.groups; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
+    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
     e = bf16 ? rows_f32<bf16_t>(a, plan.tile, plan.tiles, plan.splits, st) : rows_f32<float>(a, plan.tile, plan.tiles, plan.splits, st);
   }
   if (e != hipSuccess || part == nullptr) return e;
   return in_parts(blocks_in(y.n * (up4(N) / 4), 256), 256, [&](int64_t first, unsigned blocks) {
-    grouped_rows_join_kernel<<<blocks, 256, 0, st>>>(epi, N, y.n, at.start, (int)y.groups, far_bias, first, plan.splits, part);
+    grouped_rows_join_kernel<<<blocks, 256, 0, st>>>(epi, N, at, far_bias, first, plan.splits, part);
   });
 }
 
@@ -439,7 +474,7 @@ hipError_t sums_product(const ilargi_groups_t& y, const Held& P, const Held& Q, 
     a.p.Q = {Q.p, Q.ld, 1, 0, 0, up8(Q.cols)};
     a.p.M = y.k; a.p.N = y.m; a.p.K = y.n; a.p.batches = 1; a.p.kind = kMm16Bf16;
     a.p.epi = epi;
-    a.at = at; a.groups = (int)y.groups; a.far_out = far_out; a.part = plan.part; a.partial = partial;
+    a.at = at; a.far_out = far_out; a.part = plan.part; a.partial = partial;
     e = launch_grouped16_sums(a, plan.tile, plan.parts, st);
   } else {
     GroupedSums<Product> a{};
@@ -447,14 +482,14 @@ hipError_t sums_product(const ilargi_groups_t& y, const Held& P, const Held& Q, 
     a.p.Q = {Q.p, Q.ld, 1, bf16, 0};
     a.p.M = y.k; a.p.N = y.m; a.p.K = y.n; a.p.batches = 1;
     a.p.epi = epi;
-    a.at = at; a.groups = (int)y.groups; a.far_out = far_out; a.part = plan.part; a.partial = partial;
+    a.at = at; a.far_out = far_out; a.part = plan.part; a.partial = partial;
     e = bf16 ? sums_f32<bf16_t>(a, plan.tile, plan.parts, st) : sums_f32<float>(a, plan.tile, plan.parts, st);
   }
   if (e != hipSuccess || plan.several == 0) return e;
   // (the longest groups come first, where they are sorted)
   const unsigned places = (unsigned)(y.groups <= kMostSorted ? plan.several : y.groups);
   return in_parts(blocks_in(y.k * (up4(y.m) / 4), 256), 256, [&](int64_t first, unsigned blocks) {
-    grouped_sums_join_kernel<<<dim3(blocks, places), 256, 0, st>>>(epi, y.k, y.m, at, far_out, first, partial);
+    grouped_sums_join_kernel<<<dim3(blocks, places), 256, 0, st>>>(epi, y.k, y.m, at, plan.part, far_out, first, partial);
   });
 }
 
@@ -474,14 +509,13 @@ void grouped_bytes(const ilargi_groups_t& y, size_t* forward, size_t* gradient) 
 hipError_t launch_grouped(const GroupedArgs& a, char* ws, hipStream_t st) {
   const ilargi_groups_t& y = a.y;
   const GroupedLayout l = grouped_layout(y);
-  const GroupIndex at = index_in(ws, y.groups);
+  const GroupIndex at = index_in(ws, y, a.offsets);
   Held x{a.X, a.ld_x, y.n, y.k, 0, false}, w{a.W, a.ld_w, y.k, y.m, a.stride_w, false};
   if (hipError_t e = lay_out(y, &x, 1, ws + l.x, st); e != hipSuccess) return e;
   if (hipError_t e = lay_out(y, &w, y.groups, ws + l.w, st); e != hipSuccess) return e;
   const bool h16 = y.type == ILARGI_TYPE_BF16 && in_pieces(x) && in_pieces(w);
   const RowsPlan plan = rows_plan(y, y.m, y.k, h16);
-  group_index_kernel<<<1, kIndexThreads, 0, st>>>(a.offsets, (int)y.groups, (int)y.n, at, plan.tile, 0, 0);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (hipError_t e = find_groups(at, plan.tile, 0, 0, st); e != hipSuccess) return e;
   Epilogue epi{};
   epi.mode = kEpiLinear;
   epi.bias = a.bias; epi.src = a.residual; epi.ld_src = a.ld_res; epi.src_bf16 = y.type == ILARGI_TYPE_BF16;
@@ -493,7 +527,7 @@ hipError_t launch_grouped(const GroupedArgs& a, char* ws, hipStream_t st) {
 hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   const ilargi_groups_t& y = a.y;
   const GroupedLayout l = grouped_layout(y);
-  const GroupIndex at = index_in(ws, y.groups);
+  const GroupIndex at = index_in(ws, y, a.offsets);
   const int bf16 = y.type == ILARGI_TYPE_BF16;
   const bool bent = y.act != ILARGI_ACT_NONE, products = a.d_X != nullptr || a.d_W != nullptr;
   Held x{a.X, a.ld_x, y.n, y.k, 0, false}, w{a.W, a.ld_w, y.k, y.m, a.stride_w, false}, z{a.d_out, a.ld_dout, y.n, y.m, 0, false};
@@ -511,12 +545,11 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   const SumsPlan sums = sums_plan(y, sums16);
   const int chunk = chunk_rows(y);
   const bool passes = dz != nullptr || a.d_bias != nullptr;
-  group_index_kernel<<<1, kIndexThreads, 0, st>>>(a.offsets, (int)y.groups, (int)y.n, at, a.d_X != nullptr ? rows.tile : 0, a.d_W != nullptr ? sums.part : 0, passes ? chunk : 0);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (hipError_t e = find_groups(at, a.d_X != nullptr ? rows.tile : 0, a.d_W != nullptr ? sums.part : 0, passes ? chunk : 0, st); e != hipSuccess) return e;
   if (passes) {
     GroupedGrad g{};
     g.g = {y.n, y.m, a.d_out, a.ld_dout, a.pre_in, a.ld_pre, y.act, bf16, dz, up8(y.m), a.d_bias, a.accumulate};
-    g.at = at; g.groups = (int)y.groups; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
+    g.at = at; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
     g.partial = a.d_bias != nullptr ? (float*)(ws + l.chunks) : nullptr;
     const int64_t chunks = chunks_in(y), wide = blocks_in(dz != nullptr ? up8(y.m) : y.m, 128);
     for (int64_t c = 0; c < chunks; c += kMostAcross) {

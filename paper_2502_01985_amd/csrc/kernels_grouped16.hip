@@ -11,9 +11,84 @@ namespace {
 template <bool QK, int B, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_rows_kernel(GroupedRows<Product16> a, int first, int tn) {
   __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, B, B, WM, WN>()];
-  grouped_rows_block<2>(a, first + blockIdx.x, tn, [&](Product16 b, int ti, int tj, float* to) {
+  grouped_rows_block<2>(a, first + blockIdx.x, B, tn, [&](Product16 b, int ti, int tj, float* to) {
     b.P.across = b.M;
     mm16_block<false, QK, B, B, WM, WN>(b, ti, tj, (int)blockIdx.z, (int)a.share, to, lds);
+  });
+}
+
+// The same where groups have few rows: what counts is the bytes of the matrices, and so how many of them are on their way.  A workgroup
+// forms 32 rows by 64 columns, its steps of 64 k fetched kFewStages - 1 ahead; each wavefront has 16 of the columns.
+constexpr int kFewRows = 32, kFewCols = 64, kFewStages = 6;
+template <bool QK>
+__global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Product16> a, int first_block, int tn) {
+  constexpr int NT = 256, FM = kFewRows / 16;
+  using TileP = Tile<false, kFewRows, NT>;
+  using TileQ = Tile<QK, kFewCols, NT>;
+  constexpr int kStage = TileP::kBytes + TileQ::kBytes, kEach = TileP::kLoads + TileQ::kLoads;
+  __shared__ __attribute__((aligned(1024))) char lds_all[kFewStages * kStage];
+  grouped_rows_block<2>(a, first_block + blockIdx.x, kFewRows, tn, [&](const Product16& b, int ti, int tj, float* to) {
+    const int64_t i0 = (int64_t)ti * kFewRows, j0 = (int64_t)tj * kFewCols;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t step_q = QK ? kBK * b.Q.ld * 2 : kBK * 2;
+    const int first = (int)(blockIdx.z * a.share), all = (int)((b.K + kBK - 1) / kBK), steps = all - first < a.share ? all - first : (int)a.share;
+    const char* P = (const char*)b.P.p + 2 * i0 * b.P.ld + (int64_t)first * kBK * 2;
+    const char* Q = (const char*)b.Q.p + 2 * (QK ? j0 : j0 * b.Q.ld) + first * step_q;
+    TileP tp;
+    TileQ tq;
+    tp.plan(b.P.ld, b.M - i0);
+    tq.plan(b.Q.ld, b.Q.across - j0);
+    Fragments<false, kFewRows, FM> fp;
+    Fragments<QK, kFewCols, 1> fq;
+    fp.plan(0);
+    fq.plan(16 * wave);
+    const uint32_t base = lds_address(lds_all);
+    auto fetch = [&](int t, int stage) {
+      const char *p = P + (int64_t)t * kBK * 2, *q = Q + t * step_q;
+      const int64_t left = b.K - (int64_t)(first + t) * kBK;
+      const uint32_t at = base + stage * kStage;
+      if (left >= kBK) {
+        tp.template fetch_some<0, TileP::kLoads>(p, at);
+        tq.template fetch_some<0, TileQ::kLoads>(q, at + TileP::kBytes);
+      } else {
+        tp.fetch_last(p, at, (int)left);
+        tq.fetch_last(q, at + TileP::kBytes, (int)left);
+      }
+    };
+    f32x4 acc[FM];
+#pragma unroll
+    for (int x = 0; x < FM; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < kFewStages - 1 && t < steps; ++t) fetch(t, t);
+    int stage = 0;
+    for (int t = 0; t < steps; ++t) {
+      // step t is in LDS, and everyone has done with the one before, whose place the next fetch takes
+      if (t + kFewStages - 1 <= steps) arrived_and_together<kEach*(kFewStages - 2)>();
+      else arrived_and_together<0>();
+      const uint32_t here = base + stage * kStage;
+      if (t + kFewStages - 1 < steps) fetch(t + kFewStages - 1, stage == 0 ? kFewStages - 1 : stage - 1);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const s16x8 q = fq.read(here + TileP::kBytes, half, 0);
+#pragma unroll
+        for (int x = 0; x < FM; ++x) acc[x] = mfma16<kMm16Bf16>(q, fp.read(here, half, x), acc[x]);
+      }
+      stage = stage + 1 == kFewStages ? 0 : stage + 1;
+    }
+    const int64_t j = j0 + 16 * wave + (lane >> 4) * 4;
+    float bias[4];
+    epilogue_bias(b.epi, j, (int)(b.N - j < 4 ? b.N - j : 4), bias);
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+      const int64_t i = i0 + 16 * x + (lane & 15);
+      const int valid = quad_valid(i, j, b.M, b.N);
+      if (valid == 0) continue;
+      if (to != nullptr) {
+        *reinterpret_cast<f32x4*>(to + i * ((b.N + 3) / 4 * 4) + j) = acc[x];
+        continue;
+      }
+      float v[4] = {acc[x][0], acc[x][1], acc[x][2], acc[x][3]};
+      epilogue4(b.epi, 1.0f, 0, i, j, valid, bias, epilogue_ask(b.epi, 0, i, j, valid), v);
+    }
   });
 }
 
@@ -29,6 +104,14 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_s
 }  // namespace
 
 hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int64_t tiles, int splits, hipStream_t st) {
+  if (tile == kFewRows) {
+    const int tn = (int)((a.p.N + kFewCols - 1) / kFewCols);
+    return in_parts(tiles * tn, 256, [&](int64_t first, unsigned blocks) {
+      const dim3 grid(blocks, 1, (unsigned)splits);
+      if (a.p.Q.k_rows) grouped16_few_kernel<true><<<grid, 256, 0, st>>>(a, (int)first, tn);
+      else grouped16_few_kernel<false><<<grid, 256, 0, st>>>(a, (int)first, tn);
+    });
+  }
   const int tn = (int)((a.p.N + tile - 1) / tile);
   return in_parts(tiles * tn, tile * 2, [&](int64_t first, unsigned blocks) {
     const dim3 grid(blocks, 1, (unsigned)splits);
