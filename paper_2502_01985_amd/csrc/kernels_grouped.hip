@@ -1,12 +1,6 @@
 // Layers by group of rows: the index of the groups, products in float32, the elementwise pass of the gradient, the sums of parts, and
 // what runs where.
 #include "grouped.h"
-#ifndef AIM
-#define AIM 256
-#endif
-#ifndef FEWAIM
-#define FEWAIM 256
-#endif
 #include "mm_f32_block.h"
 
 namespace ilargi {
@@ -201,47 +195,73 @@ struct GroupedGrad {
   float* partial;        // m sums a chunk
 };
 
-// g = d_out f'(pre) of a chunk of a group's rows, in the layer's type, and the column sums of the unrounded g: as layer_grad_kernel,
-// with chunks that end where groups do.  blockIdx: 128 columns (from `first` on), chunk.
+// g = d_out f'(pre) of a chunk of a group's rows, in the layer's type, and the column sums of the unrounded g: as layer_grad_kernel, with
+// chunks that end where groups do, 16 bytes a lane and kTurns rows of a lane on their way.  blockIdx: kGradCols columns (from `first` on),
+// chunk.
+constexpr int kGradCols = 128, kTurns = 4;
 template <class T>
 __global__ __launch_bounds__(256) void grouped_grad_kernel(GroupedGrad a, int64_t first, int first_chunk) {
-  __shared__ float4 part[8][32];
+  constexpr int V = ElemOf<T>::kVec, kLanes = kGradCols / V, kRows = 256 / kLanes;
+  using Raw = Piece<T, V>;
+  __shared__ float part[kRows][kGradCols];
   const int u = first_chunk + blockIdx.y;
   const Blocks chunks(a.at, a.at.chunks, a.chunk);
   if (u >= chunks.total) return;
   const LayerGradArgs& y = a.g;
   const Unit b = chunks.find(u);
-  const int cl = threadIdx.x % 32, rl = threadIdx.x / 32;
-  const int64_t j = ((first + blockIdx.x) * 32 + cl) * 4;
+  const int cl = threadIdx.x % kLanes, rl = threadIdx.x / kLanes;
+  const int64_t j = ((first + blockIdx.x) * kLanes + cl) * V;
   const int64_t r0 = b.first + (int64_t)b.number * a.chunk, end = (int64_t)b.first + b.rows, r1 = end - r0 < a.chunk ? end : r0 + a.chunk;
-  const int valid = (int)(y.m - j < 0 ? 0 : y.m - j < 4 ? y.m - j : 4);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (valid > 0 || (y.dz != nullptr && j < y.ld_dz)) {
-#pragma unroll 2
-    for (int64_t i = r0 + rl; i < r1; i += 8) {
-      float f[4];
-      load_piece<T, 4>((const T*)y.d_out + i * y.ld_out + (valid > 0 ? j : 0), valid, f);
-      if (y.act != ILARGI_ACT_NONE) {
-        float z[4];
-        load_piece<T, 4>((const T*)y.pre + i * y.ld_pre + (valid > 0 ? j : 0), valid, z);
+  const int valid = (int)(y.m - j < 0 ? 0 : y.m - j < V ? y.m - j : V);
+  const bool stored = y.dz != nullptr && j < y.ld_dz, bent = y.act != ILARGI_ACT_NONE;
+  float s[V];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) f[q] *= act_slope(z[q], y.act);
+  for (int q = 0; q < V; ++q) s[q] = 0.0f;
+  auto finish = [&](int64_t i, const Raw& d, const Raw& z) {
+    float f[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      f[q] = (float)d.v[q];
+      if (bent) f[q] *= act_slope((float)z.v[q], y.act);
+      s[q] += f[q];
+    }
+    // (rows of dz are whole pieces of eight, with zeros behind their end)
+    if (stored) store_piece<T, V>((T*)y.dz + i * y.ld_dz + j, V, f);
+  };
+  if (valid == V) {
+    for (int64_t i0 = r0 + rl; i0 < r1; i0 += kRows * kTurns) {
+      Raw d[kTurns], z[kTurns];
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const int64_t i = i0 + t * kRows < r1 ? i0 + t * kRows : r1 - 1;
+        d[t] = *reinterpret_cast<const Raw*>((const T*)y.d_out + i * y.ld_out + j);
+        if (bent) z[t] = *reinterpret_cast<const Raw*>((const T*)y.pre + i * y.ld_pre + j);
       }
-      // (rows of dz are whole pieces of eight, with zeros behind their end)
-      if (y.dz != nullptr) store_piece<T, 4>((T*)y.dz + i * y.ld_dz + j, 4, f);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += f[q];
+      for (int t = 0; t < kTurns; ++t)
+        if (i0 + t * kRows < r1) finish(i0 + t * kRows, d[t], z[t]);
+    }
+  } else if (valid > 0 || stored) {
+    for (int64_t i = r0 + rl; i < r1; i += kRows) {
+      Raw d, z;
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        d.v[q] = q < valid ? ((const T*)y.d_out)[i * y.ld_out + j + q] : (T)0.0f;
+        z.v[q] = bent && q < valid ? ((const T*)y.pre)[i * y.ld_pre + j + q] : (T)0.0f;
+      }
+      finish(i, d, z);
     }
   }
   if (a.partial == nullptr) return;
-  part[rl][cl] = make_float4(s[0], s[1], s[2], s[3]);
+#pragma unroll
+  for (int q = 0; q < V; ++q) part[rl][cl * V + q] = s[q];
   __syncthreads();
-  if (rl == 0 && valid > 0) {
-    float4 t = part[0][cl];
-    for (int q = 1; q < 8; ++q) { t.x += part[q][cl].x; t.y += part[q][cl].y; t.z += part[q][cl].z; t.w += part[q][cl].w; }
-    const float f[4] = {t.x, t.y, t.z, t.w};
-    store_piece<float, 4>(a.partial + (int64_t)u * y.m + j, valid, f);
-  }
+  const int64_t c = (first + blockIdx.x) * kGradCols + threadIdx.x;
+  if (threadIdx.x >= kGradCols || c >= y.m) return;
+  float t = part[0][threadIdx.x];
+#pragma unroll
+  for (int q = 1; q < kRows; ++q) t += part[q][threadIdx.x];
+  a.partial[(int64_t)u * y.m + c] = t;
 }
 
 // The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in
@@ -313,7 +333,7 @@ RowsPlan rows_plan(const ilargi_groups_t& y, int64_t N, int64_t K, bool h) {
   const double some = (double)filled(y), each = (double)y.n / (some > 0 ? some : 1.0);
   if (h && each <= 24.0) {
     const int64_t blocks = filled(y) * blocks_in(N, 64), steps = K > 64 ? blocks_in(K, 64) : 1;
-    int64_t splits = blocks > 0 ? FEWAIM / blocks : 1;
+    int64_t splits = blocks > 0 ? 256 / blocks : 1;
     if (splits > steps / 8) splits = steps / 8;
     if (splits < 1) splits = 1;
     const int64_t share = blocks_in(steps, splits);
@@ -352,8 +372,10 @@ struct SumsPlan {
   int64_t parts, several;     // most parts; most groups of several
   size_t partial_bytes;
 };
-// Long groups are split into parts of rows where the blocks of one matrix do not fill the card: then a group of most rows would run on
-// while the rest of it is idle.
+// Long groups are split into parts of rows where the blocks of one matrix fill less than half of the card: then a group of most rows
+// would run on while the rest of it is idle.  (40 skewed groups of 5003 rows, 333 x 129: parts for 128 / 256 / 512 / 1024 blocks 81 / 62 /
+// 58 / 58 us in all.  8 groups of 16384 rows, 2048 x 4096, 128 blocks each: one part 712, two 724, four 777, eight 858: the longest
+// first, they fill the card by themselves.)
 SumsPlan sums_plan(const ilargi_groups_t& y, bool h) {
   SumsPlan p{};
   int tile = h ? 256 : 128;
@@ -361,7 +383,7 @@ SumsPlan sums_plan(const ilargi_groups_t& y, bool h) {
   auto blocks = [&](int t) { return blocks_in(y.k, t) * blocks_in(y.m, t); };
   if (blocks(tile) * filled(y) < 512) tile = least;
   p.tile = tile;
-  const int64_t aim = AIM / blocks(tile);       // parts that fill it
+  const int64_t aim = blocks(tile) < 128 ? 512 / blocks(tile) : 1;
   int64_t rows = aim > 1 ? blocks_in(y.n, aim) : y.n;
   rows = rows < 256 ? 256 : (rows + 63) / 64 * 64;
   p.part = (int)(rows < (1 << 30) ? rows : 1 << 30);
@@ -374,7 +396,7 @@ SumsPlan sums_plan(const ilargi_groups_t& y, bool h) {
 }
 
 int chunk_rows(const ilargi_groups_t& y) {
-  int64_t rows = blocks_in(y.n * blocks_in(y.m, 128), 1024);
+  int64_t rows = blocks_in(y.n * blocks_in(y.m, kGradCols), 2048);
   rows = rows < 32 ? 32 : (rows + 7) / 8 * 8;
   return (int)(rows < 65536 ? rows : 65536);
 }
@@ -551,7 +573,7 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
     g.g = {y.n, y.m, a.d_out, a.ld_dout, a.pre_in, a.ld_pre, y.act, bf16, dz, up8(y.m), a.d_bias, a.accumulate};
     g.at = at; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
     g.partial = a.d_bias != nullptr ? (float*)(ws + l.chunks) : nullptr;
-    const int64_t chunks = chunks_in(y), wide = blocks_in(dz != nullptr ? up8(y.m) : y.m, 128);
+    const int64_t chunks = chunks_in(y), wide = blocks_in(dz != nullptr ? up8(y.m) : y.m, kGradCols);
     for (int64_t c = 0; c < chunks; c += kMostAcross) {
       const hipError_t e = in_parts(wide, 256, [&](int64_t first, unsigned blocks) {
         const dim3 grid(blocks, (unsigned)(chunks - c < kMostAcross ? chunks - c : kMostAcross));
