@@ -191,16 +191,17 @@ __device__ __forceinline__ Prod sums_of(const GroupedSums<Prod>& a, int g, int64
   return b;
 }
 
-// run(product, block of rows, block of columns, sums_to) for block `id` of a launch of rows, `tn` blocks of columns.
+// run(product, block of rows, block of columns, first row of the group) for block `id` of a launch of rows, `tn` blocks of columns.
 template <int SIZE, class Prod, class F>
-__device__ __forceinline__ void grouped_rows_block(const GroupedRows<Prod>& a, int id, int tile, int tn, F run) {
-  const Blocks blocks(a.at, a.at.tiles, tile);
-  if (id >= blocks.total * tn) return;
+__device__ __forceinline__ void grouped_rows_block(const GroupedRows<Prod>& a, const Blocks& blocks, int id, int tn, F run) {
   int u, tj;
   block_of(id, blocks.total, tn, &u, &tj);
   const Unit b = blocks.find(u);
-  float* to = a.partial != nullptr ? a.partial + ((int64_t)blockIdx.z * a.p.M + b.first) * ((a.p.N + 3) / 4 * 4) : nullptr;
-  run(rows_of(a, b.group, b.first, b.rows, SIZE), b.number, tj, to);
+  run(rows_of(a, b.group, b.first, b.rows, SIZE), b.number, tj, (int64_t)b.first);
+}
+template <class Prod>
+__device__ __forceinline__ float* sums_of_rows(const GroupedRows<Prod>& a, int64_t first) {
+  return a.partial != nullptr ? a.partial + ((int64_t)blockIdx.z * a.p.M + first) * ((a.p.N + 3) / 4 * 4) : nullptr;
 }
 template <int SIZE, class Prod, class F>
 __device__ __forceinline__ void grouped_sums_block(const GroupedSums<Prod>& a, int id, int tm, int tn, F run) {
@@ -216,6 +217,22 @@ __device__ __forceinline__ void grouped_sums_block(const GroupedSums<Prod>& a, i
   run(sums_of(a, q.group, r0, rows, SIZE), ti, tj, to);
 }
 
+// Blocks of 256: one workgroup fits a compute unit, so the blocks go in rounds of kUnits, and those of the last round, where they are less
+// than half of one, are split into shares of k that fill it (`partial`: kTailBytes for their sums; a launch adds them).
+constexpr int kUnits = 256;
+constexpr size_t kTailBytes = (size_t)kUnits * 256 * 256 * 4;
+struct Tail {
+  int full, rest, shares, share;      // blocks of whole rounds, blocks of the last, shares of each of those, steps of a share
+};
+__host__ __device__ inline Tail tail_of(int total, int steps) {
+  Tail t{total - total % kUnits, total % kUnits, 1, steps};
+  if (t.rest == 0) return t;
+  const int most = kUnits / t.rest < steps / 4 ? kUnits / t.rest : steps / 4;
+  if (most < 2) return t;
+  t.share = (steps + most - 1) / most;
+  t.shares = (steps + t.share - 1) / t.share;
+  return t;
+}
 hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int64_t tiles, int splits, hipStream_t st);
 hipError_t launch_grouped16_sums(const GroupedSums<Product16>& a, int tile, int64_t parts, hipStream_t st);
 

@@ -231,7 +231,7 @@ struct Operand16 {
   int64_t batch, plane, across;
 };
 inline void shift_operand(Operand* o, int64_t by) { o->p = (const char*)o->p + (o->k_rows ? by : by * o->ld) * (o->bf16 ? 2 : 4); }
-inline void shift_operand(Operand16* o, int64_t by) {
+__host__ __device__ inline void shift_operand(Operand16* o, int64_t by) {
   o->p = (const char*)o->p + (o->k_rows ? by : by * o->ld) * 2;
   o->across -= by;
 }

@@ -93,8 +93,11 @@ __global__ __launch_bounds__(kIndexThreads) void group_index_kernel(GroupIndex a
 template <class T, bool QK, int TILE, int STEP>
 __global__ __launch_bounds__(256) void grouped_rows_kernel(GroupedRows<Product> a, int first, int tn) {
   __shared__ __attribute__((aligned(16))) MmF32Lds<TILE, STEP> lds;
-  grouped_rows_block<sizeof(T)>(a, first + blockIdx.x, TILE, tn, [&](const Product& b, int ti, int tj, float* to) {
-    mm_f32_block<T, T, false, QK, TILE, STEP>(b, ti, tj, 0, blockIdx.z, a.share, to, lds);
+  const Blocks blocks(a.at, a.at.tiles, TILE);
+  const int id = first + blockIdx.x;
+  if (id >= blocks.total * tn) return;
+  grouped_rows_block<sizeof(T)>(a, blocks, id, tn, [&](const Product& b, int ti, int tj, int64_t row) {
+    mm_f32_block<T, T, false, QK, TILE, STEP>(b, ti, tj, 0, blockIdx.z, a.share, sums_of_rows(a, row), lds);
   });
 }
 
@@ -346,13 +349,15 @@ RowsPlan rows_plan(const ilargi_groups_t& y, int64_t N, int64_t K, bool h) {
     for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
       const int64_t share = blocks_in(steps, splits);
       if (splits > 1 && (blocks_in(steps, share) != splits || blocks * (double)splits > 2048.0 || (h && share < 4))) continue;
+      if (tile == 256 && splits > 1) continue;         // (they split what does not fill a round by themselves)
       const double groups = blocks * (double)splits, rounds = ceil(groups / 256.0);
       double cost;
       if (!h) {
         const double work = tile == 64 ? 0.47 : 0.8, alone = tile == 64 ? 0.8 : 1.1;
         cost = (double)share * (rounds * work > alone ? rounds * work : alone);
       } else if (tile == 256) {
-        cost = (double)share * 1.7 * rounds;
+        const Tail t = tail_of(groups < 1e9 ? (int)ceil(groups) : 0, (int)steps);
+        cost = 1.7 * ((double)t.full / kUnits * (double)steps + (t.rest > 0 ? (double)t.share : 0.0)) + (t.shares > 1 ? 3.0 + 2.0 * t.rest * t.shares * 0.26 / 8.0 : 0.0);
       } else {
         cost = (double)share * (groups <= 256.0 ? 0.75 : 1.08 * ceil(groups / 512.0));
       }
@@ -360,7 +365,7 @@ RowsPlan rows_plan(const ilargi_groups_t& y, int64_t N, int64_t K, bool h) {
       if (splits > 1) cost += 3.0 + 2.0 * bytes / 8e6;
       if (cost < least) {
         least = cost;
-        best = {tile, (int)splits, h ? share : share * step, y.n / tile + filled(y), splits > 1 ? (size_t)bytes : 0};
+        best = {tile, (int)splits, h ? share : share * step, y.n / tile + filled(y), splits > 1 ? (size_t)bytes : tile == 256 ? kTailBytes : 0};
       }
     }
   }
@@ -469,7 +474,7 @@ hipError_t rows_product(const ilargi_groups_t& y, const Held& P, const Held& Q, 
     a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1; a.p.kind = kMm16Bf16;
     a.p.epi = epi;
     a.p.past = part == nullptr && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
-    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
+    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = plan.tile == 256 ? partial : part;
     e = launch_grouped16_rows(a, plan.tile, plan.tiles, plan.splits, st);
   } else {
     GroupedRows<Product> a{};

@@ -7,13 +7,80 @@ namespace ilargi {
 
 namespace {
 
-// blockIdx: block (from `first` on), none, share of k.  Q: a matrix for each group, its rows over k (QK) or its columns.
-template <bool QK, int B, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_rows_kernel(GroupedRows<Product16> a, int first, int tn) {
-  __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, B, B, WM, WN>()];
-  grouped_rows_block<2>(a, first + blockIdx.x, B, tn, [&](Product16 b, int ti, int tj, float* to) {
+// blockIdx: block of 128 (from `first` on), none, share of k.  Q: a matrix for each group, its rows over k (QK) or its columns.
+template <bool QK>
+__global__ __launch_bounds__(256, 2) void grouped16_rows_kernel(GroupedRows<Product16> a, int first, int tn) {
+  constexpr int B = 128;
+  __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, B, B, 2, 2>()];
+  const Blocks blocks(a.at, a.at.tiles, B);
+  const int id = first + blockIdx.x;
+  if (id >= blocks.total * tn) return;
+  grouped_rows_block<2>(a, blocks, id, tn, [&](Product16 b, int ti, int tj, int64_t row) {
     b.P.across = b.M;
-    mm16_block<false, QK, B, B, WM, WN>(b, ti, tj, (int)blockIdx.z, (int)a.share, to, lds);
+    mm16_block<false, QK, B, B, 2, 2>(b, ti, tj, (int)blockIdx.z, (int)a.share, sums_of_rows(a, row), lds);
+  });
+}
+
+// A block of 256 as a product of its own.
+__device__ __forceinline__ Product16 block_alone(const Product16& b, int ti, int tj) {
+  Product16 c = b;
+  const int64_t i = (int64_t)ti * 256, j = (int64_t)tj * 256;
+  shift_operand(&c.P, i);
+  shift_operand(&c.Q, j);
+  c.M = b.M - i < 256 ? b.M - i : 256;
+  c.N = b.N - j < 256 ? b.N - j : 256;
+  return c;
+}
+
+// blockIdx: block of 256, or a share of one of the last round (from `first` on).
+template <bool QK>
+__global__ __launch_bounds__(512, 1) void grouped16_rounds_kernel(GroupedRows<Product16> a, int first, int tn) {
+  constexpr int B = 256;
+  __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, B, B, 2, 4>()];
+  const Blocks blocks(a.at, a.at.tiles, B);
+  const int steps = (int)((a.p.K + kBK - 1) / kBK), id = first + blockIdx.x;
+  const Tail tail = tail_of(blocks.total * tn, steps);
+  const int over = id - tail.full, block = over < 0 ? id : tail.full + over / tail.shares;
+  if (block >= tail.full + tail.rest) return;
+  grouped_rows_block<2>(a, blocks, block, tn, [&](Product16 b, int ti, int tj, int64_t) {
+    b.P.across = b.M;
+    int z = 0, share = steps;
+    float* to = nullptr;
+    if (over >= 0 && tail.shares > 1) {
+      b = block_alone(b, ti, tj);
+      ti = tj = 0;
+      z = over % tail.shares;
+      share = tail.share;
+      to = a.partial + (int64_t)over * (B * B);
+    }
+    mm16_block<false, QK, B, B, 2, 4>(b, ti, tj, z, share, to, lds);
+  });
+}
+
+// The shares of the last round's blocks, four sums of a row a thread and four rows of a block a workgroup.  blockIdx: rows, block.
+__global__ __launch_bounds__(256) void grouped16_tail_kernel(GroupedRows<Product16> a, int tn) {
+  constexpr int B = 256;
+  const Blocks blocks(a.at, a.at.tiles, B);
+  const Tail tail = tail_of(blocks.total * tn, (int)((a.p.K + kBK - 1) / kBK));
+  if (tail.shares < 2 || (int)blockIdx.y >= tail.rest) return;
+  grouped_rows_block<2>(a, blocks, tail.full + blockIdx.y, tn, [&](const Product16& b, int ti, int tj, int64_t) {
+    const Product16 c = block_alone(b, ti, tj);
+    const int64_t i = blockIdx.x * 4 + threadIdx.x / 64, j = threadIdx.x % 64 * 4, ldp = (c.N + 3) / 4 * 4;
+    const int valid = quad_valid(i, j, c.M, c.N);
+    if (valid == 0) return;
+    const int64_t row = (int64_t)ti * B + i, col = (int64_t)tj * B + j;
+    const SrcQuad raw = epilogue_ask(b.epi, 0, row, col, valid);
+    float bias[4];
+    epilogue_bias(b.epi, col, valid, bias);
+    const float* p = a.partial + (int64_t)blockIdx.y * tail.shares * (B * B) + i * ldp + j;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int z = 0; z < tail.shares; ++z) {
+      const f32x4 t = *reinterpret_cast<const f32x4*>(p + (int64_t)z * (B * B));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += t[q];
+    }
+    epilogue4(b.epi, 1.0f, 0, row, col, valid, bias, raw, v);
   });
 }
 
@@ -27,7 +94,11 @@ __global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Produ
   using TileQ = Tile<QK, kFewCols, NT>;
   constexpr int kStage = TileP::kBytes + TileQ::kBytes, kEach = TileP::kLoads + TileQ::kLoads;
   __shared__ __attribute__((aligned(1024))) char lds_all[kFewStages * kStage];
-  grouped_rows_block<2>(a, first_block + blockIdx.x, kFewRows, tn, [&](const Product16& b, int ti, int tj, float* to) {
+  const Blocks blocks(a.at, a.at.tiles, kFewRows);
+  const int id = first_block + blockIdx.x;
+  if (id >= blocks.total * tn) return;
+  grouped_rows_block<2>(a, blocks, id, tn, [&](const Product16& b, int ti, int tj, int64_t row) {
+    float* const to = sums_of_rows(a, row);
     const int64_t i0 = (int64_t)ti * kFewRows, j0 = (int64_t)tj * kFewCols;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t step_q = QK ? kBK * b.Q.ld * 2 : kBK * 2;
@@ -113,16 +184,20 @@ hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int6
     });
   }
   const int tn = (int)((a.p.N + tile - 1) / tile);
-  return in_parts(tiles * tn, tile * 2, [&](int64_t first, unsigned blocks) {
-    const dim3 grid(blocks, 1, (unsigned)splits);
-    if (tile == 256) {
-      if (a.p.Q.k_rows) grouped16_rows_kernel<true, 256, 2, 4><<<grid, 512, 0, st>>>(a, (int)first, tn);
-      else grouped16_rows_kernel<false, 256, 2, 4><<<grid, 512, 0, st>>>(a, (int)first, tn);
-    } else {
-      if (a.p.Q.k_rows) grouped16_rows_kernel<true, 128, 2, 2><<<grid, 256, 0, st>>>(a, (int)first, tn);
-      else grouped16_rows_kernel<false, 128, 2, 2><<<grid, 256, 0, st>>>(a, (int)first, tn);
-    }
+  if (tile == 128)
+    return in_parts(tiles * tn, 256, [&](int64_t first, unsigned blocks) {
+      const dim3 grid(blocks, 1, (unsigned)splits);
+      if (a.p.Q.k_rows) grouped16_rows_kernel<true><<<grid, 256, 0, st>>>(a, (int)first, tn);
+      else grouped16_rows_kernel<false><<<grid, 256, 0, st>>>(a, (int)first, tn);
+    });
+  // (a last round of less than half has at most kUnits shares)
+  const hipError_t e = in_parts(tiles * tn + kUnits, 512, [&](int64_t first, unsigned blocks) {
+    if (a.p.Q.k_rows) grouped16_rounds_kernel<true><<<blocks, 512, 0, st>>>(a, (int)first, tn);
+    else grouped16_rounds_kernel<false><<<blocks, 512, 0, st>>>(a, (int)first, tn);
   });
+  if (e != hipSuccess || (a.p.K + kBK - 1) / kBK < 8) return e;       // (shares have four steps at least)
+  grouped16_tail_kernel<<<dim3(64, kUnits / 2), 256, 0, st>>>(a, tn);
+  return hipGetLastError();
 }
 
 hipError_t launch_grouped16_sums(const GroupedSums<Product16>& a, int tile, int64_t parts, hipStream_t st) {
