@@ -89,24 +89,40 @@ __global__ __launch_bounds__(kIndexThreads) void group_index_kernel(GroupIndex a
 }
 
 // --------------------------------------------------------------------------------------------------------- float32 products
-// blockIdx: block (from `first` on), none, share of k.
 template <class T, bool QK, int TILE, int STEP>
-__global__ __launch_bounds__(256) void grouped_rows_kernel(GroupedRows<Product> a, int first, int tn) {
-  __shared__ __attribute__((aligned(16))) MmF32Lds<TILE, STEP> lds;
+__device__ __forceinline__ void rows_block(const GroupedRows<Product>& a, int id, int tn, MmF32Lds<TILE, STEP>& lds) {
   const Blocks blocks(a.at, a.at.tiles, TILE);
-  const int id = first + blockIdx.x;
   if (id >= blocks.total * tn) return;
   grouped_rows_block<sizeof(T)>(a, blocks, id, tn, [&](const Product& b, int ti, int tj, int64_t row) {
     mm_f32_block<T, T, false, QK, TILE, STEP>(b, ti, tj, 0, blockIdx.z, a.share, sums_of_rows(a, row), lds);
   });
 }
+template <class T, int TILE, int STEP>
+__device__ __forceinline__ void sums_block(const GroupedSums<Product>& a, int id, int tm, int tn, MmF32Lds<TILE, STEP>& lds) {
+  grouped_sums_block<sizeof(T)>(a, id, tm, tn, [&](const Product& b, int ti, int tj, float* to) {
+    mm_f32_block<T, T, true, true, TILE, STEP>(b, ti, tj, 0, 0, b.K, to, lds);
+  });
+}
+
+// blockIdx: block (from `first` on), none, share of k.
+template <class T, bool QK, int TILE, int STEP>
+__global__ __launch_bounds__(256) void grouped_rows_kernel(GroupedRows<Product> a, int first, int tn) {
+  __shared__ __attribute__((aligned(16))) MmF32Lds<TILE, STEP> lds;
+  rows_block<T, QK, TILE, STEP>(a, first + blockIdx.x, tn, lds);
+}
 
 template <class T, int TILE, int STEP>
 __global__ __launch_bounds__(256) void grouped_sums_kernel(GroupedSums<Product> a, int first, int tm, int tn) {
   __shared__ __attribute__((aligned(16))) MmF32Lds<TILE, STEP> lds;
-  grouped_sums_block<sizeof(T)>(a, first + blockIdx.x, tm, tn, [&](const Product& b, int ti, int tj, float* to) {
-    mm_f32_block<T, T, true, true, TILE, STEP>(b, ti, tj, 0, 0, b.K, to, lds);
-  });
+  sums_block<T, TILE, STEP>(a, first + blockIdx.x, tm, tn, lds);
+}
+
+// Both products of a gradient in one launch, where neither fills the card for long: `sums` blocks of d_W, then those of d_X.
+template <class T>
+__global__ __launch_bounds__(256) void grouped_both_kernel(GroupedSums<Product> w, int sums, int tm, int tn, GroupedRows<Product> x, int tn_x) {
+  __shared__ __attribute__((aligned(16))) MmF32Lds<64, 32> lds;
+  if ((int)blockIdx.x < sums) sums_block<T, 64, 32>(w, blockIdx.x, tm, tn, lds);
+  else rows_block<T, false, 64, 32>(x, blockIdx.x - sums, tn_x, lds);
 }
 
 template <class T>
@@ -462,62 +478,80 @@ hipError_t lay_out(const ilargi_groups_t& y, Held* m, int64_t batch, char* at, h
 }
 
 // out = P Q_g by group (Q's rows over k, or its columns).
+template <class Prod>
+GroupedRows<Prod> rows_of_layer(const ilargi_groups_t& y, int64_t N, int64_t K, const Epilogue& epi, int64_t far_q, int64_t far_bias, const GroupIndex& at, const RowsPlan& plan, float* partial) {
+  GroupedRows<Prod> a{};
+  a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1;
+  a.p.epi = epi;
+  a.at = at; a.far_q = far_q; a.far_bias = far_bias; a.share = plan.share;
+  a.partial = plan.splits > 1 || plan.tile == 256 ? partial : nullptr;
+  return a;
+}
+GroupedRows<Product> rows_in_f32(const ilargi_groups_t& y, const Held& P, const Held& Q, int q_rows, int64_t N, int64_t K, const Epilogue& epi, int64_t far_bias, const GroupIndex& at,
+                                 const RowsPlan& plan, float* partial) {
+  const int bf16 = y.type == ILARGI_TYPE_BF16;
+  GroupedRows<Product> a = rows_of_layer<Product>(y, N, K, epi, Q.stride, far_bias, at, plan, partial);
+  a.p.P = {P.p, P.ld, 0, bf16, 0};
+  a.p.Q = {Q.p, Q.ld, q_rows, bf16, 0};
+  return a;
+}
 hipError_t rows_product(const ilargi_groups_t& y, const Held& P, const Held& Q, int q_rows, int64_t N, int64_t K, const Epilogue& epi, int64_t far_bias, const GroupIndex& at,
                         const RowsPlan& plan, bool h16, float* partial, hipStream_t st) {
-  const int bf16 = y.type == ILARGI_TYPE_BF16;
-  float* part = plan.splits > 1 ? partial : nullptr;
   hipError_t e;
   if (h16) {
-    GroupedRows<Product16> a{};
+    GroupedRows<Product16> a = rows_of_layer<Product16>(y, N, K, epi, Q.stride, far_bias, at, plan, partial);
     a.p.P = {P.p, P.ld, 0, 0, 0, y.n};
     a.p.Q = {Q.p, Q.ld, q_rows, 0, 0, q_rows ? up8(Q.cols) : Q.rows};
-    a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1; a.p.kind = kMm16Bf16;
-    a.p.epi = epi;
-    a.p.past = part == nullptr && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
-    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = plan.tile == 256 ? partial : part;
+    a.p.kind = kMm16Bf16;
+    a.p.past = plan.splits == 1 && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
     e = launch_grouped16_rows(a, plan.tile, plan.tiles, plan.splits, st);
   } else {
-    GroupedRows<Product> a{};
-    a.p.P = {P.p, P.ld, 0, bf16, 0};
-    a.p.Q = {Q.p, Q.ld, q_rows, bf16, 0};
-    a.p.M = y.n; a.p.N = N; a.p.K = K; a.p.batches = 1;
-    a.p.epi = epi;
-    a.at = at; a.far_q = Q.stride; a.far_bias = far_bias; a.share = plan.share; a.partial = part;
-    e = bf16 ? rows_f32<bf16_t>(a, plan.tile, plan.tiles, plan.splits, st) : rows_f32<float>(a, plan.tile, plan.tiles, plan.splits, st);
+    const GroupedRows<Product> a = rows_in_f32(y, P, Q, q_rows, N, K, epi, far_bias, at, plan, partial);
+    e = y.type == ILARGI_TYPE_BF16 ? rows_f32<bf16_t>(a, plan.tile, plan.tiles, plan.splits, st) : rows_f32<float>(a, plan.tile, plan.tiles, plan.splits, st);
   }
-  if (e != hipSuccess || part == nullptr) return e;
+  if (e != hipSuccess || plan.splits == 1) return e;
   return in_parts(blocks_in(y.n * (up4(N) / 4), 256), 256, [&](int64_t first, unsigned blocks) {
-    grouped_rows_join_kernel<<<blocks, 256, 0, st>>>(epi, N, at, far_bias, first, plan.splits, part);
+    grouped_rows_join_kernel<<<blocks, 256, 0, st>>>(epi, N, at, far_bias, first, plan.splits, partial);
   });
 }
 
-hipError_t sums_product(const ilargi_groups_t& y, const Held& P, const Held& Q, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, bool h16, float* partial,
-                        hipStream_t st) {
+template <class Prod>
+GroupedSums<Prod> sums_of_layer(const ilargi_groups_t& y, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, float* partial) {
+  GroupedSums<Prod> a{};
+  a.p.M = y.k; a.p.N = y.m; a.p.K = y.n; a.p.batches = 1;
+  a.p.epi = epi;
+  a.at = at; a.far_out = far_out; a.part = plan.part; a.partial = partial;
+  return a;
+}
+GroupedSums<Product> sums_in_f32(const ilargi_groups_t& y, const Held& P, const Held& Q, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, float* partial) {
   const int bf16 = y.type == ILARGI_TYPE_BF16;
-  hipError_t e;
-  if (h16) {
-    GroupedSums<Product16> a{};
-    a.p.P = {P.p, P.ld, 1, 0, 0, up8(P.cols)};
-    a.p.Q = {Q.p, Q.ld, 1, 0, 0, up8(Q.cols)};
-    a.p.M = y.k; a.p.N = y.m; a.p.K = y.n; a.p.batches = 1; a.p.kind = kMm16Bf16;
-    a.p.epi = epi;
-    a.at = at; a.far_out = far_out; a.part = plan.part; a.partial = partial;
-    e = launch_grouped16_sums(a, plan.tile, plan.parts, st);
-  } else {
-    GroupedSums<Product> a{};
-    a.p.P = {P.p, P.ld, 1, bf16, 0};
-    a.p.Q = {Q.p, Q.ld, 1, bf16, 0};
-    a.p.M = y.k; a.p.N = y.m; a.p.K = y.n; a.p.batches = 1;
-    a.p.epi = epi;
-    a.at = at; a.far_out = far_out; a.part = plan.part; a.partial = partial;
-    e = bf16 ? sums_f32<bf16_t>(a, plan.tile, plan.parts, st) : sums_f32<float>(a, plan.tile, plan.parts, st);
-  }
-  if (e != hipSuccess || plan.several == 0) return e;
+  GroupedSums<Product> a = sums_of_layer<Product>(y, epi, far_out, at, plan, partial);
+  a.p.P = {P.p, P.ld, 1, bf16, 0};
+  a.p.Q = {Q.p, Q.ld, 1, bf16, 0};
+  return a;
+}
+hipError_t add_parts(const ilargi_groups_t& y, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, const float* partial, hipStream_t st) {
+  if (plan.several == 0) return hipSuccess;
   // (the longest groups come first, where they are sorted)
   const unsigned places = (unsigned)(y.groups <= kMostSorted ? plan.several : y.groups);
   return in_parts(blocks_in(y.k * (up4(y.m) / 4), 256), 256, [&](int64_t first, unsigned blocks) {
     grouped_sums_join_kernel<<<dim3(blocks, places), 256, 0, st>>>(epi, y.k, y.m, at, plan.part, far_out, first, partial);
   });
+}
+hipError_t sums_product(const ilargi_groups_t& y, const Held& P, const Held& Q, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, bool h16, float* partial,
+                        hipStream_t st) {
+  hipError_t e;
+  if (h16) {
+    GroupedSums<Product16> a = sums_of_layer<Product16>(y, epi, far_out, at, plan, partial);
+    a.p.P = {P.p, P.ld, 1, 0, 0, up8(P.cols)};
+    a.p.Q = {Q.p, Q.ld, 1, 0, 0, up8(Q.cols)};
+    a.p.kind = kMm16Bf16;
+    e = launch_grouped16_sums(a, plan.tile, plan.parts, st);
+  } else {
+    const GroupedSums<Product> a = sums_in_f32(y, P, Q, epi, far_out, at, plan, partial);
+    e = y.type == ILARGI_TYPE_BF16 ? sums_f32<bf16_t>(a, plan.tile, plan.parts, st) : sums_f32<float>(a, plan.tile, plan.parts, st);
+  }
+  return e != hipSuccess ? e : add_parts(y, epi, far_out, at, plan, partial, st);
 }
 
 }  // namespace
@@ -596,19 +630,27 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
       if (e != hipSuccess) return e;
     }
   }
-  Epilogue epi{};
-  epi.mode = kEpiLinear;
-  epi.out_bf16 = bf16;
-  if (a.d_X != nullptr && y.n > 0) {
-    epi.out = a.d_X; epi.ld_out = a.ld_dx;
-    if (hipError_t e = rows_product(y, z, w, 0, y.k, y.m, epi, 0, at, rows, rows16, (float*)(ws + l.shares), st); e != hipSuccess) return e;
+  Epilogue epi{}, epi_w{};
+  epi.mode = epi_w.mode = kEpiLinear;
+  epi.out_bf16 = epi_w.out_bf16 = bf16;
+  epi.out = a.d_X; epi.ld_out = a.ld_dx;
+  epi_w.out = a.d_W; epi_w.ld_out = a.ld_dw;
+  if (a.accumulate) { epi_w.src = a.d_W; epi_w.ld_src = a.ld_dw; epi_w.src_bf16 = bf16; }
+  float* partial = (float*)(ws + l.shares);
+  if (a.d_X != nullptr && a.d_W != nullptr && y.n > 0 && !rows16 && !sums16 && rows.tile == 64 && sums.tile == 64 && rows.splits == 1) {
+    const int64_t tm = blocks_in(y.k, 64), tn = blocks_in(y.m, 64), w_blocks = sums.parts * tm * tn, all = w_blocks + rows.tiles * tm;
+    if (all <= kMostThreads / 256) {
+      const GroupedSums<Product> sw = sums_in_f32(y, x, z, epi_w, a.stride_dw, at, sums, partial);
+      const GroupedRows<Product> rx = rows_in_f32(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial);
+      if (bf16) grouped_both_kernel<bf16_t><<<(unsigned)all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)tm);
+      else grouped_both_kernel<float><<<(unsigned)all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)tm);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      return add_parts(y, epi_w, a.stride_dw, at, sums, partial, st);
+    }
   }
-  if (a.d_W != nullptr) {
-    epi.out = a.d_W; epi.ld_out = a.ld_dw;
-    if (a.accumulate) { epi.src = a.d_W; epi.ld_src = a.ld_dw; epi.src_bf16 = bf16; }
-    return sums_product(y, x, z, epi, a.stride_dw, at, sums, sums16, (float*)(ws + l.shares), st);
-  }
-  return hipSuccess;
+  if (a.d_X != nullptr && y.n > 0)
+    if (hipError_t e = rows_product(y, z, w, 0, y.k, y.m, epi, 0, at, rows, rows16, partial, st); e != hipSuccess) return e;
+  return a.d_W != nullptr ? sums_product(y, x, z, epi_w, a.stride_dw, at, sums, sums16, partial, st) : hipSuccess;
 }
 
 }  // namespace ilargi
