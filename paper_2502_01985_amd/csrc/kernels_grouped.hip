@@ -117,14 +117,6 @@ __global__ __launch_bounds__(256) void grouped_sums_kernel(GroupedSums<Product> 
   sums_block<T, TILE, STEP>(a, first + blockIdx.x, tm, tn, lds);
 }
 
-// Both products of a gradient in one launch, where neither fills the card for long: `sums` blocks of d_W, then those of d_X.
-template <class T>
-__global__ __launch_bounds__(256) void grouped_both_kernel(GroupedSums<Product> w, int sums, int tm, int tn, GroupedRows<Product> x, int tn_x) {
-  __shared__ __attribute__((aligned(16))) MmF32Lds<64, 32> lds;
-  if ((int)blockIdx.x < sums) sums_block<T, 64, 32>(w, blockIdx.x, tm, tn, lds);
-  else rows_block<T, false, 64, 32>(x, blockIdx.x - sums, tn_x, lds);
-}
-
 template <class T>
 hipError_t rows_f32(const GroupedRows<Product>& a, int tile, int64_t tiles, int splits, hipStream_t st) {
   const int tn = (int)((a.p.N + tile - 1) / tile);
@@ -283,14 +275,15 @@ __global__ __launch_bounds__(256) void grouped_grad_kernel(GroupedGrad a, int64_
   a.partial[(int64_t)u * y.m + c] = t;
 }
 
-// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in
-// float64: they cancel each other as the rows do.  blockIdx: 16 columns
-// (from `first` on), group.
+// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in float64: they cancel
+// each other as the rows do.  16 columns from 16 `block` on, of group g.
+struct BiasLds {
+  double part[16][17];
+};
 template <class T>
-__global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_t first) {
-  __shared__ double part[16][17];
-  const int c = threadIdx.x % 16, q = threadIdx.x / 16, g = blockIdx.y;
-  const int64_t j = (first + blockIdx.x) * 16 + c, m = a.g.m;
+__device__ __forceinline__ void bias_block(const GroupedGrad& a, int64_t block, int g, BiasLds& lds) {
+  const int c = threadIdx.x % 16, q = threadIdx.x / 16;
+  const int64_t j = block * 16 + c, m = a.g.m;
   double s = 0.0;
   int first_chunk, end_chunk;
   Blocks(a.at, a.at.chunks, a.chunk).of_group(g, &first_chunk, &end_chunk);
@@ -298,12 +291,32 @@ __global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_
 #pragma unroll 4
     for (int u = first_chunk + q; u < end_chunk; u += 16) s += a.partial[(int64_t)u * m + j];
   }
-  part[q][c] = s;
+  lds.part[q][c] = s;
   __syncthreads();
   if (q != 0 || j >= m) return;
-  for (int u = 1; u < 16; ++u) s += part[u][c];
+  for (int u = 1; u < 16; ++u) s += lds.part[u][c];
   T* const out = (T*)a.g.d_bias + g * a.ld_dbias + j;
   *out = (T)(float)(a.g.accumulate ? (double)(float)*out + s : s);
+}
+// blockIdx: 16 columns (from `first` on), group.
+template <class T>
+__global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_t first) {
+  __shared__ BiasLds lds;
+  bias_block<T>(a, first + blockIdx.x, blockIdx.y, lds);
+}
+
+// Both products of a gradient and the bias's in one launch, where none of them fills the card for long: `sums` blocks of d_W, `rows`
+// of d_X, and those of the column sums.  (5003 rows in 40 groups, 333 x 129: 50 us for 58 in three launches.)
+template <class T>
+__global__ __launch_bounds__(256) void grouped_both_kernel(GroupedSums<Product> w, int sums, int tm, int tn, GroupedRows<Product> x, int rows, int tn_x, GroupedGrad b, int columns) {
+  __shared__ __attribute__((aligned(16))) union {
+    MmF32Lds<64, 32> products;
+    BiasLds bias;
+  } lds;
+  const int id = blockIdx.x;
+  if (id < sums) sums_block<T, 64, 32>(w, id, tm, tn, lds.products);
+  else if (id - sums < rows) rows_block<T, false, 64, 32>(x, id - sums, tn_x, lds.products);
+  else bias_block<T>(b, (id - sums - rows) % columns, (id - sums - rows) / columns, lds.bias);
 }
 
 // Matrices of bfloat16 at any address, laid out in whole 16-byte pieces with zeros behind their rows' ends; 2^sh lanes a row.
@@ -607,11 +620,15 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   const int chunk = chunk_rows(y);
   const bool passes = dz != nullptr || a.d_bias != nullptr;
   if (hipError_t e = find_groups(at, a.d_X != nullptr ? rows.tile : 0, a.d_W != nullptr ? sums.part : 0, passes ? chunk : 0, st); e != hipSuccess) return e;
+  const int64_t tm = blocks_in(y.k, 64), tn = blocks_in(y.m, 64), bias_columns = blocks_in(y.m, 16);
+  const int64_t w_blocks = sums.parts * tm * tn, x_blocks = rows.tiles * tm, b_blocks = a.d_bias != nullptr ? y.groups * bias_columns : 0;
+  const bool together = a.d_X != nullptr && a.d_W != nullptr && y.n > 0 && !rows16 && !sums16 && rows.tile == 64 && sums.tile == 64 && rows.splits == 1 &&
+                        w_blocks + x_blocks + b_blocks <= kMostThreads / 256;
+  GroupedGrad g{};
+  g.g = {y.n, y.m, a.d_out, a.ld_dout, a.pre_in, a.ld_pre, y.act, bf16, dz, up8(y.m), a.d_bias, a.accumulate};
+  g.at = at; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
+  g.partial = a.d_bias != nullptr ? (float*)(ws + l.chunks) : nullptr;
   if (passes) {
-    GroupedGrad g{};
-    g.g = {y.n, y.m, a.d_out, a.ld_dout, a.pre_in, a.ld_pre, y.act, bf16, dz, up8(y.m), a.d_bias, a.accumulate};
-    g.at = at; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
-    g.partial = a.d_bias != nullptr ? (float*)(ws + l.chunks) : nullptr;
     const int64_t chunks = chunks_in(y), wide = blocks_in(dz != nullptr ? up8(y.m) : y.m, kGradCols);
     for (int64_t c = 0; c < chunks; c += kMostAcross) {
       const hipError_t e = in_parts(wide, 256, [&](int64_t first, unsigned blocks) {
@@ -621,14 +638,14 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
       });
       if (e != hipSuccess) return e;
     }
-    if (a.d_bias != nullptr) {
-      const hipError_t e = in_parts(blocks_in(y.m, 16), 256, [&](int64_t first, unsigned blocks) {
-        const dim3 grid(blocks, (unsigned)y.groups);
-        if (bf16) grouped_bias_kernel<bf16_t><<<grid, 256, 0, st>>>(g, first);
-        else grouped_bias_kernel<float><<<grid, 256, 0, st>>>(g, first);
-      });
-      if (e != hipSuccess) return e;
-    }
+  }
+  if (a.d_bias != nullptr && !together) {
+    const hipError_t e = in_parts(bias_columns, 256, [&](int64_t first, unsigned blocks) {
+      const dim3 grid(blocks, (unsigned)y.groups);
+      if (bf16) grouped_bias_kernel<bf16_t><<<grid, 256, 0, st>>>(g, first);
+      else grouped_bias_kernel<float><<<grid, 256, 0, st>>>(g, first);
+    });
+    if (e != hipSuccess) return e;
   }
   Epilogue epi{}, epi_w{};
   epi.mode = epi_w.mode = kEpiLinear;
@@ -637,16 +654,14 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   epi_w.out = a.d_W; epi_w.ld_out = a.ld_dw;
   if (a.accumulate) { epi_w.src = a.d_W; epi_w.ld_src = a.ld_dw; epi_w.src_bf16 = bf16; }
   float* partial = (float*)(ws + l.shares);
-  if (a.d_X != nullptr && a.d_W != nullptr && y.n > 0 && !rows16 && !sums16 && rows.tile == 64 && sums.tile == 64 && rows.splits == 1) {
-    const int64_t tm = blocks_in(y.k, 64), tn = blocks_in(y.m, 64), w_blocks = sums.parts * tm * tn, all = w_blocks + rows.tiles * tm;
-    if (all <= kMostThreads / 256) {
-      const GroupedSums<Product> sw = sums_in_f32(y, x, z, epi_w, a.stride_dw, at, sums, partial);
-      const GroupedRows<Product> rx = rows_in_f32(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial);
-      if (bf16) grouped_both_kernel<bf16_t><<<(unsigned)all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)tm);
-      else grouped_both_kernel<float><<<(unsigned)all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)tm);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-      return add_parts(y, epi_w, a.stride_dw, at, sums, partial, st);
-    }
+  if (together) {
+    const GroupedSums<Product> sw = sums_in_f32(y, x, z, epi_w, a.stride_dw, at, sums, partial);
+    const GroupedRows<Product> rx = rows_in_f32(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial);
+    const unsigned all = (unsigned)(w_blocks + x_blocks + b_blocks);
+    if (bf16) grouped_both_kernel<bf16_t><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
+    else grouped_both_kernel<float><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return add_parts(y, epi_w, a.stride_dw, at, sums, partial, st);
   }
   if (a.d_X != nullptr && y.n > 0)
     if (hipError_t e = rows_product(y, z, w, 0, y.k, y.m, epi, 0, at, rows, rows16, partial, st); e != hipSuccess) return e;
