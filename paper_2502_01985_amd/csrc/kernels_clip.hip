@@ -1,7 +1,8 @@
 // The norm over many tensors and the tensors scaled by it: every workgroup leaves the sum of the squares of its part, in float64; the
 // workgroups of the second pass add those sums up themselves, all in the same order, and where they are many a workgroup does it for all.
 //
-// Tensors go sixty-four to a launch, in the launch's arguments: nothing is copied to the device before.  A workgroup takes a run of one
+// Tensors go sixty-four to a launch, in the launch's arguments (sixteen, where there are no more: 4 KB of arguments cost the host 2 us a
+// launch): nothing is copied to the device before.  A workgroup takes a run of one
 // tensor's pieces of 16 bytes; a tensor whose rows follow each other counts as one row.  The second pass goes through the parts from
 // the last to the first, whose data the caches still hold.  Bound by memory.
 #include "ilargi_layers.h"
@@ -10,7 +11,7 @@ namespace ilargi {
 
 namespace {
 
-constexpr int kMostTensors = 64, kMostSums = 1024, kLoads = 4;
+constexpr int kMostTensors = 64, kFewTensors = 16, kMostSums = 1024, kLoads = 4;
 constexpr int64_t kLeastPart = 2048, kMostPart = 8192;         // pieces
 
 struct Part {
@@ -19,18 +20,20 @@ struct Part {
   int64_t row_pieces, pieces;       // of a row, of all
   int64_t cols, ld_in, ld_out;
 };
+template <int MOST>
 struct Parts {
-  Part t[kMostTensors];
-  int first[kMostTensors + 1];      // its first workgroup
+  Part t[MOST];
+  int first[MOST + 1];      // its first workgroup
   int count;
   uint64_t bf16;                    // a bit a tensor
   int64_t part;                     // pieces of a workgroup
 };
 
 // The tensor of a workgroup.
-__device__ __forceinline__ int tensor_of(const Parts& a, int group) {
+template <int MOST>
+__device__ __forceinline__ int tensor_of(const Parts<MOST>& a, int group) {
   const int lane = threadIdx.x % kWave;
-  const bool before = lane < a.count && a.first[lane] <= group;
+  const bool before = lane < a.count && a.first[lane < MOST ? lane : 0] <= group;
   return __popcll(__ballot(before)) - 1;
 }
 
@@ -77,7 +80,8 @@ __device__ __forceinline__ double workgroup_sum(double s, double (&lds)[4]) {
   return lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-__global__ __launch_bounds__(256) void squares_kernel(Parts a, double* __restrict__ partial) {
+template <int MOST>
+__global__ __launch_bounds__(256) void squares_kernel(Parts<MOST> a, double* __restrict__ partial) {
   __shared__ double lds[4];
   const int q = tensor_of(a, blockIdx.x);
   const Part& t = a.t[q];
@@ -108,7 +112,8 @@ __global__ __launch_bounds__(256) void add_sums_kernel(const double* __restrict_
 
 // blockIdx: the part of a tensor, each tensor's from its last on; without tensors one workgroup that stores the norm.  `past`: what is written is larger
 // than the caches.
-__global__ __launch_bounds__(256) void clip_kernel(Parts a, const double* __restrict__ partial, int sums, float max_norm, float* __restrict__ norm, bool past) {
+template <int MOST>
+__global__ __launch_bounds__(256) void clip_kernel(Parts<MOST> a, const double* __restrict__ partial, int sums, float max_norm, float* __restrict__ norm, bool past) {
   __shared__ double lds[4];
   const double total = sqrt(add_sums(partial, sums, lds));
   if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
@@ -164,7 +169,10 @@ ClipPlan clip_plan(const ilargi_tensor_t* t, int64_t count) {
 
 size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)(clip_plan(t, count).groups + 1) * 8; }
 
-hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
+namespace {
+
+template <int MOST>
+hipError_t clip_in(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
   const ClipPlan plan = clip_plan(t, count);
   if (plan.groups > 2147483647ll) return hipErrorInvalidValue;
   int64_t written = 0;
@@ -172,9 +180,9 @@ hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, 
     if (t[q].out != nullptr && t[q].out != t[q].in) written += pieces_in(t[q]) * 16;
   const bool past = written >= kStreamBytes;
   auto next = [&](int64_t& q, int step, bool outputs) {                  // tensors from q on, until a launch is full
-    Parts a{};
+    Parts<MOST> a{};
     a.part = plan.part;
-    for (; q >= 0 && q < count && a.count < kMostTensors; q += step) {
+    for (; q >= 0 && q < count && a.count < MOST; q += step) {
       const int64_t pieces = pieces_in(t[q]);
       if (pieces == 0 || (outputs && t[q].out == nullptr)) continue;
       const bool one = in_one_row(t[q]);
@@ -187,7 +195,7 @@ hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, 
   };
   int64_t done = 0;
   for (int64_t q = 0; q < count;) {
-    const Parts a = next(q, 1, false);
+    const Parts<MOST> a = next(q, 1, false);
     if (a.count == 0) break;
     squares_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, partial + done);
     done += a.first[a.count];
@@ -202,14 +210,20 @@ hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, 
   }
   bool stored = norm == nullptr;
   for (int64_t q = count - 1; q >= 0;) {
-    const Parts a = next(q, -1, true);
+    const Parts<MOST> a = next(q, -1, true);
     if (a.count == 0) break;
     clip_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, from, sums, max_norm, stored ? nullptr : norm, past);
     stored = true;
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  if (!stored) clip_kernel<<<1, 256, 0, st>>>(Parts{}, from, sums, max_norm, norm, false);
+  if (!stored) clip_kernel<<<1, 256, 0, st>>>(Parts<MOST>{}, from, sums, max_norm, norm, false);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_clip(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
+  return count <= kFewTensors ? clip_in<kFewTensors>(t, count, max_norm, norm, partial, st) : clip_in<kMostTensors>(t, count, max_norm, norm, partial, st);
 }
 
 }  // namespace ilargi
