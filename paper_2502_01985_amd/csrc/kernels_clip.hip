@@ -12,7 +12,8 @@ namespace ilargi {
 namespace {
 
 constexpr int kMostTensors = 64, kFewTensors = 16, kMostSums = 1024, kLoads = 4;
-constexpr int64_t kLeastPart = 2048, kMostPart = 8192;         // pieces
+// Pieces of a part: at least what a workgroup asks for at once (12 tensors, 250 KB: 9.6 us, 11.8 with twice and 11.5 with half of it).
+constexpr int64_t kLeastPart = 256 * kLoads, kMostPart = 8192;
 
 struct Part {
   const char* in;
