@@ -965,33 +965,44 @@ def ilargi_norm_grad(d_r, d_y, h, first="rms", gain1=None, bias1=None, gate=None
     where = "ilargi_norm_grad"
     block, _, gate_rows = _norm_block(where, h, first, gain1, bias1, gate, gate_act, scale, x, second, gain2, bias2, eps)
     n, m = h.shape
-    dtype = h.dtype
-    given = dict(d_h=(d_h, h), d_x=(d_x, x), d_gate=(d_gate, gate), d_gain1=(d_gain1, gain1), d_bias1=(d_bias1, bias1),
-                 d_gain2=(d_gain2, gain2), d_bias2=(d_bias2, bias2))
-    got = {}
-    for name, (t, of) in given.items():
+    dtype, device = h.dtype, h.device
+
+    def matrix(t, of, name):
+        """A result that is a matrix, its address and its leading dimension."""
+        if t is None or isinstance(t, str) and of is None:
+            return None, 0, 0
         if isinstance(t, str):
-            matrix = name in ("d_h", "d_x") or (name == "d_gate" and gate_rows)
-            if accumulate and of is not None and not matrix:
+            t = _new((n, m), dtype, device, stream)
+        return t, t.data_ptr(), _rows_of(t, name, n, m, dtype)
+
+    def sums(t, of, name):
+        """A result that is a vector of sums over the rows, and its address."""
+        if t is None or isinstance(t, str) and of is None:
+            return None, 0
+        if isinstance(t, str):
+            if accumulate:
                 raise ValueError(f"accumulate needs {name} (or None)")
-            t = _new((n, m) if matrix else (m,), dtype, h.device, stream) if of is not None else None
-        got[name] = t
-    _together(where, h.device, d_r, d_y, *got.values())
-    lds = {}
-    for name, t in got.items():
-        if name in ("d_h", "d_x") or (name == "d_gate" and gate_rows):
-            lds[name] = _rows_of(t, name, n, m, dtype) if t is not None else 0
-        else:
-            _vector(t, name, m, dtype)
-    out = _NORM_GRADS.pack(*(t.data_ptr() if t is not None else 0 for t in got.values()), lds["d_h"], lds["d_x"], lds.get("d_gate", 0))
+            t = _new((m,), dtype, device, stream)
+        return t, _vector(t, name, m, dtype)
+
+    d_h, p_h, ld_h = matrix(d_h, h, "d_h")
+    d_x, p_x, ld_x = matrix(d_x, x, "d_x")
+    if gate_rows:
+        d_gate, p_gate, ld_gate = matrix(d_gate, gate, "d_gate")
+    else:
+        (d_gate, p_gate), ld_gate = sums(d_gate, gate, "d_gate"), 0
+    d_gain1, p_gain1 = sums(d_gain1, gain1, "d_gain1")
+    d_bias1, p_bias1 = sums(d_bias1, bias1, "d_bias1")
+    d_gain2, p_gain2 = sums(d_gain2, gain2, "d_gain2")
+    d_bias2, p_bias2 = sums(d_bias2, bias2, "d_bias2")
+    out = _NORM_GRADS.pack(p_h, p_x, p_gate, p_gain1, p_bias1, p_gain2, p_bias2, ld_h, ld_x, ld_gate)
     lddr = _rows_of(d_r, "d_r", n, m, dtype) if d_r is not None else 0
     lddy = _rows_of(d_y, "d_y", n, m, dtype) if d_y is not None else 0
     need = ilargi_norm_grad_workspace_bytes(n, m, dtype) if workspace is None else 0
-    workspace, ws, ws_bytes = _scratch(workspace, need, h.device, stream)
-    _together(where, h.device, workspace)
-    _call(lib.ilargi_norm_grad, where, h.device, stream, block, _ptr(d_r), lddr, _ptr(d_y), lddy, out,
-          int(accumulate), ws, ws_bytes)
-    return tuple(got.values())
+    workspace, ws, ws_bytes = _scratch(workspace, need, device, stream)
+    _together(where, device, d_r, d_y, d_h, d_x, d_gate, d_gain1, d_bias1, d_gain2, d_bias2, workspace)
+    _call(lib.ilargi_norm_grad, where, device, stream, block, _ptr(d_r), lddr, _ptr(d_y), lddy, out, int(accumulate), ws, ws_bytes)
+    return d_h, d_x, d_gate, d_gain1, d_bias1, d_gain2, d_bias2
 
 
 def ilargi_grouped_linear_workspace_bytes(groups: int, n: int, k: int, m: int, dtype) -> Tuple[int, int]:

@@ -11,7 +11,7 @@ namespace ilargi {
 
 namespace {
 
-enum { kFull, kWhole, kRagged };       // rows that fill their threads; of whole pieces; of any length
+enum { kFull, kWhole, kRagged, kShort };       // rows that fill their threads; of whole pieces; of any length; shorter than a piece
 
 template <class T, int W, int P, int SHAPE>
 struct Row {
@@ -25,6 +25,7 @@ struct Row {
   }
   using Raw = Piece<T, V>;
   int c[P], lo[P], hi[P], m;
+  uint32_t keep[SHAPE >= kRagged ? P : 1][4];      // the bits of a piece that are the thread's own
 
   __device__ __forceinline__ void plan(int64_t cols) {
     m = (int)cols;
@@ -32,15 +33,37 @@ struct Row {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int at = (t + W * p) * V;
-      c[p] = m < V ? 0 : at < m - V ? at : m - V;
+      c[p] = SHAPE == kShort ? 0 : at < m - V ? at : m - V;
       lo[p] = at - c[p] < V ? at - c[p] : V;
-      hi[p] = m < V ? m : V;
+      hi[p] = SHAPE == kShort ? m : V;
+      if constexpr (SHAPE >= kRagged) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          keep[p][w] = V == 4 ? (live(p, w) ? ~0u : 0u) : (live(p, 2 * w) ? 0xffffu : 0u) | (live(p, 2 * w + 1) ? 0xffff0000u : 0u);
+          asm volatile("" : "+v"(keep[p][w]));     // (held: worked out again at each use they cost more than the products)
+        }
+      }
     }
   }
-  __device__ __forceinline__ bool live(int p, int j) const { return SHAPE == kRagged ? j >= lo[p] && j < hi[p] : SHAPE == kFull || lo[p] == 0; }
+  __device__ __forceinline__ void own(Raw& r, int p) const {
+    if constexpr (SHAPE >= kRagged) {
+      uint4 w = __builtin_bit_cast(uint4, r);
+      w.x &= keep[p][0]; w.y &= keep[p][1]; w.z &= keep[p][2]; w.w &= keep[p][3];
+      r = __builtin_bit_cast(Raw, w);
+    }
+  }
+  // v, or 0 for a column that is another thread's or none
+  __device__ __forceinline__ float own(float v, int e) const {
+    if constexpr (SHAPE == kFull) return v;
+    if constexpr (SHAPE == kWhole) return lo[e / V] == 0 ? v : 0.0f;
+    const int p = e / V, j = e % V;
+    const uint32_t bits = V == 4 ? keep[p][j] : (uint32_t)(j % 2 != 0 ? (int)keep[p][j / 2] >> 16 : (int)(keep[p][j / 2] << 16) >> 16);
+    return __uint_as_float(__float_as_uint(v) & bits);
+  }
+  __device__ __forceinline__ bool live(int p, int j) const { return SHAPE == kFull || (SHAPE == kWhole ? lo[p] == 0 : SHAPE == kRagged ? j >= lo[p] : lo[p] == 0 && j < hi[p]); }
   __device__ __forceinline__ void load(const void* row, Raw (&r)[P]) const {
     const T* at = (const T*)row;
-    if (SHAPE != kRagged || m >= V) {
+    if constexpr (SHAPE != kShort) {
 #pragma unroll
       for (int p = 0; p < P; ++p) r[p] = *reinterpret_cast<const Raw*>(at + c[p]);
     } else {
@@ -52,15 +75,29 @@ struct Row {
   }
   __device__ __forceinline__ void values(const Raw (&r)[P], float (&f)[E]) const {
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      Raw mine = r[p];
+      own(mine, p);
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[p * V + j] = live(p, j) ? (float)r[p].v[j] : 0.0f;
+      for (int j = 0; j < V; ++j) f[p * V + j] = SHAPE != kWhole || lo[p] == 0 ? (float)mine.v[j] : 0.0f;
+    }
+  }
+  // a gain or a bias, for good: zeros in others' columns, where a number that is not finite would spoil the sums
+  __device__ __forceinline__ void load_vector(const void* at, Raw (&r)[P]) const {
+    if (at == nullptr) return;
+    load(at, r);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      own(r[p], p);
+      if constexpr (SHAPE == kWhole)
+        if (lo[p] != 0) r[p] = __builtin_bit_cast(Raw, make_uint4(0, 0, 0, 0));
+    }
   }
   __device__ __forceinline__ void store(void* row, const float (&f)[E], bool past) const {
     T* at = (T*)row;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      if (SHAPE == kFull || (lo[p] == 0 && (SHAPE == kWhole || hi[p] == V))) {
+      if (SHAPE == kFull || (SHAPE != kShort && lo[p] == 0)) {
         Raw r;
 #pragma unroll
         for (int j = 0; j < V; ++j) r.v[j] = (T)f[p * V + j];
@@ -70,7 +107,7 @@ struct Row {
         } else {
           *reinterpret_cast<Raw*>(at + c[p]) = r;
         }
-      } else if (SHAPE == kRagged) {
+      } else if (SHAPE >= kRagged) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (live(p, j)) at[c[p] + j] = (T)f[p * V + j];
@@ -85,7 +122,7 @@ __device__ __forceinline__ float from_lane(float v) {
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 
-// Sums over the threads of a row, the same for all of them: over sixteen lanes by lane permutations of the vector units (through LDS,
+// Sums over the threads of a row (4 at least), the same for all of them: over sixteen lanes by lane permutations of the vector units (through LDS,
 // each of the six steps of a wavefront would wait a hundred cycles), then wavefronts through LDS.  `turn` alternates between two
 // places there, so one barrier a sum is enough.
 template <int W, int R>
@@ -99,8 +136,8 @@ __device__ __forceinline__ void row_sums(float (&v)[K], RowLds<W, R>& lds, int& 
   for (int k = 0; k < K; ++k) {
     v[k] += from_lane<0xB1>(v[k]);       // lanes 1 away
     v[k] += from_lane<0x4E>(v[k]);       // 2 away
-    v[k] += from_lane<0x141>(v[k]);      // mirrored in eight
-    v[k] += from_lane<0x140>(v[k]);      // mirrored in sixteen
+    if constexpr (W >= 8) v[k] += from_lane<0x141>(v[k]);       // mirrored in eight
+    if constexpr (W >= 16) v[k] += from_lane<0x140>(v[k]);      // mirrored in sixteen
     if constexpr (W >= kWave) v[k] = (lane_value(v[k], 0) + lane_value(v[k], 16)) + (lane_value(v[k], 32) + lane_value(v[k], 48));
   }
   if constexpr (W > kWave) {
@@ -134,7 +171,7 @@ __device__ __forceinline__ float normalise(const L& row, int kind, float eps, fl
     row_sums<W, L::R>(s, lds, turn);
     const float mean = s[0] * share;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = row.live(e / V, e % V) ? v[e] - mean : 0.0f;
+    for (int e = 0; e < E; ++e) v[e] = row.own(v[e] - mean, e);
   }
   s[0] = 0.0f;
 #pragma unroll
@@ -169,7 +206,7 @@ template <class L, int P>
 __device__ __forceinline__ void plus_bias(const L& row, const void* is, const typename L::Raw (&bias)[P], float (&v)[L::E]) {
   if (is == nullptr) return;
 #pragma unroll
-  for (int e = 0; e < L::E; ++e) v[e] += row.live(e / L::V, e % L::V) ? (float)bias[e / L::V].v[e % L::V] : 0.0f;
+  for (int e = 0; e < L::E; ++e) v[e] += (float)bias[e / L::V].v[e % L::V];
 }
 
 struct NormOut {
@@ -186,11 +223,11 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a
   row.plan(a.m);
   int turn = 0;
   typename L::Raw g1[P], b1[P], gr[P], g2[P], b2[P];
-  if (a.gain1 != nullptr) row.load(a.gain1, g1);
-  if (a.bias1 != nullptr) row.load(a.bias1, b1);
-  if (a.gate != nullptr && !a.gate_rows) row.load(a.gate, gr);
-  if (a.gain2 != nullptr) row.load(a.gain2, g2);
-  if (a.bias2 != nullptr) row.load(a.bias2, b2);
+  row.load_vector(a.gain1, g1);
+  row.load_vector(a.bias1, b1);
+  if (!a.gate_rows) row.load_vector(a.gate, gr);
+  row.load_vector(a.gain2, g2);
+  row.load_vector(a.bias2, b2);
   for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < a.n; i0 += (int64_t)gridDim.x * R) {
     const int64_t mine = i0 + L::slot(), i = mine < a.n ? mine : a.n - 1;
     typename L::Raw h[P], x[P];
@@ -243,7 +280,7 @@ __device__ __forceinline__ void normalise_back(const L& row, int kind, float by,
     row_sums<W, L::R>(s, lds, turn);
     const float along = s[0] * share, mean = s[1] * share;
 #pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = by * (fmaf(-along, unit[e], t[e]) - (row.live(e / L::V, e % L::V) ? mean : 0.0f));
+    for (int e = 0; e < E; ++e) t[e] = by * row.own(fmaf(-along, unit[e], t[e]) - mean, e);
   } else {
     float s[1] = {0.0f};
 #pragma unroll
@@ -292,15 +329,84 @@ struct NormGradIn {
   int64_t ld_dr, ld_dy;
 };
 constexpr int kGradWaves = 2;        // of a SIMD, at least: with 128 registers (four) a thread's values did not fit, 173 us for 132 at 8192 x 4096
-enum { kSumGain1, kSumGain2, kSumGate, kSumBias1, kSumBias2, kSums };
+enum { kSumGate, kSumGain1, kSumGain2, kSumBias1, kSumBias2, kSums };
+// Whether all five sums of such rows are held in LDS (beyond 8192 columns they do not fit), and the bytes of it.
+template <class L>
+constexpr bool kSumsInLds = L::kW == 512 && L::E == 16;
+template <class L>
+constexpr size_t kSumsLds = kSumsInLds<L> ? sizeof(float) * (kSums - 1) * L::E * L::kW : 0;
+
+// Sums over a workgroup's rows, of the columns that a thread holds: in registers, or where all five of a wide row's are wanted (8192
+// columns: 80 registers of 256) all but the gate's in LDS, each thread's in places of its own.  (3600 x 8192, bfloat16, centred: 284 us in
+// registers that spill, 111 so.)
+template <class L, int HELD, bool IN_LDS>
+struct RowSums {
+  static constexpr int E = L::E;
+  float held[IN_LDS ? 1 : HELD][E];
+  float4* mine;              // [sum][four columns][thread]
+  __device__ __forceinline__ explicit RowSums(float4* lds) : mine(lds + threadIdx.x) {
+#pragma unroll
+    for (int q = 0; q < (IN_LDS ? 1 : HELD); ++q)
+#pragma unroll
+      for (int e = 0; e < E; ++e) held[q][e] = 0.0f;
+    if constexpr (IN_LDS)
+#pragma unroll
+      for (int q = 0; q < (HELD - 1) * E / 4; ++q) mine[q * L::kW] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  static __device__ __forceinline__ constexpr bool registers(int q) { return !IN_LDS || q == 0; }
+  __device__ __forceinline__ float4& place(int q, int e) const { return mine[((q - 1) * (E / 4) + e / 4) * L::kW]; }
+  // a o b, or a
+  template <int Q>
+  __device__ __forceinline__ void add(const float (&a)[E], const float (&b)[E]) {
+    if constexpr (registers(Q)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) held[Q][e] = fmaf(a[e], b[e], held[Q][e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float4& p = place(Q, e);
+        const float4 v = p;
+        p = make_float4(fmaf(a[e], b[e], v.x), fmaf(a[e + 1], b[e + 1], v.y), fmaf(a[e + 2], b[e + 2], v.z), fmaf(a[e + 3], b[e + 3], v.w));
+      }
+    }
+  }
+  template <int Q>
+  __device__ __forceinline__ void add(const float (&a)[E]) {
+    if constexpr (registers(Q)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) held[Q][e] += a[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float4& p = place(Q, e);
+        const float4 v = p;
+        p = make_float4(a[e] + v.x, a[e + 1] + v.y, a[e + 2] + v.z, a[e + 3] + v.w);
+      }
+    }
+  }
+  template <int Q>
+  __device__ __forceinline__ void take(float (&f)[E]) const {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      if constexpr (registers(Q)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f[e + u] = held[Q][e + u];
+      } else {
+        const float4 v = place(Q, e);
+        f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
+      }
+    }
+  }
+};
 
 // The sums over this workgroup's rows go to partial[workgroup][sum][column].  FEW: there is no bias1, and those
 // of the gains alone are wanted.  A row's data are
-// asked for as soon as those of the row before have been taken out of their registers.
+// asked for as soon as those of the row before have been taken out of their registers
+// (8192 columns of bfloat16, two pieces a thread: 106 us for 3600 rows; asked for when the row begins, 148).
 template <class T, int W, int P, int SHAPE, bool FEW>
 __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial, bool past) {
   using L = Row<T, W, P, SHAPE>;
-  constexpr int E = L::E, R = L::R, V = L::V, S = sizeof(T), kHeld = FEW ? 2 : kSums;
+  constexpr int E = L::E, R = L::R, V = L::V, S = sizeof(T), kHeld = FEW ? 3 : kSums;
   __shared__ __attribute__((aligned(16))) RowLds<W, R> lds;
   __shared__ float rows_sums[R > 1 ? R : 1][R > 1 ? W * E : 1];
   L row;
@@ -310,20 +416,20 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
   typename L::Raw g1[P], b1[P], gr[P], g2[P], h[P], x[P], dr[P], dy[P];
   const int64_t first = (int64_t)blockIdx.x * R + L::slot(), step = (int64_t)gridDim.x * R;
   auto at = [&](int64_t i) { return i < a.n ? i : a.n - 1; };
-  row.load(row_at(a.h, at(first), a.ld_h, S), h);
-  if (a.gate_rows) row.load(row_at(a.gate, at(first), a.ld_gate, S), gr);
-  if (with_x) row.load(row_at(a.x, at(first), a.ld_x, S), x);
-  if (second) row.load(row_at(d.d_y, at(first), d.ld_dy, S), dy);
-  if (d.d_r != nullptr) row.load(row_at(d.d_r, at(first), d.ld_dr, S), dr);
-  if (a.gain1 != nullptr) row.load(a.gain1, g1);
-  if (!FEW && a.bias1 != nullptr) row.load(a.bias1, b1);
-  if (a.gate != nullptr && !a.gate_rows) row.load(a.gate, gr);
-  if (a.gain2 != nullptr) row.load(a.gain2, g2);
-  float sums[kHeld][E];
-#pragma unroll
-  for (int q = 0; q < kHeld; ++q)
-#pragma unroll
-    for (int e = 0; e < E; ++e) sums[q][e] = 0.0f;
+  auto load_row = [&](int64_t i) {
+    row.load(row_at(a.h, i, a.ld_h, S), h);
+    if (a.gate_rows) row.load(row_at(a.gate, i, a.ld_gate, S), gr);
+    if (with_x) row.load(row_at(a.x, i, a.ld_x, S), x);
+    if (second) row.load(row_at(d.d_y, i, d.ld_dy, S), dy);
+    if (d.d_r != nullptr) row.load(row_at(d.d_r, i, d.ld_dr, S), dr);
+  };
+  load_row(at(first));
+  row.load_vector(a.gain1, g1);
+  if constexpr (!FEW) row.load_vector(a.bias1, b1);
+  if (!a.gate_rows) row.load_vector(a.gate, gr);
+  row.load_vector(a.gain2, g2);
+  extern __shared__ __attribute__((aligned(16))) float4 sums_lds[];
+  RowSums<L, kHeld, !FEW && kSumsInLds<L>> sums(sums_lds);
   for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < a.n; i0 += step) {
     const int64_t mine = i0 + L::slot(), i = at(mine), next = at(mine + step);
     const bool is = mine < a.n;
@@ -363,11 +469,8 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
       row.values(dy, back);
       row.load(row_at(d.d_y, next, d.ld_dy, S), dy);
       if (is) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          sums[kSumGain2][e] = fmaf(back[e], r[e], sums[kSumGain2][e]);
-          if constexpr (!FEW) sums[kSumBias2][e] += back[e];
-        }
+        sums.template add<kSumGain2>(back, r);
+        if constexpr (!FEW) sums.template add<kSumBias2>(back);
       }
       times_gain(row, a.gain2, g2, back);
       normalise_back<L, W>(row, a.second, by2, r, back, lds, turn);
@@ -399,18 +502,14 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
       } else if (a.gate_rows) {
         row.store((char*)o.d_gate + i * o.ld_gate * S, u, past);
       } else if constexpr (!FEW) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) sums[kSumGate][e] += u[e];
+        sums.template add<kSumGate>(u);
       }
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) t[e] *= f[e];
     if (is) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        sums[kSumGain1][e] = fmaf(t[e], unit[e], sums[kSumGain1][e]);
-        if constexpr (!FEW) sums[kSumBias1][e] += t[e];
-      }
+      sums.template add<kSumGain1>(t, unit);
+      if constexpr (!FEW) sums.template add<kSumBias1>(t);
     }
     if (o.d_h == nullptr) continue;
     times_gain(row, a.gain1, g1, t);
@@ -419,27 +518,35 @@ __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kerne
   }
   if (partial == nullptr) return;
   float* const to = partial + (int64_t)blockIdx.x * kSums * a.m;
-  const void* const wanted[kSums] = {o.d_gain1, o.d_gain2, gate_sum ? o.d_gate : nullptr, o.d_bias1, o.d_bias2};
-#pragma unroll
-  for (int q = 0; q < kHeld; ++q) {
-    if (wanted[q] == nullptr) continue;
+  auto leave = [&](auto which, const void* wanted) {
+    constexpr int Q = decltype(which)::value;
+    if (wanted == nullptr) return;
+    float f[E];
+    sums.template take<Q>(f);
     if constexpr (R == 1) {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (row.live(e / V, e % V)) to[(int64_t)q * a.m + row.c[e / V] + e % V] = sums[q][e];
+        if (row.live(e / V, e % V)) to[(int64_t)Q * a.m + row.c[e / V] + e % V] = f[e];
     } else {
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (row.live(e / V, e % V)) rows_sums[threadIdx.x / W][row.c[e / V] + e % V] = sums[q][e];
+        if (row.live(e / V, e % V)) rows_sums[threadIdx.x / W][row.c[e / V] + e % V] = f[e];
       __syncthreads();
       for (int j = threadIdx.x; j < a.m; j += L::NT) {
         float s = rows_sums[0][j];
 #pragma unroll
         for (int r = 1; r < R; ++r) s += rows_sums[r][j];
-        to[(int64_t)q * a.m + j] = s;
+        to[(int64_t)Q * a.m + j] = s;
       }
     }
+  };
+  leave(std::integral_constant<int, kSumGain1>(), o.d_gain1);
+  leave(std::integral_constant<int, kSumGain2>(), o.d_gain2);
+  if constexpr (!FEW) {
+    leave(std::integral_constant<int, kSumGate>(), gate_sum ? o.d_gate : nullptr);
+    leave(std::integral_constant<int, kSumBias1>(), o.d_bias1);
+    leave(std::integral_constant<int, kSumBias2>(), o.d_bias2);
   }
 }
 
@@ -464,22 +571,35 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict_
   out[j] = (T)(float)(accumulate ? (double)(float)out[j] + s : s);
 }
 
-// f(row): threads of a row and pieces of a thread, the least that hold it.
-template <class T, class F>
+// f(row): threads of a row and pieces of a thread, the least that hold it.  WIDE: 512 threads, which have twice the registers of 1024, for
+// rows of up to 32 KB too.  (Gradients, 8192 columns: bfloat16 106 us for 3600 rows where 1024 threads take 197; float32 126 for 1800 and
+// 159, but 144 and 126 for 2115 x 5441 with all five sums.)
+template <class T, bool WIDE, class F>
 hipError_t by_columns(int64_t m, F f) {
   constexpr int V = ElemOf<T>::kVec;
   const int64_t pieces = (m + V - 1) / V;
   auto with = [&](auto w, auto p) {
     constexpr int W = decltype(w)::value, P = decltype(p)::value;
+    if constexpr (W == 4)
+      if (m < V) return f(Row<T, W, P, kShort>());
     return m % V != 0 ? f(Row<T, W, P, kRagged>()) : m == W * P * V ? f(Row<T, W, P, kFull>()) : f(Row<T, W, P, kWhole>());
   };
   using std::integral_constant;
   constexpr integral_constant<int, 1> one;
+  if (pieces <= 4) return with(integral_constant<int, 4>(), one);
+  if (pieces <= 8) return with(integral_constant<int, 8>(), one);
   if (pieces <= 16) return with(integral_constant<int, 16>(), one);
   if (pieces <= 64) return with(integral_constant<int, 64>(), one);
   if (pieces <= 128) return with(integral_constant<int, 128>(), one);
   if (pieces <= 256) return with(integral_constant<int, 256>(), one);
   if (pieces <= 512) return with(integral_constant<int, 512>(), one);
+  if constexpr (WIDE) {
+    if constexpr (V == 8) {
+      if (pieces <= 1024) return with(integral_constant<int, 512>(), integral_constant<int, 2>());
+    } else {
+      if (pieces > 1024 && pieces <= 2048) return with(integral_constant<int, 512>(), integral_constant<int, 4>());
+    }
+  }
   if (pieces <= 1024) return with(integral_constant<int, 1024>(), one);
   if (pieces <= 2048) return with(integral_constant<int, 1024>(), integral_constant<int, 2>());
   if constexpr (V == 4)
@@ -497,7 +617,7 @@ int64_t groups_of(int64_t n, int rows, int64_t most) {
 template <class T>
 int64_t grad_groups(int64_t n, int64_t m) {
   int64_t g = 0;
-  const hipError_t e = by_columns<T>(m, [&](auto row) {
+  const hipError_t e = by_columns<T, false>(m, [&](auto row) {
     using L = decltype(row);
     g = groups_of(n, L::R, L::NT == 256 ? 768 : 256);
     return hipSuccess;
@@ -508,7 +628,7 @@ int64_t grad_groups(int64_t n, int64_t m) {
 template <class T>
 hipError_t norm_typed(const ilargi_norm_t& a, const NormOut& o, hipStream_t st) {
   const bool past = (int64_t)sizeof(T) * a.n * a.m * ((o.r != nullptr) + (o.y != nullptr)) >= kStreamBytes;
-  return by_columns<T>(a.m, [&](auto row) {
+  return by_columns<T, false>(a.m, [&](auto row) {
     using L = decltype(row);
     norm_kernel<T, L::kW, L::kP, L::kShape><<<(unsigned)groups_of(a.n, L::R, 256 * (2048 / L::NT)), L::NT, 0, st>>>(a, o, past);
     return hipGetLastError();
@@ -524,15 +644,21 @@ hipError_t norm_grad_typed(const ilargi_norm_t& a, const NormGradIn& d, const il
   if (!sums) partial = nullptr;
   const int64_t groups = grad_groups<T>(a.n, a.m);
   if (groups > 0) {
-    const hipError_t e = by_columns<T>(a.m, [&](auto row) {
+    auto launch = [&](auto row, auto which) {
       using L = decltype(row);
-      if (few) norm_grad_kernel<T, L::kW, L::kP, L::kShape, true><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial, past);
-      else norm_grad_kernel<T, L::kW, L::kP, L::kShape, false><<<(unsigned)groups, L::NT, 0, st>>>(a, d, o, partial, past);
+      constexpr bool FEW = decltype(which)::value;
+      const auto kernel = norm_grad_kernel<T, L::kW, L::kP, L::kShape, FEW>;
+      const size_t bytes = FEW ? 0 : kSumsLds<L>;
+      if (bytes > 0)
+        if (hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); e != hipSuccess) return e;
+      kernel<<<(unsigned)groups, L::NT, bytes, st>>>(a, d, o, partial, past);
       return hipGetLastError();
-    });
+    };
+    const hipError_t e = few ? by_columns<T, true>(a.m, [&](auto row) { return launch(row, std::true_type()); })
+                             : by_columns<T, true>(a.m, [&](auto row) { return launch(row, std::false_type()); });
     if (e != hipSuccess) return e;
   }
-  if (sums) norm_join_kernel<T><<<dim3((unsigned)((a.m + 15) / 16), few ? 2 : kSums), 256, 0, st>>>(partial, (int)groups, a.m, o, gate_sum, accumulate);
+  if (sums) norm_join_kernel<T><<<dim3((unsigned)((a.m + 15) / 16), few ? 3 : kSums), 256, 0, st>>>(partial, (int)groups, a.m, o, gate_sum, accumulate);
   return hipGetLastError();
 }
 
