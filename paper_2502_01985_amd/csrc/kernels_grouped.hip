@@ -89,6 +89,8 @@ __global__ __launch_bounds__(kIndexThreads) void group_index_kernel(GroupIndex a
 }
 
 // --------------------------------------------------------------------------------------------------------- float32 products
+// As in kernels_mm.hip, bound by the starts and ends of short products: 10,000 rows in 64 groups, 220 x 256: 24 us (46 TFLOP/s).  Fetching
+// two steps ahead instead of one changed nothing there and cost large products 9 %.
 template <class T, bool QK, int TILE, int STEP>
 __device__ __forceinline__ void rows_block(const GroupedRows<Product>& a, int id, int tn, MmF32Lds<TILE, STEP>& lds) {
   const Blocks blocks(a.at, a.at.tiles, TILE);
@@ -207,7 +209,8 @@ struct GroupedGrad {
 };
 
 // g = d_out f'(pre) of a chunk of a group's rows, in the layer's type, and the column sums of the unrounded g: as layer_grad_kernel, with
-// chunks that end where groups do, 16 bytes a lane and kTurns rows of a lane on their way.  blockIdx: kGradCols columns (from `first` on),
+// chunks that end where groups do, 16 bytes a lane and kTurns rows of a lane on their way.  16384 x 4096, bfloat16, gelu: 90 us for 403 MB
+// (4.5 TB/s), 126 with 8 bytes a lane and two rows.  blockIdx: kGradCols columns (from `first` on),
 // chunk.
 constexpr int kGradCols = 128, kTurns = 4;
 template <class T>

@@ -1,4 +1,9 @@
 // Products over ragged groups of rows on the 16-bit matrix cores: the blocks of mm16_block.h, each of one group.
+//
+// Groups of equal size take as long as one layer of all rows (16384 x 2048 x 4096, gelu and z kept: 287 us both; the product without them
+// 235, the library's 232).  Skewed ones pay for the blocks that their ends leave part empty and for the last round: 1088 blocks for 1024
+// 327 us.  Bound by the matrix cores; the epilogue, 50 us of it, is not hidden, as one workgroup of 256 x 256 fills a compute unit (blocks of 128,
+// two to a unit: 386 us).
 #include "mm16_block.h"
 
 #include "grouped.h"
@@ -32,7 +37,8 @@ __device__ __forceinline__ Product16 block_alone(const Product16& b, int ti, int
   return c;
 }
 
-// blockIdx: block of 256, or a share of one of the last round (from `first` on).
+// blockIdx: block of 256, or a share of one of the last round (from `first` on).  (544 blocks of 64 steps: 327 us where the last 32 take a
+// round of their own, 260 in shares of eight steps and 17 for their sums.)
 template <bool QK>
 __global__ __launch_bounds__(512, 1) void grouped16_rounds_kernel(GroupedRows<Product16> a, int first, int tn) {
   constexpr int B = 256;
@@ -57,7 +63,8 @@ __global__ __launch_bounds__(512, 1) void grouped16_rounds_kernel(GroupedRows<Pr
   });
 }
 
-// The shares of the last round's blocks, four sums of a row a thread and four rows of a block a workgroup.  blockIdx: rows, block.
+// The shares of the last round's blocks, four sums of a row a thread and kTailRows rows of a block a workgroup.  blockIdx: rows, block.
+constexpr int kTailRows = 8;
 __global__ __launch_bounds__(256) void grouped16_tail_kernel(GroupedRows<Product16> a, int tn) {
   constexpr int B = 256;
   const Blocks blocks(a.at, a.at.tiles, B);
@@ -65,27 +72,32 @@ __global__ __launch_bounds__(256) void grouped16_tail_kernel(GroupedRows<Product
   if (tail.shares < 2 || (int)blockIdx.y >= tail.rest) return;
   grouped_rows_block<2>(a, blocks, tail.full + blockIdx.y, tn, [&](const Product16& b, int ti, int tj, int64_t) {
     const Product16 c = block_alone(b, ti, tj);
-    const int64_t i = blockIdx.x * 4 + threadIdx.x / 64, j = threadIdx.x % 64 * 4, ldp = (c.N + 3) / 4 * 4;
-    const int valid = quad_valid(i, j, c.M, c.N);
-    if (valid == 0) return;
-    const int64_t row = (int64_t)ti * B + i, col = (int64_t)tj * B + j;
-    const SrcQuad raw = epilogue_ask(b.epi, 0, row, col, valid);
+    const int64_t j = threadIdx.x % 64 * 4, ldp = (c.N + 3) / 4 * 4, col = (int64_t)tj * B + j;
     float bias[4];
-    epilogue_bias(b.epi, col, valid, bias);
-    const float* p = a.partial + (int64_t)blockIdx.y * tail.shares * (B * B) + i * ldp + j;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int z = 0; z < tail.shares; ++z) {
-      const f32x4 t = *reinterpret_cast<const f32x4*>(p + (int64_t)z * (B * B));
+    epilogue_bias(b.epi, col, (int)(c.N - j < 4 ? c.N - j : 4), bias);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += t[q];
+    for (int t = 0; t < kTailRows; t += 4) {
+      const int64_t i = blockIdx.x * kTailRows + t + threadIdx.x / 64, row = (int64_t)ti * B + i;
+      const int valid = quad_valid(i, j, c.M, c.N);
+      if (valid == 0) continue;
+      const SrcQuad raw = epilogue_ask(b.epi, 0, row, col, valid);
+      const float* p = a.partial + (int64_t)blockIdx.y * tail.shares * (B * B) + i * ldp + j;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int z = 0; z < tail.shares; ++z) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(p + (int64_t)z * (B * B));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += s[q];
+      }
+      epilogue4(b.epi, 1.0f, 0, row, col, valid, bias, raw, v);
     }
-    epilogue4(b.epi, 1.0f, 0, row, col, valid, bias, raw, v);
   });
 }
 
 // The same where groups have few rows: what counts is the bytes of the matrices, and so how many of them are on their way.  A workgroup
-// forms 32 rows by 64 columns, its steps of 64 k fetched kFewStages - 1 ahead; each wavefront has 16 of the columns.
+// forms 32 rows by 64 columns, its steps of 64 k fetched kFewStages - 1 ahead; each wavefront has 16 of the columns.  8 rows, 16 groups of
+// 2048 x 2048: 13 us, 4.2 TB/s of 54 MB, in one launch; in blocks of 128 with shares of k 22 in three.  Shares for two workgroups a compute unit
+// instead of one: 17.6 with the launch that adds them; eight stages: the same.
 constexpr int kFewRows = 32, kFewCols = 64, kFewStages = 6;
 template <bool QK>
 __global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Product16> a, int first_block, int tn) {
@@ -196,7 +208,7 @@ hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int6
     else grouped16_rounds_kernel<false><<<blocks, 512, 0, st>>>(a, (int)first, tn);
   });
   if (e != hipSuccess || (a.p.K + kBK - 1) / kBK < 8) return e;       // (shares have four steps at least)
-  grouped16_tail_kernel<<<dim3(64, kUnits / 2), 256, 0, st>>>(a, tn);
+  grouped16_tail_kernel<<<dim3(256 / kTailRows, kUnits / 2), 256, 0, st>>>(a, tn);
   return hipGetLastError();
 }
 
