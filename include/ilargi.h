@@ -472,7 +472,8 @@ ilargi_status_t ilargi_grouped_linear_grad(const ilargi_groups_t* layer, const i
  * out of the call is refused, except that of column blocks of one matrix (equal leading dimensions).  norm: device float32 (optional).
  * (It is stored in 32 bits: infinite beyond 3.4e38, where the tensors are scaled all the same.)
  * max_norm may be infinite: outputs are copies.  count may be 0 (norm 0).
- * Errors: NULL (tensors, an in, workspace), SHAPE (count outside [0, 65535], rows or cols < 0, a leading dimension below cols, a
+ * Errors: NULL (tensors, an in, workspace), SHAPE (count outside [0, 65535], rows or cols < 0, rows above 2^31 - 1, more than 2^46
+ * elements from a tensor's first to its last, a leading dimension below cols, a
  * max_norm below 0 or no number, overlaps), UNSUPPORTED (type), WORKSPACE, DEVICE. */
 typedef struct {
   const void* in;

@@ -209,7 +209,9 @@ ilargi_status_t check_tensors(const ilargi_tensor_t* t, int64_t count) {
     if (!is_type(t[q].type)) return refuse(ILARGI_ERR_UNSUPPORTED, "clip_norm: tensor %lld is of no such element type", (long long)q);
     if (t[q].rows < 0 || t[q].rows > kMost || t[q].cols < 0 || t[q].cols > (1ll << 40))
       return refuse(ILARGI_ERR_SHAPE, "clip_norm: tensor %lld is %lld x %lld", (long long)q, (long long)t[q].rows, (long long)t[q].cols);
-    const int64_t most = 1ll << 40;
+    const int64_t most = 1ll << 40, ld = std::max(t[q].ld_in, t[q].out != nullptr ? t[q].ld_out : 0);
+    if (t[q].rows > 1 && ld > (1ll << 46) / t[q].rows)
+      return refuse(ILARGI_ERR_SHAPE, "clip_norm: tensor %lld is %lld x %lld", (long long)q, (long long)t[q].rows, (long long)t[q].cols);
     if (t[q].ld_in < t[q].cols || t[q].ld_in > most || (t[q].out != nullptr && (t[q].ld_out < t[q].cols || t[q].ld_out > most)))
       return refuse(ILARGI_ERR_SHAPE, "clip_norm: a leading dimension of tensor %lld below its columns, or above 2^40", (long long)q);
     if (t[q].rows > 0 && t[q].cols > 0 && t[q].in == nullptr) return refuse(ILARGI_ERR_NULL, "clip_norm: tensor %lld is NULL", (long long)q);
@@ -377,7 +379,9 @@ ilargi_status_t ilargi_norm(const ilargi_norm_t* block, void* r, int64_t ld_r, v
   if ((r != nullptr && ld_r < block->m) || (y != nullptr && ld_y < block->m))
     return refuse(ILARGI_ERR_SHAPE, "norm: a leading dimension below m = %lld", (long long)block->m);
   if (block->n == 0 || (r == nullptr && y == nullptr)) return ILARGI_OK;
-  return done("norm", launch_norm(*block, r, ld_r, y, ld_y, (hipStream_t)stream));
+  ilargi_norm_t a = *block;
+  if (a.gate == nullptr) a.gate_rows = 0;               // (no gate has no rows)
+  return done("norm", launch_norm(a, r, ld_r, y, ld_y, (hipStream_t)stream));
 }
 
 ilargi_status_t ilargi_norm_grad_workspace_bytes(int64_t n, int64_t m, ilargi_type_t type, size_t* bytes) {
@@ -392,7 +396,8 @@ ilargi_status_t ilargi_norm_grad(const ilargi_norm_t* block, const void* d_r, in
                                  const ilargi_norm_grads_t* out, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
   if (ilargi_status_t e = check_norm("norm_grad", block); e != ILARGI_OK) return e;
   if (out == nullptr) return refuse(ILARGI_ERR_NULL, "norm_grad: out is NULL");
-  const ilargi_norm_t& a = *block;
+  ilargi_norm_t a = *block;
+  if (a.gate == nullptr) a.gate_rows = 0;
   const bool second = a.second != ILARGI_NORM_NONE;
   if (!second && (d_y != nullptr || out->d_gain2 != nullptr || out->d_bias2 != nullptr))
     return refuse(ILARGI_ERR_UNSUPPORTED, "norm_grad: d_y, d_gain2 or d_bias2 without a second norm");

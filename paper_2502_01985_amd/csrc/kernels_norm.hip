@@ -259,11 +259,11 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(ilargi_norm_t a
       for (int e = 0; e < E; ++e) v[e] *= a.scale;
     }
     if (o.r != nullptr && mine < a.n) row.store((char*)o.r + i * o.ld_r * S, v, past);
-    if (a.second == ILARGI_NORM_NONE) continue;
+    if (a.second == ILARGI_NORM_NONE || o.y == nullptr) continue;
     normalise<L, W>(row, a.second, a.eps, v, lds, turn);
     times_gain(row, a.gain2, g2, v);
     plus_bias(row, a.bias2, b2, v);
-    if (o.y != nullptr && mine < a.n) row.store((char*)o.y + i * o.ld_y * S, v, past);
+    if (mine < a.n) row.store((char*)o.y + i * o.ld_y * S, v, past);
   }
 }
 

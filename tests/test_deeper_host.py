@@ -115,7 +115,7 @@ def _clip(entries, max_norm=1.0, ws=P, nbytes=1 << 40, count=None):
 
 @pytest.mark.parametrize("entry,status", [
     ((P, P, -1, 8, 8, 8, 0), il.ERR_SHAPE), ((P, P, 4, -1, 8, 8, 0), il.ERR_SHAPE), ((P, P, 4, 8, 7, 8, 0), il.ERR_SHAPE), ((P, P, 4, 8, 8, 7, 0), il.ERR_SHAPE),
-    ((P, P, 4, 8, 8, 9, 0), il.ERR_SHAPE), ((None, P, 4, 8, 8, 8, 0), il.ERR_NULL), ((P, P, 4, 8, 8, 8, 2), il.ERR_UNSUPPORTED),
+    ((P, P, 4, 8, 8, 9, 0), il.ERR_SHAPE), ((None, P, 4, 8, 8, 8, 0), il.ERR_NULL), ((P, P, 1 << 30, 8, 1 << 20, 1 << 20, 0), il.ERR_SHAPE), ((P, None, (1 << 31) - 1, 1 << 40, 1 << 40, 0, 0), il.ERR_SHAPE), ((P, P, 4, 8, 8, 8, 2), il.ERR_UNSUPPORTED),
     ((P, P + 4, 4, 8, 8, 8, 0), il.ERR_SHAPE), ((P, P + 32, 4, 8, 8, 8, 0), il.ERR_SHAPE),
 ])
 def test_clip_refuses_tensors(entry, status):

@@ -392,6 +392,49 @@ def test_on_another_stream_and_in_a_graph(il):
             assert all(torch.equal(a, b) for a, b in zip(want, all_of()))
 
 
+def test_no_gate_with_rows(il):
+    """A block that says gate_rows and has no gate, as the C interface allows: as without."""
+    import ctypes
+    gen = _gen(7)
+    n, m = 20, 100
+    h, d = _matrix(n, m, F32, gen), _matrix(n, m, F32, gen)
+    r, dh = torch.empty_like(h), torch.empty_like(h)
+    block = il.NormStruct(n, m, 0, 1, 0, 3, 1, 0.5, EPS, h.data_ptr(), None, None, None, None, None, None, m, 0, 0)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert il.lib.ilargi_norm(ctypes.byref(block), r.data_ptr(), m, None, 0, stream) == il.OK
+    grads = il.NormGradsStruct(dh.data_ptr(), None, None, None, None, None, None, m, 0, 0)
+    assert il.lib.ilargi_norm_grad(ctypes.byref(block), d.data_ptr(), m, None, 0, ctypes.byref(grads), 0, None, 0, stream) == il.OK
+    assert torch.equal(r, il.ilargi_norm(h, scale=0.5, eps=EPS)[0]) and torch.equal(dh, il.ilargi_norm_grad(d, None, h, scale=0.5, eps=EPS)[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m", [8192, 6001, 12_000])
+def test_wide_rows_with_all_their_sums(il, dtype, m):
+    """Rows whose sums do not fit the registers, eagerly and in a graph."""
+    gen = _gen(m)
+    n = 300
+    h, x, dr, dy = (_matrix(n, m, dtype, gen) for _ in range(4))
+    v = [torch.randn(m, generator=gen, device="cuda").to(dtype) for _ in range(5)]
+    args = dict(first="centred", gain1=v[0], bias1=v[1], gate=v[2], gate_act="silu", x=x, second="centred", gain2=v[3], bias2=v[4])
+    want = _oracle(("centred", "centred"), h, x, v[2], v[0], v[1], v[3], v[4], "silu", 1.0, dr, dy)
+    out = {k: torch.empty(n, m, dtype=dtype, device="cuda") if k in ("d_h", "d_x") else torch.empty(m, dtype=dtype, device="cuda") for k in GRADS}
+    ws = torch.empty(il.ilargi_norm_grad_workspace_bytes(n, m, dtype), dtype=torch.uint8, device="cuda")
+    step = lambda: il.ilargi_norm_grad(dr, dy, h, workspace=ws, **args, **out)
+    step()
+    for k in GRADS:
+        _close(out[k], want[k], dtype, k)
+    kept = [out[k].clone() for k in GRADS]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for k in GRADS:
+            out[k].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], t) for k, t in zip(GRADS, kept))
+
+
 def test_python_refuses(il):
     a, v = torch.zeros(4, 8, device="cuda"), torch.zeros(8, device="cuda")
     bad = [lambda: il.ilargi_norm(a, first="layer"), lambda: il.ilargi_norm(a, x=a[:3]), lambda: il.ilargi_norm(a, gain1=v[:7]), lambda: il.ilargi_norm(a, gate_act="tanh"),
