@@ -217,6 +217,39 @@ __device__ __forceinline__ void grouped_sums_block(const GroupedSums<Prod>& a, i
   run(sums_of(a, q.group, r0, rows, SIZE), ti, tj, to);
 }
 
+// The elementwise pass of a gradient and its column sums.
+struct GroupedGrad {
+  LayerGradArgs g;
+  GroupIndex at;
+  int chunk;
+  int64_t ld_dbias;
+  float* partial;        // m sums a chunk
+};
+
+// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in float64: they cancel
+// each other as the rows do.  16 columns from 16 `block` on, of group g.
+struct BiasLds {
+  double part[16][17];
+};
+template <class T>
+__device__ __forceinline__ void bias_block(const GroupedGrad& a, int64_t block, int g, BiasLds& lds) {
+  const int c = threadIdx.x % 16, q = threadIdx.x / 16;
+  const int64_t j = block * 16 + c, m = a.g.m;
+  double s = 0.0;
+  int first_chunk, end_chunk;
+  Blocks(a.at, a.at.chunks, a.chunk).of_group(g, &first_chunk, &end_chunk);
+  if (j < m) {
+#pragma unroll 4
+    for (int u = first_chunk + q; u < end_chunk; u += 16) s += a.partial[(int64_t)u * m + j];
+  }
+  lds.part[q][c] = s;
+  __syncthreads();
+  if (q != 0 || j >= m) return;
+  for (int u = 1; u < 16; ++u) s += lds.part[u][c];
+  T* const out = (T*)a.g.d_bias + g * a.ld_dbias + j;
+  *out = (T)(float)(a.g.accumulate ? (double)(float)*out + s : s);
+}
+
 // Blocks of 256: one workgroup fits a compute unit, so the blocks go in rounds of kUnits, and those of the last round, where they are less
 // than half of one, are split into shares of k that fill it (`partial`: kTailBytes for their sums; a launch adds them).
 constexpr int kUnits = 256;
@@ -235,6 +268,9 @@ __host__ __device__ inline Tail tail_of(int total, int steps) {
 }
 hipError_t launch_grouped16_rows(const GroupedRows<Product16>& a, int tile, int64_t tiles, int splits, hipStream_t st);
 hipError_t launch_grouped16_sums(const GroupedSums<Product16>& a, int tile, int64_t parts, hipStream_t st);
+// Both products of a small gradient and its bias in one launch: `tile` of the rows 128 or 32, of the sums 128.
+hipError_t launch_grouped16_both(const GroupedSums<Product16>& w, int64_t w_blocks, const GroupedRows<Product16>& x, int tile, int64_t x_blocks, const GroupedGrad& b,
+                                 int64_t b_blocks, hipStream_t st);
 
 }  // namespace ilargi
 #endif

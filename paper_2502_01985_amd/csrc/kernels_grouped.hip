@@ -200,14 +200,6 @@ __global__ __launch_bounds__(256) void grouped_sums_join_kernel(Epilogue epi, in
 }
 
 // ------------------------------------------------------------------------------------- the elementwise pass of the gradient
-struct GroupedGrad {
-  LayerGradArgs g;
-  GroupIndex at;
-  int chunk;
-  int64_t ld_dbias;
-  float* partial;        // m sums a chunk
-};
-
 // g = d_out f'(pre) of a chunk of a group's rows, in the layer's type, and the column sums of the unrounded g: as layer_grad_kernel, with
 // chunks that end where groups do, 16 bytes a lane and kTurns rows of a lane on their way.  16384 x 4096, bfloat16, gelu: 90 us for 403 MB
 // (4.5 TB/s), 126 with 8 bytes a lane and two rows.  blockIdx: kGradCols columns (from `first` on),
@@ -278,29 +270,6 @@ __global__ __launch_bounds__(256) void grouped_grad_kernel(GroupedGrad a, int64_
   a.partial[(int64_t)u * y.m + c] = t;
 }
 
-// The chunks of every group, sixteen threads a column: each adds every sixteenth, then they are added in order, in float64: they cancel
-// each other as the rows do.  16 columns from 16 `block` on, of group g.
-struct BiasLds {
-  double part[16][17];
-};
-template <class T>
-__device__ __forceinline__ void bias_block(const GroupedGrad& a, int64_t block, int g, BiasLds& lds) {
-  const int c = threadIdx.x % 16, q = threadIdx.x / 16;
-  const int64_t j = block * 16 + c, m = a.g.m;
-  double s = 0.0;
-  int first_chunk, end_chunk;
-  Blocks(a.at, a.at.chunks, a.chunk).of_group(g, &first_chunk, &end_chunk);
-  if (j < m) {
-#pragma unroll 4
-    for (int u = first_chunk + q; u < end_chunk; u += 16) s += a.partial[(int64_t)u * m + j];
-  }
-  lds.part[q][c] = s;
-  __syncthreads();
-  if (q != 0 || j >= m) return;
-  for (int u = 1; u < 16; ++u) s += lds.part[u][c];
-  T* const out = (T*)a.g.d_bias + g * a.ld_dbias + j;
-  *out = (T)(float)(a.g.accumulate ? (double)(float)*out + s : s);
-}
 // blockIdx: 16 columns (from `first` on), group.
 template <class T>
 __global__ __launch_bounds__(256) void grouped_bias_kernel(GroupedGrad a, int64_t first) {
@@ -511,16 +480,20 @@ GroupedRows<Product> rows_in_f32(const ilargi_groups_t& y, const Held& P, const 
   a.p.Q = {Q.p, Q.ld, q_rows, bf16, 0};
   return a;
 }
+GroupedRows<Product16> rows_in_16(const ilargi_groups_t& y, const Held& P, const Held& Q, int q_rows, int64_t N, int64_t K, const Epilogue& epi, int64_t far_bias, const GroupIndex& at,
+                                  const RowsPlan& plan, float* partial) {
+  GroupedRows<Product16> a = rows_of_layer<Product16>(y, N, K, epi, Q.stride, far_bias, at, plan, partial);
+  a.p.P = {P.p, P.ld, 0, 0, 0, y.n};
+  a.p.Q = {Q.p, Q.ld, q_rows, 0, 0, q_rows ? up8(Q.cols) : Q.rows};
+  a.p.kind = kMm16Bf16;
+  a.p.past = plan.splits == 1 && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
+  return a;
+}
 hipError_t rows_product(const ilargi_groups_t& y, const Held& P, const Held& Q, int q_rows, int64_t N, int64_t K, const Epilogue& epi, int64_t far_bias, const GroupIndex& at,
                         const RowsPlan& plan, bool h16, float* partial, hipStream_t st) {
   hipError_t e;
   if (h16) {
-    GroupedRows<Product16> a = rows_of_layer<Product16>(y, N, K, epi, Q.stride, far_bias, at, plan, partial);
-    a.p.P = {P.p, P.ld, 0, 0, 0, y.n};
-    a.p.Q = {Q.p, Q.ld, q_rows, 0, 0, q_rows ? up8(Q.cols) : Q.rows};
-    a.p.kind = kMm16Bf16;
-    a.p.past = plan.splits == 1 && (epi.pre != nullptr ? 4 : 2) * y.n * N >= kStreamBytes;
-    e = launch_grouped16_rows(a, plan.tile, plan.tiles, plan.splits, st);
+    e = launch_grouped16_rows(rows_in_16(y, P, Q, q_rows, N, K, epi, far_bias, at, plan, partial), plan.tile, plan.tiles, plan.splits, st);
   } else {
     const GroupedRows<Product> a = rows_in_f32(y, P, Q, q_rows, N, K, epi, far_bias, at, plan, partial);
     e = y.type == ILARGI_TYPE_BF16 ? rows_f32<bf16_t>(a, plan.tile, plan.tiles, plan.splits, st) : rows_f32<float>(a, plan.tile, plan.tiles, plan.splits, st);
@@ -554,15 +527,18 @@ hipError_t add_parts(const ilargi_groups_t& y, const Epilogue& epi, int64_t far_
     grouped_sums_join_kernel<<<dim3(blocks, places), 256, 0, st>>>(epi, y.k, y.m, at, plan.part, far_out, first, partial);
   });
 }
+GroupedSums<Product16> sums_in_16(const ilargi_groups_t& y, const Held& P, const Held& Q, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, float* partial) {
+  GroupedSums<Product16> a = sums_of_layer<Product16>(y, epi, far_out, at, plan, partial);
+  a.p.P = {P.p, P.ld, 1, 0, 0, up8(P.cols)};
+  a.p.Q = {Q.p, Q.ld, 1, 0, 0, up8(Q.cols)};
+  a.p.kind = kMm16Bf16;
+  return a;
+}
 hipError_t sums_product(const ilargi_groups_t& y, const Held& P, const Held& Q, const Epilogue& epi, int64_t far_out, const GroupIndex& at, const SumsPlan& plan, bool h16, float* partial,
                         hipStream_t st) {
   hipError_t e;
   if (h16) {
-    GroupedSums<Product16> a = sums_of_layer<Product16>(y, epi, far_out, at, plan, partial);
-    a.p.P = {P.p, P.ld, 1, 0, 0, up8(P.cols)};
-    a.p.Q = {Q.p, Q.ld, 1, 0, 0, up8(Q.cols)};
-    a.p.kind = kMm16Bf16;
-    e = launch_grouped16_sums(a, plan.tile, plan.parts, st);
+    e = launch_grouped16_sums(sums_in_16(y, P, Q, epi, far_out, at, plan, partial), plan.tile, plan.parts, st);
   } else {
     const GroupedSums<Product> a = sums_in_f32(y, P, Q, epi, far_out, at, plan, partial);
     e = y.type == ILARGI_TYPE_BF16 ? sums_f32<bf16_t>(a, plan.tile, plan.parts, st) : sums_f32<float>(a, plan.tile, plan.parts, st);
@@ -623,10 +599,11 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   const int chunk = chunk_rows(y);
   const bool passes = dz != nullptr || a.d_bias != nullptr;
   if (hipError_t e = find_groups(at, a.d_X != nullptr ? rows.tile : 0, a.d_W != nullptr ? sums.part : 0, passes ? chunk : 0, st); e != hipSuccess) return e;
-  const int64_t tm = blocks_in(y.k, 64), tn = blocks_in(y.m, 64), bias_columns = blocks_in(y.m, 16);
-  const int64_t w_blocks = sums.parts * tm * tn, x_blocks = rows.tiles * tm, b_blocks = a.d_bias != nullptr ? y.groups * bias_columns : 0;
-  const bool together = a.d_X != nullptr && a.d_W != nullptr && y.n > 0 && !rows16 && !sums16 && rows.tile == 64 && sums.tile == 64 && rows.splits == 1 &&
-                        w_blocks + x_blocks + b_blocks <= kMostThreads / 256;
+  const int64_t side = sums16 ? 128 : 64, cols = rows16 && rows.tile != 32 ? 128 : 64;
+  const int64_t tm = blocks_in(y.k, side), tn = blocks_in(y.m, side), bias_columns = blocks_in(y.m, 16);
+  const int64_t w_blocks = sums.parts * tm * tn, x_blocks = rows.tiles * blocks_in(y.k, cols), b_blocks = a.d_bias != nullptr ? y.groups * bias_columns : 0;
+  const bool alike = rows16 == sums16 && sums.tile == side && rows.splits == 1 && (rows16 ? rows.tile != 256 : rows.tile == 64);
+  const bool together = a.d_X != nullptr && a.d_W != nullptr && y.n > 0 && alike && w_blocks + x_blocks + b_blocks <= kMostThreads / 256;
   GroupedGrad g{};
   g.g = {y.n, y.m, a.d_out, a.ld_dout, a.pre_in, a.ld_pre, y.act, bf16, dz, up8(y.m), a.d_bias, a.accumulate};
   g.at = at; g.chunk = chunk; g.ld_dbias = a.ld_dbias;
@@ -658,12 +635,19 @@ hipError_t launch_grouped_grad(const GroupedArgs& a, char* ws, hipStream_t st) {
   if (a.accumulate) { epi_w.src = a.d_W; epi_w.ld_src = a.ld_dw; epi_w.src_bf16 = bf16; }
   float* partial = (float*)(ws + l.shares);
   if (together) {
-    const GroupedSums<Product> sw = sums_in_f32(y, x, z, epi_w, a.stride_dw, at, sums, partial);
-    const GroupedRows<Product> rx = rows_in_f32(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial);
-    const unsigned all = (unsigned)(w_blocks + x_blocks + b_blocks);
-    if (bf16) grouped_both_kernel<bf16_t><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
-    else grouped_both_kernel<float><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipError_t e;
+    if (rows16) {
+      e = launch_grouped16_both(sums_in_16(y, x, z, epi_w, a.stride_dw, at, sums, partial), w_blocks, rows_in_16(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial), rows.tile, x_blocks, g,
+                                b_blocks, st);
+    } else {
+      const GroupedSums<Product> sw = sums_in_f32(y, x, z, epi_w, a.stride_dw, at, sums, partial);
+      const GroupedRows<Product> rx = rows_in_f32(y, z, w, 0, y.k, y.m, epi, 0, at, rows, partial);
+      const unsigned all = (unsigned)(w_blocks + x_blocks + b_blocks);
+      if (bf16) grouped_both_kernel<bf16_t><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
+      else grouped_both_kernel<float><<<all, 256, 0, st>>>(sw, (int)w_blocks, (int)tm, (int)tn, rx, (int)x_blocks, (int)tm, g, (int)bias_columns);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
     return add_parts(y, epi_w, a.stride_dw, at, sums, partial, st);
   }
   if (a.d_X != nullptr && y.n > 0)

@@ -12,18 +12,22 @@ namespace ilargi {
 
 namespace {
 
-// blockIdx: block of 128 (from `first` on), none, share of k.  Q: a matrix for each group, its rows over k (QK) or its columns.
+// Block `id` of 128.  Q: a matrix for each group, its rows over k (QK) or its columns.
 template <bool QK>
-__global__ __launch_bounds__(256, 2) void grouped16_rows_kernel(GroupedRows<Product16> a, int first, int tn) {
+__device__ __forceinline__ void rows128_block(const GroupedRows<Product16>& a, int id, int tn, char* lds) {
   constexpr int B = 128;
-  __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, B, B, 2, 2>()];
   const Blocks blocks(a.at, a.at.tiles, B);
-  const int id = first + blockIdx.x;
   if (id >= blocks.total * tn) return;
   grouped_rows_block<2>(a, blocks, id, tn, [&](Product16 b, int ti, int tj, int64_t row) {
     b.P.across = b.M;
     mm16_block<false, QK, B, B, 2, 2>(b, ti, tj, (int)blockIdx.z, (int)a.share, sums_of_rows(a, row), lds);
   });
+}
+// blockIdx: block (from `first` on), none, share of k.
+template <bool QK>
+__global__ __launch_bounds__(256, 2) void grouped16_rows_kernel(GroupedRows<Product16> a, int first, int tn) {
+  __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<false, QK, 128, 128, 2, 2>()];
+  rows128_block<QK>(a, first + blockIdx.x, tn, lds);
 }
 
 // A block of 256 as a product of its own.
@@ -98,16 +102,15 @@ __global__ __launch_bounds__(256) void grouped16_tail_kernel(GroupedRows<Product
 // forms 32 rows by 64 columns, its steps of 64 k fetched kFewStages - 1 ahead; each wavefront has 16 of the columns.  8 rows, 16 groups of
 // 2048 x 2048: 13 us, 4.2 TB/s of 54 MB, in one launch; in blocks of 128 with shares of k 22 in three.  Shares for two workgroups a compute unit
 // instead of one: 17.6 with the launch that adds them; eight stages: the same.
-constexpr int kFewRows = 32, kFewCols = 64, kFewStages = 6;
+constexpr int kFewRows = 32, kFewCols = 64, kFewStages = 6, kFewLds = kFewStages * (kFewRows + kFewCols) * kBK * 2;
 template <bool QK>
-__global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Product16> a, int first_block, int tn) {
+__device__ __forceinline__ void few_block(const GroupedRows<Product16>& a, int id, int tn, char* lds_all) {
   constexpr int NT = 256, FM = kFewRows / 16;
   using TileP = Tile<false, kFewRows, NT>;
   using TileQ = Tile<QK, kFewCols, NT>;
   constexpr int kStage = TileP::kBytes + TileQ::kBytes, kEach = TileP::kLoads + TileQ::kLoads;
-  __shared__ __attribute__((aligned(1024))) char lds_all[kFewStages * kStage];
+  static_assert(kFewStages * kStage == kFewLds, "the stages fill it");
   const Blocks blocks(a.at, a.at.tiles, kFewRows);
-  const int id = first_block + blockIdx.x;
   if (id >= blocks.total * tn) return;
   grouped_rows_block<2>(a, blocks, id, tn, [&](const Product16& b, int ti, int tj, int64_t row) {
     float* const to = sums_of_rows(a, row);
@@ -175,6 +178,12 @@ __global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Produ
   });
 }
 
+template <bool QK>
+__global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Product16> a, int first, int tn) {
+  __shared__ __attribute__((aligned(1024))) char lds[kFewLds];
+  few_block<QK>(a, first + blockIdx.x, tn, lds);
+}
+
 // blockIdx: block of a part of a group's rows (from `first` on).
 template <int B, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_sums_kernel(GroupedSums<Product16> a, int first, int tm, int tn) {
@@ -182,6 +191,26 @@ __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_s
   grouped_sums_block<2>(a, first + blockIdx.x, tm, tn, [&](const Product16& b, int ti, int tj, float* to) {
     mm16_block<true, true, B, B, WM, WN>(b, ti, tj, 0, (int)((b.K + kBK - 1) / kBK), to, lds);
   });
+}
+
+// Both products of a small gradient and its bias: `sums` blocks of d_W, `rows` of d_X (FEW: of few rows), and those of the bias.  2102 rows in 4
+// groups, 64 x 512: 24 us in all for 36 in launches of their own; 4000 in 8, 1024 x 1024: 68 for 79.
+template <bool FEW>
+__global__ __launch_bounds__(256, 2) void grouped16_both_kernel(GroupedSums<Product16> w, int sums, int tm, int tn, GroupedRows<Product16> x, int rows, int tn_x, GroupedGrad b, int columns) {
+  constexpr int kSumsLds = mm16_lds<true, true, 128, 128, 2, 2>(), kRowsLds = FEW ? kFewLds : mm16_lds<false, false, 128, 128, 2, 2>();
+  __shared__ __attribute__((aligned(1024))) char lds[kSumsLds > kRowsLds ? kSumsLds : kRowsLds];
+  static_assert(sizeof(BiasLds) <= sizeof(lds), "the column sums fit too");
+  const int id = blockIdx.x;
+  if (id < sums) {
+    grouped_sums_block<2>(w, id, tm, tn, [&](const Product16& p, int ti, int tj, float* to) {
+      mm16_block<true, true, 128, 128, 2, 2>(p, ti, tj, 0, (int)((p.K + kBK - 1) / kBK), to, lds);
+    });
+  } else if (id - sums < rows) {
+    if constexpr (FEW) few_block<false>(x, id - sums, tn_x, lds);
+    else rows128_block<false>(x, id - sums, tn_x, lds);
+  } else {
+    bias_block<bf16_t>(b, (id - sums - rows) % columns, (id - sums - rows) / columns, *reinterpret_cast<BiasLds*>(lds));
+  }
 }
 
 }  // namespace
@@ -218,6 +247,16 @@ hipError_t launch_grouped16_sums(const GroupedSums<Product16>& a, int tile, int6
     if (tile == 256) grouped16_sums_kernel<256, 2, 4><<<blocks, 512, 0, st>>>(a, (int)first, tm, tn);
     else grouped16_sums_kernel<128, 2, 2><<<blocks, 256, 0, st>>>(a, (int)first, tm, tn);
   });
+}
+
+hipError_t launch_grouped16_both(const GroupedSums<Product16>& w, int64_t w_blocks, const GroupedRows<Product16>& x, int tile, int64_t x_blocks, const GroupedGrad& b,
+                                 int64_t b_blocks, hipStream_t st) {
+  const int tm = (int)((w.p.M + 127) / 128), tn = (int)((w.p.N + 127) / 128), cols = tile == kFewRows ? kFewCols : 128, tn_x = (int)((x.p.N + cols - 1) / cols);
+  const int columns = (int)((b.g.m + 15) / 16);
+  const unsigned all = (unsigned)(w_blocks + x_blocks + b_blocks);
+  if (tile == kFewRows) grouped16_both_kernel<true><<<all, 256, 0, st>>>(w, (int)w_blocks, tm, tn, x, (int)x_blocks, tn_x, b, columns);
+  else grouped16_both_kernel<false><<<all, 256, 0, st>>>(w, (int)w_blocks, tm, tn, x, (int)x_blocks, tn_x, b, columns);
+  return hipGetLastError();
 }
 
 }  // namespace ilargi
