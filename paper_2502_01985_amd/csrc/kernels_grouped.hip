@@ -101,7 +101,7 @@ __device__ __forceinline__ void rows_block(const GroupedRows<Product>& a, int id
 }
 template <class T, int TILE, int STEP>
 __device__ __forceinline__ void sums_block(const GroupedSums<Product>& a, int id, int tm, int tn, MmF32Lds<TILE, STEP>& lds) {
-  grouped_sums_block<sizeof(T)>(a, id, tm, tn, [&](const Product& b, int ti, int tj, float* to) {
+  grouped_sums_block<sizeof(T)>(a, id, TILE, tm, tn, [&](const Product& b, int ti, int tj, float* to) {
     mm_f32_block<T, T, true, true, TILE, STEP>(b, ti, tj, 0, 0, b.K, to, lds);
   });
 }

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void grouped16_few_kernel(GroupedRows<Produ
 template <int B, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 512 / (WM * WN * 64)) void grouped16_sums_kernel(GroupedSums<Product16> a, int first, int tm, int tn) {
   __shared__ __attribute__((aligned(1024))) char lds[mm16_lds<true, true, B, B, WM, WN>()];
-  grouped_sums_block<2>(a, first + blockIdx.x, tm, tn, [&](const Product16& b, int ti, int tj, float* to) {
+  grouped_sums_block<2>(a, first + blockIdx.x, B, tm, tn, [&](const Product16& b, int ti, int tj, float* to) {
     mm16_block<true, true, B, B, WM, WN>(b, ti, tj, 0, (int)((b.K + kBK - 1) / kBK), to, lds);
   });
 }
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void grouped16_both_kernel(GroupedSums<Prod
   static_assert(sizeof(BiasLds) <= sizeof(lds), "the column sums fit too");
   const int id = blockIdx.x;
   if (id < sums) {
-    grouped_sums_block<2>(w, id, tm, tn, [&](const Product16& p, int ti, int tj, float* to) {
+    grouped_sums_block<2>(w, id, 128, tm, tn, [&](const Product16& p, int ti, int tj, float* to) {
       mm16_block<true, true, 128, 128, 2, 2>(p, ti, tj, 0, (int)((p.K + kBK - 1) / kBK), to, lds);
     });
   } else if (id - sums < rows) {

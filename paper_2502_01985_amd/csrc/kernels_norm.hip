@@ -333,15 +333,16 @@ struct NormGradIn {
 };
 constexpr int kGradWaves = 2;        // of a SIMD, at least: with 128 registers (four) a thread's values did not fit, 173 us for 132 at 8192 x 4096
 enum { kSumGate, kSumGain1, kSumGain2, kSumBias1, kSumBias2, kSums };
-// Whether all five sums of such rows are held in LDS (beyond 8192 columns they do not fit), and the bytes of it.
+// Whether all five sums of such rows are held in LDS (those of more than 8192 columns do not fit), and the bytes of it.
 template <class L>
-constexpr bool kSumsInLds = L::kW == 512 && L::E == 16;
+constexpr bool kSumsInLds = (L::kW == 512 && L::E == 16) || (L::V == 8 && L::NT == 256);
 template <class L>
-constexpr size_t kSumsLds = kSumsInLds<L> ? sizeof(float) * (kSums - 1) * L::E * L::kW : 0;
+constexpr size_t kSumsLds = kSumsInLds<L> ? sizeof(float) * (kSums - 1) * L::E * L::NT : 0;
 
-// Sums over a workgroup's rows, of the columns that a thread holds: in registers, or where all five of a wide row's are wanted (8192
-// columns: 80 registers of 256) all but the gate's in LDS, each thread's in places of its own.  (3600 x 8192, bfloat16, centred: 284 us in
-// registers that spill, 111 so.)
+// Sums over a workgroup's rows, of the columns that a thread holds: in registers, or where all five of many columns are wanted all but the
+// gate's in LDS, each thread's in places of its own: of 16 columns a thread (80 registers of 256; 3600 x 8192, bfloat16, centred: 284 us in
+// registers that spill, 111 so), and of eight in workgroups of 256, three of which then fit a compute unit (18,976 x 1544 115 and 109, 30,000 x
+// 768 108 and 97).
 template <class L, int HELD, bool IN_LDS>
 struct RowSums {
   static constexpr int E = L::E;
@@ -354,10 +355,10 @@ struct RowSums {
       for (int e = 0; e < E; ++e) held[q][e] = 0.0f;
     if constexpr (IN_LDS)
 #pragma unroll
-      for (int q = 0; q < (HELD - 1) * E / 4; ++q) mine[q * L::kW] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int q = 0; q < (HELD - 1) * E / 4; ++q) mine[q * L::NT] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   static __device__ __forceinline__ constexpr bool registers(int q) { return !IN_LDS || q == 0; }
-  __device__ __forceinline__ float4& place(int q, int e) const { return mine[((q - 1) * (E / 4) + e / 4) * L::kW]; }
+  __device__ __forceinline__ float4& place(int q, int e) const { return mine[((q - 1) * (E / 4) + e / 4) * L::NT]; }
   // a o b, or a
   template <int Q>
   __device__ __forceinline__ void add(const float (&a)[E], const float (&b)[E]) {
