@@ -398,8 +398,8 @@ ilargi_status_t ilargi_orthogonalize(const void* G, ilargi_type_t g_type, int64_
  *   CENTRED  (v - mean v) / sqrt(mean (v - mean v)^2 + eps) o gain + bias
  * over the m columns of a row; gains and biases are vectors of m, NULL for ones and zeros.  gate is n x m, one row of m for all rows
  * (gate_rows = 0), or NULL for ones; x may be NULL for zeros.  With second = NONE there is no y (then gain2 and bias2 are NULL).
- * All matrices and vectors are of one type; a row is held in float32 from its loads to its stores, each output is rounded once,
- * and y follows from the r that was not rounded.  A mean of squares that no float32 holds gives what float32 arithmetic gives. */
+ * All matrices and vectors are of one type; a row is held in float32 from its loads to its stores (its mean is summed in float64), each
+ * output is rounded once, and y follows from the r that was not rounded.  A mean of squares that no float32 holds gives what float32 arithmetic gives. */
 typedef enum { ILARGI_NORM_NONE = 0, ILARGI_NORM_RMS = 1, ILARGI_NORM_CENTRED = 2 } ilargi_norm_kind_t;
 
 typedef struct {
