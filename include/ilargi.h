@@ -466,7 +466,7 @@ ilargi_status_t ilargi_grouped_linear_grad(const ilargi_groups_t* layer, const i
 /* The norm over all entries of `count` matrices together, and the matrices scaled so that it is at most max_norm:
  *   norm = sqrt(sum of all squares);   out_t = in_t (max_norm / norm)  if norm > max_norm,  else in_t.
  * A norm that is no finite number scales nothing: the outputs are the inputs, and `norm` says so.  Squares are summed in float64 in an
- * order that depends on the sizes only, so no float32 or bfloat16 entries are too large or too small for it.
+ * order that depends on the inputs' sizes, types and leading dimensions only, so no float32 or bfloat16 entries are too large or too small for it.
  * tensors: host array, read during the call; a vector is a matrix of one row.  out NULL: the tensor counts and is not written; out may
  * be `in` itself (with ld_out = ld_in: scaled in place, and not written where nothing is scaled).  Any other overlap of an out with an in or
  * out of the call is refused, except that of column blocks of one matrix (equal leading dimensions).  norm: device float32 (optional).

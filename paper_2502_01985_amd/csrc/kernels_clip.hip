@@ -151,59 +151,69 @@ __global__ __launch_bounds__(256) void clip_kernel(Parts<MOST> a, const double* 
 }
 
 int64_t vec_of(const ilargi_tensor_t& t) { return t.type == ILARGI_TYPE_BF16 ? ElemOf<bf16_t>::kVec : ElemOf<float>::kVec; }
-bool in_one_row(const ilargi_tensor_t& t) { return t.rows <= 1 || (t.ld_in == t.cols && (t.out == nullptr || t.ld_out == t.cols)); }
-int64_t row_pieces(const ilargi_tensor_t& t) { return ((in_one_row(t) ? t.rows * t.cols : t.cols) + vec_of(t) - 1) / vec_of(t); }
-int64_t pieces_in(const ilargi_tensor_t& t) { return t.rows == 0 || t.cols == 0 ? 0 : row_pieces(t) * (in_one_row(t) ? 1 : t.rows); }
+// How a pass cuts a tensor into pieces and parts.  The first goes by the inputs alone (WRITTEN false): what is written, and where to, does not
+// change the order of its sums.
+template <bool WRITTEN>
+bool in_one_row(const ilargi_tensor_t& t) { return t.rows <= 1 || (t.ld_in == t.cols && (!WRITTEN || t.ld_out == t.cols)); }
+template <bool WRITTEN>
+int64_t row_pieces(const ilargi_tensor_t& t) { return ((in_one_row<WRITTEN>(t) ? t.rows * t.cols : t.cols) + vec_of(t) - 1) / vec_of(t); }
+template <bool WRITTEN>
+int64_t pieces_in(const ilargi_tensor_t& t) {
+  return t.rows == 0 || t.cols == 0 || (WRITTEN && t.out == nullptr) ? 0 : row_pieces<WRITTEN>(t) * (in_one_row<WRITTEN>(t) ? 1 : t.rows);
+}
 
 struct ClipPlan {
   int64_t part, groups;      // pieces of a workgroup, workgroups
 };
+template <bool WRITTEN>
 ClipPlan clip_plan(const ilargi_tensor_t* t, int64_t count) {
   int64_t all = 0;
-  for (int64_t q = 0; q < count; ++q) all += pieces_in(t[q]);
+  for (int64_t q = 0; q < count; ++q) all += pieces_in<WRITTEN>(t[q]);
   ClipPlan p{all / kMostSums, 0};
   p.part = p.part < kLeastPart ? kLeastPart : p.part > kMostPart ? kMostPart : (p.part + 255) / 256 * 256;
-  for (int64_t q = 0; q < count; ++q) p.groups += (pieces_in(t[q]) + p.part - 1) / p.part;
+  for (int64_t q = 0; q < count; ++q) p.groups += (pieces_in<WRITTEN>(t[q]) + p.part - 1) / p.part;
   return p;
 }
 
 }  // namespace
 
-size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)(clip_plan(t, count).groups + 1) * 8; }
+size_t clip_bytes(const ilargi_tensor_t* t, int64_t count) { return (size_t)(clip_plan<false>(t, count).groups + 1) * 8; }
 
 namespace {
 
 template <int MOST>
 hipError_t clip_in(const ilargi_tensor_t* t, int64_t count, float max_norm, float* norm, double* partial, hipStream_t st) {
-  const ClipPlan plan = clip_plan(t, count);
-  if (plan.groups > 2147483647ll) return hipErrorInvalidValue;
+  const ClipPlan read = clip_plan<false>(t, count), write = clip_plan<true>(t, count);
+  if (read.groups > 2147483647ll || write.groups > 2147483647ll) return hipErrorInvalidValue;
   int64_t written = 0;
   for (int64_t q = 0; q < count; ++q)
-    if (t[q].out != nullptr && t[q].out != t[q].in) written += pieces_in(t[q]) * 16;
+    if (t[q].out != t[q].in) written += pieces_in<true>(t[q]) * 16;
   const bool past = written >= kStreamBytes;
-  auto next = [&](int64_t& q, int step, bool outputs) {                  // tensors from q on, until a launch is full
+  auto next = [&](int64_t& q, int step, auto which) {                  // tensors from q on, until a launch is full
+    constexpr bool WRITTEN = decltype(which)::value;
+    const int64_t part = WRITTEN ? write.part : read.part;
     Parts<MOST> a{};
-    a.part = plan.part;
+    a.part = part;
     for (; q >= 0 && q < count && a.count < MOST; q += step) {
-      const int64_t pieces = pieces_in(t[q]);
-      if (pieces == 0 || (outputs && t[q].out == nullptr)) continue;
-      const bool one = in_one_row(t[q]);
-      a.t[a.count] = {(const char*)t[q].in, (char*)t[q].out, row_pieces(t[q]), pieces, one ? t[q].rows * t[q].cols : t[q].cols, t[q].ld_in, t[q].ld_out};
+      const int64_t pieces = pieces_in<WRITTEN>(t[q]);
+      if (pieces == 0) continue;
+      const bool one = in_one_row<WRITTEN>(t[q]);
+      a.t[a.count] = {(const char*)t[q].in, (char*)t[q].out, row_pieces<WRITTEN>(t[q]), pieces, one ? t[q].rows * t[q].cols : t[q].cols, t[q].ld_in, t[q].ld_out};
       a.bf16 |= (uint64_t)(t[q].type == ILARGI_TYPE_BF16) << a.count;
-      a.first[a.count + 1] = a.first[a.count] + (int)((pieces + plan.part - 1) / plan.part);
+      a.first[a.count + 1] = a.first[a.count] + (int)((pieces + part - 1) / part);
       ++a.count;
     }
     return a;
   };
   int64_t done = 0;
   for (int64_t q = 0; q < count;) {
-    const Parts<MOST> a = next(q, 1, false);
+    const Parts<MOST> a = next(q, 1, std::false_type());
     if (a.count == 0) break;
     squares_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, partial + done);
     done += a.first[a.count];
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  int sums = (int)plan.groups;
+  int sums = (int)read.groups;
   const double* from = partial;
   if (sums > kMostSums) {
     add_sums_kernel<<<1, 256, 0, st>>>(partial, sums, partial + sums);
@@ -212,7 +222,7 @@ hipError_t clip_in(const ilargi_tensor_t* t, int64_t count, float max_norm, floa
   }
   bool stored = norm == nullptr;
   for (int64_t q = count - 1; q >= 0;) {
-    const Parts<MOST> a = next(q, -1, true);
+    const Parts<MOST> a = next(q, -1, std::true_type());
     if (a.count == 0) break;
     clip_kernel<<<(unsigned)a.first[a.count], 256, 0, st>>>(a, from, sums, max_norm, stored ? nullptr : norm, past);
     stored = true;
