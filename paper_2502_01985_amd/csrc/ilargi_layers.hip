@@ -215,7 +215,7 @@ ilargi_status_t check_tensors(const ilargi_tensor_t* t, int64_t count) {
     if (t[q].ld_in < t[q].cols || t[q].ld_in > most || (t[q].out != nullptr && (t[q].ld_out < t[q].cols || t[q].ld_out > most)))
       return refuse(ILARGI_ERR_SHAPE, "clip_norm: a leading dimension of tensor %lld below its columns, or above 2^40", (long long)q);
     if (t[q].rows > 0 && t[q].cols > 0 && t[q].in == nullptr) return refuse(ILARGI_ERR_NULL, "clip_norm: tensor %lld is NULL", (long long)q);
-    if (t[q].out == t[q].in && t[q].rows > 1 && t[q].ld_out != t[q].ld_in)
+    if (t[q].out == t[q].in && t[q].rows > 1 && t[q].cols > 0 && t[q].ld_out != t[q].ld_in)
       return refuse(ILARGI_ERR_SHAPE, "clip_norm: tensor %lld in place with another leading dimension", (long long)q);
   }
   return ILARGI_OK;
