@@ -469,7 +469,8 @@ ilargi_status_t ilargi_grouped_linear_grad(const ilargi_groups_t* layer, const i
  * order that depends on the inputs' sizes, types and leading dimensions only, so no float32 or bfloat16 entries are too large or too small for it.
  * tensors: host array, read during the call; a vector is a matrix of one row.  out NULL: the tensor counts and is not written; out may
  * be `in` itself (with ld_out = ld_in: scaled in place, and not written where nothing is scaled).  Any other overlap of an out with an in or
- * out of the call is refused, except that of column blocks of one matrix (equal leading dimensions).  norm: device float32 (optional).
+ * out of the call is refused, except that of column blocks of one matrix (rows of one distance in bytes).  norm: device float32
+ * (optional), in none of the tensors.
  * (It is stored in 32 bits: infinite beyond 3.4e38, where the tensors are scaled all the same.)
  * max_norm may be infinite: outputs are copies.  count may be 0 (norm 0).
  * Errors: NULL (tensors, an in, workspace), SHAPE (count outside [0, 65535], rows or cols < 0, rows above 2^31 - 1, more than 2^46

@@ -165,25 +165,25 @@ ilargi_status_t check_groups(const char* what, const ilargi_groups_t* y) {
 }
 bool apart(const ilargi_groups_t& y, int64_t ld, int64_t stride) { return ld >= y.m && (y.groups <= 1 || stride >= (y.k - 1) * ld + y.m); }
 
-// Where the matrices of a call lie.
+// Where the matrices of a call lie: rows of `row` bytes, `step` bytes apart.
 struct Range {
   const char *lo, *hi;
-  int64_t rows, cols, ld, size;
+  int64_t rows, row, step;
   bool written;
 };
 Range range_of(const void* p, const ilargi_tensor_t& t, int64_t ld, bool written) {
   const int64_t size = t.type == ILARGI_TYPE_BF16 ? 2 : 4;
-  return {(const char*)p, (const char*)p + ((t.rows - 1) * ld + t.cols) * size, t.rows, t.cols, ld, size, written};
+  return {(const char*)p, (const char*)p + ((t.rows - 1) * ld + t.cols) * size, t.rows, t.cols * size, ld * size, written};
 }
-// Column blocks of one matrix: they interleave and share no element.  (a begins first.)
+// Column blocks of one matrix: they interleave and share no byte.  (a begins first.)
 bool column_blocks(const Range& a, const Range& b) {
-  const int64_t ld = a.rows > 1 ? a.ld : b.ld, far = b.lo - a.lo;
-  if (a.size != b.size || far % a.size != 0 || (a.rows > 1 && b.rows > 1 && a.ld != b.ld)) return false;
-  const int64_t at = far / a.size % ld;
-  return a.cols <= at && at + b.cols <= ld;
+  if (a.rows > 1 && b.rows > 1 && a.step != b.step) return false;
+  const int64_t step = a.rows > 1 ? a.step : b.step, at = (b.lo - a.lo) % step;
+  return a.row <= at && at + b.row <= step;
 }
-bool overlapping(const ilargi_tensor_t* t, int64_t count) {
+bool overlapping(const ilargi_tensor_t* t, int64_t count, const float* norm) {
   std::vector<Range> all, open;
+  if (norm != nullptr) all.push_back({(const char*)norm, (const char*)(norm + 1), 1, 4, 4, true});
   for (int64_t q = 0; q < count; ++q) {
     if (t[q].rows == 0 || t[q].cols == 0) continue;
     if (t[q].out != t[q].in) all.push_back(range_of(t[q].in, t[q], t[q].ld_in, false));
@@ -475,7 +475,7 @@ ilargi_status_t ilargi_clip_norm(const ilargi_tensor_t* tensors, int64_t count, 
   if (ilargi_status_t e = check_tensors(tensors, count); e != ILARGI_OK) return e;
   if (!(max_norm >= 0.0f)) return refuse(ILARGI_ERR_SHAPE, "clip_norm: max_norm = %g", (double)max_norm);
   try {
-    if (overlapping(tensors, count)) return refuse(ILARGI_ERR_SHAPE, "clip_norm: an output overlaps another tensor");
+    if (overlapping(tensors, count, norm)) return refuse(ILARGI_ERR_SHAPE, "clip_norm: an output or the norm overlaps another tensor");
   } catch (...) {
     return refuse(ILARGI_ERR_DEVICE, "clip_norm: out of host memory");
   }
