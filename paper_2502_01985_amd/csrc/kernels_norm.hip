@@ -6,8 +6,9 @@
 // stored ([lo, hi) is what a piece has of its own).  Rows of whole pieces have only pieces of their own and others.
 //
 // Bound by memory: 16384 x 4096, bfloat16, rms on both sides 108 us for 537 MB (5.0 TB/s); the gradient of 8192 x 4096 with gates 120 for 537 MB
-// (4.5) and of 100,000 x 220, float32, 101 for 528 MB (5.2), with 5 for the sums over rows.  Rows of 8193 columns and more do not fit the
-// registers: the gradient of 1800 x 16384 takes 490 us (237 MB).
+// (4.5) and of 100,000 x 220, float32, 101 for 528 MB (5.2), with 6 for the sums over rows.  Gradients of float32 rows of 4097 columns and more, and
+// of bfloat16 rows of 8193 and more, do not fit the registers, nor do norms of more than 8192: what spills grows from 20 of a thread's
+// registers to 660 (1800 x 16384, float32, centred on both sides with all sums: 926 us for 708 MB; the norm alone, rms on both sides, 112 for 472).
 #include "ilargi_layers.h"
 
 namespace ilargi {
@@ -613,8 +614,8 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict_
 }
 
 // f(row): threads of a row and pieces of a thread, the least that hold it.  WIDE: 512 threads, which have twice the registers of 1024, for
-// rows of up to 32 KB too.  (Gradients, 8192 columns: bfloat16 106 us for 3600 rows where 1024 threads take 197; float32 126 for 1800 and
-// 159, but 144 and 126 for 2115 x 5441 with all five sums.)
+// rows of up to 32 KB too.  (Gradients: bfloat16, 3600 x 8192, 106 us where 1024 threads take 197.  float32, with 512 threads and 1024: rms on both sides and
+// gates 126 and 159 at 1800 x 8192, 158 and 188 at 2115 x 5441; centred on both sides with all five sums 122 and 267, 257 and 329.)
 template <class T, bool WIDE, class F>
 hipError_t by_columns(int64_t m, F f) {
   constexpr int V = ElemOf<T>::kVec;
@@ -634,15 +635,16 @@ hipError_t by_columns(int64_t m, F f) {
   if (pieces <= 128) return with(integral_constant<int, 128>(), one);
   if (pieces <= 256) return with(integral_constant<int, 256>(), one);
   if (pieces <= 512) return with(integral_constant<int, 512>(), one);
-  if constexpr (WIDE) {
-    if constexpr (V == 8) {
-      if (pieces <= 1024) return with(integral_constant<int, 512>(), integral_constant<int, 2>());
-    } else {
-      if (pieces > 1024 && pieces <= 2048) return with(integral_constant<int, 512>(), integral_constant<int, 4>());
-    }
+  if constexpr (WIDE && V == 8) {
+    if (pieces <= 1024) return with(integral_constant<int, 512>(), integral_constant<int, 2>());
+  } else {
+    if (pieces <= 1024) return with(integral_constant<int, 1024>(), one);
   }
-  if (pieces <= 1024) return with(integral_constant<int, 1024>(), one);
-  if (pieces <= 2048) return with(integral_constant<int, 1024>(), integral_constant<int, 2>());
+  if constexpr (WIDE && V == 4) {
+    if (pieces <= 2048) return with(integral_constant<int, 512>(), integral_constant<int, 4>());
+  } else {
+    if (pieces <= 2048) return with(integral_constant<int, 1024>(), integral_constant<int, 2>());
+  }
   if constexpr (V == 4)
     if (pieces <= 4096) return with(integral_constant<int, 1024>(), integral_constant<int, 4>());
   return hipErrorInvalidValue;
