@@ -442,7 +442,8 @@ ilargi_status_t ilargi_norm_grad(const ilargi_norm_t* block, const void* d_r, in
  * W: `groups` matrices k x m, stride_w elements apart (>= (k - 1) ld_w + m); bias groups x m (optional) with ld_bias.
  * type, act, pre, residual and the sums are those of ilargi_linear; residual may be `out`.
  * The gradient: g = d_out o act'(pre); d_X[i, :] = g[i, :] W_g^T (rows of no group are not written); d_W_g = X_g^T g_g and
- * d_bias_g = column sums of g_g, zeros for groups without rows; with accumulate not 0 they are added to what is there.  Each
+ * d_bias_g = column sums of g_g, zeros for groups without rows; with accumulate not 0 they are added to what is there.  g is formed
+ * in float32 and rounded to the layer's type before the two products, and not rounded for d_bias, as in ilargi_linear_grad.  Each
  * result is optional; X is not read without d_W, nor W without d_X; pre is NULL if act is NONE.
  * Errors: NULL, SHAPE (groups < 0 or above 65535, n < 0, k or m < 1, any above 2^31 - 1, leading dimensions, matrices of the groups
  * that overlap, more than 2^31 - 1 blocks of 64 x 64 results), UNSUPPORTED (type, act), WORKSPACE, DEVICE. */

@@ -1126,7 +1126,8 @@ def _as_matrix(t, name: str):
 class TensorList:
     """Tensors for ``ilargi_clip_norm`` (float32 and bfloat16, of one device), and where they go: ``outs`` are tensors of the same
     shapes and types, the tensors themselves to scale them in place, ``None`` entries where nothing is to be written, or ``None``
-    for no outputs at all.  Programs that clip the same gradients at every step keep the list."""
+    for no outputs at all.  Programs that clip the same gradients at every step keep the list; it holds their addresses, so a tensor
+    whose storage is replaced or resized needs a new one."""
 
     def __init__(self, tensors, outs=None):
         self.tensors = list(tensors)
