@@ -5,10 +5,11 @@
 // earlier instead, so that every load is a whole one: the columns that the neighbour holds already count as zeros here and are not
 // stored ([lo, hi) is what a piece has of its own).  Rows of whole pieces have only pieces of their own and others.
 //
-// Bound by memory: 16384 x 4096, bfloat16, rms on both sides 108 us for 537 MB (5.0 TB/s); the gradient of 8192 x 4096 with gates 120 for 537 MB
-// (4.5) and of 100,000 x 220, float32, 101 for 528 MB (5.2), with 6 for the sums over rows.  Gradients of float32 rows of 4097 columns and more, and
-// of bfloat16 rows of 8193 and more, do not fit the registers, nor do norms of more than 8192: what spills grows from 20 of a thread's
-// registers to 660 (1800 x 16384, float32, centred on both sides with all sums: 926 us for 708 MB; the norm alone, rms on both sides, 112 for 472).
+// Bound by memory: 16384 x 4096, bfloat16, rms on both sides 95 us for 537 MB (5.7 TB/s; two workgroups a compute unit, with three 108); the
+// gradient of 8192 x 4096 with gates 121 for 537 MB (4.4) and of 100,000 x 220, float32, 103 for 528 MB (5.1), with 6 for the sums over rows.  By the
+// vector units where all sums are wanted of narrower bfloat16 rows (30,000 x 768, centred on both sides: 103 us for 276 MB).  Gradients of float32 rows of 4097
+// columns and more, and of bfloat16 rows of 8193 and more, do not fit the registers, nor do norms of more than 8192: what spills grows from 20 of a
+// thread's registers to 660 (1800 x 16384, float32, centred on both sides with all sums: 975 us for 708 MB; the norm alone, rms on both sides, 112 for 472).
 #include "ilargi_layers.h"
 
 namespace ilargi {
@@ -379,8 +380,8 @@ constexpr size_t kSumsLds = kSumsInLds<L> ? sizeof(float) * (kSums - 1) * L::E *
 
 // Sums over a workgroup's rows, of the columns that a thread holds: in registers, or where all five of many columns are wanted all but the
 // gate's in LDS, each thread's in places of its own: of 16 columns a thread (80 registers of 256; 3600 x 8192, bfloat16, centred: 284 us in
-// registers that spill, 111 so), and of eight in workgroups of 256, three of which then fit a compute unit (18,976 x 1544 115 and 109, 30,000 x
-// 768 108 and 97).
+// registers that spill, 111 so), and of eight in workgroups of 256, three of which then fit a compute unit (centred on both sides, a gate row: 18,976 x
+// 1544 164 and 132, 30,000 x 768 134 and 103).
 template <class L, int HELD, bool IN_LDS>
 struct RowSums {
   static constexpr int E = L::E;
@@ -444,7 +445,7 @@ struct RowSums {
 // The sums over this workgroup's rows go to partial[workgroup][sum][column].  FEW: there is no bias1, and those
 // of the gains alone are wanted.  A row's data are
 // asked for as soon as those of the row before have been taken out of their registers
-// (8192 columns of bfloat16, two pieces a thread: 106 us for 3600 rows; asked for when the row begins, 148).
+// (8192 columns of bfloat16, two pieces a thread, means in float32: 106 us for 3600 rows; asked for when the row begins, 148).
 template <class T, int W, int P, int SHAPE, bool FEW>
 __global__ __launch_bounds__(W < 256 ? 256 : W, kGradWaves) void norm_grad_kernel(ilargi_norm_t a, NormGradIn d, ilargi_norm_grads_t o, float* __restrict__ partial, bool past) {
   using L = Row<T, W, P, SHAPE>;
@@ -614,8 +615,8 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict_
 }
 
 // f(row): threads of a row and pieces of a thread, the least that hold it.  WIDE: 512 threads, which have twice the registers of 1024, for
-// rows of up to 32 KB too.  (Gradients: bfloat16, 3600 x 8192, 106 us where 1024 threads take 197.  float32, with 512 threads and 1024: rms on both sides and
-// gates 126 and 159 at 1800 x 8192, 158 and 188 at 2115 x 5441; centred on both sides with all five sums 122 and 267, 257 and 329.)
+// rows of up to 32 KB too.  (Gradients with 512 threads and with 1024.  bfloat16, 3600 x 8192: rms on both sides and gates 92 and 157 us, centred on both
+// sides with all five sums 113 and 464.  float32, the same two: 126 and 159, 122 and 267 at 1800 x 8192; 158 and 188, 257 and 329 at 2115 x 5441.)
 template <class T, bool WIDE, class F>
 hipError_t by_columns(int64_t m, F f) {
   constexpr int V = ElemOf<T>::kVec;
